@@ -348,6 +348,142 @@ apack_status apack_decode_attention(int32_t num_seqs, const int32_t *cu_seqlens_
                                     const void *v, int64_t kv_token_stride, int32_t num_q_heads,
                                     int32_t num_kv_heads, float *out, void *ws, size_t ws_bytes, void *stream);
 
+/* ---- Paged key-value caches.
+   Sec. 3.2 drops tokens "together with their key-value entries": what a step frees is of use to other
+   sequences only where a cache is kept in pages.  A pool holds num_pages pages of page_tokens tokens for
+   every layer; row r of sequence b is slot r % page_tokens of page
+   page_table[b*table_stride + r/page_tokens].  Token rows of a page may lie [token][head][D] or
+   [head][token][D], pages and layers in either order: the strides say so.  One page that holds a whole
+   contiguous cache is a pool too (num_pages 1, page_tokens T), so that contiguous caches and pages are
+   sources and destinations of the same calls.
+
+   The device memory that the calls below are given is the current device's.
+
+   Element types of the calls below. */
+enum { APACK_BF16 = 0, APACK_FP16 = 1, APACK_FP32 = 2 };
+
+typedef struct apack_paged_cache {
+  void *k, *v;                  /* layer 0, page 0, token 0, head 0; device memory, 16-byte aligned */
+  int64_t layer_stride;         /* bytes, multiples of 16, the same for k and v; of the last four a stride */
+  int64_t page_stride;          /*   whose extent is 1 is not read.  Heads and tokens of a page must not */
+  int64_t token_stride;         /*   overlap, nor pages and layers of the pool (APACK_EINVAL) */
+  int64_t head_stride;
+  int32_t num_layers, num_pages;
+  int32_t page_tokens;          /* tokens per page, 1 .. 2^30 */
+  int32_t num_kv_heads;         /* 1 .. 256 */
+  int32_t head_dim;             /* D: 64 or 128 (APACK_EUNSUPPORTED otherwise) */
+  int32_t dtype;                /* APACK_BF16 or APACK_FP16 */
+  const int32_t *page_table;    /* device [num_seqs][max_pages]; entries behind a sequence's last row are not read */
+  int64_t table_stride;         /* int32 entries between the rows of page_table, >= max_pages */
+  int32_t num_seqs;             /* 1 .. APACK_MAX_SEQS */
+  int32_t max_pages;            /* columns of page_table, >= 1 */
+} apack_paged_cache;
+
+/* Rotary positions.  Pair i of a head's first rotary_dim elements turns by the angle
+   t = positions[axis(i)][token] * freq_h[i]:
+     (a, b) -> magnitude * (a cos t - b sin t, b cos t + a sin t);
+   APACK_ROTARY_HALF pairs elements (i, i + rotary_dim/2), APACK_ROTARY_PAIRS elements (2i, 2i + 1); the
+   elements from rotary_dim on pass unchanged.  With num_axes 2 or 3 (time, height and width of a visual
+   token) the first section[0] pairs take their position from axis 0, the next section[1] from axis 1 and so
+   on; the sections add up to rotary_dim/2.  Angles are reduced modulo one turn in 64-bit fixed point, so
+   that far positions keep them to 2^-24 of a turn, whatever int32 the position is; arithmetic in fp32, one
+   rounding. */
+enum { APACK_ROTARY_HALF = 0, APACK_ROTARY_PAIRS = 1 };
+typedef struct apack_rotary_spec {
+  int32_t layout;               /* APACK_ROTARY_* */
+  int32_t rotary_dim;           /* even, 2 .. head_dim */
+  int32_t num_axes;             /* 1 .. 3 */
+  int32_t section[3];           /* pairs per axis, >= 0; not read when num_axes is 1 */
+  float magnitude;              /* finite */
+  const double *freq_h;         /* HOST [rotary_dim/2], radians per position, finite; read before the call returns */
+} apack_rotary_spec;
+
+/* The frequencies freq_h[i] = base^(-2i/rotary_dim) and their forms for contexts `factor` times longer than
+   the original_len tokens that a model was trained on:
+     LINEAR  freq / factor (position interpolation);
+     NTK     base * factor^(r/(r-2)) in the place of base, r = rotary_dim >= 4;
+     YARN    (arXiv 2309.00071, Eqs. 10-13) freq * g + freq / factor * (1 - g), where g rises from 0 to 1
+             as the turns original_len * freq / 2 pi of the pair rise from beta_slow to beta_fast;
+             magnitude = 0.1 ln(factor) + 1.
+   magnitude_h receives 1 in the other forms.  Host only. */
+enum { APACK_ROTARY_NONE = 0, APACK_ROTARY_LINEAR = 1, APACK_ROTARY_NTK = 2, APACK_ROTARY_YARN = 3 };
+apack_status apack_rotary_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor,
+                                      int64_t original_len, double beta_fast, double beta_slow, double *freq_h,
+                                      float *magnitude_h);
+
+/* Rotates num_heads heads of D elements in each of n_tokens rows.  x: token t's heads, back to back, at
+   x + t*x_token_stride bytes; out likewise; out == x with equal strides rotates in place, and the two must not
+   overlap otherwise.  positions: int32, axis a's position of token t at positions[a*pos_axis_stride + t].
+   transpose non-zero: the transposed map, the gradient with respect to x of a rotation (it turns back by the
+   same angles and keeps the magnitude).  dtype: APACK_BF16, APACK_FP16 or APACK_FP32.  head_dim: 2 .. 256,
+   even.  x and out aligned to the element; 16-byte aligned rows and rotary_dim, head_dim multiples of 16 take
+   wide loads.  n_tokens up to 2^31 - 1; 0 does nothing. */
+apack_status apack_rotary(const apack_rotary_spec *spec, int32_t dtype, int64_t n_tokens, int32_t num_heads,
+                          int32_t head_dim, const void *x, int64_t x_token_stride, void *out, int64_t out_token_stride,
+                          const int32_t *positions, int64_t pos_axis_stride, int32_t transpose, void *stream);
+
+/* A decode step's or a prompt's new tokens: rotates their queries into q_out and their keys into the pages of
+   `layer`, and writes their values there.  Token t goes to row rows[t] of sequence seqs[t] (seqs NULL: of
+   sequence t, n_tokens <= num_seqs); a negative row writes neither key nor value (padding of a captured batch;
+   its query is rotated all the same).  No two tokens of a call may name one slot.  q [n][num_q_heads][D] (at
+   any token stride, as k and v: slices of one projection's output), q_out likewise (q_out == q with equal strides in
+   place), k and v [n][num_kv_heads][D]; dtype and D of the cache; every pointer and stride a multiple of 16
+   bytes.  spec NULL: nothing is rotated.  num_q_heads 0 .. 1024; with 0, q and q_out are NULL (keys and values
+   alone).
+   ws: NULL, or a workspace whose error word (its first 16 bytes) receives APACK_EDEVICE when a row lies behind
+   the page table or a page number outside the pool; such a token is not written, with or without ws. */
+apack_status apack_rotary_append(const apack_rotary_spec *spec, const apack_paged_cache *cache, int32_t layer,
+                                 int64_t n_tokens, const void *q, int64_t q_token_stride, void *q_out,
+                                 int64_t q_out_token_stride, int32_t num_q_heads, const void *k,
+                                 int64_t k_token_stride, const void *v, int64_t v_token_stride,
+                                 const int32_t *positions, int64_t pos_axis_stride, const int32_t *rows,
+                                 const int32_t *seqs, void *ws, void *stream);
+
+/* apack_decode_attention over pages: one token per sequence,
+     out[b][h] = sum_r softmax_r(scale q[b][h] . k[r][g]) v[r][g],  g = h / (Hq / Hkv), r < seqlens[b],
+   the lengths on the DEVICE, so that a captured call follows growing caches.  An empty sequence gives zeros
+   and an lse of -infinity; what lies behind a sequence's last row (infinities and NaN too) has no influence.
+   A NaN or infinity among the rows themselves makes what it enters NaN (an infinite value: infinite or NaN).
+   q: [num_seqs][Hq][D] at q_token_stride bytes, cache dtype, 16-byte aligned; scale > 0 (1/sqrt(D) is usual).
+   out: [num_seqs][Hq][D], contiguous, 16-byte aligned, out_dtype the cache's or APACK_FP32.  lse: fp32
+   [num_seqs][Hq] or NULL, ln sum_r exp(scale q.k).  Hq / Hkv <= 32 (APACK_EUNSUPPORTED otherwise), Hq <= 1024.
+   fp32 softmax and accumulation; the sums' order depends on the lengths alone (deterministic).
+   A length below 0 or above max_pages*page_tokens is read as the nearest of the two, and a page number outside
+   the pool as a page of zeros; both record APACK_EDEVICE in the error word of ws.
+   ws: 256-byte aligned, apack_paged_decode_workspace_size bytes (for this pool and Hq, whatever the lengths;
+   query it on the device that runs the call), its error word (first 16 bytes) zeroed once by the caller.
+   Two captured graphs may share a workspace as long as they do not overlap.  Two kernel launches. */
+apack_status apack_paged_decode_workspace_size(const apack_paged_cache *cache, int32_t num_q_heads, size_t *bytes);
+apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_t layer, const int32_t *seqlens,
+                                          const void *q, int64_t q_token_stride, int32_t num_q_heads, float scale,
+                                          void *out, int32_t out_dtype, float *lse, void *ws, size_t ws_bytes,
+                                          void *stream);
+
+/* apack_compact between pools: row j - cu_dst[b] of dst's sequence b receives, for K and V of num_layers
+   layers (src_layer and dst_layer on), bit for bit, row
+     keep_idx[j] - cu_src[b]   (keep_idx as apack_select writes it, packed over the batch; cu_src: the packed
+                                offsets that entered the step, device [B+1])
+     keep_idx[j]               where cu_src is NULL (one page that holds the packed batch)
+     j - cu_dst[b]             where keep_idx is NULL (every sequence's first rows; cu_src must be NULL)
+   of src's sequence b, for j in [cu_dst[b], cu_dst[b+1]); cu_dst: device [B+1], apack_select's new_cu_seqlens.
+   n_out: cu_dst[B], or an upper bound of it.  B = num_seqs of both pools; heads, D and dtype equal; page sizes
+   and strides may differ.  Slots of dst that no j names keep what they hold.
+   Out of place, no page that is written may be read by the same call.  In place: src and dst are the same
+   pool (k, v and strides), table (pointer and stride) and layer, keep_idx is given and ascending within each
+   sequence, and each sequence's pages are its own; rows move towards the front of their sequence.
+   ws: NULL, or a workspace whose error word receives APACK_EDEVICE when a row lies behind a page table or a
+   page number outside its pool; such a row is not copied, with or without ws. */
+apack_status apack_paged_compact(const apack_paged_cache *src, const apack_paged_cache *dst, int32_t src_layer,
+                                 int32_t dst_layer, int32_t num_layers, const int32_t *keep_idx,
+                                 const int32_t *cu_src, const int32_t *cu_dst, int64_t n_out, void *ws, void *stream);
+
+/* Copies page pairs[i][0] to page pairs[i][1] in every layer, K and V, i < n_pairs (device int32 [n_pairs][2]):
+   the pages that a forked sequence needs of its own.  No page may be written twice, nor written and read by
+   the same call (a pair of one page with itself changes nothing).  page_table is not read and may be NULL.
+   ws as in apack_paged_compact; a pair with a page outside the pool is not copied. */
+apack_status apack_copy_pages(const apack_paged_cache *cache, const int32_t *pairs, int64_t n_pairs, void *ws,
+                              void *stream);
+
 /* Synchronises `stream`, then reads the device error word of `ws` into
    *code_out (APACK_OK, APACK_ETIMEOUT or APACK_EDEVICE) and clears it when
    `clear` is non-zero. */

@@ -6,6 +6,7 @@ CUDA library: the two share no code.  See ``apack_oracle.py``.
 """
 
 from .prellm_oracle import frame_embeddings, window_cka, gate, frame_alignment  # noqa: F401
+from . import paged_oracle  # noqa: F401
 from .decode_oracle import decode_attention  # noqa: F401
 from .apack_oracle import (  # noqa: F401
     MOD_OTHER, MOD_AUDIO, MOD_VISUAL, SOFTMAX_MM, SOFTMAX_CAUSAL_ROW,

@@ -13,6 +13,7 @@ There is no fallback.
 """
 
 import ctypes
+import math
 import os
 
 import numpy as np
@@ -25,12 +26,17 @@ APACK_MOD_OTHER, APACK_MOD_AUDIO, APACK_MOD_VISUAL = 0, 1, 2
 APACK_SELECT_PER_MODALITY, APACK_SELECT_JOINT = 0, 1
 APACK_SOFTMAX_MM, APACK_SOFTMAX_CAUSAL_ROW = 0, 1
 APACK_HEAD_DIM = 128
+APACK_BF16, APACK_FP16, APACK_FP32 = 0, 1, 2
+APACK_ROTARY_HALF, APACK_ROTARY_PAIRS = 0, 1
+APACK_ROTARY_NONE, APACK_ROTARY_LINEAR, APACK_ROTARY_NTK, APACK_ROTARY_YARN = range(4)
 
 EXPORTED = ("apack_workspace_size", "apack_keep_counts", "apack_score", "apack_select", "apack_compact",
             "apack_prune_step", "apack_device_error", "apack_launch_count", "apack_status_string",
             "apack_score_static", "apack_frame_alignment_workspace_size", "apack_frame_alignment",
             "apack_decode_workspace_size", "apack_decode_attention", "apack_prune_schedule",
-            "apack_prune_schedule_graph", "apack_graph_launch", "apack_graph_destroy")
+            "apack_prune_schedule_graph", "apack_graph_launch", "apack_graph_destroy",
+            "apack_rotary_frequencies", "apack_rotary", "apack_rotary_append", "apack_paged_decode_workspace_size",
+            "apack_paged_decode_attention", "apack_paged_compact", "apack_copy_pages")
 
 
 class ApackError(RuntimeError):
@@ -69,6 +75,21 @@ class apack_step(ctypes.Structure):
                 ("new_cu_seqlens_h", ctypes.POINTER(ctypes.c_int32)), ("new_cu_seqlens", ctypes.c_void_p)]
 
 
+class apack_paged_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("layer_stride", ctypes.c_int64),
+                ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("num_layers", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("page_tokens", ctypes.c_int32),
+                ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("page_table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("num_seqs", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32)]
+
+
+class apack_rotary_spec(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("num_axes", ctypes.c_int32),
+                ("section", ctypes.c_int32 * 3), ("magnitude", ctypes.c_float),
+                ("freq_h", ctypes.POINTER(ctypes.c_double))]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"libapack.so is not built ({LIB_PATH}); run __graft_entry__.build()")
@@ -96,6 +117,15 @@ def _load():
                                                VP, VP, SZ, P(VP)]
     lib.apack_graph_launch.argtypes = [VP, VP]
     lib.apack_graph_destroy.argtypes = [VP]
+    F32, F64 = ctypes.c_float, ctypes.c_double
+    lib.apack_rotary_frequencies.argtypes = [I32, F64, I32, F64, I64, F64, F64, VP, P(F32)]
+    lib.apack_rotary.argtypes = [VP, I32, I64, I32, I32, VP, I64, VP, I64, VP, I64, I32, VP]
+    lib.apack_rotary_append.argtypes = [VP, VP, I32, I64, VP, I64, VP, I64, I32, VP, I64, VP, I64, VP, I64, VP, VP,
+                                        VP, VP]
+    lib.apack_paged_decode_workspace_size.argtypes = [VP, I32, P(SZ)]
+    lib.apack_paged_decode_attention.argtypes = [VP, I32, VP, VP, I64, I32, F32, VP, I32, VP, VP, SZ, VP]
+    lib.apack_paged_compact.argtypes = [VP, VP, I32, I32, I32, VP, VP, VP, I64, VP, VP]
+    lib.apack_copy_pages.argtypes = [VP, VP, I64, VP, VP]
     lib.apack_launch_count.argtypes = []
     lib.apack_launch_count.restype = ctypes.c_uint64
     lib.apack_status_string.argtypes = [I32]
@@ -406,6 +436,213 @@ def apack_decode_attention(cu_seqlens, q, k, v, kv_token_stride, num_q_heads, nu
                                        int(kv_token_stride), int(num_q_heads), int(num_kv_heads), _ptr(out),
                                        _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)),
            "apack_decode_attention")
+
+
+# ---------------------------------------------------------------- paged caches
+
+
+def _dtype_code(dtype):
+    import torch
+    codes = {torch.bfloat16: APACK_BF16, torch.float16: APACK_FP16, torch.float32: APACK_FP32}
+    if dtype not in codes:
+        raise ValueError(f"{dtype}: bfloat16, float16 or float32 expected")
+    return codes[dtype]
+
+
+def _on_device(*tensors):
+    """The calls run on the current device: tensors elsewhere are refused."""
+    import torch
+    if not torch.cuda.is_initialized() and not torch.cuda.is_available():
+        return                              # no device: the library's own checks answer
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != dev:
+            raise ValueError(f"a tensor on {t.device}; the current device is cuda:{dev}")
+
+
+def _int32(t, what, shape=None):
+    import torch
+    if t.dtype != torch.int32 or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{what}: contiguous int32{'' if shape is None else f' of shape {tuple(shape)}'} expected, "
+                         f"not {t.dtype} {tuple(t.shape)}")
+
+
+def _head_rows(t, what, dtype=None, shape=None):
+    """A [tokens, heads, D] tensor whose heads are back to back; returns its token stride in bytes."""
+    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise ValueError(f"{what}: [tokens, heads, D] with heads back to back expected")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{what}: {dtype} expected, not {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: shape {tuple(shape)} expected, not {tuple(t.shape)}")
+    return t.stride(0) * t.element_size() if t.shape[0] > 1 else t.shape[1] * t.shape[2] * t.element_size()
+
+
+class PagedCache:
+    """A pool of key-value pages and the page tables of a batch (apack_paged_cache).
+
+    k, v: [layers, pages, page_tokens, Hkv, D] bfloat16 or float16 tensors of equal strides, D contiguous; any
+    order of the other dimensions in memory (permute a [layers, pages, Hkv, page_tokens, D] pool).  page_table:
+    int32 [num_seqs, max_pages].  Holds the tensors."""
+
+    def __init__(self, k, v, page_table):
+        import torch
+        if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.stride(4) != 1:
+            raise ValueError("k and v: [layers, pages, page_tokens, heads, D] of one shape, type and strides expected")
+        if page_table.dtype != torch.int32 or page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+            raise ValueError("page_table: int32 [sequences, pages] with contiguous rows expected")
+        if k.device != v.device or k.device != page_table.device:
+            raise ValueError("k, v and page_table: one device expected")
+        self.k, self.v, self.page_table = k, v, page_table
+        self.dtype, self.device = k.dtype, k.device
+        size = k.element_size()
+        layers, pages, tokens, heads, dim = k.shape
+        seqs, columns = page_table.shape
+        self.num_kv_heads, self.head_dim, self.num_seqs, self.num_layers = heads, dim, seqs, layers
+        # a stride of an extent of one says nothing, and may be anything
+        stride = [k.stride(i) * size if k.shape[i] > 1 else 0 for i in range(4)]
+        self.struct = apack_paged_cache(
+            k=k.data_ptr(), v=v.data_ptr(), layer_stride=stride[0], page_stride=stride[1], token_stride=stride[2],
+            head_stride=stride[3], num_layers=layers, num_pages=pages, page_tokens=tokens, num_kv_heads=heads,
+            head_dim=dim, dtype=_dtype_code(k.dtype), page_table=page_table.data_ptr(),
+            table_stride=page_table.stride(0) if seqs > 1 else columns, num_seqs=seqs, max_pages=columns)
+        self._address = ctypes.addressof(self.struct)
+
+
+class Rotary:
+    """Rotary positions (apack_rotary_spec): frequencies of a form of scaling, or given ones.
+
+    scaling: "none", "linear", "ntk" or "yarn" (see apack_rotary_frequencies); frequencies: radians per position
+    of the rotary_dim / 2 pairs, in the place of base and scaling.  sections: pairs per position axis (2 or 3
+    axes).  interleaved: pairs of neighbouring elements, else of the two halves."""
+
+    def __init__(self, rotary_dim, base=10000.0, interleaved=False, scaling="none", factor=1.0, original_len=0,
+                 beta_fast=32.0, beta_slow=1.0, sections=None, magnitude=None, frequencies=None):
+        modes = {"none": APACK_ROTARY_NONE, "linear": APACK_ROTARY_LINEAR, "ntk": APACK_ROTARY_NTK,
+                 "yarn": APACK_ROTARY_YARN}
+        if scaling not in modes:
+            raise ValueError(f"scaling {scaling!r}: one of {', '.join(modes)} expected")
+        pairs = max(1, int(rotary_dim) // 2)
+        m = ctypes.c_float(1.0)
+        if frequencies is None:
+            self.frequencies = np.zeros(pairs, np.float64)
+            _check(_lib.apack_rotary_frequencies(int(rotary_dim), float(base), modes[scaling], float(factor),
+                                                 int(original_len), float(beta_fast), float(beta_slow),
+                                                 _host(self.frequencies), ctypes.byref(m)), "apack_rotary_frequencies")
+        else:
+            self.frequencies = np.array(frequencies, np.float64)
+            if self.frequencies.shape != (pairs,):
+                raise ValueError(f"frequencies: {pairs} expected")
+        self.rotary_dim = int(rotary_dim)
+        self.magnitude = float(m.value if magnitude is None else magnitude)
+        sec = [] if sections is None else [int(x) for x in sections]
+        if len(sec) > 3:
+            raise ValueError("sections: at most three axes")
+        self.num_axes = max(1, len(sec))
+        self.struct = apack_rotary_spec(
+            layout=APACK_ROTARY_PAIRS if interleaved else APACK_ROTARY_HALF, rotary_dim=self.rotary_dim,
+            num_axes=self.num_axes, section=(ctypes.c_int32 * 3)(*(sec + [0] * (3 - len(sec)))),
+            magnitude=self.magnitude, freq_h=self.frequencies.ctypes.data_as(ctypes.POINTER(ctypes.c_double)))
+        self._address = ctypes.addressof(self.struct)
+
+    def _positions(self, positions, n):
+        """Checks int32 [n] or [axes, n]; returns the stride between axes."""
+        import torch
+        one = positions.dim() == 1 and self.num_axes == 1
+        if positions.dtype != torch.int32 or positions.shape[-1] != n or positions.dim() not in (1, 2) or not (
+                one or (positions.dim() == 2 and positions.shape[0] == self.num_axes)) or (n > 1 and positions.stride(-1) != 1):
+            raise ValueError(f"positions: int32 [{self.num_axes}, {n}] expected, not {positions.dtype} {tuple(positions.shape)}")
+        return positions.stride(0) if positions.dim() == 2 and self.num_axes > 1 else n
+
+
+def apack_rotary(rotary, x, positions, out, transpose=False, stream=None):
+    """Rotary positions of x [tokens, heads, D] into out (out is x: in place); transpose: the gradient."""
+    _on_device(x, positions, out)
+    xs = _head_rows(x, "x")
+    outs = _head_rows(out, "out", x.dtype, x.shape)
+    n, heads, dim = x.shape
+    axis = rotary._positions(positions, n)
+    _check(_lib.apack_rotary(rotary._address, _dtype_code(x.dtype), n, heads, dim, x.data_ptr(), xs, out.data_ptr(),
+                             outs, positions.data_ptr(), axis, 1 if transpose else 0, _stream(stream)), "apack_rotary")
+
+
+def apack_rotary_append(rotary, cache, layer, q, k, v, q_out, positions, rows, seqs=None, ws=None, stream=None):
+    """Rotates new tokens' queries into q_out and their keys into the pages of `layer`, with their values.
+    rotary None: no rotation; q (and q_out) None: keys and values alone."""
+    _on_device(cache, q, k, v, q_out, positions, rows, seqs, ws)
+    n = k.shape[0]
+    shape = (n, cache.num_kv_heads, cache.head_dim)
+    ks, vs = _head_rows(k, "k", cache.dtype, shape), _head_rows(v, "v", cache.dtype, shape)
+    qs = qos = heads = 0
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out: both or neither expected")
+    if q is not None:
+        heads = q.shape[1]
+        qs = _head_rows(q, "q", cache.dtype, (n, heads, cache.head_dim))
+        qos = _head_rows(q_out, "q_out", cache.dtype, q.shape)
+    axis = 0
+    if rotary is not None:
+        axis = rotary._positions(positions, n)
+    _int32(rows, "rows", (n,))
+    if seqs is not None:
+        _int32(seqs, "seqs", (n,))
+    _check(_lib.apack_rotary_append(None if rotary is None else rotary._address, cache._address, int(layer), n,
+                                    _ptr(q), qs, _ptr(q_out), qos, heads, k.data_ptr(), ks, v.data_ptr(), vs,
+                                    None if rotary is None else positions.data_ptr(), axis, rows.data_ptr(),
+                                    _ptr(seqs), _ptr(ws), _stream(stream)), "apack_rotary_append")
+
+
+def apack_paged_decode_workspace_size(cache, num_q_heads):
+    n = ctypes.c_size_t(0)
+    _check(_lib.apack_paged_decode_workspace_size(cache._address, int(num_q_heads), ctypes.byref(n)),
+           "apack_paged_decode_workspace_size")
+    return n.value
+
+
+def apack_paged_decode_attention(cache, layer, seqlens, q, out, ws, scale=None, lse=None, stream=None):
+    """Attention of one decode token per sequence over its pages; seqlens: int32 [num_seqs] on the device.
+    q [num_seqs, Hq, D]; out: the same shape, contiguous, of q's type or float32; lse: float32 [num_seqs, Hq]."""
+    import torch
+    _on_device(cache, seqlens, q, out, ws, lse)
+    heads = q.shape[1]
+    shape = (cache.num_seqs, heads, cache.head_dim)
+    qs = _head_rows(q, "q", cache.dtype, shape)
+    _int32(seqlens, "seqlens", (cache.num_seqs,))
+    if tuple(out.shape) != shape or not out.is_contiguous():
+        raise ValueError(f"out: contiguous {shape} expected")
+    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != shape[:2] or not lse.is_contiguous()):
+        raise ValueError(f"lse: contiguous float32 {shape[:2]} expected")
+    _check(_lib.apack_paged_decode_attention(
+        cache._address, int(layer), seqlens.data_ptr(), q.data_ptr(), qs, heads,
+        1.0 / math.sqrt(cache.head_dim) if scale is None else float(scale), out.data_ptr(), _dtype_code(out.dtype),
+        _ptr(lse), ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)), "apack_paged_decode_attention")
+
+
+def apack_paged_compact(src, dst, cu_dst, n_out, keep_idx=None, cu_src=None, src_layer=0, dst_layer=0,
+                        num_layers=None, ws=None, stream=None):
+    """The kept rows of every sequence of pool src, in order, to the first rows of its pages in dst (src is dst:
+    in place).  cu_dst, cu_src: int32 [num_seqs + 1] on the device; num_layers: all that both have by default."""
+    _on_device(src, dst, cu_dst, keep_idx, cu_src, ws)
+    _int32(cu_dst, "cu_dst", (dst.num_seqs + 1,))
+    if cu_src is not None:
+        _int32(cu_src, "cu_src", (src.num_seqs + 1,))
+    if keep_idx is not None:
+        _int32(keep_idx, "keep_idx")
+        if keep_idx.numel() < n_out:
+            raise ValueError(f"keep_idx: {n_out} entries expected, not {keep_idx.numel()}")
+    if num_layers is None:
+        num_layers = min(src.num_layers - src_layer, dst.num_layers - dst_layer)
+    _check(_lib.apack_paged_compact(src._address, dst._address, int(src_layer), int(dst_layer), int(num_layers),
+                                    _ptr(keep_idx), _ptr(cu_src), cu_dst.data_ptr(), int(n_out), _ptr(ws),
+                                    _stream(stream)), "apack_paged_compact")
+
+
+def apack_copy_pages(cache, pairs, ws=None, stream=None):
+    """Copies page pairs[i, 0] to page pairs[i, 1] in every layer; pairs: int32 [n, 2] on the device."""
+    _on_device(cache, pairs, ws)
+    _int32(pairs, "pairs", (pairs.shape[0], 2))
+    _check(_lib.apack_copy_pages(cache._address, pairs.data_ptr(), pairs.shape[0], _ptr(ws), _stream(stream)),
+           "apack_copy_pages")
 
 
 def apack_device_error(ws, stream=None, clear=True):

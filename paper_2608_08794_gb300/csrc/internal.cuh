@@ -141,6 +141,11 @@ using CompactPlanPtr = std::unique_ptr<CompactPlan, CompactPlanDelete>;
 apack_status plan_compact(CompactPlan &plan, const int32_t *keep_idx, int64_t n_out, const apack_plane *planes,
                           int32_t num_groups, DeviceError *err);
 apack_status launch_compact(const CompactPlan &plan, cudaStream_t stream);
+// The driver's cuTensorMapEncodeTiled (null when it has none).
+using EncodeTiledFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                   const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled_fn();
 // 3-D TMA map over a K slab [tokens][hkv][128] bf16 (token_stride bytes between tokens):
 // boxes of 64 features x 1 head x box_tokens tokens, 128-byte swizzle.
 bool make_kv_tile_map(CUtensorMap *map, const void *k, int hkv, int64_t tokens, int64_t token_stride,

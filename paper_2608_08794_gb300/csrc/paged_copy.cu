@@ -1,0 +1,259 @@
+// paged_copy.cu -- rows and pages of paged caches moved: the compaction of Sec. 3.2 ("slice their KV-cache
+// entries") between pools (apack_paged_compact), and whole pages (apack_copy_pages).
+//
+// Bound by HBM: every byte is read once and written once.  A plane is K or V of one layer (of one head, where a
+// token's heads are not back to back).  A CTA resolves the page of each row of its run once and then moves those
+// rows in several planes.
+#include <algorithm>
+#include <cstring>
+
+#include "paged.cuh"
+
+namespace apack {
+namespace {
+
+constexpr int kRows = 32;              // rows whose addresses a CTA holds
+constexpr int kMoveThreads = 256;
+constexpr int kMoveUnroll = 8;         // 16-byte pieces a thread has in flight
+
+struct MovePlan {
+  PoolView src, dst;
+  int64_t n_rows;
+  int32_t num_seqs;
+  const int32_t *keep_idx, *cu_src, *cu_dst;
+  const int32_t *pairs;                // apack_copy_pages
+  int32_t layers, heads;               // planes = 2 * layers * heads
+  int32_t pieces;                      // 16-byte pieces of a row
+  FastDiv piece_div;
+  int32_t planes_cta, planes;
+  DeviceError *err;
+};
+
+// Sequence of output row j: the last b with cu[b] <= j.
+__device__ __forceinline__ int find_seq(const int32_t *cu, int n, int64_t j) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (__ldg(cu + mid) <= j) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// Source and destination byte offsets of output row j within a layer's planes (src -1: not copied).
+__device__ __forceinline__ void resolve(const MovePlan &P, int64_t j, int64_t *src, int64_t *dst) {
+  *src = -1;
+  *dst = -1;
+  if (j >= P.n_rows) return;
+  if (P.pairs) {
+    const uint32_t i = P.src.page_tokens.div(static_cast<uint32_t>(j)), r = static_cast<uint32_t>(j) - i * P.src.page_tokens.d;
+    const int32_t a = __ldg(P.pairs + 2 * static_cast<int64_t>(i)), b = __ldg(P.pairs + 2 * static_cast<int64_t>(i) + 1);
+    if (static_cast<uint32_t>(a) >= static_cast<uint32_t>(P.src.num_pages) ||
+        static_cast<uint32_t>(b) >= static_cast<uint32_t>(P.src.num_pages)) {
+      if (P.err) raise_device_error(P.err, APACK_EDEVICE, 92, a, b);
+      return;
+    }
+    *src = a * P.src.page_stride + r * P.src.token_stride;
+    *dst = b * P.src.page_stride + r * P.src.token_stride;
+    return;
+  }
+  if (j >= __ldg(P.cu_dst + P.num_seqs)) return;
+  const int b = find_seq(P.cu_dst, P.num_seqs, j);
+  const int32_t to = static_cast<int32_t>(j - __ldg(P.cu_dst + b));
+  int32_t from = to;
+  if (P.keep_idx) from = __ldg(P.keep_idx + j) - (P.cu_src ? __ldg(P.cu_src + b) : 0);
+  const int64_t s = P.src.row_offset(b, from), d = P.dst.row_offset(b, to);
+  if (s < 0 || d < 0) {
+    if (P.err) raise_device_error(P.err, APACK_EDEVICE, 91, b, static_cast<int32_t>(j));
+    return;
+  }
+  *src = s;
+  *dst = d;
+}
+
+__device__ __forceinline__ void plane_bases(const MovePlan &P, int plane, const uint8_t **src, uint8_t **dst) {
+  const int head = plane % P.heads, lp = plane / P.heads;
+  const int layer = lp >> 1;
+  const bool v = lp & 1;
+  *src = (v ? P.src.v : P.src.k) + layer * P.src.layer_stride + head * P.src.head_stride;
+  *dst = (v ? P.dst.v : P.dst.k) + layer * P.dst.layer_stride + head * P.dst.head_stride;
+}
+
+__global__ void __launch_bounds__(kMoveThreads) move_rows_kernel(const __grid_constant__ MovePlan P) {
+  __shared__ int64_t so[kRows], to[kRows];
+  pdl_wait_and_release();
+  if (threadIdx.x < kRows)
+    resolve(P, static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x, &so[threadIdx.x], &to[threadIdx.x]);
+  __syncthreads();
+  const int total = kRows * P.pieces;
+  const int p1 = min(P.planes, static_cast<int>(blockIdx.y + 1) * P.planes_cta);
+  for (int plane = blockIdx.y * P.planes_cta; plane < p1; ++plane) {
+    const uint8_t *src;
+    uint8_t *dst;
+    plane_bases(P, plane, &src, &dst);
+    for (int e0 = threadIdx.x; e0 < total; e0 += kMoveThreads * kMoveUnroll) {
+      uint4 x[kMoveUnroll];
+      uint8_t *at[kMoveUnroll];
+#pragma unroll
+      for (int u = 0; u < kMoveUnroll; ++u) {
+        const int e = e0 + u * kMoveThreads;
+        at[u] = nullptr;
+        if (e < total) {
+          const int r = P.piece_div.div(e), c = e - r * P.pieces;
+          if (so[r] >= 0) {
+            at[u] = dst + to[r] + c * 16;
+            x[u] = *reinterpret_cast<const uint4 *>(src + so[r] + c * 16);
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kMoveUnroll; ++u)
+        if (at[u]) *reinterpret_cast<uint4 *>(at[u]) = x[u];
+    }
+  }
+}
+
+// In place: output row j of a sequence reads row from(j) >= j of the same sequence, from ascending.  A warp owns
+// 128 bytes of every row of one plane of one sequence and walks the rows upwards, 32 at a time; the rows a step
+// reads are loaded whole before it writes, and no later step reads a row below those this step writes.  So no
+// warp waits for another.
+__global__ void __launch_bounds__(128) move_in_place_kernel(const __grid_constant__ MovePlan P, int segs, int64_t units) {
+  pdl_wait_and_release();
+  const int lane = threadIdx.x & 31;
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
+  if (unit >= units) return;
+  const int seg = static_cast<int>(unit % segs);
+  const int64_t rest = unit / segs;
+  const int plane = static_cast<int>(rest % P.planes), b = static_cast<int>(rest / P.planes);
+  const int64_t j0 = max(__ldg(P.cu_dst + b), 0), j1 = min(static_cast<int64_t>(__ldg(P.cu_dst + b + 1)), P.n_rows);
+  const uint8_t *src;
+  uint8_t *dst;
+  plane_bases(P, plane, &src, &dst);
+  const int c = seg * 8 + (lane & 7);
+  const bool mine = c < P.pieces;
+  const int64_t base = P.cu_src ? __ldg(P.cu_src + b) : 0;
+  for (int64_t j = j0; j < j1; j += 32) {
+    uint4 x[8];
+    uint8_t *at[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int64_t r = j + u * 4 + (lane >> 3);
+      at[u] = nullptr;
+      if (r < j1 && mine) {
+        const int32_t to = static_cast<int32_t>(r - j0);
+        const int64_t s = P.src.row_offset(b, static_cast<int32_t>(__ldg(P.keep_idx + r) - base));
+        const int64_t d = P.dst.row_offset(b, to);
+        if (s >= 0 && d >= 0) {
+          at[u] = dst + d + c * 16;
+          x[u] = *reinterpret_cast<const uint4 *>(src + s + c * 16);
+        } else if (P.err) {
+          raise_device_error(P.err, APACK_EDEVICE, 93, b, to);
+        }
+      }
+    }
+    __syncwarp();
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (at[u]) *reinterpret_cast<uint4 *>(at[u]) = x[u];
+    __syncwarp();
+  }
+}
+
+// Heads of a token back to back: one plane per layer and tensor.
+bool fused_heads(const apack_paged_cache *c) { return c->num_kv_heads == 1 || c->head_stride == c->head_dim * 2; }
+
+apack_status launch_move(MovePlan &P, const apack_paged_cache *a, const apack_paged_cache *b, int32_t layers,
+                         bool in_place, cudaStream_t stream) {
+  const bool fused = fused_heads(a) && fused_heads(b);
+  P.layers = layers;
+  P.heads = fused ? 1 : a->num_kv_heads;
+  P.pieces = a->head_dim / 8 * (fused ? a->num_kv_heads : 1);
+  P.piece_div = fast_div(P.pieces);
+  P.planes = 2 * layers * P.heads;
+  if (in_place) {
+    const int segs = (P.pieces + 7) / 8;
+    const int64_t units = static_cast<int64_t>(P.num_seqs) * P.planes * segs;
+    const int64_t grid = (units + 3) / 4;
+    if (grid > INT32_MAX) return APACK_EUNSUPPORTED;
+    if (check_cuda(launch_pdl(move_in_place_kernel, dim3(static_cast<unsigned>(grid)), dim3(128), 0, stream, P, segs, units)) != APACK_OK)
+      return APACK_ECUDA;
+    count_launches(1);
+    return APACK_OK;
+  }
+  const int64_t chunks = (P.n_rows + kRows - 1) / kRows;
+  // planes of a CTA: as many as leave 16 CTAs per SM
+  const int64_t want = 16 * static_cast<int64_t>(device_sm_count());
+  int64_t splits = std::min<int64_t>(P.planes, std::max<int64_t>(1, (want + chunks - 1) / chunks));
+  splits = std::max<int64_t>(splits, (P.planes + 65534) / 65535);
+  P.planes_cta = static_cast<int32_t>((P.planes + splits - 1) / splits);
+  splits = (P.planes + P.planes_cta - 1) / P.planes_cta;
+  if (check_cuda(launch_pdl(move_rows_kernel, dim3(static_cast<unsigned>(chunks), static_cast<unsigned>(splits)),
+                            dim3(kMoveThreads), 0, stream, P)) != APACK_OK)
+    return APACK_ECUDA;
+  count_launches(1);
+  return APACK_OK;
+}
+
+}  // namespace
+}  // namespace apack
+
+using namespace apack;
+
+extern "C" {
+
+apack_status apack_paged_compact(const apack_paged_cache *src, const apack_paged_cache *dst, int32_t src_layer,
+                                 int32_t dst_layer, int32_t num_layers, const int32_t *keep_idx,
+                                 const int32_t *cu_src, const int32_t *cu_dst, int64_t n_out, void *ws, void *stream) {
+  apack_status st = validate_pool(src, true);
+  if (st == APACK_OK) st = validate_pool(dst, true);
+  if (st != APACK_OK) return st;
+  if (src->num_kv_heads != dst->num_kv_heads || src->head_dim != dst->head_dim || src->dtype != dst->dtype ||
+      src->num_seqs != dst->num_seqs)
+    return APACK_EINVAL;
+  if (num_layers < 1 || src_layer < 0 || dst_layer < 0 || num_layers > src->num_layers - src_layer ||
+      num_layers > dst->num_layers - dst_layer || n_out < 0 || n_out > INT32_MAX || !cu_dst || (cu_src && !keep_idx))
+    return APACK_EINVAL;
+  if ((reinterpret_cast<uintptr_t>(keep_idx) | reinterpret_cast<uintptr_t>(cu_src) | reinterpret_cast<uintptr_t>(cu_dst) |
+       reinterpret_cast<uintptr_t>(ws)) & 3)
+    return APACK_EINVAL;
+  // the same memory on both sides is compacted in place, or refused
+  const bool in_place = src->k == dst->k || src->v == dst->v;
+  if (in_place && (src->k != dst->k || src->v != dst->v || src->page_table != dst->page_table ||
+                   src->table_stride != dst->table_stride || src->max_pages != dst->max_pages ||
+                   src->num_pages != dst->num_pages || src->page_tokens != dst->page_tokens ||
+                   src->page_stride != dst->page_stride || src->token_stride != dst->token_stride ||
+                   src->head_stride != dst->head_stride || src->layer_stride != dst->layer_stride ||
+                   src_layer != dst_layer || !keep_idx))
+    return APACK_EINVAL;
+  if (n_out == 0) return APACK_OK;
+  MovePlan P;
+  std::memset(&P, 0, sizeof(P));
+  P.src = pool_view(src, src_layer);
+  P.dst = pool_view(dst, dst_layer);
+  P.n_rows = n_out;
+  P.num_seqs = src->num_seqs;
+  P.keep_idx = keep_idx;
+  P.cu_src = cu_src;
+  P.cu_dst = cu_dst;
+  P.err = static_cast<DeviceError *>(ws);
+  return launch_move(P, src, dst, num_layers, in_place, static_cast<cudaStream_t>(stream));
+}
+
+apack_status apack_copy_pages(const apack_paged_cache *cache, const int32_t *pairs, int64_t n_pairs, void *ws,
+                              void *stream) {
+  const apack_status st = validate_pool(cache, false);
+  if (st != APACK_OK) return st;
+  if (n_pairs < 0 || n_pairs > INT32_MAX / cache->page_tokens) return APACK_EINVAL;
+  if (n_pairs == 0) return APACK_OK;
+  if (!pairs || ((reinterpret_cast<uintptr_t>(pairs) | reinterpret_cast<uintptr_t>(ws)) & 3)) return APACK_EINVAL;
+  MovePlan P;
+  std::memset(&P, 0, sizeof(P));
+  P.src = pool_view(cache, 0);
+  P.dst = P.src;
+  P.n_rows = n_pairs * cache->page_tokens;
+  P.num_seqs = 1;
+  P.pairs = pairs;
+  P.err = static_cast<DeviceError *>(ws);
+  return launch_move(P, cache, cache, cache->num_layers, false, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"

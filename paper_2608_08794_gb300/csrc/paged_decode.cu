@@ -1,0 +1,779 @@
+// paged_decode.cu -- attention of one decode token per sequence over a paged key-value cache
+// (the cost that Sec. 3.2's pruning shortens, over pages).
+//
+//   out[b, h] = sum_r softmax_r(scale q[b, h] . k[r, g(h)]) v[r, g(h)],  g(h) = h / (Hq / Hkv).
+//
+// Bound by HBM: K and V are read once, 4 D flop per query row and cached token.  With the G <= 8 query rows of a KV
+// head as the N = 8 of a warp-level matrix instruction (keys, then features, as M) nothing is padded, the scores
+// stay in registers from S^T = K Q^T over the softmax to O^T = V^T P^T, and no warp waits for another.
+//
+// Split over the cache's length.  The work is the list of all (sequence, head group, 16-token tile) in that
+// order; every CTA takes an equal contiguous share of it and finds its start from the lengths on the device,
+// so that the launch does not depend on them (a captured call follows growing caches).  Within a CTA each warp has
+// one KV head and every wph-th tile of the share, and its own ring of TMA stages: lane 0 refills a stage as soon
+// as the warp has used it.  At the end of a (sequence, head group) the warps of a head merge through shared
+// memory; what a share holds whole is written out, what it holds in part goes to the workspace, and a second
+// kernel merges those parts in order.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <numeric>
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "paged.cuh"
+#include "ptx.cuh"
+
+namespace apack {
+namespace {
+
+constexpr int kTile = 16;                       // tokens of a stage
+constexpr int kWarps = 8;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kMergeFloats = 3584;              // shared-memory buffer of the warps' merge: 7 warps, 4 m-tiles
+constexpr int kStageBytesCta = 196608;          // of all warps' rings
+// Accumulators are rescaled only when a row's maximum has grown by more than this (log2 units): sums stay
+// below 2^8 times their number, far inside fp32, and most tiles need one vote instead of the reduction.
+constexpr float kRescale = 8.f;
+
+struct PdPlan {
+  PoolView pool;
+  const int32_t *seqlens;
+  const uint8_t *q;
+  int64_t q_stride;                  // bytes between sequences
+  int32_t hq, group;                 // query heads, per KV head
+  int32_t heads_cta, wph, groups;    // KV heads of a CTA, warps per head, head groups
+  int32_t box_tokens, boxes;         // tokens of one TMA box, boxes of a tile
+  int32_t max_rows;
+  int32_t min_tiles;                 // smallest share of a CTA
+  float scale2;                      // scale * log2(e)
+  void *out;
+  int32_t out_fp32;
+  float *lse;
+  int4 *info;                        // [grid]: (sequence, head group, parts, first slot) of a cut segment that starts here
+  float2 *ml;                        // [slot][heads_cta * NT][8]
+  float *part;                       // [slot][heads_cta * NT][D / 16][128]
+  DeviceError *err;
+};
+
+template <class T>
+struct Half16;
+template <>
+struct Half16<__nv_bfloat16> {
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<uint32_t *>(&v);
+  }
+  static __device__ __forceinline__ float2 unpack(uint32_t w) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+  }
+  static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  }
+};
+template <>
+struct Half16<__half> {
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    __half2 v = __floats2half2_rn(a, b);
+    return *reinterpret_cast<uint32_t *>(&v);
+  }
+  static __device__ __forceinline__ float2 unpack(uint32_t w) { return __half22float2(*reinterpret_cast<__half2 *>(&w)); }
+  static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  }
+};
+
+__device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+// Transposes an 8 x 8 matrix of 16-bit elements held by the warp (lane: row lane / 4, columns 2 (lane % 4) and + 1).
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map, uint64_t *bar, int32_t c1, int32_t c2,
+                                            int32_t c3, int32_t c4) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], "
+      "[%2];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
+      : "memory");
+}
+
+__device__ __forceinline__ void head_barrier(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
+
+__device__ __forceinline__ int clamped_length(const PdPlan &P, int b, bool report) {
+  const int n = __ldg(P.seqlens + b);
+  const int c = min(max(n, 0), P.max_rows);
+  if (report && c != n) raise_device_error(P.err, APACK_EDEVICE, 81, b, n);
+  return c;
+}
+__device__ __forceinline__ int tiles_of(int len) { return (len >> 4) + ((len & 15) != 0); }
+
+// A walk over the (sequence, head group) segments of a share of the work list.
+struct Walk {
+  int b, g, len, nt;     // segment, its sequence's length and tiles
+  int ts, te;            // this share's tiles of it
+  int64_t left;          // tiles of the share behind te
+  __device__ __forceinline__ void span(int start) {
+    ts = start;
+    te = static_cast<int>(min(static_cast<int64_t>(nt), ts + left));
+    left -= te - ts;
+  }
+  __device__ __forceinline__ bool next(const PdPlan &P) {
+    if (left <= 0) return false;
+    if (++g >= P.groups) {
+      g = 0;
+      do {
+        len = clamped_length(P, ++b, false);
+      } while (len == 0);
+      nt = tiles_of(len);
+    }
+    span(0);
+    return true;
+  }
+};
+
+// Share of CTA c: tiles [share(c), share(c + 1)) of W over C CTAs.
+__device__ __forceinline__ int64_t share(int64_t W, int C, int c) { return W * c / C; }
+
+template <class T, int D, int NT>
+__global__ void __launch_bounds__(kThreads, 1)
+    paged_chunk_kernel(const __grid_constant__ PdPlan P, const __grid_constant__ CUtensorMap kmap,
+                       const __grid_constant__ CUtensorMap vmap) {
+  constexpr int KS = D / 16;                          // k-steps of S, m-tiles of O^T
+  constexpr int kHalf = kTile * D * 2;                // bytes of a stage's K (and V)
+  constexpr int kStages = kStageBytesCta / kWarps / (2 * kHalf);
+  constexpr int kBlk = kTile * 128;                   // bytes of one 64-feature block of a stage
+  extern __shared__ __align__(1024) uint8_t smem[];
+  float *merge = reinterpret_cast<float *>(smem + kStageBytesCta);
+  float2 *stat = reinterpret_cast<float2 *>(merge + kMergeFloats);        // [warp][NT * 8]
+  uint64_t *bars = reinterpret_cast<uint64_t *>(stat + kWarps * 32);      // [warp][kStages]
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint64_t *full = bars + warp * kStages;
+  const uint32_t ring = smem_u32(smem) + warp * (kStages * 2 * kHalf);
+  if (lane == 0) {
+    for (int i = 0; i < kStages; ++i) mbar_init(&full[i], 1);
+    fence_mbar_init();
+  }
+  __syncwarp();
+  pdl_wait_and_release();
+
+  // ---- this CTA's share (every warp by itself: no barrier before the first load)
+  const int B = P.pool.num_seqs, grid = gridDim.x, cta = blockIdx.x;
+  const int per = (B + 31) / 32;
+  int64_t mine = 0;
+  for (int i = 0; i < per; ++i) {
+    const int b = lane * per + i;
+    if (b < B) mine += tiles_of(clamped_length(P, b, warp == 0 && cta == 0));
+  }
+  int64_t incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o *= 2) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += y;
+  }
+  const int64_t W = __shfl_sync(0xffffffffu, incl, 31) * P.groups;
+  const int C = static_cast<int>(min(static_cast<int64_t>(grid), max(W / P.min_tiles, static_cast<int64_t>(1))));
+  if (threadIdx.x == 0) P.info[cta] = make_int4(0, 0, 0, 0);
+  // empty sequences: zeros and -infinity
+  for (int b = cta; b < B; b += grid) {
+    if (clamped_length(P, b, false) > 0) continue;
+    for (int i = threadIdx.x; i < P.hq * D; i += kThreads) {
+      const int64_t o = static_cast<int64_t>(b) * P.hq * D + i;
+      if (P.out_fp32)
+        static_cast<float *>(P.out)[o] = 0.f;
+      else
+        static_cast<uint16_t *>(P.out)[o] = 0;
+    }
+    if (P.lse)
+      for (int i = threadIdx.x; i < P.hq; i += kThreads) P.lse[static_cast<int64_t>(b) * P.hq + i] = -INFINITY;
+  }
+  const int hw = warp % P.heads_cta, sub = warp / P.heads_cta;
+  if (W == 0 || cta >= C || sub >= P.wph) return;
+  const int active = 32 * P.heads_cta * P.wph;        // threads of the warps at work
+  const int64_t u0 = share(W, C, cta), u1 = share(W, C, cta + 1);
+  Walk seg;
+  {
+    const int64_t lo = (incl - mine) * P.groups, hi = incl * P.groups;
+    const int src = __ffs(__ballot_sync(0xffffffffu, u0 >= lo && u0 < hi)) - 1;
+    int64_t off = u0 - __shfl_sync(0xffffffffu, lo, src);
+    int b = src * per;
+    for (;; ++b) {
+      seg.len = clamped_length(P, b, false);
+      seg.nt = tiles_of(seg.len);
+      if (off < static_cast<int64_t>(seg.nt) * P.groups) break;
+      off -= static_cast<int64_t>(seg.nt) * P.groups;
+    }
+    seg.b = b;
+    seg.g = static_cast<int>(off / seg.nt);
+    seg.left = u1 - u0;
+    seg.span(static_cast<int>(off - static_cast<int64_t>(seg.g) * seg.nt));
+  }
+
+  // ---- producer: the walk of this warp's tiles, kStages ahead of the consumer
+  Walk pw = seg;
+  int pt = pw.ts + sub;
+  bool more = true;
+  int32_t page = -1;                                  // of box `lane` of tile pt, read one tile ahead
+  uint32_t in_page = 0;
+  auto find = [&] {                                   // the next tile of this warp, and its page
+    while (pt >= pw.te) {
+      if (!pw.next(P)) {
+        more = false;
+        return;
+      }
+      pt = pw.ts + sub;
+    }
+    const int row = pt * kTile + lane * P.box_tokens;
+    if (lane < P.boxes && row < pw.len) {
+      const uint32_t p = P.pool.page_tokens.div(row);
+      page = __ldg(P.pool.table + pw.b * P.pool.table_stride + p);
+      in_page = row - p * P.pool.page_tokens.d;
+    } else {
+      page = INT32_MIN;                               // nothing to load
+    }
+  };
+  auto issue = [&](int slot) {
+    const int rows = pw.len - pt * kTile;             // boxes that hold a row of the sequence
+    const int nbox = min(P.boxes, (rows + P.box_tokens - 1) / P.box_tokens);
+    if (lane == 0) mbar_arrive_expect_tx(&full[slot], nbox * P.box_tokens * D * 4);
+    __syncwarp();
+    if (lane < nbox) {
+      if (static_cast<uint32_t>(page) >= static_cast<uint32_t>(P.pool.num_pages)) {
+        raise_device_error(P.err, APACK_EDEVICE, 82, pw.b, page);
+        page = P.pool.num_pages;                      // outside the map: reads as zeros
+      }
+      const int head = pw.g * P.heads_cta + hw;
+      const uint32_t dst = ring + slot * (2 * kHalf);
+      if (P.boxes == 1) {
+        tma_load_5d(dst, &kmap, &full[slot], in_page, 0, head, page);
+        tma_load_5d(dst + kHalf, &vmap, &full[slot], in_page, 0, head, page);
+      } else {
+        for (int blk = 0; blk < D / 64; ++blk) {
+          const uint32_t o = blk * kBlk + lane * P.box_tokens * 128;
+          tma_load_5d(dst + o, &kmap, &full[slot], in_page, blk, head, page);
+          tma_load_5d(dst + kHalf + o, &vmap, &full[slot], in_page, blk, head, page);
+        }
+      }
+    }
+  };
+  int issued = 0, used = 0;
+  find();
+  while (issued < kStages && more) {
+    issue(issued);
+    ++issued;
+    pt += P.wph;
+    find();
+  }
+
+  // ---- consumer
+  const int t4 = lane & 3, g8 = lane >> 2;
+  // ldmatrix rows of this lane: K fragments (keys x features) and, transposed, V fragments (features x keys)
+  const uint32_t krow = (lane & 7) + ((lane >> 3) & 1) * 8, kchunk = lane >> 4;
+  const uint32_t vrow = (lane & 7) + (lane >> 4) * 8, vchunk = (lane >> 3) & 1;
+  bool dead = false;                                  // a wait gave up: no more loads are issued or waited for
+  int first_seg = 1;
+  do {
+    const int head = seg.g * P.heads_cta + hw;
+    uint32_t qf[NT][KS][2];
+    {
+      const uint8_t *qb = P.q + seg.b * P.q_stride + static_cast<int64_t>(head) * P.group * D * 2;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int r = nt * 8 + g8;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            qf[nt][ks][e] = r < P.group ? __ldg(reinterpret_cast<const uint32_t *>(qb + (r * D + ks * 16 + e * 8 + t4 * 2) * 2)) : 0u;
+      }
+    }
+    float o[NT][KS][4], m[NT][2], l[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      m[nt][0] = m[nt][1] = -INFINITY;
+      l[nt][0] = l[nt][1] = 0.f;
+#pragma unroll
+      for (int i = 0; i < KS; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
+    }
+    for (int t = seg.ts + sub; t < seg.te; t += P.wph) {
+      if (dead) break;
+      const int slot = used % kStages;
+      if (!__all_sync(0xffffffffu, mbar_wait(&full[slot], (used / kStages) & 1u, kWaitLimitNs))) {
+        if (lane == 0) raise_device_error(P.err, APACK_ETIMEOUT, 83, cta, warp);
+        dead = true;
+        break;
+      }
+      ++used;
+      const uint32_t kb = ring + slot * (2 * kHalf), vb = kb + kHalf;
+      const int valid = seg.len - t * kTile;          // rows of the tile that belong to the sequence
+      if (valid < kTile) {
+        // what lies behind the last row takes no part: its logits become -infinity below, and its values
+        // zeros here (0 times a stale infinity would be NaN)
+        for (int i = lane; i < (kTile - valid) * (D / 8); i += 32) {
+          const int row = valid + i / (D / 8), ch = i % (D / 8);
+          const uint32_t a = vb + (ch >> 3) * kBlk + row * 128 + (ch & 7) * 16;
+          asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(a), "r"(0) : "memory");
+        }
+        fence_proxy_async_smem();                     // before TMA writes the slot again
+        __syncwarp();
+      }
+      float s[NT][4];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        uint32_t a[4];
+        const uint32_t ch = ks * 2 + kchunk;
+        ldmatrix4(kb + (ch >> 3) * kBlk + krow * 128 + (((ch & 7) ^ (krow & 7)) << 4), a);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) Half16<T>::mma(s[nt], a, qf[nt][ks][0], qf[nt][ks][1]);
+      }
+      // lane: keys g8 and g8 + 8, query rows 2 t4 and 2 t4 + 1
+      bool grow = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[nt][i] = (g8 + (i >> 1) * 8) < valid ? s[nt][i] * P.scale2 : -INFINITY;
+          grow |= !(s[nt][i] <= m[nt][i & 1] + kRescale);
+        }
+      }
+      if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float x = fmaxf(s[nt][e], s[nt][e + 2]);
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+            const float mn = fmaxf(m[nt][e], x);
+            const float f = mn == -INFINITY ? 1.f : ex2_approx(m[nt][e] - mn);
+            m[nt][e] = mn;
+            l[nt][e] *= f;
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+              o[nt][i][e] *= f;
+              o[nt][i][e + 2] *= f;
+            }
+          }
+      }
+      // P as the sum of two 16-bit numbers (2^-17 of it are left out in bf16, 2^-22 in fp16; one alone would cost
+      // 2^-9), transposed into B fragments
+      uint32_t hi[NT][2], lo[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = ex2_approx(s[nt][i] - m[nt][i & 1]);
+        l[nt][0] += p[0] + p[2];
+        l[nt][1] += p[1] + p[3];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t h = Half16<T>::pack(p[2 * e], p[2 * e + 1]);
+          const float2 hf = Half16<T>::unpack(h);
+          hi[nt][e] = transpose8x8(h);
+          lo[nt][e] = transpose8x8(Half16<T>::pack(p[2 * e] - hf.x, p[2 * e + 1] - hf.y));
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        uint32_t a[4];
+        const uint32_t ch = i * 2 + vchunk;
+        ldmatrix4_trans(vb + (ch >> 3) * kBlk + vrow * 128 + (((ch & 7) ^ (vrow & 7)) << 4), a);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          Half16<T>::mma(o[nt][i], a, hi[nt][0], hi[nt][1]);
+          Half16<T>::mma(o[nt][i], a, lo[nt][0], lo[nt][1]);
+        }
+      }
+      __syncwarp();                                   // every lane has read the stage
+      if (more) {
+        issue(slot);
+        ++issued;
+        pt += P.wph;
+        find();
+      }
+    }
+
+    // ---- end of the segment: the warps of each head merge
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float x = l[nt][e];
+        x += __shfl_xor_sync(0xffffffffu, x, 4);
+        x += __shfl_xor_sync(0xffffffffu, x, 8);
+        x += __shfl_xor_sync(0xffffffffu, x, 16);
+        l[nt][e] = x;
+      }
+    if (P.wph > 1) {
+      if (g8 == 0)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) stat[warp * 32 + nt * 8 + t4 * 2 + e] = make_float2(m[nt][e], l[nt][e]);
+      head_barrier(active);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float M = -INFINITY, L = 0.f;
+          for (int w = 0; w < P.wph; ++w) M = fmaxf(M, stat[(w * P.heads_cta + hw) * 32 + nt * 8 + t4 * 2 + e].x);
+          for (int w = 0; w < P.wph; ++w) {
+            const float2 x = stat[(w * P.heads_cta + hw) * 32 + nt * 8 + t4 * 2 + e];
+            L += x.y * (x.x == M ? 1.f : ex2_approx(x.x - M));
+          }
+          const float f = m[nt][e] == M ? 1.f : ex2_approx(m[nt][e] - M);
+          m[nt][e] = M;
+          l[nt][e] = L;
+#pragma unroll
+          for (int i = 0; i < KS; ++i) {
+            o[nt][i][e] *= f;
+            o[nt][i][e + 2] *= f;
+          }
+        }
+      // through a buffer, kSlice m-tiles at a time ((wph - 1) * heads_cta is at most 7)
+      constexpr int kSlice = 4 / NT;
+      float4 *buf = reinterpret_cast<float4 *>(merge);
+#pragma unroll
+      for (int i0 = 0; i0 < KS; i0 += kSlice) {
+        if (sub > 0)
+#pragma unroll
+          for (int k = 0; k < kSlice; ++k)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              const float(&x)[4] = o[nt][i0 + k];
+              buf[((((sub - 1) * P.heads_cta + hw) * kSlice + k) * NT + nt) * 32 + lane] = make_float4(x[0], x[1], x[2], x[3]);
+            }
+        head_barrier(active);
+        if (sub == 0)
+          for (int w = 1; w < P.wph; ++w)
+#pragma unroll
+            for (int k = 0; k < kSlice; ++k)
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                const float4 x = buf[((((w - 1) * P.heads_cta + hw) * kSlice + k) * NT + nt) * 32 + lane];
+                float(&y)[4] = o[nt][i0 + k];
+                y[0] += x.x;
+                y[1] += x.y;
+                y[2] += x.z;
+                y[3] += x.w;
+              }
+        head_barrier(active);
+      }
+    }
+    if (sub == 0) {
+      if (seg.ts == 0 && seg.te == seg.nt) {          // the whole segment: write it out
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int r = nt * 8 + t4 * 2 + e;
+            if (r >= P.group) continue;
+            const int64_t row = static_cast<int64_t>(seg.b) * P.hq + head * P.group + r;
+            const float inv = l[nt][e] == 0.f ? 0.f : 1.f / l[nt][e];
+            if (P.lse && g8 == 0) P.lse[row] = (m[nt][e] + log2f(l[nt][e])) * 0.6931471805599453f;
+#pragma unroll
+            for (int i = 0; i < KS; ++i)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const int64_t at = row * D + i * 16 + h * 8 + g8;
+                const float x = o[nt][i][e + 2 * h] * inv;
+                if (P.out_fp32)
+                  static_cast<float *>(P.out)[at] = x;
+                else
+                  static_cast<T *>(P.out)[at] = static_cast<T>(x);
+              }
+          }
+      } else {
+        const int slot = 2 * cta + (first_seg ? 0 : 1);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const int64_t at = (static_cast<int64_t>(slot) * P.heads_cta + hw) * NT + nt;
+          if (g8 == 0) {
+            P.ml[at * 8 + t4 * 2] = make_float2(m[nt][0], l[nt][0]);
+            P.ml[at * 8 + t4 * 2 + 1] = make_float2(m[nt][1], l[nt][1]);
+          }
+          float4 *pp = reinterpret_cast<float4 *>(P.part) + at * KS * 32 + lane;
+#pragma unroll
+          for (int i = 0; i < KS; ++i) pp[i * 32] = make_float4(o[nt][i][0], o[nt][i][1], o[nt][i][2], o[nt][i][3]);
+        }
+        if (threadIdx.x == 0 && seg.ts == 0) {
+          // this share starts the segment; the one that holds its last tile ends it
+          const int64_t last = u1 - (seg.te - seg.ts) - seg.left + seg.nt - 1;
+          const int c_end = static_cast<int>(((last + 1) * C + W - 1) / W) - 1;
+          P.info[cta] = make_int4(seg.b, seg.g, c_end - cta + 1, slot);
+        }
+      }
+    }
+    first_seg = 0;
+  } while (seg.next(P));
+  if (dead)   // loads of the stages that were issued and not used may still be in flight
+    for (int n = used; n < issued; ++n) mbar_wait(&full[n % kStages], (n / kStages) & 1u, kWaitLimitNs / 4);
+}
+
+// Merges the parts of the cut segments.  A CTA first counts the shares that start one (info); its warps then take
+// (segment, head, 8 query rows, 16 features) units in turn, each warp a run of the parts in order, and
+// merge in warp order.
+constexpr int kCombineWarps = 8;
+constexpr int kCombineBatch = 8;       // parts whose loads are in flight
+constexpr int kMaxGrid = 1024;
+
+template <class T, int D, int NT>
+__global__ void __launch_bounds__(32 * kCombineWarps)
+    paged_combine_kernel(const __grid_constant__ PdPlan P, int grid) {
+  constexpr int KS = D / 16;
+  __shared__ int lead[kMaxGrid];
+  __shared__ int n_lead;
+  __shared__ float4 so[kCombineWarps][32];
+  __shared__ float4 sml[kCombineWarps][4];     // (m, l) of query rows 2 t, 2 t + 1
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  pdl_wait_and_release();
+  if (warp == 0) {
+    int n = 0;
+    for (int c = 0; c < grid; c += 32) {
+      const bool is = c + lane < grid && P.info[c + lane].z > 0;
+      const unsigned mask = __ballot_sync(0xffffffffu, is);
+      if (is) lead[n + __popc(mask & ((1u << lane) - 1))] = c + lane;
+      n += __popc(mask);
+    }
+    if (lane == 0) n_lead = n;
+  }
+  __syncthreads();
+  const int per_seg = P.heads_cta * NT * KS;
+  const int t4 = lane & 3, g8 = lane >> 2;
+  for (int u = blockIdx.x; u < n_lead * per_seg; u += gridDim.x) {
+    const int c = lead[u / per_seg], rest = u % per_seg;
+    const int hn = rest / KS, i = rest % KS;                       // (head of the group, 8 rows), 16 features
+    const int4 inf = P.info[c];
+    const int parts = inf.z;
+    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int p0 = parts * warp / kCombineWarps, p1 = parts * (warp + 1) / kCombineWarps;
+    for (int p = p0; p < p1; p += kCombineBatch) {
+      float4 ml[kCombineBatch], x[kCombineBatch];
+#pragma unroll
+      for (int k = 0; k < kCombineBatch; ++k) {
+        ml[k] = make_float4(-INFINITY, 0.f, -INFINITY, 0.f);
+        x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (p + k < p1) {
+          const int slot = p + k == 0 ? inf.w : 2 * (c + p + k);
+          const int64_t at = static_cast<int64_t>(slot) * P.heads_cta * NT + hn;
+          ml[k] = *reinterpret_cast<const float4 *>(P.ml + at * 8 + t4 * 2);
+          x[k] = reinterpret_cast<const float4 *>(P.part)[(at * KS + i) * 32 + lane];
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kCombineBatch; ++k) {
+        if (p + k >= p1) break;
+        const float n0 = fmaxf(m0, ml[k].x), n1 = fmaxf(m1, ml[k].z);
+        const float a0 = m0 == n0 ? 1.f : ex2_approx(m0 - n0), b0 = ml[k].x == n0 ? 1.f : ex2_approx(ml[k].x - n0);
+        const float a1 = m1 == n1 ? 1.f : ex2_approx(m1 - n1), b1 = ml[k].z == n1 ? 1.f : ex2_approx(ml[k].z - n1);
+        l0 = l0 * a0 + ml[k].y * b0;
+        l1 = l1 * a1 + ml[k].w * b1;
+        acc.x = acc.x * a0 + x[k].x * b0;
+        acc.y = acc.y * a1 + x[k].y * b1;
+        acc.z = acc.z * a0 + x[k].z * b0;
+        acc.w = acc.w * a1 + x[k].w * b1;
+        m0 = n0;
+        m1 = n1;
+      }
+    }
+    so[warp][lane] = acc;
+    if (g8 == 0) sml[warp][t4] = make_float4(m0, l0, m1, l1);
+    __syncthreads();
+    if (warp == 0) {
+      float M0 = -INFINITY, M1 = -INFINITY, L0 = 0.f, L1 = 0.f;
+      float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kCombineWarps; ++w) {
+        const float4 s = sml[w][t4];
+        M0 = fmaxf(M0, s.x);
+        M1 = fmaxf(M1, s.z);
+      }
+#pragma unroll
+      for (int w = 0; w < kCombineWarps; ++w) {
+        const float4 s = sml[w][t4], x = so[w][lane];
+        const float a0 = s.x == M0 ? 1.f : ex2_approx(s.x - M0), a1 = s.z == M1 ? 1.f : ex2_approx(s.z - M1);
+        L0 += s.y * a0;
+        L1 += s.w * a1;
+        O.x += x.x * a0;
+        O.y += x.y * a1;
+        O.z += x.z * a0;
+        O.w += x.w * a1;
+      }
+      const int head = inf.y * P.heads_cta + hn / NT;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = (hn % NT) * 8 + t4 * 2 + e;
+        if (r >= P.group) continue;
+        const int64_t row = static_cast<int64_t>(inf.x) * P.hq + head * P.group + r;
+        const float L = e ? L1 : L0, inv = L == 0.f ? 0.f : 1.f / L;
+        if (P.lse && i == 0 && g8 == 0) P.lse[row] = ((e ? M1 : M0) + log2f(L)) * 0.6931471805599453f;
+        const float x0 = (e ? O.y : O.x) * inv, x1 = (e ? O.w : O.z) * inv;
+        const int64_t at = row * D + i * 16 + g8;
+        if (P.out_fp32) {
+          static_cast<float *>(P.out)[at] = x0;
+          static_cast<float *>(P.out)[at + 8] = x1;
+        } else {
+          static_cast<T *>(P.out)[at] = static_cast<T>(x0);
+          static_cast<T *>(P.out)[at + 8] = static_cast<T>(x1);
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------ host side
+struct PdShape {
+  int group, nt, heads_cta, wph, groups, grid;
+  size_t info_off, ml_off, part_off, total;
+};
+
+apack_status plan_shape(const apack_paged_cache *c, int32_t hq, PdShape *s) {
+  if (hq < 1 || hq > 1024 || hq % c->num_kv_heads != 0) return APACK_EINVAL;
+  s->group = hq / c->num_kv_heads;
+  if (s->group > 32) return APACK_EUNSUPPORTED;
+  s->nt = s->group > 16 ? 4 : s->group > 8 ? 2 : 1;
+  // KV heads of a CTA: the largest divisor of their number that its warps cover
+  s->heads_cta = 1;
+  for (int h = 1; h <= kWarps; ++h)
+    if (c->num_kv_heads % h == 0) s->heads_cta = h;
+  s->wph = kWarps / s->heads_cta;
+  s->groups = c->num_kv_heads / s->heads_cta;
+  s->grid = std::min(device_sm_count(), kMaxGrid);
+  auto up = [](size_t x) { return (x + 255) & ~static_cast<size_t>(255); };
+  const size_t rows = static_cast<size_t>(2 * s->grid) * s->heads_cta * s->nt * 8;
+  s->info_off = 256;
+  s->ml_off = up(s->info_off + s->grid * sizeof(int4));
+  s->part_off = up(s->ml_off + rows * sizeof(float2));
+  s->total = up(s->part_off + rows * c->head_dim * sizeof(float));
+  return APACK_OK;
+}
+
+constexpr size_t kSmem = kStageBytesCta + kMergeFloats * sizeof(float) + kWarps * 32 * sizeof(float2) +
+                         kWarps * 8 * sizeof(uint64_t);
+
+template <class T, int D, int NT>
+cudaError_t launch_paged(const PdPlan &P, const CUtensorMap &kmap, const CUtensorMap &vmap, int grid,
+                         cudaStream_t stream) {
+  static std::atomic<uint64_t> attr{0};
+  cudaError_t e = once_per_device(attr, [] {
+    return cudaFuncSetAttribute(paged_chunk_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                static_cast<int>(kSmem));
+  });
+  if (e != cudaSuccess) return e;
+  e = launch_pdl(paged_chunk_kernel<T, D, NT>, dim3(grid), dim3(kThreads), kSmem, stream, P, kmap, vmap);
+  if (e != cudaSuccess) return e;
+  count_launches(1);
+  e = launch_pdl(paged_combine_kernel<T, D, NT>, dim3(grid), dim3(32 * kCombineWarps), 0, stream, P, grid);
+  if (e == cudaSuccess) count_launches(1);
+  return e;
+}
+
+template <class T>
+cudaError_t launch_typed(const PdPlan &P, int D, int NT, const CUtensorMap &kmap, const CUtensorMap &vmap, int grid,
+                         cudaStream_t s) {
+  if (D == 128) {
+    if (NT == 1) return launch_paged<T, 128, 1>(P, kmap, vmap, grid, s);
+    if (NT == 2) return launch_paged<T, 128, 2>(P, kmap, vmap, grid, s);
+    return launch_paged<T, 128, 4>(P, kmap, vmap, grid, s);
+  }
+  if (NT == 1) return launch_paged<T, 64, 1>(P, kmap, vmap, grid, s);
+  if (NT == 2) return launch_paged<T, 64, 2>(P, kmap, vmap, grid, s);
+  return launch_paged<T, 64, 4>(P, kmap, vmap, grid, s);
+}
+
+}  // namespace
+}  // namespace apack
+
+using namespace apack;
+
+extern "C" {
+
+apack_status apack_paged_decode_workspace_size(const apack_paged_cache *cache, int32_t num_q_heads, size_t *bytes) {
+  if (!bytes) return APACK_EINVAL;
+  apack_status st = validate_pool(cache, true);
+  if (st != APACK_OK) return st;
+  PdShape s;
+  st = plan_shape(cache, num_q_heads, &s);
+  if (st == APACK_OK) *bytes = s.total;
+  return st;
+}
+
+apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_t layer, const int32_t *seqlens,
+                                          const void *q, int64_t q_token_stride, int32_t num_q_heads, float scale,
+                                          void *out, int32_t out_dtype, float *lse, void *ws, size_t ws_bytes,
+                                          void *stream) {
+  apack_status st = validate_pool(cache, true);
+  if (st != APACK_OK) return st;
+  PdShape s;
+  st = plan_shape(cache, num_q_heads, &s);
+  if (st != APACK_OK) return st;
+  if (layer < 0 || layer >= cache->num_layers || !seqlens || !q || !out || !ws || !(scale > 0.f) || !std::isfinite(scale))
+    return APACK_EINVAL;
+  if (out_dtype != cache->dtype && out_dtype != APACK_FP32) return APACK_EINVAL;
+  const int64_t row = static_cast<int64_t>(num_q_heads) * cache->head_dim * 2;
+  if ((reinterpret_cast<uintptr_t>(q) & 15) || (q_token_stride & 15) || (cache->num_seqs > 1 && q_token_stride < row) ||
+      (reinterpret_cast<uintptr_t>(out) & 15) || (reinterpret_cast<uintptr_t>(ws) & 255) ||
+      ((reinterpret_cast<uintptr_t>(seqlens) | reinterpret_cast<uintptr_t>(lse)) & 3))
+    return APACK_EINVAL;
+  if (ws_bytes < s.total) return APACK_EWORKSPACE;
+  if (!on_current_device(cache->k) || !on_current_device(cache->v)) return APACK_EINVAL;   // read by TMA
+  PdPlan P;
+  std::memset(&P, 0, sizeof(P));
+  P.pool = pool_view(cache, layer);
+  P.seqlens = seqlens;
+  P.q = static_cast<const uint8_t *>(q);
+  P.q_stride = q_token_stride;
+  P.hq = num_q_heads;
+  P.group = s.group;
+  P.heads_cta = s.heads_cta;
+  P.wph = s.wph;
+  P.groups = s.groups;
+  P.box_tokens = std::gcd(cache->page_tokens, kTile);
+  P.boxes = kTile / P.box_tokens;
+  P.max_rows = static_cast<int32_t>(
+      std::min<int64_t>(INT32_MAX - kTile, static_cast<int64_t>(cache->max_pages) * cache->page_tokens));
+  P.min_tiles = s.wph;
+  P.scale2 = scale * 1.4426950408889634f;
+  P.out = out;
+  P.out_fp32 = out_dtype == APACK_FP32;
+  P.lse = lse;
+  uint8_t *w = static_cast<uint8_t *>(ws);
+  P.info = reinterpret_cast<int4 *>(w + s.info_off);
+  P.ml = reinterpret_cast<float2 *>(w + s.ml_off);
+  P.part = reinterpret_cast<float *>(w + s.part_off);
+  P.err = static_cast<DeviceError *>(ws);
+  CUtensorMap kmap, vmap;
+  const uint32_t blocks = P.boxes == 1 ? cache->head_dim / 64 : 1;
+  if (!make_page_map(&kmap, cache, P.pool.k, P.box_tokens, blocks) ||
+      !make_page_map(&vmap, cache, P.pool.v, P.box_tokens, blocks))
+    return APACK_ECUDA;
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  return check_cuda(cache->dtype == APACK_BF16
+                        ? launch_typed<__nv_bfloat16>(P, cache->head_dim, s.nt, kmap, vmap, s.grid, cs)
+                        : launch_typed<__half>(P, cache->head_dim, s.nt, kmap, vmap, s.grid, cs));
+}
+
+}  // extern "C"

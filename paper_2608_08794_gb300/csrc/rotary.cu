@@ -1,0 +1,369 @@
+// rotary.cu -- rotary positions of packed token rows, alone (apack_rotary) or with the write of new
+// tokens into the pages of a cache (apack_rotary_append).
+//
+// Pair i of a head turns by t = position * freq[i]; (a, b) -> m (a cos t - b sin t, b cos t + a sin t).
+// The transposed map (the gradient) turns by -t.
+//
+// Angles: in 32 bits position * freq loses the angle of far positions (at 10^6 radians one ulp is 0.06).
+// The host turns each frequency into 64-bit fixed point, in turns; position * freq mod 2^64 is then the
+// phase with whole turns dropped, exactly, in one integer multiplication, for negative positions too.  Its top
+// 32 bits as a signed fraction of a half turn go to sincospif.
+//
+// Bound by HBM: a row is read once and written once; 2 sincospif a pair are shared by all heads of a token.  A
+// thread owns one 16-byte chunk position of a head (both halves of its pairs) and keeps its (cos, sin) in registers
+// over the heads it walks through, so that the division by the head's chunks is done once per thread.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "paged.cuh"
+
+namespace apack {
+namespace {
+
+constexpr int kRotThreads = 256;
+constexpr int kMaxPairs = 128;          // head_dim <= 256
+constexpr int kRotUnroll = 4;           // heads whose loads a thread has in flight
+
+struct RotPlan {
+  uint64_t freq[kMaxPairs];             // 2^-64 turns per position
+  float magnitude;
+  int32_t pairs, axis1, axis2;          // pairs from axis1 on take axis 1, from axis2 on axis 2
+  int32_t n1, n2;                       // chunk positions of a head: rotated, passed through
+  int32_t half_off;                     // elements from a chunk to its partner (HALF)
+  int32_t head_slots, tok_slots;        // a CTA's threads: chunk positions x head_slots x tok_slots
+  int32_t heads, rot_heads, q_heads;    // heads in all; the first rot_heads are rotated; q_heads of them are q
+  int32_t kv_heads, head_dim;
+  int64_t n_tokens;
+  const uint8_t *x, *k, *v;
+  uint8_t *out;
+  int64_t xs, ks, vs, outs;             // token strides in bytes
+  const int32_t *positions;
+  int64_t pos_axis_stride;
+  const int32_t *rows, *seqs;
+  PoolView pool;
+  DeviceError *err;
+};
+
+template <class T>
+struct Elem;
+template <>
+struct Elem<__nv_bfloat16> {
+  static __device__ float to(__nv_bfloat16 v) { return __bfloat162float(v); }
+  static __device__ __nv_bfloat16 from(float v) { return __float2bfloat16_rn(v); }
+};
+template <>
+struct Elem<__half> {
+  static __device__ float to(__half v) { return __half2float(v); }
+  static __device__ __half from(float v) { return __float2half_rn(v); }
+};
+template <>
+struct Elem<float> {
+  static __device__ float to(float v) { return v; }
+  static __device__ float from(float v) { return v; }
+};
+
+// V consecutive elements, moved in one access (V = 1, or 16 bytes).
+template <class T, int V>
+struct __align__(sizeof(T) * V) Chunk {
+  T e[V];
+};
+
+// V: elements of an access.  PAIRS: neighbouring elements form a pair; a chunk then holds its pairs whole (V = 1:
+// two accesses, as in the HALF layout with the partner one element on).  APPEND: k and v go to pages.
+template <class T, int V, bool PAIRS, bool APPEND>
+__global__ void __launch_bounds__(kRotThreads) rotary_kernel(const __grid_constant__ RotPlan P, float sign) {
+  using C = Chunk<T, V>;
+  constexpr bool kSplit = !PAIRS || V == 1;            // a rotated chunk has a partner chunk
+  constexpr int kAngles = kSplit ? V : V / 2;          // pairs of a chunk position
+  __shared__ float2 cs[2 * kRotThreads * 4];           // [token slot][pair]
+  __shared__ int64_t slot[kRotThreads];                // byte offset of a token's slot, -1: none
+  pdl_wait_and_release();
+  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * P.tok_slots;
+  const int pairs = P.pairs;
+  for (int e = threadIdx.x; e < P.tok_slots * pairs; e += kRotThreads) {
+    const int tok = e / pairs, i = e - tok * pairs;
+    if (t0 + tok >= P.n_tokens) break;
+    const int axis = (i >= P.axis1) + (i >= P.axis2);
+    const int64_t pos = __ldg(P.positions + axis * P.pos_axis_stride + t0 + tok);
+    const uint64_t phase = static_cast<uint64_t>(pos) * P.freq[i];
+    float s, c;
+    sincospif(static_cast<float>(static_cast<int32_t>(phase >> 32)) * 4.656612873077393e-10f, &s, &c);   // 2^-31
+    cs[e] = make_float2(P.magnitude * c, sign * P.magnitude * s);
+  }
+  if (APPEND && threadIdx.x < P.tok_slots && t0 + threadIdx.x < P.n_tokens) {
+    const int64_t t = t0 + threadIdx.x;
+    const int32_t row = __ldg(P.rows + t);
+    const int32_t seq = P.seqs ? __ldg(P.seqs + t) : static_cast<int32_t>(t);
+    int64_t off = -1;
+    if (row >= 0) {
+      if (static_cast<uint32_t>(seq) < static_cast<uint32_t>(P.pool.num_seqs)) off = P.pool.row_offset(seq, row);
+      if (off < 0 && P.err) raise_device_error(P.err, APACK_EDEVICE, 71, seq, row);
+    }
+    slot[threadIdx.x] = off;
+  }
+  __syncthreads();
+  const int n = P.n1 + P.n2;
+  const int c = threadIdx.x % n, rest = threadIdx.x / n;
+  const int h0 = rest % P.head_slots, tok = rest / P.head_slots;
+  const int64_t t = t0 + tok;
+  if (tok >= P.tok_slots || t >= P.n_tokens) return;
+  const bool turns = c < P.n1;
+  // this thread's elements of a head: first .. first + V, and the partner's
+  const int first = turns ? (PAIRS && V == 1 ? 2 * c : c * V) : 2 * pairs + (c - P.n1) * V;
+  const int partner = first + (PAIRS ? 1 : P.half_off);
+  float2 a[kAngles];
+  if (turns) {
+#pragma unroll
+    for (int j = 0; j < kAngles; ++j) a[j] = cs[tok * pairs + c * kAngles + j];
+  }
+  const int64_t off = APPEND ? slot[tok] : 0;
+  const int hd = P.head_dim;
+  for (int hb = h0; hb < P.heads; hb += kRotUnroll * P.head_slots) {
+    C lo[kRotUnroll], hi[kRotUnroll];
+    T *dst[kRotUnroll];
+#pragma unroll
+    for (int u = 0; u < kRotUnroll; ++u) {
+      const int h = hb + u * P.head_slots;
+      dst[u] = nullptr;
+      if (h >= P.heads) continue;
+      const uint8_t *src;
+      if (!APPEND || h < P.q_heads) {
+        const int64_t ho = static_cast<int64_t>(h) * hd * sizeof(T);
+        src = P.x + t * P.xs + ho;
+        dst[u] = reinterpret_cast<T *>(P.out + t * P.outs + ho);
+      } else {
+        const int kh = h - P.q_heads;
+        const bool is_v = kh >= P.kv_heads;
+        const int hh = is_v ? kh - P.kv_heads : kh;
+        if (off < 0) continue;
+        src = (is_v ? P.v + t * P.vs : P.k + t * P.ks) + static_cast<int64_t>(hh) * hd * sizeof(T);
+        dst[u] = reinterpret_cast<T *>((is_v ? P.pool.v : P.pool.k) + off + hh * P.pool.head_stride);
+      }
+      const T *s = reinterpret_cast<const T *>(src);
+      lo[u] = *reinterpret_cast<const C *>(s + first);
+      if (kSplit && turns) hi[u] = *reinterpret_cast<const C *>(s + partner);
+    }
+#pragma unroll
+    for (int u = 0; u < kRotUnroll; ++u) {
+      if (!dst[u]) continue;
+      if (turns && hb + u * P.head_slots < P.rot_heads) {
+#pragma unroll
+        for (int j = 0; j < kAngles; ++j) {
+          T &pa = kSplit ? lo[u].e[j] : lo[u].e[(2 * j) % V];
+          T &pb = kSplit ? hi[u].e[j] : lo[u].e[(2 * j + 1) % V];
+          const float x = Elem<T>::to(pa), y = Elem<T>::to(pb);
+          pa = Elem<T>::from(x * a[j].x - y * a[j].y);
+          pb = Elem<T>::from(y * a[j].x + x * a[j].y);
+        }
+      }
+      *reinterpret_cast<C *>(dst[u] + first) = lo[u];
+      if (kSplit && turns) *reinterpret_cast<C *>(dst[u] + partner) = hi[u];
+    }
+  }
+}
+
+template <class T, bool APPEND>
+cudaError_t launch_rotary(RotPlan &P, bool pairs_layout, bool wide, float sign, cudaStream_t stream) {
+  constexpr int W = 16 / sizeof(T);
+  const int D = P.head_dim, r = 2 * P.pairs;
+  const int V = wide ? W : 1;
+  P.n1 = (pairs_layout && V > 1) ? r / V : r / 2 / V;
+  P.n2 = (D - r) / V;
+  P.half_off = r / 2;
+  const int n = P.n1 + P.n2;
+  // one thread per head as far as the CTA reaches; more tokens per CTA only when there are enough CTAs
+  const int room = kRotThreads / n;
+  P.head_slots = std::min(P.heads, room);
+  P.tok_slots = 1;
+  const int64_t sms = device_sm_count();
+  if (P.n_tokens >= 4 * sms) {
+    P.head_slots = std::min(std::max(1, (P.heads + kRotUnroll - 1) / kRotUnroll), room);
+    P.tok_slots = room / P.head_slots;
+  }
+  const int64_t grid = (P.n_tokens + P.tok_slots - 1) / P.tok_slots;
+  void (*fn)(RotPlan, float);
+  if (wide)
+    fn = pairs_layout ? rotary_kernel<T, W, true, APPEND> : rotary_kernel<T, W, false, APPEND>;
+  else
+    fn = pairs_layout ? rotary_kernel<T, 1, true, APPEND> : rotary_kernel<T, 1, false, APPEND>;
+  const cudaError_t e = launch_pdl(fn, dim3(static_cast<unsigned>(grid)), dim3(kRotThreads), 0, stream, P, sign);
+  if (e == cudaSuccess) count_launches(1);
+  return e;
+}
+
+apack_status plan_spec(const apack_rotary_spec *s, int32_t head_dim, RotPlan &P) {
+  if (s->layout != APACK_ROTARY_HALF && s->layout != APACK_ROTARY_PAIRS) return APACK_EINVAL;
+  if (s->rotary_dim < 2 || s->rotary_dim > head_dim || (s->rotary_dim & 1) || !s->freq_h) return APACK_EINVAL;
+  if (s->num_axes < 1 || s->num_axes > 3 || !std::isfinite(s->magnitude)) return APACK_EINVAL;
+  P.pairs = s->rotary_dim / 2;
+  P.axis1 = P.axis2 = P.pairs;
+  if (s->num_axes > 1) {
+    int64_t sum = 0;
+    for (int a = 0; a < s->num_axes; ++a) {
+      if (s->section[a] < 0) return APACK_EINVAL;
+      sum += s->section[a];
+    }
+    if (sum != P.pairs) return APACK_EINVAL;
+    P.axis1 = s->section[0];
+    if (s->num_axes > 2) P.axis2 = s->section[0] + s->section[1];
+  }
+  P.magnitude = s->magnitude;
+  for (int i = 0; i < P.pairs; ++i) {
+    const double f = s->freq_h[i] / 6.283185307179586476925286766559;
+    if (!std::isfinite(f)) return APACK_EINVAL;
+    double turns = f - std::floor(f);                       // in [0, 1]
+    if (turns >= 1.0) turns = 0.0;
+    P.freq[i] = static_cast<uint64_t>(std::ldexp(turns, 64));
+  }
+  return APACK_OK;
+}
+
+bool aligned16(std::initializer_list<int64_t> v) {
+  int64_t all = 0;
+  for (int64_t x : v) all |= x;
+  return (all & 15) == 0;
+}
+int64_t addr(const void *p) { return static_cast<int64_t>(reinterpret_cast<uintptr_t>(p)); }
+
+// Chunks of 16 bytes fit the rotated part, its halves and the rest of the head.
+bool wide_heads(int32_t rotary_dim, int32_t head_dim, int size) {
+  const int w = 16 / size;
+  return head_dim % w == 0 && rotary_dim % (2 * w) == 0;
+}
+
+}  // namespace
+}  // namespace apack
+
+using namespace apack;
+
+extern "C" {
+
+apack_status apack_rotary_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor,
+                                      int64_t original_len, double beta_fast, double beta_slow, double *freq_h,
+                                      float *magnitude_h) {
+  if (rotary_dim < 2 || rotary_dim > 2 * kMaxPairs || (rotary_dim & 1) || !freq_h || !magnitude_h) return APACK_EINVAL;
+  if (!(base > 0) || !std::isfinite(base)) return APACK_EINVAL;
+  if (scaling < APACK_ROTARY_NONE || scaling > APACK_ROTARY_YARN) return APACK_EINVAL;
+  if (scaling != APACK_ROTARY_NONE && (!(factor >= 1) || !std::isfinite(factor))) return APACK_EINVAL;
+  if (scaling == APACK_ROTARY_NTK && rotary_dim < 4) return APACK_EINVAL;
+  if (scaling == APACK_ROTARY_YARN &&
+      (original_len < 1 || !std::isfinite(beta_fast) || !(beta_slow >= 0) || !(beta_fast > beta_slow)))
+    return APACK_EINVAL;
+  const double r = rotary_dim;
+  const double b = scaling == APACK_ROTARY_NTK ? base * std::pow(factor, r / (r - 2)) : base;
+  for (int i = 0; i < rotary_dim / 2; ++i) {
+    double f = std::pow(b, -2.0 * i / r);
+    if (scaling == APACK_ROTARY_LINEAR) f /= factor;
+    if (scaling == APACK_ROTARY_YARN) {
+      const double turns = static_cast<double>(original_len) * f / 6.283185307179586476925286766559;
+      const double g = std::min(1.0, std::max(0.0, (turns - beta_slow) / (beta_fast - beta_slow)));
+      f = f * g + f / factor * (1 - g);
+    }
+    if (!std::isfinite(f)) return APACK_EINVAL;
+    freq_h[i] = f;
+  }
+  *magnitude_h = scaling == APACK_ROTARY_YARN ? static_cast<float>(0.1 * std::log(factor) + 1.0) : 1.f;
+  return APACK_OK;
+}
+
+apack_status apack_rotary(const apack_rotary_spec *spec, int32_t dtype, int64_t n_tokens, int32_t num_heads,
+                          int32_t head_dim, const void *x, int64_t x_token_stride, void *out, int64_t out_token_stride,
+                          const int32_t *positions, int64_t pos_axis_stride, int32_t transpose, void *stream) {
+  if (!spec || n_tokens < 0 || n_tokens > INT32_MAX || num_heads < 1 || num_heads > (1 << 16)) return APACK_EINVAL;
+  if (head_dim < 2 || head_dim > 2 * kMaxPairs || (head_dim & 1)) return APACK_EUNSUPPORTED;
+  if (dtype != APACK_BF16 && dtype != APACK_FP16 && dtype != APACK_FP32) return APACK_EUNSUPPORTED;
+  RotPlan P;
+  std::memset(&P, 0, sizeof(P));
+  const apack_status st = plan_spec(spec, head_dim, P);
+  if (st != APACK_OK) return st;
+  const int size = dtype == APACK_FP32 ? 4 : 2;
+  const int64_t row = static_cast<int64_t>(num_heads) * head_dim * size;
+  if (x_token_stride % size || out_token_stride % size || (n_tokens > 1 && (x_token_stride < row || out_token_stride < row)))
+    return APACK_EINVAL;
+  if (n_tokens == 0) return APACK_OK;
+  if (!x || !out || !positions || addr(x) % size || addr(out) % size || (addr(positions) & 3)) return APACK_EINVAL;
+  if (spec->num_axes > 1 && pos_axis_stride < n_tokens) return APACK_EINVAL;
+  if (x == out && x_token_stride != out_token_stride && n_tokens > 1) return APACK_EINVAL;
+  P.heads = P.rot_heads = P.q_heads = num_heads;
+  P.head_dim = head_dim;
+  P.n_tokens = n_tokens;
+  P.x = static_cast<const uint8_t *>(x);
+  P.out = static_cast<uint8_t *>(out);
+  P.xs = x_token_stride;
+  P.outs = out_token_stride;
+  P.positions = positions;
+  P.pos_axis_stride = pos_axis_stride;
+  const bool wide = wide_heads(spec->rotary_dim, head_dim, size) &&
+                    aligned16({addr(x), addr(out), x_token_stride, out_token_stride});
+  const bool pairs = spec->layout == APACK_ROTARY_PAIRS;
+  const float sign = transpose ? -1.f : 1.f;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  switch (dtype) {
+    case APACK_BF16: return check_cuda(launch_rotary<__nv_bfloat16, false>(P, pairs, wide, sign, s));
+    case APACK_FP16: return check_cuda(launch_rotary<__half, false>(P, pairs, wide, sign, s));
+    default: return check_cuda(launch_rotary<float, false>(P, pairs, wide, sign, s));
+  }
+}
+
+apack_status apack_rotary_append(const apack_rotary_spec *spec, const apack_paged_cache *cache, int32_t layer,
+                                 int64_t n_tokens, const void *q, int64_t q_token_stride, void *q_out,
+                                 int64_t q_out_token_stride, int32_t num_q_heads, const void *k,
+                                 int64_t k_token_stride, const void *v, int64_t v_token_stride,
+                                 const int32_t *positions, int64_t pos_axis_stride, const int32_t *rows,
+                                 const int32_t *seqs, void *ws, void *stream) {
+  apack_status st = validate_pool(cache, true);
+  if (st != APACK_OK) return st;
+  if (layer < 0 || layer >= cache->num_layers || n_tokens < 0 || n_tokens > INT32_MAX) return APACK_EINVAL;
+  if (num_q_heads < 0 || num_q_heads > 1024 || (num_q_heads == 0) != (q == nullptr) || (!q) != (!q_out))
+    return APACK_EINVAL;
+  if (!seqs && n_tokens > cache->num_seqs) return APACK_EINVAL;
+  RotPlan P;
+  std::memset(&P, 0, sizeof(P));
+  if (spec) {
+    st = plan_spec(spec, cache->head_dim, P);
+    if (st != APACK_OK) return st;
+  }
+  const int64_t head = cache->head_dim * 2;
+  const int64_t qrow = num_q_heads * head, kvrow = cache->num_kv_heads * head;
+  if (n_tokens == 0) return APACK_OK;
+  if (!k || !v || !rows || (spec && !positions) ||
+      !aligned16({addr(q), addr(q_out), addr(k), addr(v), q ? q_token_stride : 0, q ? q_out_token_stride : 0,
+                  k_token_stride, v_token_stride}) ||
+      ((addr(rows) | addr(seqs) | addr(positions) | addr(ws)) & 3))
+    return APACK_EINVAL;
+  if (n_tokens > 1 && ((q && (q_token_stride < qrow || q_out_token_stride < qrow)) || k_token_stride < kvrow ||
+                       v_token_stride < kvrow || (q && q == q_out && q_token_stride != q_out_token_stride)))
+    return APACK_EINVAL;
+  if (spec && spec->num_axes > 1 && pos_axis_stride < n_tokens) return APACK_EINVAL;
+  P.q_heads = num_q_heads;
+  P.kv_heads = cache->num_kv_heads;
+  P.heads = num_q_heads + 2 * cache->num_kv_heads;
+  P.rot_heads = num_q_heads + cache->num_kv_heads;
+  P.head_dim = cache->head_dim;
+  P.n_tokens = n_tokens;
+  P.x = static_cast<const uint8_t *>(q);
+  P.out = static_cast<uint8_t *>(q_out);
+  P.k = static_cast<const uint8_t *>(k);
+  P.v = static_cast<const uint8_t *>(v);
+  P.xs = q_token_stride;
+  P.outs = q_out_token_stride;
+  P.ks = k_token_stride;
+  P.vs = v_token_stride;
+  P.positions = positions;
+  P.pos_axis_stride = pos_axis_stride;
+  P.rows = rows;
+  P.seqs = seqs;
+  P.pool = pool_view(cache, layer);
+  P.err = static_cast<DeviceError *>(ws);
+  const bool pairs = spec && spec->layout == APACK_ROTARY_PAIRS;
+  const bool wide = wide_heads(2 * P.pairs, cache->head_dim, 2);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  return check_cuda(cache->dtype == APACK_BF16 ? launch_rotary<__nv_bfloat16, true>(P, pairs, wide, 1.f, s)
+                                               : launch_rotary<__half, true>(P, pairs, wide, 1.f, s));
+}
+
+}  // extern "C"
