@@ -441,41 +441,55 @@ def apack_decode_attention(cu_seqlens, q, k, v, kv_token_stride, num_q_heads, nu
 # ---------------------------------------------------------------- paged caches
 
 
+_DTYPES = {"torch.bfloat16": APACK_BF16, "torch.float16": APACK_FP16, "torch.float32": APACK_FP32}
+_CODES = {}                       # torch type -> code, filled as types are met
+
+
 def _dtype_code(dtype):
+    code = _CODES.get(dtype)
+    if code is None:
+        code = _DTYPES.get(str(dtype))
+        if code is None:
+            raise ValueError(f"{dtype}: bfloat16, float16 or float32 expected")
+        _CODES[dtype] = code
+    return code
+
+
+def _current_device():
+    """Index of the current device; -1 without one (the library's own checks then answer)."""
     import torch
-    codes = {torch.bfloat16: APACK_BF16, torch.float16: APACK_FP16, torch.float32: APACK_FP32}
-    if dtype not in codes:
-        raise ValueError(f"{dtype}: bfloat16, float16 or float32 expected")
-    return codes[dtype]
+    if torch.cuda.is_initialized() or torch.cuda.is_available():
+        try:
+            return torch._C._cuda_getDevice()
+        except AttributeError:
+            return torch.cuda.current_device()
+    return -1
 
 
-def _on_device(*tensors):
+def _on_device(tensors):
     """The calls run on the current device: tensors elsewhere are refused."""
-    import torch
-    if not torch.cuda.is_initialized() and not torch.cuda.is_available():
-        return                              # no device: the library's own checks answer
-    dev = torch.cuda.current_device()
+    dev = _current_device()
     for t in tensors:
-        if t is not None and t.device.index != dev:
-            raise ValueError(f"a tensor on {t.device}; the current device is cuda:{dev}")
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"a tensor on device {t.get_device()}; the current device is {dev}")
 
 
 def _int32(t, what, shape=None):
-    import torch
-    if t.dtype != torch.int32 or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
-        raise ValueError(f"{what}: contiguous int32{'' if shape is None else f' of shape {tuple(shape)}'} expected, "
+    if str(t.dtype) != "torch.int32" or not t.is_contiguous() or (shape is not None and t.shape != shape):
+        raise ValueError(f"{what}: contiguous int32{'' if shape is None else f' of shape {shape}'} expected, "
                          f"not {t.dtype} {tuple(t.shape)}")
 
 
 def _head_rows(t, what, dtype=None, shape=None):
-    """A [tokens, heads, D] tensor whose heads are back to back; returns its token stride in bytes."""
-    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
-        raise ValueError(f"{what}: [tokens, heads, D] with heads back to back expected")
+    """A [tokens, heads, D] tensor whose heads are back to back; returns its token stride in elements."""
+    dims, stride = t.shape, t.stride()
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{what}: {dtype} expected, not {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{what}: shape {tuple(shape)} expected, not {tuple(t.shape)}")
-    return t.stride(0) * t.element_size() if t.shape[0] > 1 else t.shape[1] * t.shape[2] * t.element_size()
+    if shape is not None and dims != shape:
+        raise ValueError(f"{what}: shape {tuple(shape)} expected, not {tuple(dims)}")
+    if len(dims) != 3 or stride[2] != 1 or (stride[1] != dims[2] and dims[1] > 1):
+        raise ValueError(f"{what}: [tokens, heads, D] with heads back to back expected")
+    return stride[0] if dims[0] > 1 else dims[1] * dims[2]
 
 
 class PagedCache:
@@ -491,14 +505,15 @@ class PagedCache:
             raise ValueError("k and v: [layers, pages, page_tokens, heads, D] of one shape, type and strides expected")
         if page_table.dtype != torch.int32 or page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
             raise ValueError("page_table: int32 [sequences, pages] with contiguous rows expected")
-        if k.device != v.device or k.device != page_table.device:
+        if not k.get_device() == v.get_device() == page_table.get_device():
             raise ValueError("k, v and page_table: one device expected")
         self.k, self.v, self.page_table = k, v, page_table
-        self.dtype, self.device = k.dtype, k.device
+        self.dtype, self._device = k.dtype, k.get_device()
         size = k.element_size()
         layers, pages, tokens, heads, dim = k.shape
         seqs, columns = page_table.shape
         self.num_kv_heads, self.head_dim, self.num_seqs, self.num_layers = heads, dim, seqs, layers
+        self._scale = 1.0 / math.sqrt(dim)
         # a stride of an extent of one says nothing, and may be anything
         stride = [k.stride(i) * size if k.shape[i] > 1 else 0 for i in range(4)]
         self.struct = apack_paged_cache(
@@ -507,6 +522,9 @@ class PagedCache:
             head_dim=dim, dtype=_dtype_code(k.dtype), page_table=page_table.data_ptr(),
             table_stride=page_table.stride(0) if seqs > 1 else columns, num_seqs=seqs, max_pages=columns)
         self._address = ctypes.addressof(self.struct)
+
+    def get_device(self):
+        return self._device
 
 
 class Rotary:
@@ -547,20 +565,20 @@ class Rotary:
 
     def _positions(self, positions, n):
         """Checks int32 [n] or [axes, n]; returns the stride between axes."""
-        import torch
-        one = positions.dim() == 1 and self.num_axes == 1
-        if positions.dtype != torch.int32 or positions.shape[-1] != n or positions.dim() not in (1, 2) or not (
-                one or (positions.dim() == 2 and positions.shape[0] == self.num_axes)) or (n > 1 and positions.stride(-1) != 1):
-            raise ValueError(f"positions: int32 [{self.num_axes}, {n}] expected, not {positions.dtype} {tuple(positions.shape)}")
-        return positions.stride(0) if positions.dim() == 2 and self.num_axes > 1 else n
+        dims, stride = positions.shape, positions.stride()
+        if str(positions.dtype) != "torch.int32" or not (
+                dims == (self.num_axes, n) or (self.num_axes == 1 and dims == (n,))) or (stride[-1] != 1 and n > 1):
+            raise ValueError(f"positions: int32 [{self.num_axes}, {n}] expected, not {positions.dtype} {tuple(dims)}")
+        return stride[0] if self.num_axes > 1 else n
 
 
 def apack_rotary(rotary, x, positions, out, transpose=False, stream=None):
     """Rotary positions of x [tokens, heads, D] into out (out is x: in place); transpose: the gradient."""
-    _on_device(x, positions, out)
-    xs = _head_rows(x, "x")
-    outs = _head_rows(out, "out", x.dtype, x.shape)
+    _on_device((x, positions, out))
+    size = x.element_size()
+    xs = size * _head_rows(x, "x")
     n, heads, dim = x.shape
+    outs = xs if out is x else size * _head_rows(out, "out", x.dtype, x.shape)
     axis = rotary._positions(positions, n)
     _check(_lib.apack_rotary(rotary._address, _dtype_code(x.dtype), n, heads, dim, x.data_ptr(), xs, out.data_ptr(),
                              outs, positions.data_ptr(), axis, 1 if transpose else 0, _stream(stream)), "apack_rotary")
@@ -569,17 +587,19 @@ def apack_rotary(rotary, x, positions, out, transpose=False, stream=None):
 def apack_rotary_append(rotary, cache, layer, q, k, v, q_out, positions, rows, seqs=None, ws=None, stream=None):
     """Rotates new tokens' queries into q_out and their keys into the pages of `layer`, with their values.
     rotary None: no rotation; q (and q_out) None: keys and values alone."""
-    _on_device(cache, q, k, v, q_out, positions, rows, seqs, ws)
+    _on_device((cache, q, k, v, q_out, positions, rows, seqs, ws))
     n = k.shape[0]
-    shape = (n, cache.num_kv_heads, cache.head_dim)
-    ks, vs = _head_rows(k, "k", cache.dtype, shape), _head_rows(v, "v", cache.dtype, shape)
+    dtype, dim = cache.dtype, cache.head_dim
+    shape = (n, cache.num_kv_heads, dim)
+    ks, vs = _head_rows(k, "k", dtype, shape), _head_rows(v, "v", dtype, shape)
     qs = qos = heads = 0
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out: both or neither expected")
     if q is not None:
         heads = q.shape[1]
-        qs = _head_rows(q, "q", cache.dtype, (n, heads, cache.head_dim))
-        qos = _head_rows(q_out, "q_out", cache.dtype, q.shape)
+        shape = (n, heads, dim)
+        qs = _head_rows(q, "q", dtype, shape)
+        qos = qs if q_out is q else _head_rows(q_out, "q_out", dtype, shape)
     axis = 0
     if rotary is not None:
         axis = rotary._positions(positions, n)
@@ -587,8 +607,8 @@ def apack_rotary_append(rotary, cache, layer, q, k, v, q_out, positions, rows, s
     if seqs is not None:
         _int32(seqs, "seqs", (n,))
     _check(_lib.apack_rotary_append(None if rotary is None else rotary._address, cache._address, int(layer), n,
-                                    _ptr(q), qs, _ptr(q_out), qos, heads, k.data_ptr(), ks, v.data_ptr(), vs,
-                                    None if rotary is None else positions.data_ptr(), axis, rows.data_ptr(),
+                                    _ptr(q), 2 * qs, _ptr(q_out), 2 * qos, heads, k.data_ptr(), 2 * ks, v.data_ptr(),
+                                    2 * vs, None if rotary is None else positions.data_ptr(), axis, rows.data_ptr(),
                                     _ptr(seqs), _ptr(ws), _stream(stream)), "apack_rotary_append")
 
 
@@ -602,27 +622,26 @@ def apack_paged_decode_workspace_size(cache, num_q_heads):
 def apack_paged_decode_attention(cache, layer, seqlens, q, out, ws, scale=None, lse=None, stream=None):
     """Attention of one decode token per sequence over its pages; seqlens: int32 [num_seqs] on the device.
     q [num_seqs, Hq, D]; out: the same shape, contiguous, of q's type or float32; lse: float32 [num_seqs, Hq]."""
-    import torch
-    _on_device(cache, seqlens, q, out, ws, lse)
+    _on_device((cache, seqlens, q, out, ws, lse))
     heads = q.shape[1]
     shape = (cache.num_seqs, heads, cache.head_dim)
     qs = _head_rows(q, "q", cache.dtype, shape)
-    _int32(seqlens, "seqlens", (cache.num_seqs,))
-    if tuple(out.shape) != shape or not out.is_contiguous():
+    _int32(seqlens, "seqlens", shape[:1])
+    if out.shape != shape or not out.is_contiguous():
         raise ValueError(f"out: contiguous {shape} expected")
-    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != shape[:2] or not lse.is_contiguous()):
+    if lse is not None and (str(lse.dtype) != "torch.float32" or lse.shape != shape[:2] or not lse.is_contiguous()):
         raise ValueError(f"lse: contiguous float32 {shape[:2]} expected")
     _check(_lib.apack_paged_decode_attention(
-        cache._address, int(layer), seqlens.data_ptr(), q.data_ptr(), qs, heads,
-        1.0 / math.sqrt(cache.head_dim) if scale is None else float(scale), out.data_ptr(), _dtype_code(out.dtype),
-        _ptr(lse), ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)), "apack_paged_decode_attention")
+        cache._address, int(layer), seqlens.data_ptr(), q.data_ptr(), 2 * qs, heads,
+        cache._scale if scale is None else scale, out.data_ptr(), _dtype_code(out.dtype),
+        _ptr(lse), ws.data_ptr(), ws.nbytes, _stream(stream)), "apack_paged_decode_attention")
 
 
 def apack_paged_compact(src, dst, cu_dst, n_out, keep_idx=None, cu_src=None, src_layer=0, dst_layer=0,
                         num_layers=None, ws=None, stream=None):
     """The kept rows of every sequence of pool src, in order, to the first rows of its pages in dst (src is dst:
     in place).  cu_dst, cu_src: int32 [num_seqs + 1] on the device; num_layers: all that both have by default."""
-    _on_device(src, dst, cu_dst, keep_idx, cu_src, ws)
+    _on_device((src, dst, cu_dst, keep_idx, cu_src, ws))
     _int32(cu_dst, "cu_dst", (dst.num_seqs + 1,))
     if cu_src is not None:
         _int32(cu_src, "cu_src", (src.num_seqs + 1,))
@@ -639,7 +658,7 @@ def apack_paged_compact(src, dst, cu_dst, n_out, keep_idx=None, cu_src=None, src
 
 def apack_copy_pages(cache, pairs, ws=None, stream=None):
     """Copies page pairs[i, 0] to page pairs[i, 1] in every layer; pairs: int32 [n, 2] on the device."""
-    _on_device(cache, pairs, ws)
+    _on_device((cache, pairs, ws))
     _int32(pairs, "pairs", (pairs.shape[0], 2))
     _check(_lib.apack_copy_pages(cache._address, pairs.data_ptr(), pairs.shape[0], _ptr(ws), _stream(stream)),
            "apack_copy_pages")

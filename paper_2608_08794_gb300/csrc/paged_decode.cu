@@ -37,6 +37,10 @@ constexpr int kStageBytesCta = 196608;          // of all warps' rings
 // below 2^8 times their number, far inside fp32, and most tiles need one vote instead of the reduction.
 constexpr float kRescale = 8.f;
 
+// What a (sequence, head group) costs a CTA beyond its tiles (its queries' latency, the merge, the write), as the
+// bytes of K and V that it could have streamed meanwhile.
+constexpr int kSegBytes = 65536;
+
 struct PdPlan {
   PoolView pool;
   const int32_t *seqlens;
@@ -47,6 +51,7 @@ struct PdPlan {
   int32_t box_tokens, boxes;         // tokens of one TMA box, boxes of a tile
   int32_t max_rows;
   int32_t min_tiles;                 // smallest share of a CTA
+  int32_t seg_cost;                  // what a segment costs beyond its tiles, in tiles
   float scale2;                      // scale * log2(e)
   void *out;
   int32_t out_fp32;
@@ -126,32 +131,33 @@ __device__ __forceinline__ int clamped_length(const PdPlan &P, int b, bool repor
 }
 __device__ __forceinline__ int tiles_of(int len) { return (len >> 4) + ((len & 15) != 0); }
 
-// A walk over the (sequence, head group) segments of a share of the work list.
+// A walk over the (sequence, head group) segments of a CTA's share [u0, u1) of the work list.  A segment takes up
+// seg_cost + nt units of the list, the tiles behind the cost.
 struct Walk {
   int b, g, len, nt;     // segment, its sequence's length and tiles
-  int ts, te;            // this share's tiles of it
-  int64_t left;          // tiles of the share behind te
-  __device__ __forceinline__ void span(int start) {
-    ts = start;
-    te = static_cast<int>(min(static_cast<int64_t>(nt), ts + left));
-    left -= te - ts;
+  int ts, te;            // the share's tiles of it
+  int64_t s;             // its first unit
+  __device__ __forceinline__ void span(int cost, int64_t u0, int64_t u1) {
+    ts = static_cast<int>(min(max(u0 - s - cost, static_cast<int64_t>(0)), static_cast<int64_t>(nt)));
+    te = static_cast<int>(min(max(u1 - s - cost, static_cast<int64_t>(0)), static_cast<int64_t>(nt)));
   }
-  __device__ __forceinline__ bool next(const PdPlan &P) {
-    if (left <= 0) return false;
-    if (++g >= P.groups) {
-      g = 0;
-      do {
-        len = clamped_length(P, ++b, false);
-      } while (len == 0);
-      nt = tiles_of(len);
-    }
-    span(0);
+  // The next segment with a tile in the share.
+  __device__ __forceinline__ bool next(const PdPlan &P, int64_t u0, int64_t u1) {
+    do {
+      s += P.seg_cost + nt;
+      if (s + P.seg_cost >= u1) return false;
+      if (++g >= P.groups) {
+        g = 0;
+        do {
+          len = clamped_length(P, ++b, false);
+        } while (len == 0);
+        nt = tiles_of(len);
+      }
+      span(P.seg_cost, u0, u1);
+    } while (ts >= te);
     return true;
   }
 };
-
-// Share of CTA c: tiles [share(c), share(c + 1)) of W over C CTAs.
-__device__ __forceinline__ int64_t share(int64_t W, int C, int c) { return W * c / C; }
 
 template <class T, int D, int NT>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -178,10 +184,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   // ---- this CTA's share (every warp by itself: no barrier before the first load)
   const int B = P.pool.num_seqs, grid = gridDim.x, cta = blockIdx.x;
   const int per = (B + 31) / 32;
+  const int cost = P.seg_cost;
   int64_t mine = 0;
   for (int i = 0; i < per; ++i) {
     const int b = lane * per + i;
-    if (b < B) mine += tiles_of(clamped_length(P, b, warp == 0 && cta == 0));
+    if (b < B) {
+      const int nt = tiles_of(clamped_length(P, b, warp == 0 && cta == 0));
+      if (nt > 0) mine += nt + cost;
+    }
   }
   int64_t incl = mine;
 #pragma unroll
@@ -189,7 +199,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int64_t y = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += y;
   }
-  const int64_t W = __shfl_sync(0xffffffffu, incl, 31) * P.groups;
+  // the list starts behind the first segment's cost: every CTA pays one anyway
+  const int64_t W = __shfl_sync(0xffffffffu, incl, 31) * P.groups - cost;
   const int C = static_cast<int>(min(static_cast<int64_t>(grid), max(W / P.min_tiles, static_cast<int64_t>(1))));
   if (threadIdx.x == 0) P.info[cta] = make_int4(0, 0, 0, 0);
   // empty sequences: zeros and -infinity
@@ -206,9 +217,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int i = threadIdx.x; i < P.hq; i += kThreads) P.lse[static_cast<int64_t>(b) * P.hq + i] = -INFINITY;
   }
   const int hw = warp % P.heads_cta, sub = warp / P.heads_cta;
-  if (W == 0 || cta >= C || sub >= P.wph) return;
+  if (W <= 0 || cta >= C || sub >= P.wph) return;
   const int active = 32 * P.heads_cta * P.wph;        // threads of the warps at work
-  const int64_t u0 = share(W, C, cta), u1 = share(W, C, cta + 1);
+  const int64_t u0 = cost + W * cta / C, u1 = cost + W * (cta + 1) / C;
   Walk seg;
   {
     const int64_t lo = (incl - mine) * P.groups, hi = incl * P.groups;
@@ -218,70 +229,104 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (;; ++b) {
       seg.len = clamped_length(P, b, false);
       seg.nt = tiles_of(seg.len);
-      if (off < static_cast<int64_t>(seg.nt) * P.groups) break;
-      off -= static_cast<int64_t>(seg.nt) * P.groups;
+      const int64_t all = seg.nt > 0 ? static_cast<int64_t>(seg.nt + cost) * P.groups : 0;
+      if (off < all) break;
+      off -= all;
     }
     seg.b = b;
-    seg.g = static_cast<int>(off / seg.nt);
-    seg.left = u1 - u0;
-    seg.span(static_cast<int>(off - static_cast<int64_t>(seg.g) * seg.nt));
+    seg.g = static_cast<int>(off / (seg.nt + cost));
+    seg.s = u0 - (off - static_cast<int64_t>(seg.g) * (seg.nt + cost));
+    seg.span(cost, u0, u1);
+    if (seg.ts >= seg.te && !seg.next(P, u0, u1)) return;      // the share holds no tile (for all warps alike)
   }
 
-  // ---- producer: the walk of this warp's tiles, kStages ahead of the consumer
-  Walk pw = seg;
-  int pt = pw.ts + sub;
-  bool more = true;
-  int32_t page = -1;                                  // of box `lane` of tile pt, read one tile ahead
-  uint32_t in_page = 0;
-  auto find = [&] {                                   // the next tile of this warp, and its page
-    while (pt >= pw.te) {
-      if (!pw.next(P)) {
-        more = false;
-        return;
-      }
-      pt = pw.ts + sub;
-    }
-    const int row = pt * kTile + lane * P.box_tokens;
-    if (lane < P.boxes && row < pw.len) {
-      const uint32_t p = P.pool.page_tokens.div(row);
-      page = __ldg(P.pool.table + pw.b * P.pool.table_stride + p);
-      in_page = row - p * P.pool.page_tokens.d;
-    } else {
-      page = INT32_MIN;                               // nothing to load
-    }
-  };
-  auto issue = [&](int slot) {
-    const int rows = pw.len - pt * kTile;             // boxes that hold a row of the sequence
-    const int nbox = min(P.boxes, (rows + P.box_tokens - 1) / P.box_tokens);
-    if (lane == 0) mbar_arrive_expect_tx(&full[slot], nbox * P.box_tokens * D * 4);
-    __syncwarp();
-    if (lane < nbox) {
-      if (static_cast<uint32_t>(page) >= static_cast<uint32_t>(P.pool.num_pages)) {
-        raise_device_error(P.err, APACK_EDEVICE, 82, pw.b, page);
-        page = P.pool.num_pages;                      // outside the map: reads as zeros
-      }
-      const int head = pw.g * P.heads_cta + hw;
-      const uint32_t dst = ring + slot * (2 * kHalf);
-      if (P.boxes == 1) {
-        tma_load_5d(dst, &kmap, &full[slot], in_page, 0, head, page);
-        tma_load_5d(dst + kHalf, &vmap, &full[slot], in_page, 0, head, page);
-      } else {
-        for (int blk = 0; blk < D / 64; ++blk) {
-          const uint32_t o = blk * kBlk + lane * P.box_tokens * 128;
-          tma_load_5d(dst + o, &kmap, &full[slot], in_page, blk, head, page);
-          tma_load_5d(dst + kHalf + o, &vmap, &full[slot], in_page, blk, head, page);
-        }
-      }
-    }
-  };
-  int issued = 0, used = 0;
-  find();
-  while (issued < kStages && more) {
-    issue(issued);
-    ++issued;
-    pt += P.wph;
-    find();
+  // ---- producer: a queue of this warp's next 32 tiles, one per lane; the lane of a tile issues its loads
+  Walk head_w = seg;                                  // of the first tile behind the queue
+  int head_t = seg.ts + sub;
+  bool head_ok = true;
+  while (head_ok && head_t >= head_w.te) {
+    head_ok = head_w.next(P, u0, u1);
+    head_t = head_w.ts + sub;
   }
+  int32_t q_page = 0, q_head = 0, q_b = 0, q_t = 0, q_len = 0;
+  uint32_t q_in = 0;
+  int queued = 0, issued = 0, used = 0;
+  auto refill = [&] {
+    Walk w = head_w;
+    int t = head_t, skip = lane;
+    bool ok = head_ok;
+    while (ok) {
+      const int here = t < w.te ? (w.te - t + P.wph - 1) / P.wph : 0;
+      if (skip < here) {
+        t += skip * P.wph;
+        break;
+      }
+      skip -= here;
+      ok = w.next(P, u0, u1);
+      t = w.ts + sub;
+    }
+    if (ok) {
+      q_b = w.b;
+      q_t = t;
+      q_len = w.len;
+      q_head = w.g * P.heads_cta + hw;
+      if (P.boxes == 1) {
+        const uint32_t p = P.pool.page_tokens.div(t * kTile);
+        q_page = __ldg(P.pool.table + w.b * P.pool.table_stride + p);
+        q_in = t * kTile - p * P.pool.page_tokens.d;
+      }
+    }
+    queued += __popc(__ballot_sync(0xffffffffu, ok));
+    head_ok = __shfl_sync(0xffffffffu, static_cast<int>(ok), 31);
+    head_w.b = __shfl_sync(0xffffffffu, w.b, 31);
+    head_w.g = __shfl_sync(0xffffffffu, w.g, 31);
+    head_w.len = __shfl_sync(0xffffffffu, w.len, 31);
+    head_w.nt = __shfl_sync(0xffffffffu, w.nt, 31);
+    head_w.ts = __shfl_sync(0xffffffffu, w.ts, 31);
+    head_w.te = __shfl_sync(0xffffffffu, w.te, 31);
+    head_w.s = __shfl_sync(0xffffffffu, w.s, 31);
+    head_t = __shfl_sync(0xffffffffu, t, 31) + P.wph;
+  };
+  // One TMA box pair; a page outside the pool reads as zeros (the map ends there).
+  auto load_box = [&](int slot, int32_t page, uint32_t in_page, int head, int b, int block, uint32_t offset) {
+    if (static_cast<uint32_t>(page) >= static_cast<uint32_t>(P.pool.num_pages)) {
+      raise_device_error(P.err, APACK_EDEVICE, 82, b, page);
+      page = P.pool.num_pages;
+    }
+    const uint32_t dst = ring + slot * (2 * kHalf) + offset;
+    tma_load_5d(dst, &kmap, &full[slot], in_page, block, head, page);
+    tma_load_5d(dst + kHalf, &vmap, &full[slot], in_page, block, head, page);
+  };
+  // Tile number `issued` of the warp, if there is one.
+  auto issue = [&] {
+    if (issued == queued) {
+      if (!head_ok) return;
+      refill();
+      if (issued == queued) return;
+    }
+    const int slot = issued % kStages, owner = issued & 31;
+    if (P.boxes == 1) {
+      if (lane == owner) {
+        mbar_arrive_expect_tx(&full[slot], 2 * kHalf);
+        load_box(slot, q_page, q_in, q_head, q_b, 0, 0);
+      }
+    } else {
+      // pages that are not whole tiles: a box per lane, those that hold a row of the sequence
+      const int t = __shfl_sync(0xffffffffu, q_t, owner), b = __shfl_sync(0xffffffffu, q_b, owner);
+      const int head = __shfl_sync(0xffffffffu, q_head, owner), len = __shfl_sync(0xffffffffu, q_len, owner);
+      const int nbox = min(P.boxes, (len - t * kTile + P.box_tokens - 1) / P.box_tokens);
+      if (lane == 0) mbar_arrive_expect_tx(&full[slot], nbox * P.box_tokens * D * 4);
+      __syncwarp();
+      if (lane < nbox) {
+        const uint32_t row = t * kTile + lane * P.box_tokens, p = P.pool.page_tokens.div(row);
+        const int32_t page = __ldg(P.pool.table + b * P.pool.table_stride + p);
+        for (int blk = 0; blk < D / 64; ++blk)
+          load_box(slot, page, row - p * P.pool.page_tokens.d, head, b, blk, blk * kBlk + lane * P.box_tokens * 128);
+      }
+    }
+    ++issued;
+  };
+  for (int i = 0; i < kStages; ++i) issue();
 
   // ---- consumer
   const int t4 = lane & 3, g8 = lane >> 2;
@@ -406,12 +451,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       __syncwarp();                                   // every lane has read the stage
-      if (more) {
-        issue(slot);
-        ++issued;
-        pt += P.wph;
-        find();
-      }
+      issue();
     }
 
     // ---- end of the segment: the warps of each head merge
@@ -519,128 +559,139 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (threadIdx.x == 0 && seg.ts == 0) {
           // this share starts the segment; the one that holds its last tile ends it
-          const int64_t last = u1 - (seg.te - seg.ts) - seg.left + seg.nt - 1;
-          const int c_end = static_cast<int>(((last + 1) * C + W - 1) / W) - 1;
+          const int64_t end = seg.s + seg.nt;         // unit behind the last tile, without the list's first cost
+          const int c_end = static_cast<int>((end * C + W - 1) / W) - 1;
           P.info[cta] = make_int4(seg.b, seg.g, c_end - cta + 1, slot);
         }
       }
     }
     first_seg = 0;
-  } while (seg.next(P));
+  } while (seg.next(P, u0, u1));
   if (dead)   // loads of the stages that were issued and not used may still be in flight
     for (int n = used; n < issued; ++n) mbar_wait(&full[n % kStages], (n / kStages) & 1u, kWaitLimitNs / 4);
 }
 
-// Merges the parts of the cut segments.  A CTA first counts the shares that start one (info); its warps then take
-// (segment, head, 8 query rows, 16 features) units in turn, each warp a run of the parts in order, and
-// merge in warp order.
+// Merges the parts of the cut segments.  A unit is (segment, head, 8 query rows, 16 features).  Every CTA lists the
+// shares that start a cut segment (info), then the units of segments of many parts are merged by a CTA each, a run
+// of the parts per warp, and those of few parts by a warp each.
 constexpr int kCombineWarps = 8;
-constexpr int kCombineBatch = 8;       // parts whose loads are in flight
-constexpr int kMaxGrid = 1024;
+constexpr int kCombineBatch = 8;      // parts whose loads a warp has in flight
+constexpr int kMaxGrid = 512;
+
+// (max, sum, o) of two query rows (2 t4 and + 1) and two features (g8 and + 8), in log2 units.
+struct PartState {
+  float m0, m1, l0, l1;
+  float4 o;                            // row 0 feature g8, row 1 g8, row 0 g8 + 8, row 1 g8 + 8
+};
+__device__ __forceinline__ void merge_part(PartState &a, const float4 &ml, const float4 &x) {
+  const float n0 = fmaxf(a.m0, ml.x), n1 = fmaxf(a.m1, ml.z);
+  // equal maxima (both -infinity among them) give the factor 1
+  const float a0 = a.m0 == n0 ? 1.f : ex2_approx(a.m0 - n0), b0 = ml.x == n0 ? 1.f : ex2_approx(ml.x - n0);
+  const float a1 = a.m1 == n1 ? 1.f : ex2_approx(a.m1 - n1), b1 = ml.z == n1 ? 1.f : ex2_approx(ml.z - n1);
+  a.l0 = a.l0 * a0 + ml.y * b0;
+  a.l1 = a.l1 * a1 + ml.w * b1;
+  a.o.x = a.o.x * a0 + x.x * b0;
+  a.o.y = a.o.y * a1 + x.y * b1;
+  a.o.z = a.o.z * a0 + x.z * b0;
+  a.o.w = a.o.w * a1 + x.w * b1;
+  a.m0 = n0;
+  a.m1 = n1;
+}
 
 template <class T, int D, int NT>
-__global__ void __launch_bounds__(32 * kCombineWarps)
+__device__ __forceinline__ PartState merge_run(const PdPlan &P, const int4 &inf, int hn, int i, int p0, int p1, int lane) {
+  PartState a = {-INFINITY, -INFINITY, 0.f, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+  for (int p = p0; p < p1; p += kCombineBatch) {
+    float4 ml[kCombineBatch], x[kCombineBatch];
+#pragma unroll
+    for (int k = 0; k < kCombineBatch; ++k) {
+      // the first part lies where its share put it, the others are their shares' first
+      const int q = min(p + k, p1 - 1);
+      const int slot = q == 0 ? inf.w : 2 * ((inf.w >> 1) + q);
+      const int64_t at = static_cast<int64_t>(slot) * P.heads_cta * NT + hn;
+      ml[k] = *reinterpret_cast<const float4 *>(P.ml + at * 8 + (lane & 3) * 2);
+      x[k] = reinterpret_cast<const float4 *>(P.part)[(at * (D / 16) + i) * 32 + lane];
+    }
+#pragma unroll
+    for (int k = 0; k < kCombineBatch; ++k)
+      if (p + k < p1) merge_part(a, ml[k], x[k]);
+  }
+  return a;
+}
+
+template <class T, int D, int NT>
+__device__ __forceinline__ void write_unit(const PdPlan &P, const int4 &inf, int hn, int i, const PartState &a, int lane) {
+  const int t4 = lane & 3, g8 = lane >> 2;
+  const int head = inf.y * P.heads_cta + hn / NT;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int r = (hn % NT) * 8 + t4 * 2 + e;
+    if (r >= P.group) continue;
+    const int64_t row = static_cast<int64_t>(inf.x) * P.hq + head * P.group + r;
+    const float L = e ? a.l1 : a.l0, inv = L == 0.f ? 0.f : 1.f / L;
+    if (P.lse && i == 0 && g8 == 0) P.lse[row] = ((e ? a.m1 : a.m0) + log2f(L)) * 0.6931471805599453f;
+    const float x0 = (e ? a.o.y : a.o.x) * inv, x1 = (e ? a.o.w : a.o.z) * inv;
+    const int64_t at = row * D + i * 16 + g8;
+    if (P.out_fp32) {
+      static_cast<float *>(P.out)[at] = x0;
+      static_cast<float *>(P.out)[at + 8] = x1;
+    } else {
+      static_cast<T *>(P.out)[at] = static_cast<T>(x0);
+      static_cast<T *>(P.out)[at + 8] = static_cast<T>(x1);
+    }
+  }
+}
+
+template <class T, int D, int NT>
+__global__ void __launch_bounds__(32 * kCombineWarps, 3)
     paged_combine_kernel(const __grid_constant__ PdPlan P, int grid) {
   constexpr int KS = D / 16;
-  __shared__ int lead[kMaxGrid];
-  __shared__ int n_lead;
+  __shared__ int4 seg[kMaxGrid];
+  __shared__ uint16_t list[kMaxGrid];          // segments of few parts from the front, of many from the back
+  __shared__ int n_few, n_many;
   __shared__ float4 so[kCombineWarps][32];
   __shared__ float4 sml[kCombineWarps][4];     // (m, l) of query rows 2 t, 2 t + 1
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_wait_and_release();
-  if (warp == 0) {
-    int n = 0;
-    for (int c = 0; c < grid; c += 32) {
-      const bool is = c + lane < grid && P.info[c + lane].z > 0;
-      const unsigned mask = __ballot_sync(0xffffffffu, is);
-      if (is) lead[n + __popc(mask & ((1u << lane) - 1))] = c + lane;
-      n += __popc(mask);
+  for (int c = threadIdx.x; c < grid; c += 32 * kCombineWarps) seg[c] = P.info[c];
+  __syncthreads();
+  if (warp == 0) {                             // in one order, the same in every CTA
+    int few = 0, many = 0;
+    for (int c = lane; c - lane < grid; c += 32) {
+      const int parts = c < grid ? seg[c].z : 0;
+      const bool is_few = parts > 0 && parts <= kCombineBatch, is_many = parts > kCombineBatch;
+      const unsigned f = __ballot_sync(0xffffffffu, is_few), m = __ballot_sync(0xffffffffu, is_many), below = (1u << lane) - 1;
+      if (is_few) list[few + __popc(f & below)] = c;
+      if (is_many) list[kMaxGrid - 1 - many - __popc(m & below)] = c;
+      few += __popc(f);
+      many += __popc(m);
     }
-    if (lane == 0) n_lead = n;
+    if (lane == 0) {
+      n_few = few;
+      n_many = many;
+    }
   }
   __syncthreads();
   const int per_seg = P.heads_cta * NT * KS;
-  const int t4 = lane & 3, g8 = lane >> 2;
-  for (int u = blockIdx.x; u < n_lead * per_seg; u += gridDim.x) {
-    const int c = lead[u / per_seg], rest = u % per_seg;
-    const int hn = rest / KS, i = rest % KS;                       // (head of the group, 8 rows), 16 features
-    const int4 inf = P.info[c];
-    const int parts = inf.z;
-    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    const int p0 = parts * warp / kCombineWarps, p1 = parts * (warp + 1) / kCombineWarps;
-    for (int p = p0; p < p1; p += kCombineBatch) {
-      float4 ml[kCombineBatch], x[kCombineBatch];
-#pragma unroll
-      for (int k = 0; k < kCombineBatch; ++k) {
-        ml[k] = make_float4(-INFINITY, 0.f, -INFINITY, 0.f);
-        x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (p + k < p1) {
-          const int slot = p + k == 0 ? inf.w : 2 * (c + p + k);
-          const int64_t at = static_cast<int64_t>(slot) * P.heads_cta * NT + hn;
-          ml[k] = *reinterpret_cast<const float4 *>(P.ml + at * 8 + t4 * 2);
-          x[k] = reinterpret_cast<const float4 *>(P.part)[(at * KS + i) * 32 + lane];
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < kCombineBatch; ++k) {
-        if (p + k >= p1) break;
-        const float n0 = fmaxf(m0, ml[k].x), n1 = fmaxf(m1, ml[k].z);
-        const float a0 = m0 == n0 ? 1.f : ex2_approx(m0 - n0), b0 = ml[k].x == n0 ? 1.f : ex2_approx(ml[k].x - n0);
-        const float a1 = m1 == n1 ? 1.f : ex2_approx(m1 - n1), b1 = ml[k].z == n1 ? 1.f : ex2_approx(ml[k].z - n1);
-        l0 = l0 * a0 + ml[k].y * b0;
-        l1 = l1 * a1 + ml[k].w * b1;
-        acc.x = acc.x * a0 + x[k].x * b0;
-        acc.y = acc.y * a1 + x[k].y * b1;
-        acc.z = acc.z * a0 + x[k].z * b0;
-        acc.w = acc.w * a1 + x[k].w * b1;
-        m0 = n0;
-        m1 = n1;
-      }
-    }
-    so[warp][lane] = acc;
-    if (g8 == 0) sml[warp][t4] = make_float4(m0, l0, m1, l1);
+  for (int u = blockIdx.x; u < n_many * per_seg; u += gridDim.x) {
+    const int4 inf = seg[list[kMaxGrid - 1 - u / per_seg]];
+    const int hn = u % per_seg / KS, i = u % KS;
+    const PartState a = merge_run<T, D, NT>(P, inf, hn, i, inf.z * warp / kCombineWarps, inf.z * (warp + 1) / kCombineWarps, lane);
+    so[warp][lane] = a.o;
+    if (lane < 4) sml[warp][lane] = make_float4(a.m0, a.l0, a.m1, a.l1);
     __syncthreads();
     if (warp == 0) {
-      float M0 = -INFINITY, M1 = -INFINITY, L0 = 0.f, L1 = 0.f;
-      float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+      PartState t = {-INFINITY, -INFINITY, 0.f, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
 #pragma unroll
-      for (int w = 0; w < kCombineWarps; ++w) {
-        const float4 s = sml[w][t4];
-        M0 = fmaxf(M0, s.x);
-        M1 = fmaxf(M1, s.z);
-      }
-#pragma unroll
-      for (int w = 0; w < kCombineWarps; ++w) {
-        const float4 s = sml[w][t4], x = so[w][lane];
-        const float a0 = s.x == M0 ? 1.f : ex2_approx(s.x - M0), a1 = s.z == M1 ? 1.f : ex2_approx(s.z - M1);
-        L0 += s.y * a0;
-        L1 += s.w * a1;
-        O.x += x.x * a0;
-        O.y += x.y * a1;
-        O.z += x.z * a0;
-        O.w += x.w * a1;
-      }
-      const int head = inf.y * P.heads_cta + hn / NT;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int r = (hn % NT) * 8 + t4 * 2 + e;
-        if (r >= P.group) continue;
-        const int64_t row = static_cast<int64_t>(inf.x) * P.hq + head * P.group + r;
-        const float L = e ? L1 : L0, inv = L == 0.f ? 0.f : 1.f / L;
-        if (P.lse && i == 0 && g8 == 0) P.lse[row] = ((e ? M1 : M0) + log2f(L)) * 0.6931471805599453f;
-        const float x0 = (e ? O.y : O.x) * inv, x1 = (e ? O.w : O.z) * inv;
-        const int64_t at = row * D + i * 16 + g8;
-        if (P.out_fp32) {
-          static_cast<float *>(P.out)[at] = x0;
-          static_cast<float *>(P.out)[at + 8] = x1;
-        } else {
-          static_cast<T *>(P.out)[at] = static_cast<T>(x0);
-          static_cast<T *>(P.out)[at + 8] = static_cast<T>(x1);
-        }
-      }
+      for (int w = 0; w < kCombineWarps; ++w) merge_part(t, sml[w][lane & 3], so[w][lane]);
+      write_unit<T, D, NT>(P, inf, hn, i, t, lane);
     }
     __syncthreads();
+  }
+  for (int u = warp * gridDim.x + blockIdx.x; u < n_few * per_seg; u += gridDim.x * kCombineWarps) {
+    const int4 inf = seg[list[u / per_seg]];
+    const int hn = u % per_seg / KS, i = u % KS;
+    write_unit<T, D, NT>(P, inf, hn, i, merge_run<T, D, NT>(P, inf, hn, i, 0, inf.z, lane), lane);
   }
 }
 
@@ -756,6 +807,7 @@ apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_
   P.max_rows = static_cast<int32_t>(
       std::min<int64_t>(INT32_MAX - kTile, static_cast<int64_t>(cache->max_pages) * cache->page_tokens));
   P.min_tiles = s.wph;
+  P.seg_cost = std::max(1, kSegBytes / (kTile * s.heads_cta * cache->head_dim * 4));
   P.scale2 = scale * 1.4426950408889634f;
   P.out = out;
   P.out_fp32 = out_dtype == APACK_FP32;

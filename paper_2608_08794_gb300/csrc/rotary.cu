@@ -52,11 +52,21 @@ template <class T>
 struct Elem;
 template <>
 struct Elem<__nv_bfloat16> {
+  static __device__ float2 unpack(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+  static __device__ uint32_t pack(float a, float b) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&v);
+  }
   static __device__ float to(__nv_bfloat16 v) { return __bfloat162float(v); }
   static __device__ __nv_bfloat16 from(float v) { return __float2bfloat16_rn(v); }
 };
 template <>
 struct Elem<__half> {
+  static __device__ float2 unpack(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
+  static __device__ uint32_t pack(float a, float b) {
+    const __half2 v = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&v);
+  }
   static __device__ float to(__half v) { return __half2float(v); }
   static __device__ __half from(float v) { return __float2half_rn(v); }
 };
@@ -72,32 +82,89 @@ struct __align__(sizeof(T) * V) Chunk {
   T e[V];
 };
 
+// Turns the pairs of a chunk: element j of lo with element j of hi (SPLIT), or neighbours of lo.
+template <class T, int V, bool SPLIT, int N>
+__device__ __forceinline__ void turn(Chunk<T, V> &lo, Chunk<T, V> &hi, const float2 (&a)[N]) {
+  if constexpr (sizeof(T) == 2 && V > 1) {         // a word holds two elements
+    uint32_t(&l)[V / 2] = *reinterpret_cast<uint32_t(*)[V / 2]>(&lo), (&h)[V / 2] = *reinterpret_cast<uint32_t(*)[V / 2]>(&hi);
+#pragma unroll
+    for (int k = 0; k < V / 2; ++k) {
+      if constexpr (SPLIT) {
+        const float2 x = Elem<T>::unpack(l[k]), y = Elem<T>::unpack(h[k]);
+        const float2 p = a[2 * k], q = a[2 * k + 1];
+        l[k] = Elem<T>::pack(x.x * p.x - y.x * p.y, x.y * q.x - y.y * q.y);
+        h[k] = Elem<T>::pack(y.x * p.x + x.x * p.y, y.y * q.x + x.y * q.y);
+      } else {
+        const float2 x = Elem<T>::unpack(l[k]);
+        l[k] = Elem<T>::pack(x.x * a[k].x - x.y * a[k].y, x.y * a[k].x + x.x * a[k].y);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      T &pa = SPLIT ? lo.e[j] : lo.e[(2 * j) % V], &pb = SPLIT ? hi.e[j] : lo.e[(2 * j + 1) % V];
+      const float x = Elem<T>::to(pa), y = Elem<T>::to(pb);
+      pa = Elem<T>::from(x * a[j].x - y * a[j].y);
+      pb = Elem<T>::from(y * a[j].x + x * a[j].y);
+    }
+  }
+}
+
 // V: elements of an access.  PAIRS: neighbouring elements form a pair; a chunk then holds its pairs whole (V = 1:
 // two accesses, as in the HALF layout with the partner one element on).  APPEND: k and v go to pages.
+// The first heads' loads are under way while the angles are computed and the slots looked up.
 template <class T, int V, bool PAIRS, bool APPEND>
-__global__ void __launch_bounds__(kRotThreads) rotary_kernel(const __grid_constant__ RotPlan P, float sign) {
+__global__ void __launch_bounds__(kRotThreads, 3) rotary_kernel(const __grid_constant__ RotPlan P, float sign) {
   using C = Chunk<T, V>;
   constexpr bool kSplit = !PAIRS || V == 1;            // a rotated chunk has a partner chunk
   constexpr int kAngles = kSplit ? V : V / 2;          // pairs of a chunk position
   __shared__ float2 cs[2 * kRotThreads * 4];           // [token slot][pair]
   __shared__ int64_t slot[kRotThreads];                // byte offset of a token's slot, -1: none
+  const int n = P.n1 + P.n2;
+  const int c = threadIdx.x % n, rest = threadIdx.x / n;
+  const int h0 = rest % P.head_slots, tok = rest / P.head_slots;
+  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * P.tok_slots, t = t0 + tok;
+  const bool here = tok < P.tok_slots && t < P.n_tokens;
+  const bool turns = c < P.n1;
+  const int pairs = P.pairs, hd = P.head_dim;
+  // this thread's elements of a head: first .. first + V, and the partner's
+  const int first = turns ? (PAIRS && V == 1 ? 2 * c : c * V) : 2 * pairs + (c - P.n1) * V;
+  const int partner = first + (PAIRS ? 1 : P.half_off);
+  C lo[kRotUnroll], hi[kRotUnroll];
+  auto load = [&](int hb) {
+#pragma unroll
+    for (int u = 0; u < kRotUnroll; ++u) {
+      const int h = hb + u * P.head_slots;
+      if (h >= P.heads) continue;
+      const uint8_t *src;
+      if (!APPEND || h < P.q_heads) {
+        src = P.x + t * P.xs + static_cast<int64_t>(h) * hd * sizeof(T);
+      } else {
+        const int kh = h - P.q_heads;
+        const bool is_v = kh >= P.kv_heads;
+        src = (is_v ? P.v + t * P.vs : P.k + t * P.ks) + static_cast<int64_t>(is_v ? kh - P.kv_heads : kh) * hd * sizeof(T);
+      }
+      const T *s = reinterpret_cast<const T *>(src);
+      lo[u] = *reinterpret_cast<const C *>(s + first);
+      if (kSplit && turns) hi[u] = *reinterpret_cast<const C *>(s + partner);
+    }
+  };
   pdl_wait_and_release();
-  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * P.tok_slots;
-  const int pairs = P.pairs;
-  for (int e = threadIdx.x; e < P.tok_slots * pairs; e += kRotThreads) {
-    const int tok = e / pairs, i = e - tok * pairs;
-    if (t0 + tok >= P.n_tokens) break;
+  if (here) load(h0);
+  for (int e = threadIdx.x; e < P.tok_slots * pairs; e += blockDim.x) {
+    const int tk = e / pairs, i = e - tk * pairs;
+    if (t0 + tk >= P.n_tokens) break;
     const int axis = (i >= P.axis1) + (i >= P.axis2);
-    const int64_t pos = __ldg(P.positions + axis * P.pos_axis_stride + t0 + tok);
+    const int64_t pos = __ldg(P.positions + axis * P.pos_axis_stride + t0 + tk);
     const uint64_t phase = static_cast<uint64_t>(pos) * P.freq[i];
-    float s, c;
-    sincospif(static_cast<float>(static_cast<int32_t>(phase >> 32)) * 4.656612873077393e-10f, &s, &c);   // 2^-31
-    cs[e] = make_float2(P.magnitude * c, sign * P.magnitude * s);
+    float sn, cn;
+    sincospif(static_cast<float>(static_cast<int32_t>(phase >> 32)) * 4.656612873077393e-10f, &sn, &cn);   // 2^-31
+    cs[e] = make_float2(P.magnitude * cn, sign * P.magnitude * sn);
   }
   if (APPEND && threadIdx.x < P.tok_slots && t0 + threadIdx.x < P.n_tokens) {
-    const int64_t t = t0 + threadIdx.x;
-    const int32_t row = __ldg(P.rows + t);
-    const int32_t seq = P.seqs ? __ldg(P.seqs + t) : static_cast<int32_t>(t);
+    const int64_t tt = t0 + threadIdx.x;
+    const int32_t row = __ldg(P.rows + tt);
+    const int32_t seq = P.seqs ? __ldg(P.seqs + tt) : static_cast<int32_t>(tt);
     int64_t off = -1;
     if (row >= 0) {
       if (static_cast<uint32_t>(seq) < static_cast<uint32_t>(P.pool.num_seqs)) off = P.pool.row_offset(seq, row);
@@ -106,63 +173,35 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(const __grid_consta
     slot[threadIdx.x] = off;
   }
   __syncthreads();
-  const int n = P.n1 + P.n2;
-  const int c = threadIdx.x % n, rest = threadIdx.x / n;
-  const int h0 = rest % P.head_slots, tok = rest / P.head_slots;
-  const int64_t t = t0 + tok;
-  if (tok >= P.tok_slots || t >= P.n_tokens) return;
-  const bool turns = c < P.n1;
-  // this thread's elements of a head: first .. first + V, and the partner's
-  const int first = turns ? (PAIRS && V == 1 ? 2 * c : c * V) : 2 * pairs + (c - P.n1) * V;
-  const int partner = first + (PAIRS ? 1 : P.half_off);
+  if (!here) return;
   float2 a[kAngles];
   if (turns) {
 #pragma unroll
     for (int j = 0; j < kAngles; ++j) a[j] = cs[tok * pairs + c * kAngles + j];
   }
   const int64_t off = APPEND ? slot[tok] : 0;
-  const int hd = P.head_dim;
-  for (int hb = h0; hb < P.heads; hb += kRotUnroll * P.head_slots) {
-    C lo[kRotUnroll], hi[kRotUnroll];
-    T *dst[kRotUnroll];
+  for (int hb = h0;;) {
 #pragma unroll
     for (int u = 0; u < kRotUnroll; ++u) {
       const int h = hb + u * P.head_slots;
-      dst[u] = nullptr;
       if (h >= P.heads) continue;
-      const uint8_t *src;
+      uint8_t *dst;
       if (!APPEND || h < P.q_heads) {
-        const int64_t ho = static_cast<int64_t>(h) * hd * sizeof(T);
-        src = P.x + t * P.xs + ho;
-        dst[u] = reinterpret_cast<T *>(P.out + t * P.outs + ho);
+        dst = P.out + t * P.outs + static_cast<int64_t>(h) * hd * sizeof(T);
       } else {
         const int kh = h - P.q_heads;
         const bool is_v = kh >= P.kv_heads;
-        const int hh = is_v ? kh - P.kv_heads : kh;
         if (off < 0) continue;
-        src = (is_v ? P.v + t * P.vs : P.k + t * P.ks) + static_cast<int64_t>(hh) * hd * sizeof(T);
-        dst[u] = reinterpret_cast<T *>((is_v ? P.pool.v : P.pool.k) + off + hh * P.pool.head_stride);
+        dst = (is_v ? P.pool.v : P.pool.k) + off + (is_v ? kh - P.kv_heads : kh) * P.pool.head_stride;
       }
-      const T *s = reinterpret_cast<const T *>(src);
-      lo[u] = *reinterpret_cast<const C *>(s + first);
-      if (kSplit && turns) hi[u] = *reinterpret_cast<const C *>(s + partner);
+      if (turns && h < P.rot_heads) turn<T, V, kSplit>(lo[u], hi[u], a);
+      T *d = reinterpret_cast<T *>(dst);
+      *reinterpret_cast<C *>(d + first) = lo[u];
+      if (kSplit && turns) *reinterpret_cast<C *>(d + partner) = hi[u];
     }
-#pragma unroll
-    for (int u = 0; u < kRotUnroll; ++u) {
-      if (!dst[u]) continue;
-      if (turns && hb + u * P.head_slots < P.rot_heads) {
-#pragma unroll
-        for (int j = 0; j < kAngles; ++j) {
-          T &pa = kSplit ? lo[u].e[j] : lo[u].e[(2 * j) % V];
-          T &pb = kSplit ? hi[u].e[j] : lo[u].e[(2 * j + 1) % V];
-          const float x = Elem<T>::to(pa), y = Elem<T>::to(pb);
-          pa = Elem<T>::from(x * a[j].x - y * a[j].y);
-          pb = Elem<T>::from(y * a[j].x + x * a[j].y);
-        }
-      }
-      *reinterpret_cast<C *>(dst[u] + first) = lo[u];
-      if (kSplit && turns) *reinterpret_cast<C *>(dst[u] + partner) = hi[u];
-    }
+    hb += kRotUnroll * P.head_slots;
+    if (hb >= P.heads) break;
+    load(hb);
   }
 }
 
@@ -175,22 +214,23 @@ cudaError_t launch_rotary(RotPlan &P, bool pairs_layout, bool wide, float sign, 
   P.n2 = (D - r) / V;
   P.half_off = r / 2;
   const int n = P.n1 + P.n2;
-  // one thread per head as far as the CTA reaches; more tokens per CTA only when there are enough CTAs
+  // Few tokens: a thread per head as far as the CTA reaches.  Many: kRotUnroll heads per thread, and as many tokens
+  // as fill the CTA.
   const int room = kRotThreads / n;
   P.head_slots = std::min(P.heads, room);
   P.tok_slots = 1;
-  const int64_t sms = device_sm_count();
-  if (P.n_tokens >= 4 * sms) {
-    P.head_slots = std::min(std::max(1, (P.heads + kRotUnroll - 1) / kRotUnroll), room);
+  if (P.n_tokens >= 4 * static_cast<int64_t>(device_sm_count())) {
+    P.head_slots = std::min((P.heads + kRotUnroll - 1) / kRotUnroll, room);
     P.tok_slots = room / P.head_slots;
   }
+  const int threads = (n * P.head_slots * P.tok_slots + 31) / 32 * 32;
   const int64_t grid = (P.n_tokens + P.tok_slots - 1) / P.tok_slots;
   void (*fn)(RotPlan, float);
   if (wide)
     fn = pairs_layout ? rotary_kernel<T, W, true, APPEND> : rotary_kernel<T, W, false, APPEND>;
   else
     fn = pairs_layout ? rotary_kernel<T, 1, true, APPEND> : rotary_kernel<T, 1, false, APPEND>;
-  const cudaError_t e = launch_pdl(fn, dim3(static_cast<unsigned>(grid)), dim3(kRotThreads), 0, stream, P, sign);
+  const cudaError_t e = launch_pdl(fn, dim3(static_cast<unsigned>(grid)), dim3(threads), 0, stream, P, sign);
   if (e == cudaSuccess) count_launches(1);
   return e;
 }
