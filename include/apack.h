@@ -446,7 +446,8 @@ apack_status apack_rotary_append(const apack_rotary_spec *spec, const apack_page
    A NaN or infinity among the rows themselves makes what it enters NaN (an infinite value: infinite or NaN).
    q: [num_seqs][Hq][D] at q_token_stride bytes, cache dtype, 16-byte aligned; scale > 0 (1/sqrt(D) is usual).
    out: [num_seqs][Hq][D], contiguous, 16-byte aligned, out_dtype the cache's or APACK_FP32.  lse: fp32
-   [num_seqs][Hq] or NULL, ln sum_r exp(scale q.k).  Hq / Hkv <= 32 (APACK_EUNSUPPORTED otherwise), Hq <= 1024.
+   [num_seqs][Hq] or NULL, ln sum_r exp(scale q.k).  Hq / Hkv <= 32 and tables of at most
+   3.4e10 / Hkv tokens in all sequences together (APACK_EUNSUPPORTED otherwise), Hq <= 1024.
    fp32 softmax and accumulation; the sums' order depends on the lengths alone (deterministic).
    A length below 0 or above max_pages*page_tokens is read as the nearest of the two, and a page number outside
    the pool as a page of zeros; both record APACK_EDEVICE in the error word of ws.

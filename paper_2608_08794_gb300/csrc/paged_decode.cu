@@ -28,7 +28,8 @@
 namespace apack {
 namespace {
 
-constexpr int kTile = 16;                       // tokens of a stage
+// Tokens of a stage: 8 KB of K and V of one head.
+constexpr int tile_tokens(int D) { return D == 64 ? 32 : 16; }
 constexpr int kWarps = 8;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kMergeFloats = 3584;              // shared-memory buffer of the warps' merge: 7 warps, 4 m-tiles
@@ -39,7 +40,7 @@ constexpr float kRescale = 8.f;
 
 // What a (sequence, head group) costs a CTA beyond its tiles (its queries' latency, the merge, the write), as the
 // bytes of K and V that it could have streamed meanwhile.
-constexpr int kSegBytes = 65536;
+constexpr int kSegBytes = 196608;
 
 struct PdPlan {
   PoolView pool;
@@ -47,12 +48,13 @@ struct PdPlan {
   const uint8_t *q;
   int64_t q_stride;                  // bytes between sequences
   int32_t hq, group;                 // query heads, per KV head
-  int32_t heads_cta, wph, groups;    // KV heads of a CTA, warps per head, head groups
+  int32_t heads_cta, wph_log, groups;   // KV heads of a CTA, log2 of the warps per head, head groups
   int32_t box_tokens, boxes;         // tokens of one TMA box, boxes of a tile
   int32_t max_rows;
   int32_t min_tiles;                 // smallest share of a CTA
   int32_t seg_cost;                  // what a segment costs beyond its tiles, in tiles
   float scale2;                      // scale * log2(e)
+  float grow;                        // kRescale in units of q.k
   void *out;
   int32_t out_fp32;
   float *lse;
@@ -121,6 +123,8 @@ __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map
       : "memory");
 }
 
+__device__ __forceinline__ void prefetch_l2(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
 __device__ __forceinline__ void head_barrier(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
 
 __device__ __forceinline__ int clamped_length(const PdPlan &P, int b, bool report) {
@@ -129,31 +133,50 @@ __device__ __forceinline__ int clamped_length(const PdPlan &P, int b, bool repor
   if (report && c != n) raise_device_error(P.err, APACK_EDEVICE, 81, b, n);
   return c;
 }
-__device__ __forceinline__ int tiles_of(int len) { return (len >> 4) + ((len & 15) != 0); }
+// n / d in 32 bits where they do (a 64-bit division takes some 100 instructions).
+__device__ __forceinline__ int quotient(int64_t n, int d) {
+  return static_cast<int>((n >> 32) == 0 ? static_cast<uint32_t>(n) / static_cast<uint32_t>(d) : n / d);
+}
+template <int TILE>
+__device__ __forceinline__ int tiles_of(int len) {
+  return len / TILE + (len % TILE != 0);
+}
 
-// A walk over the (sequence, head group) segments of a CTA's share [u0, u1) of the work list.  A segment takes up
-// seg_cost + nt units of the list, the tiles behind the cost.
+// The clamped lengths of kWindow sequences from b0 on, in a warp's shared memory: a walk from sequence to sequence
+// then costs no trip to L2 per step (a share of four short sequences reached its first loads 6 us late without).
+constexpr int kWindow = 64;
+struct LengthWindow {
+  int b0;
+  const int *v;
+  __device__ __forceinline__ int at(const PdPlan &P, int b) const {
+    return b - b0 < kWindow ? v[b - b0] : clamped_length(P, b, false);
+  }
+};
+
+// A walk over the (sequence, head group) segments of a CTA's share, `n` units of the work list; positions are counted
+// from the share's first unit.  A segment takes up seg_cost + nt units, the tiles behind the cost.
+template <int TILE>
 struct Walk {
   int b, g, len, nt;     // segment, its sequence's length and tiles
   int ts, te;            // the share's tiles of it
-  int64_t s;             // its first unit
-  __device__ __forceinline__ void span(int cost, int64_t u0, int64_t u1) {
-    ts = static_cast<int>(min(max(u0 - s - cost, static_cast<int64_t>(0)), static_cast<int64_t>(nt)));
-    te = static_cast<int>(min(max(u1 - s - cost, static_cast<int64_t>(0)), static_cast<int64_t>(nt)));
+  int first;             // position of its first tile (below 0 where an earlier share starts it)
+  __device__ __forceinline__ void span(int n) {
+    ts = min(max(-first, 0), nt);
+    te = min(max(n - first, 0), nt);
   }
   // The next segment with a tile in the share.
-  __device__ __forceinline__ bool next(const PdPlan &P, int64_t u0, int64_t u1) {
+  __device__ __forceinline__ bool next(const PdPlan &P, const LengthWindow &lens, int n) {
     do {
-      s += P.seg_cost + nt;
-      if (s + P.seg_cost >= u1) return false;
+      first += nt + P.seg_cost;
+      if (first >= n) return false;
       if (++g >= P.groups) {
         g = 0;
         do {
-          len = clamped_length(P, ++b, false);
+          len = lens.at(P, ++b);
         } while (len == 0);
-        nt = tiles_of(len);
+        nt = tiles_of<TILE>(len);
       }
-      span(P.seg_cost, u0, u1);
+      span(n);
     } while (ts >= te);
     return true;
   }
@@ -164,6 +187,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     paged_chunk_kernel(const __grid_constant__ PdPlan P, const __grid_constant__ CUtensorMap kmap,
                        const __grid_constant__ CUtensorMap vmap) {
   constexpr int KS = D / 16;                          // k-steps of S, m-tiles of O^T
+  constexpr int kTile = tile_tokens(D), KM = kTile / 16;   // m-tiles of S, k-steps of O^T
   constexpr int kHalf = kTile * D * 2;                // bytes of a stage's K (and V)
   constexpr int kStages = kStageBytesCta / kWarps / (2 * kHalf);
   constexpr int kBlk = kTile * 128;                   // bytes of one 64-feature block of a stage
@@ -171,6 +195,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   float *merge = reinterpret_cast<float *>(smem + kStageBytesCta);
   float2 *stat = reinterpret_cast<float2 *>(merge + kMergeFloats);        // [warp][NT * 8]
   uint64_t *bars = reinterpret_cast<uint64_t *>(stat + kWarps * 32);      // [warp][kStages]
+  int *window = reinterpret_cast<int *>(bars + kWarps * 8);               // [warp][kWindow]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint64_t *full = bars + warp * kStages;
   const uint32_t ring = smem_u32(smem) + warp * (kStages * 2 * kHalf);
@@ -178,91 +203,116 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = 0; i < kStages; ++i) mbar_init(&full[i], 1);
     fence_mbar_init();
   }
+  if (threadIdx.x == 32) {
+    tma_prefetch_desc(&kmap);
+    tma_prefetch_desc(&vmap);
+  }
+  // lengths and page table on their way to L2 while the launch before this one ends (what that launch may still
+  // write of them is read from L2 all the same)
+  {
+    const int line = blockIdx.x * kThreads + threadIdx.x, row_lines = (P.pool.max_pages + 31) / 32;
+    if (line * 32 < P.pool.num_seqs) prefetch_l2(P.seqlens + line * 32);
+    const int b = line / row_lines;
+    if (b < P.pool.num_seqs) prefetch_l2(P.pool.table + b * P.pool.table_stride + (line - b * row_lines) * 32);
+  }
   __syncwarp();
   pdl_wait_and_release();
 
-  // ---- this CTA's share (every warp by itself: no barrier before the first load)
-  const int B = P.pool.num_seqs, grid = gridDim.x, cta = blockIdx.x;
-  const int per = (B + 31) / 32;
-  const int cost = P.seg_cost;
-  int64_t mine = 0;
-  for (int i = 0; i < per; ++i) {
-    const int b = lane * per + i;
-    if (b < B) {
-      const int nt = tiles_of(clamped_length(P, b, warp == 0 && cta == 0));
-      if (nt > 0) mine += nt + cost;
-    }
-  }
-  int64_t incl = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o *= 2) {
-    const int64_t y = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += y;
-  }
-  // the list starts behind the first segment's cost: every CTA pays one anyway
-  const int64_t W = __shfl_sync(0xffffffffu, incl, 31) * P.groups - cost;
-  const int C = static_cast<int>(min(static_cast<int64_t>(grid), max(W / P.min_tiles, static_cast<int64_t>(1))));
-  if (threadIdx.x == 0) P.info[cta] = make_int4(0, 0, 0, 0);
-  // empty sequences: zeros and -infinity
-  for (int b = cta; b < B; b += grid) {
-    if (clamped_length(P, b, false) > 0) continue;
-    for (int i = threadIdx.x; i < P.hq * D; i += kThreads) {
-      const int64_t o = static_cast<int64_t>(b) * P.hq * D + i;
-      if (P.out_fp32)
-        static_cast<float *>(P.out)[o] = 0.f;
-      else
-        static_cast<uint16_t *>(P.out)[o] = 0;
-    }
-    if (P.lse)
-      for (int i = threadIdx.x; i < P.hq; i += kThreads) P.lse[static_cast<int64_t>(b) * P.hq + i] = -INFINITY;
-  }
+  // ---- this CTA's share (every warp by itself: no barrier before the first load).  The list starts behind the first
+  // segment's cost, which every CTA pays one of anyway.
+  const int B = P.pool.num_seqs, grid = gridDim.x, cta = blockIdx.x, cost = P.seg_cost;
   const int hw = warp % P.heads_cta, sub = warp / P.heads_cta;
-  if (W <= 0 || cta >= C || sub >= P.wph) return;
-  const int active = 32 * P.heads_cta * P.wph;        // threads of the warps at work
-  const int64_t u0 = cost + W * cta / C, u1 = cost + W * (cta + 1) / C;
-  Walk seg;
+  const bool report = warp == 0 && cta == 0;
+  const int wph = 1 << P.wph_log;
+  if (threadIdx.x == 0) P.info[cta] = make_int4(0, 0, 0, 0);
+  auto units = [&](int len) { return len > 0 ? (tiles_of<kTile>(len) + cost) * P.groups : 0; };
+  auto scan = [&](int v) {                             // inclusive, over the lanes
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const int y = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += y;
+    }
+    return v;
+  };
+  LengthWindow lens;
+  lens.v = window + warp * kWindow;
+  int W, mine, n0 = 0, n1 = 0;
+  const int per = (B + 31) / 32;                       // sequences of a lane
+  if (B <= kWindow) {
+    // the window holds them all; lane and lane + 32 are its sequences
+    if (lane < B) n0 = clamped_length(P, lane, report);
+    if (lane + 32 < B) n1 = clamped_length(P, lane + 32, report);
+    window[warp * kWindow + lane] = n0;
+    window[warp * kWindow + lane + 32] = n1;
+    lens.b0 = 0;
+    mine = units(n0);
+    W = __reduce_add_sync(0xffffffffu, mine + units(n1));
+  } else {
+    mine = 0;
+    for (int i = 0; i < per; ++i)
+      if (lane * per + i < B) mine += units(clamped_length(P, lane * per + i, report));
+    W = __reduce_add_sync(0xffffffffu, mine);
+  }
+  W -= cost;
+  const int C = min(grid, max(W / P.min_tiles, 1));
+  if (W <= 0 || cta >= C || sub >= wph) return;
+  const int active = 32 * P.heads_cta * wph;        // threads of the warps at work
+  const int u0 = cost + quotient(static_cast<int64_t>(W) * cta, C);
+  const int n = cost + quotient(static_cast<int64_t>(W) * (cta + 1), C) - u0;
+  Walk<kTile> seg;
   {
-    const int64_t lo = (incl - mine) * P.groups, hi = incl * P.groups;
-    const int src = __ffs(__ballot_sync(0xffffffffu, u0 >= lo && u0 < hi)) - 1;
-    int64_t off = u0 - __shfl_sync(0xffffffffu, lo, src);
-    int b = src * per;
-    for (;; ++b) {
-      seg.len = clamped_length(P, b, false);
-      seg.nt = tiles_of(seg.len);
-      const int64_t all = seg.nt > 0 ? static_cast<int64_t>(seg.nt + cost) * P.groups : 0;
-      if (off < all) break;
-      off -= all;
+    int off = u0, b = 0, incl = scan(mine);
+    const int half = __shfl_sync(0xffffffffu, incl, 31);
+    if (B <= kWindow && u0 >= half) {                  // among the second 32
+      mine = units(n1);
+      incl = scan(mine) + half;
+      b = 32;
+    }
+    const int src = __ffs(__ballot_sync(0xffffffffu, u0 >= incl - mine && u0 < incl)) - 1;
+    off -= __shfl_sync(0xffffffffu, incl - mine, src);
+    if (B <= kWindow) {
+      b += src;
+      __syncwarp();
+    } else {
+      b = lens.b0 = src * per;
+      for (int i = lane; i < kWindow; i += 32) window[warp * kWindow + i] = b + i < B ? clamped_length(P, b + i, false) : 0;
+      __syncwarp();
+      for (; off >= units(lens.at(P, b)); ++b) off -= units(lens.at(P, b));
     }
     seg.b = b;
-    seg.g = static_cast<int>(off / (seg.nt + cost));
-    seg.s = u0 - (off - static_cast<int64_t>(seg.g) * (seg.nt + cost));
-    seg.span(cost, u0, u1);
-    if (seg.ts >= seg.te && !seg.next(P, u0, u1)) return;      // the share holds no tile (for all warps alike)
+    seg.len = lens.at(P, b);
+    seg.nt = tiles_of<kTile>(seg.len);
+    seg.g = P.groups == 1 ? 0 : off / (seg.nt + cost);
+    seg.first = cost - (off - seg.g * (seg.nt + cost));
+    seg.span(n);
+    if (seg.ts >= seg.te && !seg.next(P, lens, n)) return;      // the share holds no tile (for all warps alike)
   }
 
   // ---- producer: a queue of this warp's next 32 tiles, one per lane; the lane of a tile issues its loads
-  Walk head_w = seg;                                  // of the first tile behind the queue
+  Walk<kTile> head_w = seg;                                  // of the first tile behind the queue
   int head_t = seg.ts + sub;
   bool head_ok = true;
   while (head_ok && head_t >= head_w.te) {
-    head_ok = head_w.next(P, u0, u1);
+    head_ok = head_w.next(P, lens, n);
     head_t = head_w.ts + sub;
   }
-  int32_t q_page = 0, q_head = 0, q_b = 0, q_t = 0, q_len = 0;
+  int32_t q_page[KM], q_head = 0, q_b = 0, q_t = 0, q_len = 0;
   uint32_t q_in = 0;
   int queued = 0, issued = 0, used = 0;
+  int issue_slot = 0, use_slot = 0;
+  uint32_t use_phase = 0;
   auto refill = [&] {
-    Walk w = head_w;
+    Walk<kTile> w = head_w;
     int t = head_t, skip = lane;
     bool ok = head_ok;
     while (ok) {
-      const int here = t < w.te ? (w.te - t + P.wph - 1) / P.wph : 0;
+      const int here = t < w.te ? (w.te - t + wph - 1) >> P.wph_log : 0;
       if (skip < here) {
-        t += skip * P.wph;
+        t += skip << P.wph_log;
         break;
       }
       skip -= here;
-      ok = w.next(P, u0, u1);
+      ok = w.next(P, lens, n);
       t = w.ts + sub;
     }
     if (ok) {
@@ -270,10 +320,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       q_t = t;
       q_len = w.len;
       q_head = w.g * P.heads_cta + hw;
-      if (P.boxes == 1) {
+      if (P.boxes <= KM) {
         const uint32_t p = P.pool.page_tokens.div(t * kTile);
-        q_page = __ldg(P.pool.table + w.b * P.pool.table_stride + p);
+        const int32_t *row = P.pool.table + w.b * P.pool.table_stride + p;
         q_in = t * kTile - p * P.pool.page_tokens.d;
+        q_page[0] = __ldg(row);
+        // pages of 16 (48, ...) tokens: the tile's second half may be the next page's
+        if (KM > 1) q_page[KM - 1] = P.boxes > 1 && t * kTile + 16 < w.len && q_in + 16 >= P.pool.page_tokens.d ? __ldg(row + 1) : q_page[0];
       }
     }
     queued += __popc(__ballot_sync(0xffffffffu, ok));
@@ -282,10 +335,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     head_w.g = __shfl_sync(0xffffffffu, w.g, 31);
     head_w.len = __shfl_sync(0xffffffffu, w.len, 31);
     head_w.nt = __shfl_sync(0xffffffffu, w.nt, 31);
-    head_w.ts = __shfl_sync(0xffffffffu, w.ts, 31);
-    head_w.te = __shfl_sync(0xffffffffu, w.te, 31);
-    head_w.s = __shfl_sync(0xffffffffu, w.s, 31);
-    head_t = __shfl_sync(0xffffffffu, t, 31) + P.wph;
+    head_w.first = __shfl_sync(0xffffffffu, w.first, 31);
+    head_w.span(n);
+    head_t = __shfl_sync(0xffffffffu, t, 31) + wph;
   };
   // One TMA box pair; a page outside the pool reads as zeros (the map ends there).
   auto load_box = [&](int slot, int32_t page, uint32_t in_page, int head, int b, int block, uint32_t offset) {
@@ -304,11 +356,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       refill();
       if (issued == queued) return;
     }
-    const int slot = issued % kStages, owner = issued & 31;
-    if (P.boxes == 1) {
+    const int slot = issue_slot, owner = issued & 31;
+    issue_slot = slot + 1 == kStages ? 0 : slot + 1;
+    if (P.boxes <= KM) {
       if (lane == owner) {
-        mbar_arrive_expect_tx(&full[slot], 2 * kHalf);
-        load_box(slot, q_page, q_in, q_head, q_b, 0, 0);
+        const bool second = KM > 1 && P.boxes > 1 && q_t * kTile + 16 < q_len;
+        mbar_arrive_expect_tx(&full[slot], KM > 1 && P.boxes > 1 && !second ? kHalf : 2 * kHalf);
+        load_box(slot, q_page[0], q_in, q_head, q_b, 0, 0);
+        if (second) load_box(slot, q_page[KM - 1], q_in + 16 >= P.pool.page_tokens.d ? 0 : q_in + 16, q_head, q_b, 0, 2048);
       }
     } else {
       // pages that are not whole tiles: a box per lane, those that hold a row of the sequence
@@ -335,39 +390,48 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t vrow = (lane & 7) + (lane >> 4) * 8, vchunk = (lane >> 3) & 1;
   bool dead = false;                                  // a wait gave up: no more loads are issued or waited for
   int first_seg = 1;
-  do {
-    const int head = seg.g * P.heads_cta + hw;
-    uint32_t qf[NT][KS][2];
-    {
-      const uint8_t *qb = P.q + seg.b * P.q_stride + static_cast<int64_t>(head) * P.group * D * 2;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const int r = nt * 8 + g8;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-            qf[nt][ks][e] = r < P.group ? __ldg(reinterpret_cast<const uint32_t *>(qb + (r * D + ks * 16 + e * 8 + t4 * 2) * 2)) : 0u;
-      }
-    }
-    float o[NT][KS][4], m[NT][2], l[NT][2];
+  // query fragments; with registers to spare the next segment's are loaded during this one
+  constexpr bool kAhead = NT == 1;
+  using QFrag = uint32_t[NT][KS][2];
+  auto load_q = [&](const Walk<kTile> &w, QFrag &f) {
+    const uint8_t *qb = P.q + w.b * P.q_stride + static_cast<int64_t>(w.g * P.heads_cta + hw) * P.group * D * 2;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      m[nt][0] = m[nt][1] = -INFINITY;
+      const int r = nt * 8 + g8;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          f[nt][ks][e] = r < P.group ? __ldg(reinterpret_cast<const uint32_t *>(qb + (r * D + ks * 16 + e * 8 + t4 * 2) * 2)) : 0u;
+    }
+  };
+  QFrag qf, q_next;
+  load_q(seg, qf);
+  for (;;) {
+    Walk<kTile> after = seg;
+    const bool go_on = after.next(P, lens, n);
+    if (kAhead && go_on) load_q(after, q_next);
+    const int head = seg.g * P.heads_cta + hw;
+    float o[NT][KS][4], m[NT][2], l[NT][2], limit[NT][2];   // m: reference, log2 units; limit: of q.k, where it grows
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      m[nt][0] = m[nt][1] = limit[nt][0] = limit[nt][1] = -INFINITY;
       l[nt][0] = l[nt][1] = 0.f;
 #pragma unroll
       for (int i = 0; i < KS; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
     }
-    for (int t = seg.ts + sub; t < seg.te; t += P.wph) {
-      if (dead) break;
-      const int slot = used % kStages;
-      if (!__all_sync(0xffffffffu, mbar_wait(&full[slot], (used / kStages) & 1u, kWaitLimitNs))) {
+    for (int t = seg.ts + sub; t < seg.te && !dead; t += wph) {
+      if (!__all_sync(0xffffffffu, mbar_wait(&full[use_slot], use_phase, kWaitLimitNs))) {
         if (lane == 0) raise_device_error(P.err, APACK_ETIMEOUT, 83, cta, warp);
         dead = true;
         break;
       }
       ++used;
-      const uint32_t kb = ring + slot * (2 * kHalf), vb = kb + kHalf;
+      const uint32_t kb = ring + use_slot * (2 * kHalf), vb = kb + kHalf;
+      if (++use_slot == kStages) {
+        use_slot = 0;
+        use_phase ^= 1;
+      }
       const int valid = seg.len - t * kTile;          // rows of the tile that belong to the sequence
       if (valid < kTile) {
         // what lies behind the last row takes no part: its logits become -infinity below, and its values
@@ -380,39 +444,54 @@ __global__ void __launch_bounds__(kThreads, 1)
         fence_proxy_async_smem();                     // before TMA writes the slot again
         __syncwarp();
       }
-      float s[NT][4];
+      float s[KM][NT][4];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+      for (int km = 0; km < KM; ++km)
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        uint32_t a[4];
-        const uint32_t ch = ks * 2 + kchunk;
-        ldmatrix4(kb + (ch >> 3) * kBlk + krow * 128 + (((ch & 7) ^ (krow & 7)) << 4), a);
+        for (int nt = 0; nt < NT; ++nt) s[km][nt][0] = s[km][nt][1] = s[km][nt][2] = s[km][nt][3] = 0.f;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) Half16<T>::mma(s[nt], a, qf[nt][ks][0], qf[nt][ks][1]);
-      }
-      // lane: keys g8 and g8 + 8, query rows 2 t4 and 2 t4 + 1
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int km = 0; km < KM; ++km) {
+          uint32_t a[4];
+          const uint32_t ch = ks * 2 + kchunk;
+          ldmatrix4(kb + (ch >> 3) * kBlk + (km * 16 + krow) * 128 + (((ch & 7) ^ (krow & 7)) << 4), a);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) Half16<T>::mma(s[km][nt], a, qf[nt][ks][0], qf[nt][ks][1]);
+        }
+      // lane: keys g8 and g8 + 8 of 16, query rows 2 t4 and 2 t4 + 1
+      if (valid < kTile)
+#pragma unroll
+        for (int km = 0; km < KM; ++km)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (km * 16 + g8 + (i >> 1) * 8 >= valid) s[km][nt][i] = -INFINITY;
+      // (a NaN logit leaves the maximum to the others, and its probability NaN)
+      float top[NT][2];
       bool grow = false;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s[nt][i] = (g8 + (i >> 1) * 8) < valid ? s[nt][i] * P.scale2 : -INFINITY;
-          grow |= !(s[nt][i] <= m[nt][i & 1] + kRescale);
+        for (int e = 0; e < 2; ++e) {
+          top[nt][e] = fmaxf(s[0][nt][e], s[0][nt][e + 2]);
+          if (KM > 1) top[nt][e] = fmaxf(top[nt][e], fmaxf(s[KM - 1][nt][e], s[KM - 1][nt][e + 2]));
+          grow |= !(top[nt][e] <= limit[nt][e]);
         }
-      }
       if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float x = fmaxf(s[nt][e], s[nt][e + 2]);
+            float x = top[nt][e];
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-            const float mn = fmaxf(m[nt][e], x);
+            const float mn = fmaxf(m[nt][e], x * P.scale2);
             const float f = mn == -INFINITY ? 1.f : ex2_approx(m[nt][e] - mn);
             m[nt][e] = mn;
+            limit[nt][e] = fmaxf(limit[nt][e], x + P.grow);
             l[nt][e] *= f;
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
@@ -423,33 +502,37 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       // P as the sum of two 16-bit numbers (2^-17 of it are left out in bf16, 2^-22 in fp16; one alone would cost
       // 2^-9), transposed into B fragments
-      uint32_t hi[NT][2], lo[NT][2];
+      uint32_t hi[KM][NT][2], lo[KM][NT][2];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float p[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = ex2_approx(s[nt][i] - m[nt][i & 1]);
-        l[nt][0] += p[0] + p[2];
-        l[nt][1] += p[1] + p[3];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint32_t h = Half16<T>::pack(p[2 * e], p[2 * e + 1]);
-          const float2 hf = Half16<T>::unpack(h);
-          hi[nt][e] = transpose8x8(h);
-          lo[nt][e] = transpose8x8(Half16<T>::pack(p[2 * e] - hf.x, p[2 * e + 1] - hf.y));
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < KS; ++i) {
-        uint32_t a[4];
-        const uint32_t ch = i * 2 + vchunk;
-        ldmatrix4_trans(vb + (ch >> 3) * kBlk + vrow * 128 + (((ch & 7) ^ (vrow & 7)) << 4), a);
+      for (int km = 0; km < KM; ++km)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          Half16<T>::mma(o[nt][i], a, hi[nt][0], hi[nt][1]);
-          Half16<T>::mma(o[nt][i], a, lo[nt][0], lo[nt][1]);
+          float p[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[i] = ex2_approx(fmaf(s[km][nt][i], P.scale2, -m[nt][i & 1]));
+          l[nt][0] += p[0] + p[2];
+          l[nt][1] += p[1] + p[3];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t h = Half16<T>::pack(p[2 * e], p[2 * e + 1]);
+            const float2 hf = Half16<T>::unpack(h);
+            hi[km][nt][e] = transpose8x8(h);
+            lo[km][nt][e] = transpose8x8(Half16<T>::pack(p[2 * e] - hf.x, p[2 * e + 1] - hf.y));
+          }
         }
-      }
+#pragma unroll
+      for (int km = 0; km < KM; ++km)
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+          uint32_t a[4];
+          const uint32_t ch = i * 2 + vchunk;
+          ldmatrix4_trans(vb + (ch >> 3) * kBlk + (km * 16 + vrow) * 128 + (((ch & 7) ^ (vrow & 7)) << 4), a);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            Half16<T>::mma(o[nt][i], a, hi[km][nt][0], hi[km][nt][1]);
+            Half16<T>::mma(o[nt][i], a, lo[km][nt][0], lo[km][nt][1]);
+          }
+        }
       __syncwarp();                                   // every lane has read the stage
       issue();
     }
@@ -465,7 +548,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         x += __shfl_xor_sync(0xffffffffu, x, 16);
         l[nt][e] = x;
       }
-    if (P.wph > 1) {
+    if (wph > 1) {
       if (g8 == 0)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -477,8 +560,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           float M = -INFINITY, L = 0.f;
-          for (int w = 0; w < P.wph; ++w) M = fmaxf(M, stat[(w * P.heads_cta + hw) * 32 + nt * 8 + t4 * 2 + e].x);
-          for (int w = 0; w < P.wph; ++w) {
+          for (int w = 0; w < wph; ++w) M = fmaxf(M, stat[(w * P.heads_cta + hw) * 32 + nt * 8 + t4 * 2 + e].x);
+          for (int w = 0; w < wph; ++w) {
             const float2 x = stat[(w * P.heads_cta + hw) * 32 + nt * 8 + t4 * 2 + e];
             L += x.y * (x.x == M ? 1.f : ex2_approx(x.x - M));
           }
@@ -506,7 +589,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         head_barrier(active);
         if (sub == 0)
-          for (int w = 1; w < P.wph; ++w)
+          for (int w = 1; w < wph; ++w)
 #pragma unroll
             for (int k = 0; k < kSlice; ++k)
 #pragma unroll
@@ -559,14 +642,27 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (threadIdx.x == 0 && seg.ts == 0) {
           // this share starts the segment; the one that holds its last tile ends it
-          const int64_t end = seg.s + seg.nt;         // unit behind the last tile, without the list's first cost
-          const int c_end = static_cast<int>((end * C + W - 1) / W) - 1;
+          const int64_t end = u0 - cost + seg.first + seg.nt;      // unit behind the last tile, without the list's first cost
+          const int c_end = quotient(end * C + W - 1, W) - 1;
           P.info[cta] = make_int4(seg.b, seg.g, c_end - cta + 1, slot);
         }
       }
     }
     first_seg = 0;
-  } while (seg.next(P, u0, u1));
+    if (!go_on) break;
+    seg = after;
+    if (kAhead) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          qf[nt][ks][0] = q_next[nt][ks][0];
+          qf[nt][ks][1] = q_next[nt][ks][1];
+        }
+    } else {
+      load_q(seg, qf);
+    }
+  }
   if (dead)   // loads of the stages that were issued and not used may still be in flight
     for (int n = used; n < issued; ++n) mbar_wait(&full[n % kStages], (n / kStages) & 1u, kWaitLimitNs / 4);
 }
@@ -574,8 +670,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 // Merges the parts of the cut segments.  A unit is (segment, head, 8 query rows, 16 features).  Every CTA lists the
 // shares that start a cut segment (info), then the units of segments of many parts are merged by a CTA each, a run
 // of the parts per warp, and those of few parts by a warp each.
-constexpr int kCombineWarps = 8;
-constexpr int kCombineBatch = 8;      // parts whose loads a warp has in flight
+constexpr int kCombineWarps = 16;
+constexpr int kCombineBatch = 10;     // parts whose loads a warp has in flight
+constexpr int kCombineFew = 30;        // parts that one warp merges
 constexpr int kMaxGrid = 512;
 
 // (max, sum, o) of two query rows (2 t4 and + 1) and two features (g8 and + 8), in log2 units.
@@ -583,17 +680,30 @@ struct PartState {
   float m0, m1, l0, l1;
   float4 o;                            // row 0 feature g8, row 1 g8, row 0 g8 + 8, row 1 g8 + 8
 };
-__device__ __forceinline__ void merge_part(PartState &a, const float4 &ml, const float4 &x) {
-  const float n0 = fmaxf(a.m0, ml.x), n1 = fmaxf(a.m1, ml.z);
-  // equal maxima (both -infinity among them) give the factor 1
-  const float a0 = a.m0 == n0 ? 1.f : ex2_approx(a.m0 - n0), b0 = ml.x == n0 ? 1.f : ex2_approx(ml.x - n0);
-  const float a1 = a.m1 == n1 ? 1.f : ex2_approx(a.m1 - n1), b1 = ml.z == n1 ? 1.f : ex2_approx(ml.z - n1);
-  a.l0 = a.l0 * a0 + ml.y * b0;
-  a.l1 = a.l1 * a1 + ml.w * b1;
-  a.o.x = a.o.x * a0 + x.x * b0;
-  a.o.y = a.o.y * a1 + x.y * b1;
-  a.o.z = a.o.z * a0 + x.z * b0;
-  a.o.w = a.o.w * a1 + x.w * b1;
+// Merges N parts into a: maxima first, then the factors, which do not wait for one another.  Equal maxima (both
+// -infinity among them) give the factor 1.
+template <int N>
+__device__ __forceinline__ void merge_parts(PartState &a, const float4 (&ml)[N], const float4 (&x)[N]) {
+  float n0 = a.m0, n1 = a.m1;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    n0 = fmaxf(n0, ml[k].x);
+    n1 = fmaxf(n1, ml[k].z);
+  }
+  const float a0 = a.m0 == n0 ? 1.f : ex2_approx(a.m0 - n0), a1 = a.m1 == n1 ? 1.f : ex2_approx(a.m1 - n1);
+  a.l0 *= a0;
+  a.l1 *= a1;
+  a.o = make_float4(a.o.x * a0, a.o.y * a1, a.o.z * a0, a.o.w * a1);
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const float b0 = ml[k].x == n0 ? 1.f : ex2_approx(ml[k].x - n0), b1 = ml[k].z == n1 ? 1.f : ex2_approx(ml[k].z - n1);
+    a.l0 += ml[k].y * b0;
+    a.l1 += ml[k].w * b1;
+    a.o.x += x[k].x * b0;
+    a.o.y += x[k].y * b1;
+    a.o.z += x[k].z * b0;
+    a.o.w += x[k].w * b1;
+  }
   a.m0 = n0;
   a.m1 = n1;
 }
@@ -614,7 +724,11 @@ __device__ __forceinline__ PartState merge_run(const PdPlan &P, const int4 &inf,
     }
 #pragma unroll
     for (int k = 0; k < kCombineBatch; ++k)
-      if (p + k < p1) merge_part(a, ml[k], x[k]);
+      if (p + k >= p1) {                        // behind the run: nothing
+        ml[k] = make_float4(-INFINITY, 0.f, -INFINITY, 0.f);
+        x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+    merge_parts(a, ml, x);
   }
   return a;
 }
@@ -643,7 +757,7 @@ __device__ __forceinline__ void write_unit(const PdPlan &P, const int4 &inf, int
 }
 
 template <class T, int D, int NT>
-__global__ void __launch_bounds__(32 * kCombineWarps, 3)
+__global__ void __launch_bounds__(32 * kCombineWarps)
     paged_combine_kernel(const __grid_constant__ PdPlan P, int grid) {
   constexpr int KS = D / 16;
   __shared__ int4 seg[kMaxGrid];
@@ -659,7 +773,7 @@ __global__ void __launch_bounds__(32 * kCombineWarps, 3)
     int few = 0, many = 0;
     for (int c = lane; c - lane < grid; c += 32) {
       const int parts = c < grid ? seg[c].z : 0;
-      const bool is_few = parts > 0 && parts <= kCombineBatch, is_many = parts > kCombineBatch;
+      const bool is_few = parts > 0 && parts <= kCombineFew, is_many = parts > kCombineFew;
       const unsigned f = __ballot_sync(0xffffffffu, is_few), m = __ballot_sync(0xffffffffu, is_many), below = (1u << lane) - 1;
       if (is_few) list[few + __popc(f & below)] = c;
       if (is_many) list[kMaxGrid - 1 - many - __popc(m & below)] = c;
@@ -682,11 +796,29 @@ __global__ void __launch_bounds__(32 * kCombineWarps, 3)
     __syncthreads();
     if (warp == 0) {
       PartState t = {-INFINITY, -INFINITY, 0.f, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+      float4 ml[kCombineWarps], x[kCombineWarps];
 #pragma unroll
-      for (int w = 0; w < kCombineWarps; ++w) merge_part(t, sml[w][lane & 3], so[w][lane]);
+      for (int w = 0; w < kCombineWarps; ++w) {
+        ml[w] = sml[w][lane & 3];
+        x[w] = so[w][lane];
+      }
+      merge_parts(t, ml, x);
       write_unit<T, D, NT>(P, inf, hn, i, t, lane);
     }
     __syncthreads();
+  }
+  // empty sequences: zeros and -infinity
+  for (int b = blockIdx.x; b < P.pool.num_seqs; b += gridDim.x) {
+    if (clamped_length(P, b, false) > 0) continue;
+    for (int i = threadIdx.x; i < P.hq * D; i += 32 * kCombineWarps) {
+      const int64_t o = static_cast<int64_t>(b) * P.hq * D + i;
+      if (P.out_fp32)
+        static_cast<float *>(P.out)[o] = 0.f;
+      else
+        static_cast<uint16_t *>(P.out)[o] = 0;
+    }
+    if (P.lse)
+      for (int i = threadIdx.x; i < P.hq; i += 32 * kCombineWarps) P.lse[static_cast<int64_t>(b) * P.hq + i] = -INFINITY;
   }
   for (int u = warp * gridDim.x + blockIdx.x; u < n_few * per_seg; u += gridDim.x * kCombineWarps) {
     const int4 inf = seg[list[u / per_seg]];
@@ -697,7 +829,7 @@ __global__ void __launch_bounds__(32 * kCombineWarps, 3)
 
 // ------------------------------------------------------------------ host side
 struct PdShape {
-  int group, nt, heads_cta, wph, groups, grid;
+  int group, nt, heads_cta, wph_log, groups, grid;
   size_t info_off, ml_off, part_off, total;
 };
 
@@ -710,7 +842,8 @@ apack_status plan_shape(const apack_paged_cache *c, int32_t hq, PdShape *s) {
   s->heads_cta = 1;
   for (int h = 1; h <= kWarps; ++h)
     if (c->num_kv_heads % h == 0) s->heads_cta = h;
-  s->wph = kWarps / s->heads_cta;
+  s->wph_log = 0;                      // 8 / heads_cta, rounded down to a power of two
+  while ((s->heads_cta << (s->wph_log + 1)) <= kWarps) ++s->wph_log;
   s->groups = c->num_kv_heads / s->heads_cta;
   s->grid = std::min(device_sm_count(), kMaxGrid);
   auto up = [](size_t x) { return (x + 255) & ~static_cast<size_t>(255); };
@@ -723,7 +856,7 @@ apack_status plan_shape(const apack_paged_cache *c, int32_t hq, PdShape *s) {
 }
 
 constexpr size_t kSmem = kStageBytesCta + kMergeFloats * sizeof(float) + kWarps * 32 * sizeof(float2) +
-                         kWarps * 8 * sizeof(uint64_t);
+                         kWarps * 8 * sizeof(uint64_t) + kWarps * kWindow * sizeof(int);
 
 template <class T, int D, int NT>
 cudaError_t launch_paged(const PdPlan &P, const CUtensorMap &kmap, const CUtensorMap &vmap, int grid,
@@ -800,15 +933,20 @@ apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_
   P.hq = num_q_heads;
   P.group = s.group;
   P.heads_cta = s.heads_cta;
-  P.wph = s.wph;
+  P.wph_log = s.wph_log;
   P.groups = s.groups;
-  P.box_tokens = std::gcd(cache->page_tokens, kTile);
-  P.boxes = kTile / P.box_tokens;
+  const int tile = tile_tokens(cache->head_dim);
+  P.box_tokens = std::gcd(cache->page_tokens, tile);
+  P.boxes = tile / P.box_tokens;
   P.max_rows = static_cast<int32_t>(
-      std::min<int64_t>(INT32_MAX - kTile, static_cast<int64_t>(cache->max_pages) * cache->page_tokens));
-  P.min_tiles = s.wph;
-  P.seg_cost = std::max(1, kSegBytes / (kTile * s.heads_cta * cache->head_dim * 4));
+      std::min<int64_t>(INT32_MAX - tile, static_cast<int64_t>(cache->max_pages) * cache->page_tokens));
+  P.min_tiles = 2 << s.wph_log;
+  P.seg_cost = std::max(1, kSegBytes / (tile * s.heads_cta * cache->head_dim * 4));
+  // the work list is counted in 32 bits
+  if (static_cast<int64_t>(cache->num_seqs) * s.groups * (P.max_rows / tile + 1 + P.seg_cost) > INT32_MAX - 1024)
+    return APACK_EUNSUPPORTED;
   P.scale2 = scale * 1.4426950408889634f;
+  P.grow = kRescale / P.scale2;
   P.out = out;
   P.out_fp32 = out_dtype == APACK_FP32;
   P.lse = lse;
@@ -818,7 +956,7 @@ apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_
   P.part = reinterpret_cast<float *>(w + s.part_off);
   P.err = static_cast<DeviceError *>(ws);
   CUtensorMap kmap, vmap;
-  const uint32_t blocks = P.boxes == 1 ? cache->head_dim / 64 : 1;
+  const uint32_t blocks = P.boxes <= tile / 16 ? cache->head_dim / 64 : 1;
   if (!make_page_map(&kmap, cache, P.pool.k, P.box_tokens, blocks) ||
       !make_page_map(&vmap, cache, P.pool.v, P.box_tokens, blocks))
     return APACK_ECUDA;

@@ -295,6 +295,8 @@ def check_attention(ap, rng, lens, hq, hkv, dim, tokens, dtype, order="nhd", out
     ([100, 3, 250], 16, 2, 128, 4, "bf16", "inside", None),
     ([130, 8, 90], 22, 2, 128, 40, "bf16", "nhd", "fp32"),
     ([257], 17, 1, 64, 1000, "fp16", "nhd", None),
+    ([100, 47, 33, 16], 12, 4, 64, 48, "fp16", "nhd", None),
+    ([1000, 18], 32, 1, 64, 16, "bf16", "hnd", None),
 ])
 def test_paged_attention(ap, lens, hq, hkv, dim, tokens, dtype, order, out_dtype):
     rng = np.random.default_rng(sum(lens) + hq + tokens)
