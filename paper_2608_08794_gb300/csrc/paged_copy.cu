@@ -12,7 +12,10 @@
 namespace apack {
 namespace {
 
-constexpr int kRows = 32;              // rows whose addresses a CTA holds
+// A CTA moves the same rows, about 32 KB of a plane, in several planes: with half of that, the time of 13 caches of
+// 512-byte rows was 46 us, with this 43 (their rows' addresses take two rounds of loads to find).
+constexpr int kChunkBytes = 32768;
+constexpr int kRows = 128;             // rows whose addresses a CTA holds at most
 constexpr int kMoveThreads = 256;
 constexpr int kMoveUnroll = 8;         // 16-byte pieces a thread has in flight
 
@@ -26,21 +29,27 @@ struct MovePlan {
   int32_t pieces;                      // 16-byte pieces of a row
   FastDiv piece_div;
   int32_t planes_cta, planes;
+  int32_t rows_cta;
   DeviceError *err;
 };
+
+// Offsets of up to this many sequences are brought to shared memory in one round of loads before they are searched
+// (a search in L2 takes a round trip per step).
+constexpr int kStagedSeqs = 1024;
 
 // Sequence of output row j: the last b with cu[b] <= j.
 __device__ __forceinline__ int find_seq(const int32_t *cu, int n, int64_t j) {
   int lo = 0, hi = n;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (__ldg(cu + mid) <= j) lo = mid; else hi = mid;
+    if (cu[mid] <= j) lo = mid; else hi = mid;
   }
   return lo;
 }
 
 // Source and destination byte offsets of output row j within a layer's planes (src -1: not copied).
-__device__ __forceinline__ void resolve(const MovePlan &P, int64_t j, int64_t *src, int64_t *dst) {
+// cu: cu_dst, staged or not.
+__device__ __forceinline__ void resolve(const MovePlan &P, const int32_t *cu, int32_t keep, int64_t j, int64_t *src, int64_t *dst) {
   *src = -1;
   *dst = -1;
   if (j >= P.n_rows) return;
@@ -56,11 +65,10 @@ __device__ __forceinline__ void resolve(const MovePlan &P, int64_t j, int64_t *s
     *dst = b * P.src.page_stride + r * P.src.token_stride;
     return;
   }
-  if (j >= __ldg(P.cu_dst + P.num_seqs)) return;
-  const int b = find_seq(P.cu_dst, P.num_seqs, j);
-  const int32_t to = static_cast<int32_t>(j - __ldg(P.cu_dst + b));
-  int32_t from = to;
-  if (P.keep_idx) from = __ldg(P.keep_idx + j) - (P.cu_src ? __ldg(P.cu_src + b) : 0);
+  if (j >= cu[P.num_seqs]) return;
+  const int b = find_seq(cu, P.num_seqs, j);
+  const int32_t to = static_cast<int32_t>(j - cu[b]);
+  const int32_t from = P.keep_idx ? keep - (P.cu_src ? __ldg(P.cu_src + b) : 0) : to;
   const int64_t s = P.src.row_offset(b, from), d = P.dst.row_offset(b, to);
   if (s < 0 || d < 0) {
     if (P.err) raise_device_error(P.err, APACK_EDEVICE, 91, b, static_cast<int32_t>(j));
@@ -78,13 +86,22 @@ __device__ __forceinline__ void plane_bases(const MovePlan &P, int plane, const 
   *dst = (v ? P.dst.v : P.dst.k) + layer * P.dst.layer_stride + head * P.dst.head_stride;
 }
 
-__global__ void __launch_bounds__(kMoveThreads) move_rows_kernel(const __grid_constant__ MovePlan P) {
+__global__ void __launch_bounds__(kMoveThreads, 4) move_rows_kernel(const __grid_constant__ MovePlan P) {
   __shared__ int64_t so[kRows], to[kRows];
+  __shared__ int32_t cu_s[kStagedSeqs + 1];
   pdl_wait_and_release();
-  if (threadIdx.x < kRows)
-    resolve(P, static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x, &so[threadIdx.x], &to[threadIdx.x]);
+  const int64_t j = static_cast<int64_t>(blockIdx.x) * P.rows_cta + threadIdx.x;
+  const int32_t *cu = P.cu_dst;
+  int32_t keep = 0;
+  if (P.keep_idx && threadIdx.x < P.rows_cta && j < P.n_rows) keep = __ldg(P.keep_idx + j);
+  if (!P.pairs && P.num_seqs <= kStagedSeqs) {
+    for (int b = threadIdx.x; b <= P.num_seqs; b += kMoveThreads) cu_s[b] = __ldg(P.cu_dst + b);
+    __syncthreads();
+    cu = cu_s;
+  }
+  if (threadIdx.x < P.rows_cta) resolve(P, cu, keep, j, &so[threadIdx.x], &to[threadIdx.x]);
   __syncthreads();
-  const int total = kRows * P.pieces;
+  const int total = P.rows_cta * P.pieces;
   const int p1 = min(P.planes, static_cast<int>(blockIdx.y + 1) * P.planes_cta);
   for (int plane = blockIdx.y * P.planes_cta; plane < p1; ++plane) {
     const uint8_t *src;
@@ -92,22 +109,22 @@ __global__ void __launch_bounds__(kMoveThreads) move_rows_kernel(const __grid_co
     plane_bases(P, plane, &src, &dst);
     for (int e0 = threadIdx.x; e0 < total; e0 += kMoveThreads * kMoveUnroll) {
       uint4 x[kMoveUnroll];
-      uint8_t *at[kMoveUnroll];
 #pragma unroll
       for (int u = 0; u < kMoveUnroll; ++u) {
         const int e = e0 + u * kMoveThreads;
-        at[u] = nullptr;
         if (e < total) {
           const int r = P.piece_div.div(e), c = e - r * P.pieces;
-          if (so[r] >= 0) {
-            at[u] = dst + to[r] + c * 16;
-            x[u] = *reinterpret_cast<const uint4 *>(src + so[r] + c * 16);
-          }
+          if (so[r] >= 0) x[u] = *reinterpret_cast<const uint4 *>(src + so[r] + c * 16);
         }
       }
 #pragma unroll
-      for (int u = 0; u < kMoveUnroll; ++u)
-        if (at[u]) *reinterpret_cast<uint4 *>(at[u]) = x[u];
+      for (int u = 0; u < kMoveUnroll; ++u) {
+        const int e = e0 + u * kMoveThreads;
+        if (e < total) {
+          const int r = P.piece_div.div(e), c = e - r * P.pieces;
+          if (so[r] >= 0) *reinterpret_cast<uint4 *>(dst + to[r] + c * 16) = x[u];
+        }
+      }
     }
   }
 }
@@ -179,9 +196,10 @@ apack_status launch_move(MovePlan &P, const apack_paged_cache *a, const apack_pa
     count_launches(1);
     return APACK_OK;
   }
-  const int64_t chunks = (P.n_rows + kRows - 1) / kRows;
-  // planes of a CTA: as many as leave 16 CTAs per SM
-  const int64_t want = 16 * static_cast<int64_t>(device_sm_count());
+  P.rows_cta = static_cast<int32_t>(std::min<int64_t>(P.n_rows, std::min(kRows, std::max(1, kChunkBytes / (P.pieces * 16)))));
+  const int64_t chunks = (P.n_rows + P.rows_cta - 1) / P.rows_cta;
+  // planes of a CTA: as many as leave 32 CTAs per SM (the two-minute prompt: 172.8 us; with 8 per SM 181.3)
+  const int64_t want = 32 * static_cast<int64_t>(device_sm_count());
   int64_t splits = std::min<int64_t>(P.planes, std::max<int64_t>(1, (want + chunks - 1) / chunks));
   splits = std::max<int64_t>(splits, (P.planes + 65534) / 65535);
   P.planes_cta = static_cast<int32_t>((P.planes + splits - 1) / splits);

@@ -9,9 +9,10 @@
 // phase with whole turns dropped, exactly, in one integer multiplication, for negative positions too.  Its top
 // 32 bits as a signed fraction of a half turn go to sincospif.
 //
-// Bound by HBM: a row is read once and written once; 2 sincospif a pair are shared by all heads of a token.  A
-// thread owns one 16-byte chunk position of a head (both halves of its pairs) and keeps its (cos, sin) in registers
-// over the heads it walks through, so that the division by the head's chunks is done once per thread.
+// Bound by HBM with many tokens: a row is read once and written once, the angles are shared by all heads of a token.
+// Behind it comes instruction issue (2 loads, 2 stores and about 60 instructions per 16 elements), so a lane owns
+// one 16-byte chunk position of a head (both halves of its pairs) and keeps its (cos, sin) in registers over the
+// heads it walks through.  Few tokens are bound by latency: position -> angle -> product.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -26,7 +27,8 @@ namespace {
 
 constexpr int kRotThreads = 256;
 constexpr int kMaxPairs = 128;          // head_dim <= 256
-constexpr int kRotUnroll = 4;           // heads whose loads a thread has in flight
+constexpr int kRotUnroll = 3;           // heads whose loads a lane has in flight
+constexpr int kRotCtas = 3;             // CTAs per SM
 
 struct RotPlan {
   uint64_t freq[kMaxPairs];             // 2^-64 turns per position
@@ -34,7 +36,9 @@ struct RotPlan {
   int32_t pairs, axis1, axis2;          // pairs from axis1 on take axis 1, from axis2 on axis 2
   int32_t n1, n2;                       // chunk positions of a head: rotated, passed through
   int32_t half_off;                     // elements from a chunk to its partner (HALF)
-  int32_t head_slots, tok_slots;        // a CTA's threads: chunk positions x head_slots x tok_slots
+  int32_t head_slots;                   // a warp's lanes: chunk positions x head_slots
+  int64_t whole, units;                 // tokens that a warp takes whole, and units of work in all
+  int32_t splits, unit_heads;           // parts of the other tokens' heads, and heads of a part
   int32_t heads, rot_heads, q_heads;    // heads in all; the first rot_heads are rotated; q_heads of them are q
   int32_t kv_heads, head_dim;
   int64_t n_tokens;
@@ -110,98 +114,132 @@ __device__ __forceinline__ void turn(Chunk<T, V> &lo, Chunk<T, V> &hi, const flo
   }
 }
 
+// (m cos, sign m sin) of a pair's angle.
+__device__ __forceinline__ float2 angle(const RotPlan &P, int32_t pos, uint64_t freq, float sign) {
+  const uint64_t phase = static_cast<uint64_t>(static_cast<int64_t>(pos)) * freq;
+  float s, c;
+  sincospif(static_cast<float>(static_cast<int32_t>(phase >> 32)) * 4.656612873077393e-10f, &s, &c);   // 2^-31
+  return make_float2(P.magnitude * c, sign * P.magnitude * s);
+}
+
 // V: elements of an access.  PAIRS: neighbouring elements form a pair; a chunk then holds its pairs whole (V = 1:
 // two accesses, as in the HALF layout with the partner one element on).  APPEND: k and v go to pages.
-// The first heads' loads are under way while the angles are computed and the slots looked up.
+//
+// A warp takes a token, or with few tokens a part of its heads, and never waits for another.  Its lanes are chunk
+// positions x head_slots; the first heads' loads are under way while the angles are computed (shared by the lanes
+// through shared memory) and the slot is looked up, from a position and row that were read one token ahead.
 template <class T, int V, bool PAIRS, bool APPEND>
-__global__ void __launch_bounds__(kRotThreads, 3) rotary_kernel(const __grid_constant__ RotPlan P, float sign) {
+__global__ void __launch_bounds__(kRotThreads, kRotCtas) rotary_kernel(const __grid_constant__ RotPlan P, float sign) {
   using C = Chunk<T, V>;
   constexpr bool kSplit = !PAIRS || V == 1;            // a rotated chunk has a partner chunk
   constexpr int kAngles = kSplit ? V : V / 2;          // pairs of a chunk position
-  __shared__ float2 cs[2 * kRotThreads * 4];           // [token slot][pair]
-  __shared__ int64_t slot[kRotThreads];                // byte offset of a token's slot, -1: none
-  const int n = P.n1 + P.n2;
-  const int c = threadIdx.x % n, rest = threadIdx.x / n;
-  const int h0 = rest % P.head_slots, tok = rest / P.head_slots;
-  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * P.tok_slots, t = t0 + tok;
-  const bool here = tok < P.tok_slots && t < P.n_tokens;
-  const bool turns = c < P.n1;
+  constexpr int kAhead = kMaxPairs / 32;
+  __shared__ __align__(16) float2 cs_all[kRotThreads / 32][kMaxPairs];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  float2 *cs = cs_all[warp];
   const int pairs = P.pairs, hd = P.head_dim;
-  // this thread's elements of a head: first .. first + V, and the partner's
-  const int first = turns ? (PAIRS && V == 1 ? 2 * c : c * V) : 2 * pairs + (c - P.n1) * V;
-  const int partner = first + (PAIRS ? 1 : P.half_off);
-  C lo[kRotUnroll], hi[kRotUnroll];
-  auto load = [&](int hb) {
+  // chunk positions beyond 32 are walked through, `positions` at a time
+  const int n = P.n1 + P.n2, width = min(n, 32);
+  const int c0 = lane % width, hs = lane / width;
+  const int64_t stride = static_cast<int64_t>(gridDim.x) * (kRotThreads / 32);
+  int64_t u = static_cast<int64_t>(blockIdx.x) * (kRotThreads / 32) + warp;
+  uint64_t freq[kAhead];                               // of this lane's pairs (parameters are slow to index by lane)
 #pragma unroll
-    for (int u = 0; u < kRotUnroll; ++u) {
-      const int h = hb + u * P.head_slots;
-      if (h >= P.heads) continue;
-      const uint8_t *src;
-      if (!APPEND || h < P.q_heads) {
-        src = P.x + t * P.xs + static_cast<int64_t>(h) * hd * sizeof(T);
-      } else {
-        const int kh = h - P.q_heads;
-        const bool is_v = kh >= P.kv_heads;
-        src = (is_v ? P.v + t * P.vs : P.k + t * P.ks) + static_cast<int64_t>(is_v ? kh - P.kv_heads : kh) * hd * sizeof(T);
-      }
-      const T *s = reinterpret_cast<const T *>(src);
-      lo[u] = *reinterpret_cast<const C *>(s + first);
-      if (kSplit && turns) hi[u] = *reinterpret_cast<const C *>(s + partner);
+  for (int k = 0; k < kAhead; ++k) freq[k] = lane + 32 * k < pairs ? P.freq[lane + 32 * k] : 0;
+  pdl_wait_and_release();
+  int32_t pos[kAhead], row = -1, seq = 0;
+  auto read_ahead = [&](int64_t t) {
+    if (t >= P.n_tokens) return;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int i = lane + 32 * k;
+      if (i < pairs) pos[k] = __ldg(P.positions + ((i >= P.axis1) + (i >= P.axis2)) * P.pos_axis_stride + t);
+    }
+    if (APPEND) {
+      row = __ldg(P.rows + t);
+      seq = P.seqs ? __ldg(P.seqs + t) : static_cast<int32_t>(t);
     }
   };
-  pdl_wait_and_release();
-  if (here) load(h0);
-  for (int e = threadIdx.x; e < P.tok_slots * pairs; e += blockDim.x) {
-    const int tk = e / pairs, i = e - tk * pairs;
-    if (t0 + tk >= P.n_tokens) break;
-    const int axis = (i >= P.axis1) + (i >= P.axis2);
-    const int64_t pos = __ldg(P.positions + axis * P.pos_axis_stride + t0 + tk);
-    const uint64_t phase = static_cast<uint64_t>(pos) * P.freq[i];
-    float sn, cn;
-    sincospif(static_cast<float>(static_cast<int32_t>(phase >> 32)) * 4.656612873077393e-10f, &sn, &cn);   // 2^-31
-    cs[e] = make_float2(P.magnitude * cn, sign * P.magnitude * sn);
-  }
-  if (APPEND && threadIdx.x < P.tok_slots && t0 + threadIdx.x < P.n_tokens) {
-    const int64_t tt = t0 + threadIdx.x;
-    const int32_t row = __ldg(P.rows + tt);
-    const int32_t seq = P.seqs ? __ldg(P.seqs + tt) : static_cast<int32_t>(tt);
+  auto token_of = [&](int64_t unit) {
+    return unit < P.whole ? unit : P.whole + static_cast<uint32_t>(unit - P.whole) / static_cast<uint32_t>(P.splits);
+  };
+  read_ahead(token_of(u));
+  for (; u < P.units; u += stride) {
+    const int64_t t = token_of(u);
+    int h_begin = 0, h_end = P.heads;
+    if (u >= P.whole) {
+      h_begin = static_cast<int>(u - P.whole - (t - P.whole) * P.splits) * P.unit_heads;
+      h_end = min(P.heads, h_begin + P.unit_heads);
+    }
     int64_t off = -1;
-    if (row >= 0) {
-      if (static_cast<uint32_t>(seq) < static_cast<uint32_t>(P.pool.num_seqs)) off = P.pool.row_offset(seq, row);
-      if (off < 0 && P.err) raise_device_error(P.err, APACK_EDEVICE, 71, seq, row);
-    }
-    slot[threadIdx.x] = off;
-  }
-  __syncthreads();
-  if (!here) return;
-  float2 a[kAngles];
-  if (turns) {
+    for (int c = c0;; c += 32) {
+      const bool here = hs < P.head_slots && c < n, turns = c < P.n1;
+      // this lane's elements of a head: first .. first + V, and the partner's
+      const int first = turns ? (PAIRS && V == 1 ? 2 * c : c * V) : 2 * pairs + (c - P.n1) * V;
+      const int partner = first + (PAIRS ? 1 : P.half_off);
+      C lo[kRotUnroll], hi[kRotUnroll];
+      auto load = [&](int hb) {
 #pragma unroll
-    for (int j = 0; j < kAngles; ++j) a[j] = cs[tok * pairs + c * kAngles + j];
-  }
-  const int64_t off = APPEND ? slot[tok] : 0;
-  for (int hb = h0;;) {
+        for (int k = 0; k < kRotUnroll; ++k) {
+          const int h = hb + k * P.head_slots;
+          if (h >= h_end) continue;
+          const uint8_t *src;
+          if (!APPEND || h < P.q_heads) {
+            src = P.x + t * P.xs + h * hd * static_cast<int>(sizeof(T));
+          } else {
+            const bool is_v = h >= P.rot_heads;
+            src = (is_v ? P.v + t * P.vs : P.k + t * P.ks) + (h - (is_v ? P.rot_heads : P.q_heads)) * hd * static_cast<int>(sizeof(T));
+          }
+          const T *s = reinterpret_cast<const T *>(src);
+          lo[k] = *reinterpret_cast<const C *>(s + first);
+          if (kSplit && turns) hi[k] = *reinterpret_cast<const C *>(s + partner);
+        }
+      };
+      int hb = h_begin + hs;
+      if (here) load(hb);
+      if (c == c0) {                                   // angles and slot of the token, once
 #pragma unroll
-    for (int u = 0; u < kRotUnroll; ++u) {
-      const int h = hb + u * P.head_slots;
-      if (h >= P.heads) continue;
-      uint8_t *dst;
-      if (!APPEND || h < P.q_heads) {
-        dst = P.out + t * P.outs + static_cast<int64_t>(h) * hd * sizeof(T);
-      } else {
-        const int kh = h - P.q_heads;
-        const bool is_v = kh >= P.kv_heads;
-        if (off < 0) continue;
-        dst = (is_v ? P.pool.v : P.pool.k) + off + (is_v ? kh - P.kv_heads : kh) * P.pool.head_stride;
+        for (int k = 0; k < kAhead; ++k)
+          if (lane + 32 * k < pairs) cs[lane + 32 * k] = angle(P, pos[k], freq[k], sign);
+        if (APPEND && row >= 0) {
+          if (static_cast<uint32_t>(seq) < static_cast<uint32_t>(P.pool.num_seqs)) off = P.pool.row_offset(seq, row);
+          if (off < 0 && P.err && lane == 0) raise_device_error(P.err, APACK_EDEVICE, 71, seq, row);
+        }
+        read_ahead(token_of(u + stride));
+        __syncwarp();
       }
-      if (turns && h < P.rot_heads) turn<T, V, kSplit>(lo[u], hi[u], a);
-      T *d = reinterpret_cast<T *>(dst);
-      *reinterpret_cast<C *>(d + first) = lo[u];
-      if (kSplit && turns) *reinterpret_cast<C *>(d + partner) = hi[u];
+      if (here) {
+        float2 a[kAngles];
+        if (turns) {
+#pragma unroll
+          for (int j = 0; j < kAngles; ++j) a[j] = cs[c * kAngles + j];
+        }
+        for (;;) {
+#pragma unroll
+          for (int k = 0; k < kRotUnroll; ++k) {
+            const int h = hb + k * P.head_slots;
+            if (h >= h_end) continue;
+            uint8_t *dst;
+            if (!APPEND || h < P.q_heads) {
+              dst = P.out + t * P.outs + h * hd * static_cast<int>(sizeof(T));
+            } else {
+              const bool is_v = h >= P.rot_heads;
+              if (off < 0) continue;
+              dst = (is_v ? P.pool.v : P.pool.k) + off + (h - (is_v ? P.rot_heads : P.q_heads)) * P.pool.head_stride;
+            }
+            if (turns && h < P.rot_heads) turn<T, V, kSplit>(lo[k], hi[k], a);
+            T *d = reinterpret_cast<T *>(dst);
+            *reinterpret_cast<C *>(d + first) = lo[k];
+            if (kSplit && turns) *reinterpret_cast<C *>(d + partner) = hi[k];
+          }
+          hb += kRotUnroll * P.head_slots;
+          if (hb >= h_end) break;
+          load(hb);
+        }
+      }
+      if (c - c0 + 32 >= n) break;
     }
-    hb += kRotUnroll * P.head_slots;
-    if (hb >= P.heads) break;
-    load(hb);
+    __syncwarp();                                      // the angles are read
   }
 }
 
@@ -213,24 +251,25 @@ cudaError_t launch_rotary(RotPlan &P, bool pairs_layout, bool wide, float sign, 
   P.n1 = (pairs_layout && V > 1) ? r / V : r / 2 / V;
   P.n2 = (D - r) / V;
   P.half_off = r / 2;
-  const int n = P.n1 + P.n2;
-  // Few tokens: a thread per head as far as the CTA reaches.  Many: kRotUnroll heads per thread, and as many tokens
-  // as fill the CTA.
-  const int room = kRotThreads / n;
-  P.head_slots = std::min(P.heads, room);
-  P.tok_slots = 1;
-  if (P.n_tokens >= 4 * static_cast<int64_t>(device_sm_count())) {
-    P.head_slots = std::min((P.heads + kRotUnroll - 1) / kRotUnroll, room);
-    P.tok_slots = room / P.head_slots;
-  }
-  const int threads = (n * P.head_slots * P.tok_slots + 31) / 32 * 32;
-  const int64_t grid = (P.n_tokens + P.tok_slots - 1) / P.tok_slots;
+  P.head_slots = 32 / std::min(P.n1 + P.n2, 32);
+  // A warp per token as long as there is one for every warp of the grid; the tokens that are left over (or few) in
+  // parts of their heads, down to those whose loads a lane has in flight at once.
+  const int64_t warps = static_cast<int64_t>(kRotCtas) * (kRotThreads / 32) * device_sm_count();
+  const int batch = P.head_slots * kRotUnroll, batches = (P.heads + batch - 1) / batch;
+  P.whole = static_cast<int64_t>(P.n_tokens / warps) * warps;
+  const int64_t rest = P.n_tokens - P.whole;
+  P.splits = rest > 0 ? static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(batches, warps / rest))) : 1;
+  P.unit_heads = ((P.heads + P.head_slots - 1) / P.head_slots + P.splits - 1) / P.splits * P.head_slots;
+  P.splits = (P.heads + P.unit_heads - 1) / P.unit_heads;
+  P.units = P.whole + rest * P.splits;
+  const int64_t per = kRotThreads / 32;
+  const int64_t grid = std::min<int64_t>((P.units + per - 1) / per, static_cast<int64_t>(kRotCtas) * device_sm_count());
   void (*fn)(RotPlan, float);
   if (wide)
     fn = pairs_layout ? rotary_kernel<T, W, true, APPEND> : rotary_kernel<T, W, false, APPEND>;
   else
     fn = pairs_layout ? rotary_kernel<T, 1, true, APPEND> : rotary_kernel<T, 1, false, APPEND>;
-  const cudaError_t e = launch_pdl(fn, dim3(static_cast<unsigned>(grid)), dim3(threads), 0, stream, P, sign);
+  const cudaError_t e = launch_pdl(fn, dim3(static_cast<unsigned>(grid)), dim3(kRotThreads), 0, stream, P, sign);
   if (e == cudaSuccess) count_launches(1);
   return e;
 }
