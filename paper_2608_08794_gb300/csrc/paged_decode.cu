@@ -7,13 +7,13 @@
 // head as the N = 8 of a warp-level matrix instruction (keys, then features, as M) nothing is padded, the scores
 // stay in registers from S^T = K Q^T over the softmax to O^T = V^T P^T, and no warp waits for another.
 //
-// Split over the cache's length.  The work is the list of all (sequence, head group, 16-token tile) in that
-// order; every CTA takes an equal contiguous share of it and finds its start from the lengths on the device,
-// so that the launch does not depend on them (a captured call follows growing caches).  Within a CTA each warp has
-// one KV head and every wph-th tile of the share, and its own ring of TMA stages: lane 0 refills a stage as soon
-// as the warp has used it.  At the end of a (sequence, head group) the warps of a head merge through shared
-// memory; what a share holds whole is written out, what it holds in part goes to the workspace, and a second
-// kernel merges those parts in order.
+// Split over the cache's length.  The work is the list of all (sequence, head group, tile) in that order; every CTA
+// takes an equal contiguous share of it and finds its start from the lengths on the device, so that the launch does
+// not depend on them (a captured call follows growing caches).  Within a CTA a KV head has wph ring buffers of TMA
+// stages, each for every wph-th tile of the share; a ring is read by one warp, or with more than 8 query rows per KV
+// head by 2 or 4 warps of 8 rows each.  Its first warp refills a stage as soon as it has been used.  At the end of a
+// (sequence, head group) the warps of a head merge through shared memory; what a share holds whole is written out,
+// what it holds in part goes to the workspace, and a second kernel merges those parts in order.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -33,7 +33,9 @@ constexpr int tile_tokens(int D) { return D == 64 ? 32 : 16; }
 constexpr int kWarps = 8;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kMergeFloats = 3584;              // shared-memory buffer of the warps' merge: 7 warps, 4 m-tiles
-constexpr int kStageBytesCta = 196608;          // of all warps' rings
+constexpr int kStageBytes = 16384 / 2;          // K and V of a tile
+constexpr int kStageBytesCta = 196608;          // of all rings: three stages per warp
+constexpr int kMaxStages = kStageBytesCta / kStageBytes;
 // Accumulators are rescaled only when a row's maximum has grown by more than this (log2 units): sums stay
 // below 2^8 times their number, far inside fp32, and most tiles need one vote instead of the reduction.
 constexpr float kRescale = 8.f;
@@ -48,7 +50,8 @@ struct PdPlan {
   const uint8_t *q;
   int64_t q_stride;                  // bytes between sequences
   int32_t hq, group;                 // query heads, per KV head
-  int32_t heads_cta, wph_log, groups;   // KV heads of a CTA, log2 of the warps per head, head groups
+  int32_t heads_cta, groups;         // KV heads of a CTA, head groups
+  int32_t wph_log, rg_log;           // log2 of the rings per head, and of the warps (groups of 8 query rows) per ring
   int32_t box_tokens, boxes;         // tokens of one TMA box, boxes of a tile
   int32_t max_rows;
   int32_t min_tiles;                 // smallest share of a CTA
@@ -59,8 +62,8 @@ struct PdPlan {
   int32_t out_fp32;
   float *lse;
   int4 *info;                        // [grid]: (sequence, head group, parts, first slot) of a cut segment that starts here
-  float2 *ml;                        // [slot][heads_cta * NT][8]
-  float *part;                       // [slot][heads_cta * NT][D / 16][128]
+  float2 *ml;                        // [slot][head][row group][8]
+  float *part;                       // [slot][head][row group][D / 16][128]
   DeviceError *err;
 };
 
@@ -182,25 +185,34 @@ struct Walk {
   }
 };
 
-template <class T, int D, int NT>
+// SHARED: a ring has 2 or 4 warps (1 << rg_log); as a template, because the one-warp rings of most models are 1.5 %
+// faster without the other case's registers and branches.
+template <class T, int D, bool SHARED>
 __global__ void __launch_bounds__(kThreads, 1)
     paged_chunk_kernel(const __grid_constant__ PdPlan P, const __grid_constant__ CUtensorMap kmap,
                        const __grid_constant__ CUtensorMap vmap) {
   constexpr int KS = D / 16;                          // k-steps of S, m-tiles of O^T
   constexpr int kTile = tile_tokens(D), KM = kTile / 16;   // m-tiles of S, k-steps of O^T
   constexpr int kHalf = kTile * D * 2;                // bytes of a stage's K (and V)
-  constexpr int kStages = kStageBytesCta / kWarps / (2 * kHalf);
+  static_assert(2 * kHalf == kStageBytes, "8 KB stages");
   constexpr int kBlk = kTile * 128;                   // bytes of one 64-feature block of a stage
   extern __shared__ __align__(1024) uint8_t smem[];
   float *merge = reinterpret_cast<float *>(smem + kStageBytesCta);
-  float2 *stat = reinterpret_cast<float2 *>(merge + kMergeFloats);        // [warp][NT * 8]
-  uint64_t *bars = reinterpret_cast<uint64_t *>(stat + kWarps * 32);      // [warp][kStages]
-  int *window = reinterpret_cast<int *>(bars + kWarps * 8);               // [warp][kWindow]
+  float2 *stat = reinterpret_cast<float2 *>(merge + kMergeFloats);        // [warp][8]
+  uint64_t *bars = reinterpret_cast<uint64_t *>(stat + kWarps * 8);       // full, then empty, of all stages
+  int *window = reinterpret_cast<int *>(bars + 2 * kMaxStages);           // [warp][kWindow]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  uint64_t *full = bars + warp * kStages;
-  const uint32_t ring = smem_u32(smem) + warp * (kStages * 2 * kHalf);
-  if (lane == 0) {
-    for (int i = 0; i < kStages; ++i) mbar_init(&full[i], 1);
+  // warp = (ring of the head, row group, head)
+  const int rg_log = SHARED ? P.rg_log : 0, wph = 1 << P.wph_log, readers = 1 << rg_log;
+  const int hw = warp % P.heads_cta, rg = SHARED ? (warp / P.heads_cta) & (readers - 1) : 0, sub = (warp / P.heads_cta) >> rg_log;
+  const int ring_id = sub * P.heads_cta + hw, stages = SHARED ? (kMaxStages / kWarps) << rg_log : kMaxStages / kWarps;
+  uint64_t *full = bars + ring_id * stages, *empty = full + kMaxStages;
+  const uint32_t ring = smem_u32(smem) + ring_id * stages * kStageBytes;
+  if (sub < wph && rg == 0 && lane == 0) {
+    for (int i = 0; i < stages; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], readers);
+    }
     fence_mbar_init();
   }
   if (threadIdx.x == 32) {
@@ -215,15 +227,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int b = line / row_lines;
     if (b < P.pool.num_seqs) prefetch_l2(P.pool.table + b * P.pool.table_stride + (line - b * row_lines) * 32);
   }
-  __syncwarp();
+  if (SHARED)
+    __syncthreads();                                  // the ring's barriers, for its other warps
+  else
+    __syncwarp();
   pdl_wait_and_release();
 
   // ---- this CTA's share (every warp by itself: no barrier before the first load).  The list starts behind the first
   // segment's cost, which every CTA pays one of anyway.
   const int B = P.pool.num_seqs, grid = gridDim.x, cta = blockIdx.x, cost = P.seg_cost;
-  const int hw = warp % P.heads_cta, sub = warp / P.heads_cta;
   const bool report = warp == 0 && cta == 0;
-  const int wph = 1 << P.wph_log;
   if (threadIdx.x == 0) P.info[cta] = make_int4(0, 0, 0, 0);
   auto units = [&](int len) { return len > 0 ? (tiles_of<kTile>(len) + cost) * P.groups : 0; };
   auto scan = [&](int v) {                             // inclusive, over the lanes
@@ -256,7 +269,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   W -= cost;
   const int C = min(grid, max(W / P.min_tiles, 1));
   if (W <= 0 || cta >= C || sub >= wph) return;
-  const int active = 32 * P.heads_cta * wph;        // threads of the warps at work
+  const int active = 32 * (P.heads_cta << (P.wph_log + rg_log));   // threads of the warps at work
   const int u0 = cost + quotient(static_cast<int64_t>(W) * cta, C);
   const int n = cost + quotient(static_cast<int64_t>(W) * (cta + 1), C) - u0;
   Walk<kTile> seg;
@@ -288,7 +301,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (seg.ts >= seg.te && !seg.next(P, lens, n)) return;      // the share holds no tile (for all warps alike)
   }
 
-  // ---- producer: a queue of this warp's next 32 tiles, one per lane; the lane of a tile issues its loads
+  // ---- producer (the ring's first warp): a queue of its next 32 tiles, one per lane; the lane of a tile issues its
+  // loads
   Walk<kTile> head_w = seg;                                  // of the first tile behind the queue
   int head_t = seg.ts + sub;
   bool head_ok = true;
@@ -299,8 +313,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   int32_t q_page[KM], q_head = 0, q_b = 0, q_t = 0, q_len = 0;
   uint32_t q_in = 0;
   int queued = 0, issued = 0, used = 0;
-  int issue_slot = 0, use_slot = 0;
-  uint32_t use_phase = 0;
+  int issue_slot = 0, use_slot = 0, free_slot = 0;
+  uint32_t use_phase = 0, free_phase = 0;
   auto refill = [&] {
     Walk<kTile> w = head_w;
     int t = head_t, skip = lane;
@@ -345,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       raise_device_error(P.err, APACK_EDEVICE, 82, b, page);
       page = P.pool.num_pages;
     }
-    const uint32_t dst = ring + slot * (2 * kHalf) + offset;
+    const uint32_t dst = ring + slot * kStageBytes + offset;
     tma_load_5d(dst, &kmap, &full[slot], in_page, block, head, page);
     tma_load_5d(dst + kHalf, &vmap, &full[slot], in_page, block, head, page);
   };
@@ -357,7 +371,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (issued == queued) return;
     }
     const int slot = issue_slot, owner = issued & 31;
-    issue_slot = slot + 1 == kStages ? 0 : slot + 1;
+    issue_slot = slot + 1 == stages ? 0 : slot + 1;
     if (P.boxes <= KM) {
       if (lane == owner) {
         const bool second = KM > 1 && P.boxes > 1 && q_t * kTile + 16 < q_len;
@@ -381,7 +395,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     ++issued;
   };
-  for (int i = 0; i < kStages; ++i) issue();
+  if (rg == 0)
+    for (int i = 0; i < stages; ++i) issue();
 
   // ---- consumer
   const int t4 = lane & 3, g8 = lane >> 2;
@@ -390,36 +405,28 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t vrow = (lane & 7) + (lane >> 4) * 8, vchunk = (lane >> 3) & 1;
   bool dead = false;                                  // a wait gave up: no more loads are issued or waited for
   int first_seg = 1;
-  // query fragments; with registers to spare the next segment's are loaded during this one
-  constexpr bool kAhead = NT == 1;
-  using QFrag = uint32_t[NT][KS][2];
+  // query fragments; the next segment's are loaded during this one
+  using QFrag = uint32_t[KS][2];
   auto load_q = [&](const Walk<kTile> &w, QFrag &f) {
-    const uint8_t *qb = P.q + w.b * P.q_stride + static_cast<int64_t>(w.g * P.heads_cta + hw) * P.group * D * 2;
+    const int r = rg * 8 + g8;
+    const uint8_t *qb = P.q + w.b * P.q_stride + (static_cast<int64_t>(w.g * P.heads_cta + hw) * P.group + r) * D * 2;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int r = nt * 8 + g8;
+    for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          f[nt][ks][e] = r < P.group ? __ldg(reinterpret_cast<const uint32_t *>(qb + (r * D + ks * 16 + e * 8 + t4 * 2) * 2)) : 0u;
-    }
+      for (int e = 0; e < 2; ++e)
+        f[ks][e] = r < P.group ? __ldg(reinterpret_cast<const uint32_t *>(qb + (ks * 16 + e * 8 + t4 * 2) * 2)) : 0u;
   };
   QFrag qf, q_next;
   load_q(seg, qf);
   for (;;) {
     Walk<kTile> after = seg;
     const bool go_on = after.next(P, lens, n);
-    if (kAhead && go_on) load_q(after, q_next);
+    if (go_on) load_q(after, q_next);
     const int head = seg.g * P.heads_cta + hw;
-    float o[NT][KS][4], m[NT][2], l[NT][2], limit[NT][2];   // m: reference, log2 units; limit: of q.k, where it grows
+    // m: reference, log2 units; limit: of q.k, beyond which it grows; l and m of query rows 2 t4 and 2 t4 + 1
+    float o[KS][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, limit[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      m[nt][0] = m[nt][1] = limit[nt][0] = limit[nt][1] = -INFINITY;
-      l[nt][0] = l[nt][1] = 0.f;
-#pragma unroll
-      for (int i = 0; i < KS; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
-    }
+    for (int i = 0; i < KS; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
     for (int t = seg.ts + sub; t < seg.te && !dead; t += wph) {
       if (!__all_sync(0xffffffffu, mbar_wait(&full[use_slot], use_phase, kWaitLimitNs))) {
         if (lane == 0) raise_device_error(P.err, APACK_ETIMEOUT, 83, cta, warp);
@@ -427,15 +434,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         break;
       }
       ++used;
-      const uint32_t kb = ring + use_slot * (2 * kHalf), vb = kb + kHalf;
-      if (++use_slot == kStages) {
+      const int slot = use_slot;
+      const uint32_t kb = ring + slot * kStageBytes, vb = kb + kHalf;
+      if (++use_slot == stages) {
         use_slot = 0;
         use_phase ^= 1;
       }
       const int valid = seg.len - t * kTile;          // rows of the tile that belong to the sequence
       if (valid < kTile) {
         // what lies behind the last row takes no part: its logits become -infinity below, and its values
-        // zeros here (0 times a stale infinity would be NaN)
+        // zeros here (0 times a stale infinity would be NaN; the warps of a ring all write the same zeros)
         for (int i = lane; i < (kTile - valid) * (D / 8); i += 32) {
           const int row = valid + i / (D / 8), ch = i % (D / 8);
           const uint32_t a = vb + (ch >> 3) * kBlk + row * 128 + (ch & 7) * 16;
@@ -444,11 +452,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         fence_proxy_async_smem();                     // before TMA writes the slot again
         __syncwarp();
       }
-      float s[KM][NT][4];
+      float s[KM][4];
 #pragma unroll
-      for (int km = 0; km < KM; ++km)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) s[km][nt][0] = s[km][nt][1] = s[km][nt][2] = s[km][nt][3] = 0.f;
+      for (int km = 0; km < KM; ++km) s[km][0] = s[km][1] = s[km][2] = s[km][3] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
@@ -456,70 +462,59 @@ __global__ void __launch_bounds__(kThreads, 1)
           uint32_t a[4];
           const uint32_t ch = ks * 2 + kchunk;
           ldmatrix4(kb + (ch >> 3) * kBlk + (km * 16 + krow) * 128 + (((ch & 7) ^ (krow & 7)) << 4), a);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) Half16<T>::mma(s[km][nt], a, qf[nt][ks][0], qf[nt][ks][1]);
+          Half16<T>::mma(s[km], a, qf[ks][0], qf[ks][1]);
         }
       // lane: keys g8 and g8 + 8 of 16, query rows 2 t4 and 2 t4 + 1
       if (valid < kTile)
 #pragma unroll
         for (int km = 0; km < KM; ++km)
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (km * 16 + g8 + (i >> 1) * 8 >= valid) s[km][nt][i] = -INFINITY;
+          for (int i = 0; i < 4; ++i)
+            if (km * 16 + g8 + (i >> 1) * 8 >= valid) s[km][i] = -INFINITY;
       // (a NaN logit leaves the maximum to the others, and its probability NaN)
-      float top[NT][2];
-      bool grow = false;
+      float top[2];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int e = 0; e < 2; ++e) {
+        top[e] = fmaxf(s[0][e], s[0][e + 2]);
+        if (KM > 1) top[e] = fmaxf(top[e], fmaxf(s[KM - 1][e], s[KM - 1][e + 2]));
+      }
+      if (__any_sync(0xffffffffu, !(top[0] <= limit[0] && top[1] <= limit[1]))) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          top[nt][e] = fmaxf(s[0][nt][e], s[0][nt][e + 2]);
-          if (KM > 1) top[nt][e] = fmaxf(top[nt][e], fmaxf(s[KM - 1][nt][e], s[KM - 1][nt][e + 2]));
-          grow |= !(top[nt][e] <= limit[nt][e]);
-        }
-      if (__any_sync(0xffffffffu, grow)) {
+          float x = top[e];
+          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+          const float mn = fmaxf(m[e], x * P.scale2);
+          const float f = mn == -INFINITY ? 1.f : ex2_approx(m[e] - mn);
+          m[e] = mn;
+          limit[e] = fmaxf(limit[e], x + P.grow);
+          l[e] *= f;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float x = top[nt][e];
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-            const float mn = fmaxf(m[nt][e], x * P.scale2);
-            const float f = mn == -INFINITY ? 1.f : ex2_approx(m[nt][e] - mn);
-            m[nt][e] = mn;
-            limit[nt][e] = fmaxf(limit[nt][e], x + P.grow);
-            l[nt][e] *= f;
-#pragma unroll
-            for (int i = 0; i < KS; ++i) {
-              o[nt][i][e] *= f;
-              o[nt][i][e + 2] *= f;
-            }
+          for (int i = 0; i < KS; ++i) {
+            o[i][e] *= f;
+            o[i][e + 2] *= f;
           }
+        }
       }
       // P as the sum of two 16-bit numbers (2^-17 of it are left out in bf16, 2^-22 in fp16; one alone would cost
       // 2^-9), transposed into B fragments
-      uint32_t hi[KM][NT][2], lo[KM][NT][2];
+      uint32_t hi[KM][2], lo[KM][2];
 #pragma unroll
-      for (int km = 0; km < KM; ++km)
+      for (int km = 0; km < KM; ++km) {
+        float p[4];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float p[4];
+        for (int i = 0; i < 4; ++i) p[i] = ex2_approx(fmaf(s[km][i], P.scale2, -m[i & 1]));
+        l[0] += p[0] + p[2];
+        l[1] += p[1] + p[3];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) p[i] = ex2_approx(fmaf(s[km][nt][i], P.scale2, -m[nt][i & 1]));
-          l[nt][0] += p[0] + p[2];
-          l[nt][1] += p[1] + p[3];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const uint32_t h = Half16<T>::pack(p[2 * e], p[2 * e + 1]);
-            const float2 hf = Half16<T>::unpack(h);
-            hi[km][nt][e] = transpose8x8(h);
-            lo[km][nt][e] = transpose8x8(Half16<T>::pack(p[2 * e] - hf.x, p[2 * e + 1] - hf.y));
-          }
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t h = Half16<T>::pack(p[2 * e], p[2 * e + 1]);
+          const float2 hf = Half16<T>::unpack(h);
+          hi[km][e] = transpose8x8(h);
+          lo[km][e] = transpose8x8(Half16<T>::pack(p[2 * e] - hf.x, p[2 * e + 1] - hf.y));
         }
+      }
 #pragma unroll
       for (int km = 0; km < KM; ++km)
 #pragma unroll
@@ -527,119 +522,116 @@ __global__ void __launch_bounds__(kThreads, 1)
           uint32_t a[4];
           const uint32_t ch = i * 2 + vchunk;
           ldmatrix4_trans(vb + (ch >> 3) * kBlk + (km * 16 + vrow) * 128 + (((ch & 7) ^ (vrow & 7)) << 4), a);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            Half16<T>::mma(o[nt][i], a, hi[km][nt][0], hi[km][nt][1]);
-            Half16<T>::mma(o[nt][i], a, lo[km][nt][0], lo[km][nt][1]);
-          }
+          Half16<T>::mma(o[i], a, hi[km][0], hi[km][1]);
+          Half16<T>::mma(o[i], a, lo[km][0], lo[km][1]);
         }
       __syncwarp();                                   // every lane has read the stage
-      issue();
+      if (!SHARED) {
+        issue();
+      } else {
+        if (lane == 0) mbar_arrive(&empty[slot]);
+        // the stage before this one, which the ring's other warps have most likely left by now
+        if (rg == 0 && used >= 2 && (issued < queued || head_ok)) {
+          if (!__all_sync(0xffffffffu, mbar_wait(&empty[free_slot], free_phase, kWaitLimitNs))) {
+            if (lane == 0) raise_device_error(P.err, APACK_ETIMEOUT, 84, cta, warp);
+            dead = true;
+            break;
+          }
+          if (++free_slot == stages) {
+            free_slot = 0;
+            free_phase ^= 1;
+          }
+          issue();
+        }
+      }
     }
 
-    // ---- end of the segment: the warps of each head merge
+    // ---- end of the segment: the warps of each head and row group merge
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float x = l[nt][e];
-        x += __shfl_xor_sync(0xffffffffu, x, 4);
-        x += __shfl_xor_sync(0xffffffffu, x, 8);
-        x += __shfl_xor_sync(0xffffffffu, x, 16);
-        l[nt][e] = x;
-      }
+    for (int e = 0; e < 2; ++e) {
+      float x = l[e];
+      x += __shfl_xor_sync(0xffffffffu, x, 4);
+      x += __shfl_xor_sync(0xffffffffu, x, 8);
+      x += __shfl_xor_sync(0xffffffffu, x, 16);
+      l[e] = x;
+    }
+    const int hr = rg * P.heads_cta + hw, team = P.heads_cta << rg_log;   // warp = sub * team + hr
     if (wph > 1) {
-      if (g8 == 0)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) stat[warp * 32 + nt * 8 + t4 * 2 + e] = make_float2(m[nt][e], l[nt][e]);
+      if (g8 == 0) {
+        stat[warp * 8 + t4 * 2] = make_float2(m[0], l[0]);
+        stat[warp * 8 + t4 * 2 + 1] = make_float2(m[1], l[1]);
+      }
       head_barrier(active);
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float M = -INFINITY, L = 0.f;
-          for (int w = 0; w < wph; ++w) M = fmaxf(M, stat[(w * P.heads_cta + hw) * 32 + nt * 8 + t4 * 2 + e].x);
-          for (int w = 0; w < wph; ++w) {
-            const float2 x = stat[(w * P.heads_cta + hw) * 32 + nt * 8 + t4 * 2 + e];
-            L += x.y * (x.x == M ? 1.f : ex2_approx(x.x - M));
-          }
-          const float f = m[nt][e] == M ? 1.f : ex2_approx(m[nt][e] - M);
-          m[nt][e] = M;
-          l[nt][e] = L;
-#pragma unroll
-          for (int i = 0; i < KS; ++i) {
-            o[nt][i][e] *= f;
-            o[nt][i][e + 2] *= f;
-          }
+      for (int e = 0; e < 2; ++e) {
+        float M = -INFINITY, L = 0.f;
+        for (int w = 0; w < wph; ++w) M = fmaxf(M, stat[(w * team + hr) * 8 + t4 * 2 + e].x);
+        for (int w = 0; w < wph; ++w) {
+          const float2 x = stat[(w * team + hr) * 8 + t4 * 2 + e];
+          L += x.y * (x.x == M ? 1.f : ex2_approx(x.x - M));
         }
-      // through a buffer, kSlice m-tiles at a time ((wph - 1) * heads_cta is at most 7)
-      constexpr int kSlice = 4 / NT;
+        const float f = m[e] == M ? 1.f : ex2_approx(m[e] - M);
+        m[e] = M;
+        l[e] = L;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+          o[i][e] *= f;
+          o[i][e + 2] *= f;
+        }
+      }
+      // through a buffer, 4 m-tiles at a time ((wph - 1) * team is at most 7)
       float4 *buf = reinterpret_cast<float4 *>(merge);
 #pragma unroll
-      for (int i0 = 0; i0 < KS; i0 += kSlice) {
+      for (int i0 = 0; i0 < KS; i0 += 4) {
         if (sub > 0)
 #pragma unroll
-          for (int k = 0; k < kSlice; ++k)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              const float(&x)[4] = o[nt][i0 + k];
-              buf[((((sub - 1) * P.heads_cta + hw) * kSlice + k) * NT + nt) * 32 + lane] = make_float4(x[0], x[1], x[2], x[3]);
-            }
+          for (int k = 0; k < 4; ++k)
+            buf[(((sub - 1) * team + hr) * 4 + k) * 32 + lane] = make_float4(o[i0 + k][0], o[i0 + k][1], o[i0 + k][2], o[i0 + k][3]);
         head_barrier(active);
         if (sub == 0)
           for (int w = 1; w < wph; ++w)
 #pragma unroll
-            for (int k = 0; k < kSlice; ++k)
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt) {
-                const float4 x = buf[((((w - 1) * P.heads_cta + hw) * kSlice + k) * NT + nt) * 32 + lane];
-                float(&y)[4] = o[nt][i0 + k];
-                y[0] += x.x;
-                y[1] += x.y;
-                y[2] += x.z;
-                y[3] += x.w;
-              }
+            for (int k = 0; k < 4; ++k) {
+              const float4 x = buf[(((w - 1) * team + hr) * 4 + k) * 32 + lane];
+              o[i0 + k][0] += x.x;
+              o[i0 + k][1] += x.y;
+              o[i0 + k][2] += x.z;
+              o[i0 + k][3] += x.w;
+            }
         head_barrier(active);
       }
     }
     if (sub == 0) {
       if (seg.ts == 0 && seg.te == seg.nt) {          // the whole segment: write it out
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int e = 0; e < 2; ++e) {
+          const int r = rg * 8 + t4 * 2 + e;
+          if (r >= P.group) continue;
+          const int64_t row = static_cast<int64_t>(seg.b) * P.hq + head * P.group + r;
+          const float inv = l[e] == 0.f ? 0.f : 1.f / l[e];
+          if (P.lse && g8 == 0) P.lse[row] = (m[e] + log2f(l[e])) * 0.6931471805599453f;
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int r = nt * 8 + t4 * 2 + e;
-            if (r >= P.group) continue;
-            const int64_t row = static_cast<int64_t>(seg.b) * P.hq + head * P.group + r;
-            const float inv = l[nt][e] == 0.f ? 0.f : 1.f / l[nt][e];
-            if (P.lse && g8 == 0) P.lse[row] = (m[nt][e] + log2f(l[nt][e])) * 0.6931471805599453f;
+          for (int i = 0; i < KS; ++i)
 #pragma unroll
-            for (int i = 0; i < KS; ++i)
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const int64_t at = row * D + i * 16 + h * 8 + g8;
-                const float x = o[nt][i][e + 2 * h] * inv;
-                if (P.out_fp32)
-                  static_cast<float *>(P.out)[at] = x;
-                else
-                  static_cast<T *>(P.out)[at] = static_cast<T>(x);
-              }
-          }
+            for (int h = 0; h < 2; ++h) {
+              const int64_t at = row * D + i * 16 + h * 8 + g8;
+              const float x = o[i][e + 2 * h] * inv;
+              if (P.out_fp32)
+                static_cast<float *>(P.out)[at] = x;
+              else
+                static_cast<T *>(P.out)[at] = static_cast<T>(x);
+            }
+        }
       } else {
         const int slot = 2 * cta + (first_seg ? 0 : 1);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const int64_t at = (static_cast<int64_t>(slot) * P.heads_cta + hw) * NT + nt;
-          if (g8 == 0) {
-            P.ml[at * 8 + t4 * 2] = make_float2(m[nt][0], l[nt][0]);
-            P.ml[at * 8 + t4 * 2 + 1] = make_float2(m[nt][1], l[nt][1]);
-          }
-          float4 *pp = reinterpret_cast<float4 *>(P.part) + at * KS * 32 + lane;
-#pragma unroll
-          for (int i = 0; i < KS; ++i) pp[i * 32] = make_float4(o[nt][i][0], o[nt][i][1], o[nt][i][2], o[nt][i][3]);
+        const int64_t at = ((static_cast<int64_t>(slot) * P.heads_cta + hw) << rg_log) + rg;
+        if (g8 == 0) {
+          P.ml[at * 8 + t4 * 2] = make_float2(m[0], l[0]);
+          P.ml[at * 8 + t4 * 2 + 1] = make_float2(m[1], l[1]);
         }
+        float4 *pp = reinterpret_cast<float4 *>(P.part) + at * KS * 32 + lane;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) pp[i * 32] = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
         if (threadIdx.x == 0 && seg.ts == 0) {
           // this share starts the segment; the one that holds its last tile ends it
           const int64_t end = u0 - cost + seg.first + seg.nt;      // unit behind the last tile, without the list's first cost
@@ -651,20 +643,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     first_seg = 0;
     if (!go_on) break;
     seg = after;
-    if (kAhead) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          qf[nt][ks][0] = q_next[nt][ks][0];
-          qf[nt][ks][1] = q_next[nt][ks][1];
-        }
-    } else {
-      load_q(seg, qf);
+    for (int ks = 0; ks < KS; ++ks) {
+      qf[ks][0] = q_next[ks][0];
+      qf[ks][1] = q_next[ks][1];
     }
   }
   if (dead)   // loads of the stages that were issued and not used may still be in flight
-    for (int n = used; n < issued; ++n) mbar_wait(&full[n % kStages], (n / kStages) & 1u, kWaitLimitNs / 4);
+    for (int k = used; k < issued; ++k) mbar_wait(&full[k % stages], (k / stages) & 1u, kWaitLimitNs / 4);
 }
 
 // Merges the parts of the cut segments.  A unit is (segment, head, 8 query rows, 16 features).  Every CTA lists the
@@ -708,7 +694,7 @@ __device__ __forceinline__ void merge_parts(PartState &a, const float4 (&ml)[N],
   a.m1 = n1;
 }
 
-template <class T, int D, int NT>
+template <class T, int D>
 __device__ __forceinline__ PartState merge_run(const PdPlan &P, const int4 &inf, int hn, int i, int p0, int p1, int lane) {
   PartState a = {-INFINITY, -INFINITY, 0.f, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
   for (int p = p0; p < p1; p += kCombineBatch) {
@@ -718,7 +704,7 @@ __device__ __forceinline__ PartState merge_run(const PdPlan &P, const int4 &inf,
       // the first part lies where its share put it, the others are their shares' first
       const int q = min(p + k, p1 - 1);
       const int slot = q == 0 ? inf.w : 2 * ((inf.w >> 1) + q);
-      const int64_t at = static_cast<int64_t>(slot) * P.heads_cta * NT + hn;
+      const int64_t at = (static_cast<int64_t>(slot) * P.heads_cta << P.rg_log) + hn;
       ml[k] = *reinterpret_cast<const float4 *>(P.ml + at * 8 + (lane & 3) * 2);
       x[k] = reinterpret_cast<const float4 *>(P.part)[(at * (D / 16) + i) * 32 + lane];
     }
@@ -733,13 +719,13 @@ __device__ __forceinline__ PartState merge_run(const PdPlan &P, const int4 &inf,
   return a;
 }
 
-template <class T, int D, int NT>
+template <class T, int D>
 __device__ __forceinline__ void write_unit(const PdPlan &P, const int4 &inf, int hn, int i, const PartState &a, int lane) {
   const int t4 = lane & 3, g8 = lane >> 2;
-  const int head = inf.y * P.heads_cta + hn / NT;
+  const int head = inf.y * P.heads_cta + (hn >> P.rg_log);
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
-    const int r = (hn % NT) * 8 + t4 * 2 + e;
+    const int r = (hn & ((1 << P.rg_log) - 1)) * 8 + t4 * 2 + e;
     if (r >= P.group) continue;
     const int64_t row = static_cast<int64_t>(inf.x) * P.hq + head * P.group + r;
     const float L = e ? a.l1 : a.l0, inv = L == 0.f ? 0.f : 1.f / L;
@@ -756,7 +742,7 @@ __device__ __forceinline__ void write_unit(const PdPlan &P, const int4 &inf, int
   }
 }
 
-template <class T, int D, int NT>
+template <class T, int D>
 __global__ void __launch_bounds__(32 * kCombineWarps)
     paged_combine_kernel(const __grid_constant__ PdPlan P, int grid) {
   constexpr int KS = D / 16;
@@ -786,11 +772,11 @@ __global__ void __launch_bounds__(32 * kCombineWarps)
     }
   }
   __syncthreads();
-  const int per_seg = P.heads_cta * NT * KS;
+  const int per_seg = (P.heads_cta << P.rg_log) * KS;
   for (int u = blockIdx.x; u < n_many * per_seg; u += gridDim.x) {
     const int4 inf = seg[list[kMaxGrid - 1 - u / per_seg]];
     const int hn = u % per_seg / KS, i = u % KS;
-    const PartState a = merge_run<T, D, NT>(P, inf, hn, i, inf.z * warp / kCombineWarps, inf.z * (warp + 1) / kCombineWarps, lane);
+    const PartState a = merge_run<T, D>(P, inf, hn, i, inf.z * warp / kCombineWarps, inf.z * (warp + 1) / kCombineWarps, lane);
     so[warp][lane] = a.o;
     if (lane < 4) sml[warp][lane] = make_float4(a.m0, a.l0, a.m1, a.l1);
     __syncthreads();
@@ -803,7 +789,7 @@ __global__ void __launch_bounds__(32 * kCombineWarps)
         x[w] = so[w][lane];
       }
       merge_parts(t, ml, x);
-      write_unit<T, D, NT>(P, inf, hn, i, t, lane);
+      write_unit<T, D>(P, inf, hn, i, t, lane);
     }
     __syncthreads();
   }
@@ -823,13 +809,13 @@ __global__ void __launch_bounds__(32 * kCombineWarps)
   for (int u = warp * gridDim.x + blockIdx.x; u < n_few * per_seg; u += gridDim.x * kCombineWarps) {
     const int4 inf = seg[list[u / per_seg]];
     const int hn = u % per_seg / KS, i = u % KS;
-    write_unit<T, D, NT>(P, inf, hn, i, merge_run<T, D, NT>(P, inf, hn, i, 0, inf.z, lane), lane);
+    write_unit<T, D>(P, inf, hn, i, merge_run<T, D>(P, inf, hn, i, 0, inf.z, lane), lane);
   }
 }
 
 // ------------------------------------------------------------------ host side
 struct PdShape {
-  int group, nt, heads_cta, wph_log, groups, grid;
+  int group, rg_log, heads_cta, wph_log, groups, grid;
   size_t info_off, ml_off, part_off, total;
 };
 
@@ -837,17 +823,17 @@ apack_status plan_shape(const apack_paged_cache *c, int32_t hq, PdShape *s) {
   if (hq < 1 || hq > 1024 || hq % c->num_kv_heads != 0) return APACK_EINVAL;
   s->group = hq / c->num_kv_heads;
   if (s->group > 32) return APACK_EUNSUPPORTED;
-  s->nt = s->group > 16 ? 4 : s->group > 8 ? 2 : 1;
-  // KV heads of a CTA: the largest divisor of their number that its warps cover
+  s->rg_log = s->group > 16 ? 2 : s->group > 8 ? 1 : 0;
+  // KV heads of a CTA: the largest divisor of their number that its warps cover; the other warps split the tiles
   s->heads_cta = 1;
-  for (int h = 1; h <= kWarps; ++h)
+  for (int h = 1; h <= kWarps >> s->rg_log; ++h)
     if (c->num_kv_heads % h == 0) s->heads_cta = h;
-  s->wph_log = 0;                      // 8 / heads_cta, rounded down to a power of two
-  while ((s->heads_cta << (s->wph_log + 1)) <= kWarps) ++s->wph_log;
+  s->wph_log = 0;
+  while ((s->heads_cta << (s->rg_log + s->wph_log + 1)) <= kWarps) ++s->wph_log;
   s->groups = c->num_kv_heads / s->heads_cta;
   s->grid = std::min(device_sm_count(), kMaxGrid);
   auto up = [](size_t x) { return (x + 255) & ~static_cast<size_t>(255); };
-  const size_t rows = static_cast<size_t>(2 * s->grid) * s->heads_cta * s->nt * 8;
+  const size_t rows = (static_cast<size_t>(2 * s->grid) * s->heads_cta << s->rg_log) * 8;
   s->info_off = 256;
   s->ml_off = up(s->info_off + s->grid * sizeof(int4));
   s->part_off = up(s->ml_off + rows * sizeof(float2));
@@ -855,37 +841,30 @@ apack_status plan_shape(const apack_paged_cache *c, int32_t hq, PdShape *s) {
   return APACK_OK;
 }
 
-constexpr size_t kSmem = kStageBytesCta + kMergeFloats * sizeof(float) + kWarps * 32 * sizeof(float2) +
-                         kWarps * 8 * sizeof(uint64_t) + kWarps * kWindow * sizeof(int);
+constexpr size_t kSmem = kStageBytesCta + kMergeFloats * sizeof(float) + kWarps * 8 * sizeof(float2) +
+                         2 * kMaxStages * sizeof(uint64_t) + kWarps * kWindow * sizeof(int);
 
-template <class T, int D, int NT>
-cudaError_t launch_paged(const PdPlan &P, const CUtensorMap &kmap, const CUtensorMap &vmap, int grid,
-                         cudaStream_t stream) {
+template <class T, int D, bool SHARED>
+cudaError_t launch_chunk(const PdPlan &P, const CUtensorMap &kmap, const CUtensorMap &vmap, int grid, cudaStream_t stream) {
   static std::atomic<uint64_t> attr{0};
-  cudaError_t e = once_per_device(attr, [] {
-    return cudaFuncSetAttribute(paged_chunk_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  const cudaError_t e = once_per_device(attr, [] {
+    return cudaFuncSetAttribute(paged_chunk_kernel<T, D, SHARED>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 static_cast<int>(kSmem));
   });
   if (e != cudaSuccess) return e;
-  e = launch_pdl(paged_chunk_kernel<T, D, NT>, dim3(grid), dim3(kThreads), kSmem, stream, P, kmap, vmap);
-  if (e != cudaSuccess) return e;
-  count_launches(1);
-  e = launch_pdl(paged_combine_kernel<T, D, NT>, dim3(grid), dim3(32 * kCombineWarps), 0, stream, P, grid);
-  if (e == cudaSuccess) count_launches(1);
-  return e;
+  return launch_pdl(paged_chunk_kernel<T, D, SHARED>, dim3(grid), dim3(kThreads), kSmem, stream, P, kmap, vmap);
 }
 
-template <class T>
-cudaError_t launch_typed(const PdPlan &P, int D, int NT, const CUtensorMap &kmap, const CUtensorMap &vmap, int grid,
-                         cudaStream_t s) {
-  if (D == 128) {
-    if (NT == 1) return launch_paged<T, 128, 1>(P, kmap, vmap, grid, s);
-    if (NT == 2) return launch_paged<T, 128, 2>(P, kmap, vmap, grid, s);
-    return launch_paged<T, 128, 4>(P, kmap, vmap, grid, s);
-  }
-  if (NT == 1) return launch_paged<T, 64, 1>(P, kmap, vmap, grid, s);
-  if (NT == 2) return launch_paged<T, 64, 2>(P, kmap, vmap, grid, s);
-  return launch_paged<T, 64, 4>(P, kmap, vmap, grid, s);
+template <class T, int D>
+cudaError_t launch_paged(const PdPlan &P, const CUtensorMap &kmap, const CUtensorMap &vmap, int grid,
+                         cudaStream_t stream) {
+  cudaError_t e = P.rg_log ? launch_chunk<T, D, true>(P, kmap, vmap, grid, stream)
+                           : launch_chunk<T, D, false>(P, kmap, vmap, grid, stream);
+  if (e != cudaSuccess) return e;
+  count_launches(1);
+  e = launch_pdl(paged_combine_kernel<T, D>, dim3(grid), dim3(32 * kCombineWarps), 0, stream, P, grid);
+  if (e == cudaSuccess) count_launches(1);
+  return e;
 }
 
 }  // namespace
@@ -934,6 +913,7 @@ apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_
   P.group = s.group;
   P.heads_cta = s.heads_cta;
   P.wph_log = s.wph_log;
+  P.rg_log = s.rg_log;
   P.groups = s.groups;
   const int tile = tile_tokens(cache->head_dim);
   P.box_tokens = std::gcd(cache->page_tokens, tile);
@@ -961,9 +941,11 @@ apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_
       !make_page_map(&vmap, cache, P.pool.v, P.box_tokens, blocks))
     return APACK_ECUDA;
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
-  return check_cuda(cache->dtype == APACK_BF16
-                        ? launch_typed<__nv_bfloat16>(P, cache->head_dim, s.nt, kmap, vmap, s.grid, cs)
-                        : launch_typed<__half>(P, cache->head_dim, s.nt, kmap, vmap, s.grid, cs));
+  if (cache->dtype == APACK_BF16)
+    return check_cuda(cache->head_dim == 128 ? launch_paged<__nv_bfloat16, 128>(P, kmap, vmap, s.grid, cs)
+                                             : launch_paged<__nv_bfloat16, 64>(P, kmap, vmap, s.grid, cs));
+  return check_cuda(cache->head_dim == 128 ? launch_paged<__half, 128>(P, kmap, vmap, s.grid, cs)
+                                           : launch_paged<__half, 64>(P, kmap, vmap, s.grid, cs));
 }
 
 }  // extern "C"

@@ -297,6 +297,8 @@ def check_attention(ap, rng, lens, hq, hkv, dim, tokens, dtype, order="nhd", out
     ([257], 17, 1, 64, 1000, "fp16", "nhd", None),
     ([100, 47, 33, 16], 12, 4, 64, 48, "fp16", "nhd", None),
     ([1000, 18], 32, 1, 64, 16, "bf16", "hnd", None),
+    ([700, 45, 3000], 64, 4, 128, 16, "bf16", "nhd", None),
+    ([333, 1, 90], 96, 4, 64, 8, "fp16", "nhd", "fp32"),
 ])
 def test_paged_attention(ap, lens, hq, hkv, dim, tokens, dtype, order, out_dtype):
     rng = np.random.default_rng(sum(lens) + hq + tokens)
