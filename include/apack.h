@@ -469,9 +469,10 @@ apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_
    of src's sequence b, for j in [cu_dst[b], cu_dst[b+1]); cu_dst: device [B+1], apack_select's new_cu_seqlens.
    n_out: cu_dst[B], or an upper bound of it.  B = num_seqs of both pools; heads, D and dtype equal; page sizes
    and strides may differ.  Slots of dst that no j names keep what they hold.
-   Out of place, no page that is written may be read by the same call.  In place: src and dst are the same
-   pool (k, v and strides), table (pointer and stride) and layer, keep_idx is given and ascending within each
-   sequence, and each sequence's pages are its own; rows move towards the front of their sequence.
+   Out of place (another pool, other pages of the same one by another table, or other layers), no page that is
+   written may be read by the same call.  In place: src and dst name the same pool, table and layers; keep_idx is
+   then given and ascending within each sequence, and each sequence's pages are its own; rows move towards the
+   front of their sequence.
    ws: NULL, or a workspace whose error word receives APACK_EDEVICE when a row lies behind a page table or a
    page number outside its pool; such a row is not copied, with or without ws. */
 apack_status apack_paged_compact(const apack_paged_cache *src, const apack_paged_cache *dst, int32_t src_layer,

@@ -1,0 +1,227 @@
+"""Who holds which page of a paged key-value cache.
+
+Sec. 3.2 shortens a sequence's cache at every pruning layer; ``PagePool`` gives what that frees to other
+sequences.  It keeps the page lists, reference counts and lengths of up to ``max_seqs`` sequences on the host,
+mirrors them in the int32 page table and length tensors that the operators read, and calls ``apack_copy_pages``
+and ``apack_paged_compact`` where pages have to move.  A fork shares its parent's pages; a page that is shared is
+copied when a sequence first writes behind its last row.
+
+All device work is queued on torch's current stream; a pool's calls belong on one stream (a page that is freed
+may be handed out again by the next call).  Every method checks that it can be carried out (pages, rows) before
+it changes anything.
+"""
+
+import numpy as np
+import torch
+
+from . import PagedCache, apack_copy_pages, apack_paged_compact
+
+
+class PagePool:
+    """Pools ``k`` and ``v`` [layers, pages, page_tokens, Hkv, D], ``page_table`` [max_seqs, max_pages] and
+    ``lengths`` [max_seqs] on the device, and ``cache``, the PagedCache of all of it.
+
+    heads_first: the heads of a page outermost in memory ([layers, pages, Hkv, page_tokens, D])."""
+
+    def __init__(self, num_layers, num_pages, page_tokens, num_kv_heads, head_dim, max_seqs, max_pages=None,
+                 dtype=torch.bfloat16, device="cuda", heads_first=False):
+        max_pages = num_pages if max_pages is None else max_pages
+        shape = (num_layers, num_pages, num_kv_heads, page_tokens, head_dim) if heads_first else (
+            num_layers, num_pages, page_tokens, num_kv_heads, head_dim)
+        self.k, self.v = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
+        if heads_first:
+            self.k, self.v = self.k.permute(0, 1, 3, 2, 4), self.v.permute(0, 1, 3, 2, 4)
+        self.page_tokens, self.max_pages, self.device = page_tokens, max_pages, device
+        self.page_table = torch.full((max_seqs, max_pages), -1, dtype=torch.int32, device=device)
+        self.lengths = torch.zeros(max_seqs, dtype=torch.int32, device=device)
+        self.cache = PagedCache(self.k, self.v, self.page_table)
+        self._refs = np.zeros(num_pages, np.int64)
+        self._free = list(range(num_pages - 1, -1, -1))
+        self._pages = [None] * max_seqs          # page list of a sequence, None where the row is unused
+        self._len = np.zeros(max_seqs, np.int64)
+
+    # ------------------------------------------------------------ host state
+
+    @property
+    def free_pages(self):
+        return len(self._free)
+
+    def length(self, seq):
+        self._held(seq)
+        return int(self._len[seq])
+
+    def pages(self, seq):
+        return list(self._held(seq))
+
+    def _held(self, seq):
+        if not 0 <= seq < len(self._pages) or self._pages[seq] is None:
+            raise ValueError(f"sequence {seq} is not in the pool")
+        return self._pages[seq]
+
+    def _need(self, rows):
+        n = -(-int(rows) // self.page_tokens)
+        if rows < 0 or n > self.max_pages:
+            raise ValueError(f"{rows} rows: 0 to {self.max_pages * self.page_tokens} fit a sequence")
+        return n
+
+    def _room(self, pages, seqs=0):
+        if pages > len(self._free):
+            raise MemoryError(f"{pages} pages wanted, {len(self._free)} free")
+        rows = [i for i, p in enumerate(self._pages) if p is None]
+        if seqs > len(rows):
+            raise MemoryError(f"{seqs} sequences wanted, {len(rows)} rows of the page table free")
+        return rows[:seqs]
+
+    def _take(self, n):
+        got = [self._free.pop() for _ in range(n)]
+        self._refs[got] = 1
+        return got
+
+    def _drop(self, pages):
+        for p in pages:
+            self._refs[p] -= 1
+            if self._refs[p] == 0:
+                self._free.append(p)
+
+    def _upload(self, seqs):
+        """The rows of these sequences in the device's tables."""
+        if not len(seqs):
+            return
+        table = np.full((len(seqs), self.max_pages), -1, np.int32)
+        for i, s in enumerate(seqs):
+            pages = self._pages[s] or []
+            table[i, :len(pages)] = pages
+        at = torch.tensor(list(seqs), dtype=torch.int64, device=self.device)
+        self.page_table.index_copy_(0, at, torch.from_numpy(table).to(self.device))
+        self.lengths.index_copy_(0, at, torch.tensor([int(self._len[s]) for s in seqs], dtype=torch.int32, device=self.device))
+
+    def _ints(self, values):
+        return torch.tensor(np.asarray(values, np.int32), device=self.device)
+
+    # ------------------------------------------------------------ sequences
+
+    def add(self, rows=0):
+        """A new sequence with pages for `rows` rows, which the caller writes; returns its number."""
+        n = self._need(rows)
+        seq, = self._room(n, 1)
+        self._pages[seq], self._len[seq] = self._take(n), rows
+        self._upload([seq])
+        return seq
+
+    def fork(self, seq):
+        """A new sequence that shares the pages of `seq`; returns its number."""
+        pages = self._held(seq)
+        new, = self._room(0, 1)
+        self._refs[pages] += 1
+        self._pages[new], self._len[new] = list(pages), self._len[seq]
+        self._upload([new])
+        return new
+
+    def extend(self, seqs, rows=1):
+        """Room for `rows` more rows behind each of `seqs` (distinct), in pages of their own; the caller writes
+        them.  Returns the first new row of each (int32, on the device)."""
+        if rows < 0 or len(set(seqs)) != len(seqs):
+            raise ValueError("rows >= 0 and distinct sequences expected")
+        copied, wanted, shared = set(), 0, dict()
+        for s in seqs:
+            held, used = self._held(s), int(self._len[s])
+            wanted += self._need(used + rows) - len(held)
+            if rows and used % self.page_tokens:
+                last = held[used // self.page_tokens]
+                # of the sequences that share it, all but the last holder need a copy
+                left = shared.get(last, int(self._refs[last]))
+                if left > 1:
+                    copied.add(s)
+                    wanted += 1
+                    shared[last] = left - 1
+        self._room(wanted)
+        pairs, first = [], []
+        for s in seqs:
+            held, used = self._pages[s], int(self._len[s])
+            if s in copied:
+                i = used // self.page_tokens
+                own, = self._take(1)
+                pairs.append((held[i], own))
+                self._drop([held[i]])
+                held[i] = own
+            held += self._take(self._need(used + rows) - len(held))
+            first.append(used)
+            self._len[s] = used + rows
+        if pairs:
+            apack_copy_pages(self.cache, self._ints(pairs))
+        self._upload(seqs)
+        return self._ints(first)
+
+    def free(self, seq):
+        """Gives up a sequence; pages that no other one shares become free."""
+        self._drop(self._held(seq))
+        self._pages[seq], self._len[seq] = None, 0
+        self._upload([seq])
+
+    # ------------------------------------------------------------ pruning
+
+    def _cache_of(self, lists):
+        table = np.full((len(lists), max(1, max(map(len, lists)))), -1, np.int32)
+        for i, pages in enumerate(lists):
+            table[i, :len(pages)] = pages
+        return PagedCache(self.k, self.v, self._ints(table))
+
+    def _moved(self, need, src, cu_dst, n_out, **how):
+        """Rows of src in new pages, need[i] of them for the i-th sequence; returns the page lists."""
+        new = [self._take(n) for n in need]
+        try:
+            apack_paged_compact(src, self._cache_of(new), cu_dst, n_out, **how)
+        except Exception:
+            for pages in new:
+                self._drop(pages)
+            raise
+        return new
+
+    def prune(self, seqs, keep_idx, kept, in_place=None, ws=None):
+        """Keeps kept[i] rows of seqs[i] (distinct): keep_idx holds them, packed over the sequences in this order
+        as apack_select writes it (row r of seqs[i] is the sum of the lengths before it + r), ascending.  The kept rows
+        go to new pages and the old ones are given up, or, in place, to the first of the sequences' own pages (no
+        page of which may be shared) and only the pages behind them are given up: about a third of the speed, but
+        no page is needed.  in_place None: in place only where there are too few free pages for the other way."""
+        if not len(seqs) or len(set(seqs)) != len(seqs) or len(kept) != len(seqs):
+            raise ValueError("distinct sequences and a number of kept rows for each expected")
+        lists = [self._held(s) for s in seqs]
+        lens = [int(self._len[s]) for s in seqs]
+        if any(not 0 <= int(m) <= n for m, n in zip(kept, lens)):
+            raise ValueError("kept rows: 0 to the sequence's length")
+        need = [self._need(m) for m in kept]
+        cu_src, cu_dst = (self._ints(np.concatenate([[0], np.cumsum(x)])) for x in (lens, kept))
+        n_out = int(sum(int(m) for m in kept))
+        src = self._cache_of(lists)
+        own = all(self._refs[p] == 1 for pages in lists for p in pages)
+        if in_place and not own:
+            raise ValueError("in place: a page is shared with another sequence")
+        if in_place or (in_place is None and own and sum(need) > len(self._free)):
+            apack_paged_compact(src, src, cu_dst, n_out, keep_idx=keep_idx, cu_src=cu_src, ws=ws)
+            for s, n, pages in zip(seqs, need, lists):
+                self._drop(pages[n:])
+                self._pages[s] = pages[:n]
+        else:
+            self._room(sum(need))
+            new = self._moved(need, src, cu_dst, n_out, keep_idx=keep_idx, cu_src=cu_src, ws=ws)
+            for s, pages, own in zip(seqs, lists, new):
+                self._drop(pages)
+                self._pages[s] = own
+        for s, m in zip(seqs, kept):
+            self._len[s] = int(m)
+        self._upload(seqs)
+
+    def take(self, src, kept, keep_idx=None, cu_src=None, src_layer=0, dst_layer=0, num_layers=None, ws=None):
+        """New sequences from the kept rows of another PagedCache (a prefill's contiguous caches, say: one page of
+        all tokens), kept[i] rows of its sequence i; the arguments as in apack_paged_compact.  Returns their numbers."""
+        if len(kept) != src.num_seqs:
+            raise ValueError(f"kept: {src.num_seqs} numbers expected")
+        need = [self._need(m) for m in kept]
+        rows = self._room(sum(need), len(kept))
+        cu_dst = self._ints(np.concatenate([[0], np.cumsum(kept)]))
+        new = self._moved(need, src, cu_dst, int(sum(int(m) for m in kept)), keep_idx=keep_idx, cu_src=cu_src,
+                          src_layer=src_layer, dst_layer=dst_layer, num_layers=num_layers, ws=ws)
+        for s, pages, m in zip(rows, new, kept):
+            self._pages[s], self._len[s] = pages, int(m)
+        self._upload(rows)
+        return rows

@@ -694,3 +694,58 @@ def test_tensors_elsewhere_are_refused(ap):
     pos = torch.zeros(1, dtype=torch.int32)
     with pytest.raises(ValueError):
         ap.apack_rotary(ap.Rotary(64), x, pos, x)
+
+
+def test_page_pool_prunes_forks_and_decodes(ap):
+    """PagePool on the device: prefill caches taken with their kept rows, a fork, steps of both, a prune of one of them
+    while it shares pages and of the other in place; every decode against the rows that the model keeps."""
+    from paper_2608_08794_gb300.paged import PagePool
+    rng = np.random.default_rng(19)
+    hq, hkv, dim, layers, T = 8, 2, 128, 3, 300
+    slab_k, slab_v = (normal(rng, (layers, 1, T, hkv, dim), torch.bfloat16) for _ in range(2))
+    slab = ap.PagedCache(slab_k, slab_v, i32([[0]]))
+    pool = PagePool(layers, 60, 16, hkv, dim, 4, max_pages=24)
+    pool.k.fill_(math.nan)
+    pool.v.fill_(math.nan)
+    ws = workspace(ap.apack_paged_decode_workspace_size(pool.cache, hq))
+    keep = np.sort(rng.permutation(T)[:201])
+    a, = pool.take(slab, [201], keep_idx=i32(keep), ws=ws)
+    rows = {a: [(f64(slab_k[:, 0, r]), f64(slab_v[:, 0, r])) for r in keep]}
+
+    def step(seqs):
+        first = pool.extend(seqs)
+        kv = normal(rng, (layers, len(seqs), 2 * hkv, dim), torch.bfloat16)
+        for i in range(layers):
+            ap.apack_rotary_append(None, pool.cache, i, None, kv[i, :, :hkv], kv[i, :, hkv:], None, None, first, seqs=i32(seqs), ws=ws)
+        for j, s in enumerate(seqs):
+            rows[s] = rows[s] + [(f64(kv[:, j, :hkv]), f64(kv[:, j, hkv:]))]
+        q, out = normal(rng, (4, hq, dim), torch.bfloat16), torch.empty(4, hq, dim, device="cuda")
+        for i in range(layers):
+            ap.apack_paged_decode_attention(pool.cache, i, pool.lengths, q, out, ws)
+            for s in range(4):
+                if s not in rows:
+                    assert not out[s].any()
+                    continue
+                k, v = (np.stack([r[x][i] for r in rows[s]])[:, None] for x in (0, 1))
+                ref, _, spread, size = po.paged_decode(f64(q[s:s + 1]), k, v, np.arange(len(k))[None], [len(k)], dim ** -0.5)
+                tol = spread * (2.0 ** -16 + 120 * 2.0 ** -23 + 2.0 ** -19 * size)[..., None]
+                assert np.all(np.abs(f64(out[s:s + 1]) - ref) <= tol)
+
+    def prune(s, m, in_place=None):
+        picks = np.sort(rng.permutation(len(rows[s]))[:m])
+        pool.prune([s], i32(picks), [m], in_place=in_place, ws=ws)
+        rows[s] = [rows[s][i] for i in picks]
+
+    step([a])
+    b = pool.fork(a)
+    rows[b] = list(rows[a])
+    step([b, a])
+    prune(b, 90)                                   # shares pages with a: into new pages
+    step([a, b])
+    prune(b, 40, in_place=True)                    # its pages are its own now
+    step([b])
+    pool.free(a)
+    del rows[a]
+    step([b])
+    assert ap.apack_device_error(ws) == ap.APACK_OK
+    assert pool.free_pages == 60 - len(pool.pages(b))

@@ -178,12 +178,15 @@ def test_move_refusals(ap):
                dict(num_layers=0), dict(num_layers=3), dict(src_layer=-1), dict(src_layer=2, num_layers=1),
                dict(dst_layer=1, num_layers=2), dict(keep_idx=None, cu_src=cu)):
         assert status(ap, call(**kw)) == ap.APACK_EINVAL, kw
-    # in place: one table, one layer, and an index
-    other = ap.PagedCache(a.k, a.v, torch.zeros(2, 3, dtype=torch.int32))
-    assert status(ap, call(dst=other)) == ap.APACK_EINVAL
+    # one table on both sides: in place with an index, or layers apart
     assert status(ap, call(dst=a, keep_idx=None)) == ap.APACK_EINVAL
-    assert status(ap, call(dst=a, dst_layer=1, num_layers=1)) == ap.APACK_EINVAL
+    assert status(ap, call(src=cache(ap, layers=3), dst_layer=1, num_layers=2)) == ap.APACK_EINVAL
+    three = cache(ap, layers=3)
+    assert status(ap, call(src=three, dst=three, dst_layer=1, num_layers=2)) == ap.APACK_EINVAL
+    assert status(ap, call(src=three, dst=three, dst_layer=1, num_layers=1)) == ap.APACK_ECUDA      # goes on to the device
     assert status(ap, call(dst=ap.PagedCache(a.k, a.k, a.page_table))) == ap.APACK_EINVAL
+    other = ap.PagedCache(a.k, a.v, torch.zeros(2, 3, dtype=torch.int32))                           # other pages of a pool
+    assert status(ap, call(dst=other)) == ap.APACK_ECUDA
     for kw in (dict(n_out=5), dict(keep_idx=keep.long()), dict(cu_src=cu[:2])):
         with pytest.raises(ValueError):
             call(**kw)()
