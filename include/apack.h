@@ -446,11 +446,11 @@ apack_status apack_rotary_append(const apack_rotary_spec *spec, const apack_page
    A NaN or infinity among the rows themselves makes what it enters NaN (an infinite value: infinite or NaN).
    q: [num_seqs][Hq][D] at q_token_stride bytes, cache dtype, 16-byte aligned; scale > 0 (1/sqrt(D) is usual).
    out: [num_seqs][Hq][D], contiguous, 16-byte aligned, out_dtype the cache's or APACK_FP32.  lse: fp32
-   [num_seqs][Hq] or NULL, ln sum_r exp(scale q.k).  Hq / Hkv <= 32 and tables of at most
-   3.4e10 / Hkv tokens in all sequences together (APACK_EUNSUPPORTED otherwise), Hq <= 1024.
+   [num_seqs][Hq] or NULL, ln sum_r exp(scale q.k).  Hq / Hkv <= 32 (APACK_EUNSUPPORTED otherwise), Hq <= 1024.
    fp32 softmax and accumulation; the sums' order depends on the lengths alone (deterministic).
    A length below 0 or above max_pages*page_tokens is read as the nearest of the two, and a page number outside
-   the pool as a page of zeros; both record APACK_EDEVICE in the error word of ws.
+   the pool as a page of zeros; both record APACK_EDEVICE in the error word of ws.  So do lengths that add up to more
+   than some 1e10 tokens (shared pages), and nothing is computed.
    ws: 256-byte aligned, apack_paged_decode_workspace_size bytes (for this pool and Hq, whatever the lengths;
    query it on the device that runs the call), its error word (first 16 bytes) zeroed once by the caller.
    Two captured graphs may share a workspace as long as they do not overlap.  Two kernel launches. */

@@ -40,6 +40,8 @@ constexpr int kMaxStages = kStageBytesCta / kStageBytes;
 // below 2^8 times their number, far inside fp32, and most tiles need one vote instead of the reduction.
 constexpr float kRescale = 8.f;
 
+constexpr int64_t kMaxUnits = INT32_MAX - 1024;   // of the work list
+
 // What a (sequence, head group) costs a CTA beyond its tiles (its queries' latency, the merge, the write), as the
 // bytes of K and V that it could have streamed meanwhile.
 constexpr int kSegBytes = 196608;
@@ -238,7 +240,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int B = P.pool.num_seqs, grid = gridDim.x, cta = blockIdx.x, cost = P.seg_cost;
   const bool report = warp == 0 && cta == 0;
   if (threadIdx.x == 0) P.info[cta] = make_int4(0, 0, 0, 0);
-  auto units = [&](int len) { return len > 0 ? (tiles_of<kTile>(len) + cost) * P.groups : 0; };
+  auto units64 = [&](int len) { return len > 0 ? static_cast<int64_t>(tiles_of<kTile>(len) + cost) * P.groups : 0; };
+  auto units = [&](int len) { return static_cast<int>(units64(len)); };
+  auto sum = [&](int64_t v) {                          // over the lanes
+    const uint32_t low = static_cast<uint32_t>(v) & 0xFFFFFu, high = static_cast<uint32_t>(v >> 20);
+    return (static_cast<int64_t>(__reduce_add_sync(0xffffffffu, high)) << 20) + __reduce_add_sync(0xffffffffu, low);
+  };
   auto scan = [&](int v) {                             // inclusive, over the lanes
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) {
@@ -249,7 +256,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   };
   LengthWindow lens;
   lens.v = window + warp * kWindow;
-  int W, mine, n0 = 0, n1 = 0;
+  int mine = 0, n0 = 0, n1 = 0;
+  int64_t total = 0;
   const int per = (B + 31) / 32;                       // sequences of a lane
   if (B <= kWindow) {
     // the window holds them all; lane and lane + 32 are its sequences
@@ -259,14 +267,19 @@ __global__ void __launch_bounds__(kThreads, 1)
     window[warp * kWindow + lane + 32] = n1;
     lens.b0 = 0;
     mine = units(n0);
-    W = __reduce_add_sync(0xffffffffu, mine + units(n1));
+    total = units64(n0) + units64(n1);
   } else {
-    mine = 0;
     for (int i = 0; i < per; ++i)
-      if (lane * per + i < B) mine += units(clamped_length(P, lane * per + i, report));
-    W = __reduce_add_sync(0xffffffffu, mine);
+      if (lane * per + i < B) total += units64(clamped_length(P, lane * per + i, report));
+    mine = static_cast<int>(total);
   }
-  W -= cost;
+  total = sum(total) - cost;
+  // the list is counted in 32 bits from here on
+  if (total > kMaxUnits) {
+    if (report && lane == 0) raise_device_error(P.err, APACK_EDEVICE, 85);
+    total = 0;
+  }
+  const int W = static_cast<int>(total);
   const int C = min(grid, max(W / P.min_tiles, 1));
   if (W <= 0 || cta >= C || sub >= wph) return;
   const int active = 32 * (P.heads_cta << (P.wph_log + rg_log));   // threads of the warps at work
@@ -661,6 +674,7 @@ constexpr int kCombineBatch = 10;     // parts whose loads a warp has in flight
 constexpr int kCombineFew = 30;        // parts that one warp merges
 constexpr int kMaxGrid = 512;
 
+
 // (max, sum, o) of two query rows (2 t4 and + 1) and two features (g8 and + 8), in log2 units.
 struct PartState {
   float m0, m1, l0, l1;
@@ -922,9 +936,6 @@ apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_
       std::min<int64_t>(INT32_MAX - tile, static_cast<int64_t>(cache->max_pages) * cache->page_tokens));
   P.min_tiles = 2 << s.wph_log;
   P.seg_cost = std::max(1, kSegBytes / (tile * s.heads_cta * cache->head_dim * 4));
-  // the work list is counted in 32 bits
-  if (static_cast<int64_t>(cache->num_seqs) * s.groups * (P.max_rows / tile + 1 + P.seg_cost) > INT32_MAX - 1024)
-    return APACK_EUNSUPPORTED;
   P.scale2 = scale * 1.4426950408889634f;
   P.grow = kRescale / P.scale2;
   P.out = out;

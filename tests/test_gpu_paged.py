@@ -311,6 +311,8 @@ def test_paged_attention_of_many_sequences(ap):
     lens[5], lens[130], lens[299] = 2000, 0, 700
     check_attention(ap, rng, lens, 4, 2, 64, 16, "bf16")
     check_attention(ap, rng, [1] * 700, 2, 2, 64, 16, "fp16")
+    check_attention(ap, rng, [int(x) for x in rng.integers(0, 4, 4095)] + [900], 1, 1, 64, 16, "fp16")
+    check_attention(ap, rng, [0] * 64 + [1, 0, 40], 12, 12, 64, 16, "bf16")
 
 
 @pytest.mark.parametrize("k_scale,scale", [(8.0, None), (30.0, None), (0.0, None), (1.5, 1e-3), (1.5, 1.0)])
@@ -749,3 +751,73 @@ def test_page_pool_prunes_forks_and_decodes(ap):
     step([b])
     assert ap.apack_device_error(ws) == ap.APACK_OK
     assert pool.free_pages == 60 - len(pool.pages(b))
+
+
+FIRST_CALLS = r"""
+import sys, threading
+import torch
+sys.path.insert(0, sys.argv[1])
+import __graft_entry__
+__graft_entry__.build()
+import paper_2608_08794_gb300 as ap
+
+torch.manual_seed(0)
+n, hq, hkv = 300, 40, 4                                   # rings of two warps; the eager calls below take the same path
+k, v = (torch.randn(1, 20, 16, hkv, 128, device="cuda").bfloat16() for _ in range(2))
+table = torch.arange(19, -1, -1, dtype=torch.int32, device="cuda").view(1, 20)
+cache = ap.PagedCache(k, v, table)
+lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+row = lens - 1
+x = torch.randn(1, hq + 2 * hkv, 128, device="cuda").bfloat16()
+pos = torch.tensor([123456], dtype=torch.int32, device="cuda")
+rot = ap.Rotary(128)
+ws = torch.zeros(ap.apack_paged_decode_workspace_size(cache, hq) + 256, dtype=torch.uint8, device="cuda")
+ws = ws[(-ws.data_ptr()) % 256:][:-256]
+q, out = torch.empty(1, hq, 128, dtype=torch.bfloat16, device="cuda"), torch.empty(1, hq, 128, device="cuda")
+torch.cuda.synchronize()
+assert ap.apack_launch_count() == 0
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):                             # the first calls of the process are captured
+    ap.apack_rotary_append(rot, cache, 0, x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:], q, pos, row)
+    ap.apack_paged_decode_attention(cache, 0, lens, q, out, ws)
+for _ in range(2):
+    graph.replay()
+torch.cuda.synchronize()
+want = out.clone()
+
+# then from two threads at once, each on a stream and with tensors of its own
+go, errors, outs = threading.Barrier(2), [], {}
+def work(i):
+    try:
+        torch.cuda.set_device(0)
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            w, o, qq = ws.clone(), torch.empty_like(out), torch.empty_like(q)
+            off = (-w.data_ptr()) % 256
+            assert off == 0
+            s.synchronize()
+            go.wait()
+            for _ in range(50):
+                ap.apack_rotary(rot, x[:, :hq], pos, qq)
+                ap.apack_paged_decode_attention(cache, 0, lens, qq, o, w)
+            s.synchronize()
+        outs[i] = o
+    except Exception as e:
+        errors.append(e)
+ts = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+for t in ts: t.start()
+for t in ts: t.join()
+assert not errors, errors
+assert torch.equal(outs[0], want) and torch.equal(outs[1], want)
+assert ap.apack_device_error(ws) == ap.APACK_OK
+print("first calls ok")
+"""
+
+
+def test_first_calls_captured_and_calls_from_two_threads():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS, root], capture_output=True, text=True, cwd=root, timeout=600)
+    assert r.returncode == 0 and "first calls ok" in r.stdout, r.stdout[-2000:] + r.stderr[-4000:]
