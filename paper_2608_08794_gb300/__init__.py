@@ -455,23 +455,26 @@ def _dtype_code(dtype):
     return code
 
 
-def _current_device():
-    """Index of the current device; -1 without one (the library's own checks then answer)."""
-    import torch
-    if torch.cuda.is_initialized() or torch.cuda.is_available():
-        try:
-            return torch._C._cuda_getDevice()
-        except AttributeError:
-            return torch.cuda.current_device()
-    return -1
+_cuda = None                      # (current device, current stream of a device), looked up once CUDA is there
 
 
-def _on_device(tensors):
-    """The calls run on the current device: tensors elsewhere are refused."""
-    dev = _current_device()
+def _on_device(tensors, stream):
+    """The calls run on the current device: tensors elsewhere are refused (without a device the library's own checks
+    answer).  Returns the address of the stream, the device's current one when None."""
+    global _cuda
+    if _cuda is None:
+        import torch
+        if torch.cuda.is_initialized() or torch.cuda.is_available():
+            torch.cuda.current_device()              # initialises
+            try:
+                _cuda = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+            except AttributeError:
+                _cuda = torch.cuda.current_device, lambda dev: torch.cuda.current_stream(dev).cuda_stream
+    dev = -1 if _cuda is None else _cuda[0]()
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError(f"a tensor on device {t.get_device()}; the current device is {dev}")
+    return _cuda[1](dev) if stream is None and _cuda is not None else _stream(stream)
 
 
 def _int32(t, what, shape=None):
@@ -574,20 +577,20 @@ class Rotary:
 
 def apack_rotary(rotary, x, positions, out, transpose=False, stream=None):
     """Rotary positions of x [tokens, heads, D] into out (out is x: in place); transpose: the gradient."""
-    _on_device((x, positions, out))
+    stream = _on_device((x, positions, out), stream)
     size = x.element_size()
     xs = size * _head_rows(x, "x")
     n, heads, dim = x.shape
     outs = xs if out is x else size * _head_rows(out, "out", x.dtype, x.shape)
     axis = rotary._positions(positions, n)
     _check(_lib.apack_rotary(rotary._address, _dtype_code(x.dtype), n, heads, dim, x.data_ptr(), xs, out.data_ptr(),
-                             outs, positions.data_ptr(), axis, 1 if transpose else 0, _stream(stream)), "apack_rotary")
+                             outs, positions.data_ptr(), axis, 1 if transpose else 0, stream), "apack_rotary")
 
 
 def apack_rotary_append(rotary, cache, layer, q, k, v, q_out, positions, rows, seqs=None, ws=None, stream=None):
     """Rotates new tokens' queries into q_out and their keys into the pages of `layer`, with their values.
     rotary None: no rotation; q (and q_out) None: keys and values alone."""
-    _on_device((cache, q, k, v, q_out, positions, rows, seqs, ws))
+    stream = _on_device((cache, q, k, v, q_out, positions, rows, seqs, ws), stream)
     n = k.shape[0]
     dtype, dim = cache.dtype, cache.head_dim
     shape = (n, cache.num_kv_heads, dim)
@@ -609,7 +612,7 @@ def apack_rotary_append(rotary, cache, layer, q, k, v, q_out, positions, rows, s
     _check(_lib.apack_rotary_append(None if rotary is None else rotary._address, cache._address, int(layer), n,
                                     _ptr(q), 2 * qs, _ptr(q_out), 2 * qos, heads, k.data_ptr(), 2 * ks, v.data_ptr(),
                                     2 * vs, None if rotary is None else positions.data_ptr(), axis, rows.data_ptr(),
-                                    _ptr(seqs), _ptr(ws), _stream(stream)), "apack_rotary_append")
+                                    _ptr(seqs), _ptr(ws), stream), "apack_rotary_append")
 
 
 def apack_paged_decode_workspace_size(cache, num_q_heads):
@@ -622,7 +625,7 @@ def apack_paged_decode_workspace_size(cache, num_q_heads):
 def apack_paged_decode_attention(cache, layer, seqlens, q, out, ws, scale=None, lse=None, stream=None):
     """Attention of one decode token per sequence over its pages; seqlens: int32 [num_seqs] on the device.
     q [num_seqs, Hq, D]; out: the same shape, contiguous, of q's type or float32; lse: float32 [num_seqs, Hq]."""
-    _on_device((cache, seqlens, q, out, ws, lse))
+    stream = _on_device((cache, seqlens, q, out, ws, lse), stream)
     heads = q.shape[1]
     shape = (cache.num_seqs, heads, cache.head_dim)
     qs = _head_rows(q, "q", cache.dtype, shape)
@@ -634,14 +637,14 @@ def apack_paged_decode_attention(cache, layer, seqlens, q, out, ws, scale=None, 
     _check(_lib.apack_paged_decode_attention(
         cache._address, int(layer), seqlens.data_ptr(), q.data_ptr(), 2 * qs, heads,
         cache._scale if scale is None else scale, out.data_ptr(), _dtype_code(out.dtype),
-        _ptr(lse), ws.data_ptr(), ws.nbytes, _stream(stream)), "apack_paged_decode_attention")
+        _ptr(lse), ws.data_ptr(), ws.nbytes, stream), "apack_paged_decode_attention")
 
 
 def apack_paged_compact(src, dst, cu_dst, n_out, keep_idx=None, cu_src=None, src_layer=0, dst_layer=0,
                         num_layers=None, ws=None, stream=None):
     """The kept rows of every sequence of pool src, in order, to the first rows of its pages in dst (src is dst:
     in place).  cu_dst, cu_src: int32 [num_seqs + 1] on the device; num_layers: all that both have by default."""
-    _on_device((src, dst, cu_dst, keep_idx, cu_src, ws))
+    stream = _on_device((src, dst, cu_dst, keep_idx, cu_src, ws), stream)
     _int32(cu_dst, "cu_dst", (dst.num_seqs + 1,))
     if cu_src is not None:
         _int32(cu_src, "cu_src", (src.num_seqs + 1,))
@@ -653,14 +656,14 @@ def apack_paged_compact(src, dst, cu_dst, n_out, keep_idx=None, cu_src=None, src
         num_layers = min(src.num_layers - src_layer, dst.num_layers - dst_layer)
     _check(_lib.apack_paged_compact(src._address, dst._address, int(src_layer), int(dst_layer), int(num_layers),
                                     _ptr(keep_idx), _ptr(cu_src), cu_dst.data_ptr(), int(n_out), _ptr(ws),
-                                    _stream(stream)), "apack_paged_compact")
+                                    stream), "apack_paged_compact")
 
 
 def apack_copy_pages(cache, pairs, ws=None, stream=None):
     """Copies page pairs[i, 0] to page pairs[i, 1] in every layer; pairs: int32 [n, 2] on the device."""
-    _on_device((cache, pairs, ws))
+    stream = _on_device((cache, pairs, ws), stream)
     _int32(pairs, "pairs", (pairs.shape[0], 2))
-    _check(_lib.apack_copy_pages(cache._address, pairs.data_ptr(), pairs.shape[0], _ptr(ws), _stream(stream)),
+    _check(_lib.apack_copy_pages(cache._address, pairs.data_ptr(), pairs.shape[0], _ptr(ws), stream),
            "apack_copy_pages")
 
 
