@@ -36,10 +36,6 @@ constexpr int kMergeFloats = 3584;              // shared-memory buffer of the w
 constexpr int kStageBytes = 16384 / 2;          // K and V of a tile
 constexpr int kStageBytesCta = 196608;          // of all rings: three stages per warp
 constexpr int kMaxStages = kStageBytesCta / kStageBytes;
-// Accumulators are rescaled only when a row's maximum has grown by more than this (log2 units): sums stay
-// below 2^8 times their number, far inside fp32, and most tiles need one vote instead of the reduction.
-constexpr float kRescale = 8.f;
-
 constexpr int64_t kMaxUnits = INT32_MAX - 1024;   // of the work list
 
 // What a (sequence, head group) costs a CTA beyond its tiles (its queries' latency, the merge, the write), as the
@@ -59,7 +55,7 @@ struct PdPlan {
   int32_t min_tiles;                 // smallest share of a CTA
   int32_t seg_cost;                  // what a segment costs beyond its tiles, in tiles
   float scale2;                      // scale * log2(e)
-  float grow;                        // kRescale in units of q.k
+  float grow;                        // kGrow in units of q.k
   void *out;
   int32_t out_fp32;
   float *lse;
@@ -69,10 +65,16 @@ struct PdPlan {
   DeviceError *err;
 };
 
+// The 16-bit types of K, V and P.  A probability is exp2(logit - reference); the reference is kShift below the row's
+// maximum when it was set, and set anew only when the maximum has grown by more than kGrow (log2 units), so that most
+// tiles need one vote instead of a reduction and rescaled accumulators.  bf16 has the range of fp32.  fp16 ends at
+// 2^16 and loses what lies below 2^-25: with probabilities of up to 2^15 (kShift + kGrow) the tail is kept down to
+// 2^-36 of the maximum; up to 1, a hundred thousand keys 17 below the maximum would be lost, 2^-8 of the sum.
 template <class T>
 struct Half16;
 template <>
 struct Half16<__nv_bfloat16> {
+  static constexpr float kGrow = 8.f, kShift = 0.f;
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<uint32_t *>(&v);
@@ -88,6 +90,7 @@ struct Half16<__nv_bfloat16> {
 };
 template <>
 struct Half16<__half> {
+  static constexpr float kGrow = 4.f, kShift = 11.f;
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     __half2 v = __floats2half2_rn(a, b);
     return *reinterpret_cast<uint32_t *>(&v);
@@ -498,7 +501,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
           x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
           x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-          const float mn = fmaxf(m[e], x * P.scale2);
+          const float mn = fmaxf(m[e], fmaf(x, P.scale2, -Half16<T>::kShift));
           const float f = mn == -INFINITY ? 1.f : ex2_approx(m[e] - mn);
           m[e] = mn;
           limit[e] = fmaxf(limit[e], x + P.grow);
@@ -510,8 +513,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       }
-      // P as the sum of two 16-bit numbers (2^-17 of it are left out in bf16, 2^-22 in fp16; one alone would cost
-      // 2^-9), transposed into B fragments
+      // P as the sum of two 16-bit numbers (2^-17 of it are left out in bf16, 2^-22 or 2^-36 of the largest in fp16; one
+      // alone would cost 2^-9), transposed into B fragments
       uint32_t hi[KM][2], lo[KM][2];
 #pragma unroll
       for (int km = 0; km < KM; ++km) {
@@ -937,7 +940,7 @@ apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_
   P.min_tiles = 2 << s.wph_log;
   P.seg_cost = std::max(1, kSegBytes / (tile * s.heads_cta * cache->head_dim * 4));
   P.scale2 = scale * 1.4426950408889634f;
-  P.grow = kRescale / P.scale2;
+  P.grow = (cache->dtype == APACK_BF16 ? Half16<__nv_bfloat16>::kGrow : Half16<__half>::kGrow) / P.scale2;
   P.out = out;
   P.out_fp32 = out_dtype == APACK_FP32;
   P.lse = lse;

@@ -9,6 +9,7 @@ rotary     |got - ref| <= u |ref| + 2^-20 m (|a| + |b|) + angle * 2^-51 m (|a| +
 attention  |got - ref| <= u |ref| + A (2^-16 + n 2^-23 + 2 d), A = sum_r p_r |v_r|: P as two 16-bit numbers (2^-17),
            exp2 (2^-22), n = 2 ceil(len / 16) + 64 sequential fp32 additions at most, and logits that are off by
            d = 2^-20 * max_r scale sum_i |q_i k_i| (8 fp32 accumulations that may truncate, the scale, log2 units).
+           fp16: + len 2^-36 max |v|, the spacing of its smallest numbers against probabilities of up to 2^11 and more.
 lse        |got - ref| <= 2 d + n 2^-23 + 2^-21 (1 + |ref|).
 moves      bit for bit.
 """
@@ -261,6 +262,8 @@ def check_attention(ap, rng, lens, hq, hkv, dim, tokens, dtype, order="nhd", out
     d = 2.0 ** -20 * size
     n = (2 * -(-np.array(lens) // 16) + 64)[:, None]
     tol = unit(out.dtype) * np.abs(ref) + spread * (2.0 ** -16 + n * 2.0 ** -23 + 2 * d)[..., None]
+    if dt == torch.float16:
+        tol += np.array(lens)[:, None, None] * 2.0 ** -36 * 6
     if out.dtype == torch.float16:
         tol += 2.0 ** -25
     assert np.all(np.abs(f64(out) - ref) <= tol), float((np.abs(f64(out) - ref) / (tol + 1e-300)).max())
@@ -319,6 +322,34 @@ def test_paged_attention_of_many_sequences(ap):
 def test_paged_attention_logits_of_any_size(ap, k_scale, scale):
     rng = np.random.default_rng(9)
     check_attention(ap, rng, [700, 33], 28, 4, 128, 16, "bf16", scale=scale, k_scale=k_scale, out_dtype="fp32")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_paged_attention_long_tail(ap, dtype):
+    """One key takes nearly all of the weight and has the value 0; what comes out is the tail, each of its keys about
+    2^-25 of the largest."""
+    n, dim, dt = 30000, 64, DT[dtype]
+    pages = -(-n // 16)
+    k = torch.zeros(1, pages, 16, 1, dim, dtype=dt, device="cuda")
+    v = torch.ones_like(k)
+    for at in (0, 16111, n - 1):                       # seen first, in the middle, last
+        kk, vv = k.clone(), v.clone()
+        kk.view(-1, dim)[at, 0] = 17.25
+        vv.view(-1, dim)[at] = 0
+        vv.view(-1, dim)[n:] = math.nan
+        q = torch.zeros(1, 3, dim, dtype=dt, device="cuda")
+        q[0, :, 0] = 1.0
+        cache = ap.PagedCache(kk, vv, i32([list(range(pages))]))
+        out, lse = torch.empty(1, 3, dim, device="cuda"), torch.empty(1, 3, device="cuda")
+        ws = workspace(ap.apack_paged_decode_workspace_size(cache, 3))
+        ap.apack_paged_decode_attention(cache, 0, i32([n]), q, out, ws, scale=1.0, lse=lse)
+        w = (n - 1) * math.exp(-17.25)
+        want = w / (1 + w)
+        tol = want * (2.0 ** -16 + (2 * pages + 64) * 2.0 ** -23 + 2 * 2.0 ** -20 * 17.25)
+        if dtype == "fp16":
+            tol += n * 2.0 ** -36
+        assert float((out.double() - want).abs().max()) <= tol
+        assert float((lse.double() - 17.25 - math.log1p(w)).abs().max()) <= 2 * 2.0 ** -20 * 17.25 + (2 * pages + 64) * 2.0 ** -23 + 2.0 ** -16
 
 
 def test_paged_attention_reference_that_grows(ap):
