@@ -18,6 +18,7 @@
 #include <cmath>
 #include <cstring>
 #include <numeric>
+#include <type_traits>
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -32,7 +33,7 @@ namespace {
 constexpr int tile_tokens(int D) { return D == 64 ? 32 : 16; }
 constexpr int kWarps = 8;
 constexpr int kThreads = 32 * kWarps;
-constexpr int kMergeFloats = 3584;              // shared-memory buffer of the warps' merge: 7 warps, 4 m-tiles
+constexpr int kMergeFloats = 4096;              // shared-memory buffer of the warps' merge: 8 warps, 4 m-tiles
 constexpr int kStageBytes = 16384 / 2;          // K and V of a tile
 constexpr int kStageBytesCta = 196608;          // of all rings: three stages per warp
 constexpr int kMaxStages = kStageBytesCta / kStageBytes;
@@ -52,6 +53,7 @@ struct PdPlan {
   int32_t wph_log, rg_log;           // log2 of the rings per head, and of the warps (groups of 8 query rows) per ring
   int32_t box_tokens, boxes;         // tokens of one TMA box, boxes of a tile
   int32_t max_rows;
+  int32_t wide_lengths;              // seqlens can be read four at a time
   int32_t min_tiles;                 // smallest share of a CTA
   int32_t seg_cost;                  // what a segment costs beyond its tiles, in tiles
   float scale2;                      // scale * log2(e)
@@ -133,7 +135,10 @@ __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map
 
 __device__ __forceinline__ void prefetch_l2(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
-__device__ __forceinline__ void head_barrier(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
+// The wph warps of head and row group `team`.
+__device__ __forceinline__ void team_barrier(int team, int wph) {
+  asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(32 * wph) : "memory");
+}
 
 __device__ __forceinline__ int clamped_length(const PdPlan &P, int b, bool report) {
   const int n = __ldg(P.seqlens + b);
@@ -261,7 +266,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   lens.v = window + warp * kWindow;
   int mine = 0, n0 = 0, n1 = 0;
   int64_t total = 0;
-  const int per = (B + 31) / 32;                       // sequences of a lane
+  const int per = ((B + 31) / 32 + 3) & ~3;            // consecutive sequences of a lane
   if (B <= kWindow) {
     // the window holds them all; lane and lane + 32 are its sequences
     if (lane < B) n0 = clamped_length(P, lane, report);
@@ -272,8 +277,28 @@ __global__ void __launch_bounds__(kThreads, 1)
     mine = units(n0);
     total = units64(n0) + units64(n1);
   } else {
-    for (int i = 0; i < per; ++i)
-      if (lane * per + i < B) total += units64(clamped_length(P, lane * per + i, report));
+#pragma unroll 4
+    for (int i = 0; i < per; i += 4) {
+      const int b = lane * per + i;
+      int len[4] = {0, 0, 0, 0};
+      if (P.wide_lengths && b + 4 <= B) {
+        const int4 v = __ldg(reinterpret_cast<const int4 *>(P.seqlens + b));
+        len[0] = v.x;
+        len[1] = v.y;
+        len[2] = v.z;
+        len[3] = v.w;
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (b + k < B) len[k] = __ldg(P.seqlens + b + k);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int c = min(max(len[k], 0), P.max_rows);
+        if (report && c != len[k]) raise_device_error(P.err, APACK_EDEVICE, 81, b + k, len[k]);
+        total += units64(c);
+      }
+    }
     mine = static_cast<int>(total);
   }
   total = sum(total) - cost;
@@ -285,7 +310,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int W = static_cast<int>(total);
   const int C = min(grid, max(W / P.min_tiles, 1));
   if (W <= 0 || cta >= C || sub >= wph) return;
-  const int active = 32 * (P.heads_cta << (P.wph_log + rg_log));   // threads of the warps at work
   const int u0 = cost + quotient(static_cast<int64_t>(W) * cta, C);
   const int n = cost + quotient(static_cast<int64_t>(W) * (cta + 1), C) - u0;
   Walk<kTile> seg;
@@ -301,13 +325,26 @@ __global__ void __launch_bounds__(kThreads, 1)
     off -= __shfl_sync(0xffffffffu, incl - mine, src);
     if (B <= kWindow) {
       b += src;
-      __syncwarp();
     } else {
-      b = lens.b0 = src * per;
-      for (int i = lane; i < kWindow; i += 32) window[warp * kWindow + i] = b + i < B ? clamped_length(P, b + i, false) : 0;
-      __syncwarp();
-      for (; off >= units(lens.at(P, b)); ++b) off -= units(lens.at(P, b));
+      // among the lane's sequences, 32 at a time; they and the 32 behind them become the window
+      for (b = src * per;; b += 32) {
+        const int len = b + lane < B ? clamped_length(P, b + lane, false) : 0;
+        mine = units(len);
+        incl = scan(mine);
+        const unsigned hit = __ballot_sync(0xffffffffu, off < incl);
+        if (hit) {
+          const int at = __ffs(hit) - 1;
+          off -= __shfl_sync(0xffffffffu, incl - mine, at);
+          lens.b0 = b;
+          window[warp * kWindow + lane] = len;
+          window[warp * kWindow + lane + 32] = b + lane + 32 < B ? clamped_length(P, b + lane + 32, false) : 0;
+          b += at;
+          break;
+        }
+        off -= __shfl_sync(0xffffffffu, incl, 31);
+      }
     }
+    __syncwarp();
     seg.b = b;
     seg.len = lens.at(P, b);
     seg.nt = tiles_of<kTile>(seg.len);
@@ -571,66 +608,68 @@ __global__ void __launch_bounds__(kThreads, 1)
       x += __shfl_xor_sync(0xffffffffu, x, 16);
       l[e] = x;
     }
+    // Pairs of them exchange halves of their m-tiles until each holds its own of the sums, o[0] on from m-tile `base`
     const int hr = rg * P.heads_cta + hw, team = P.heads_cta << rg_log;   // warp = sub * team + hr
-    if (wph > 1) {
+    int base = 0;
+    bool mine_to_write = true;
+    auto halve = [&](auto half, int bit) {
+      constexpr int H = decltype(half)::value;        // 0: one m-tile each, which the lower of the two keeps
+      constexpr int M = H ? H : 1;
+      const bool upper = sub & bit;
+      const int other = warp ^ (bit * team);
+      float4 *give = reinterpret_cast<float4 *>(merge) + warp * (KS / 2) * 32 + lane;
+      const float4 *take = reinterpret_cast<float4 *>(merge) + other * (KS / 2) * 32 + lane;
+      team_barrier(hr, wph);                          // the last exchange's halves have been read
+#pragma unroll
+      for (int i = 0; i < M; ++i) {
+        float(&x)[4] = o[i], (&y)[4] = o[i + H];
+        give[i * 32] = upper && H ? make_float4(x[0], x[1], x[2], x[3]) : make_float4(y[0], y[1], y[2], y[3]);
+        if (H)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) x[k] = upper ? y[k] : x[k];
+      }
       if (g8 == 0) {
         stat[warp * 8 + t4 * 2] = make_float2(m[0], l[0]);
         stat[warp * 8 + t4 * 2 + 1] = make_float2(m[1], l[1]);
       }
-      head_barrier(active);
+      team_barrier(hr, wph);
+      float a[2], b[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        float M = -INFINITY, L = 0.f;
-        for (int w = 0; w < wph; ++w) M = fmaxf(M, stat[(w * team + hr) * 8 + t4 * 2 + e].x);
-        for (int w = 0; w < wph; ++w) {
-          const float2 x = stat[(w * team + hr) * 8 + t4 * 2 + e];
-          L += x.y * (x.x == M ? 1.f : ex2_approx(x.x - M));
-        }
-        const float f = m[e] == M ? 1.f : ex2_approx(m[e] - M);
-        m[e] = M;
-        l[e] = L;
-#pragma unroll
-        for (int i = 0; i < KS; ++i) {
-          o[i][e] *= f;
-          o[i][e + 2] *= f;
-        }
+        const float2 x = stat[other * 8 + t4 * 2 + e];
+        const float top = fmaxf(m[e], x.x);
+        a[e] = m[e] == top ? 1.f : ex2_approx(m[e] - top);
+        b[e] = x.x == top ? 1.f : ex2_approx(x.x - top);
+        l[e] = l[e] * a[e] + x.y * b[e];
+        m[e] = top;
       }
-      // through a buffer, 4 m-tiles at a time ((wph - 1) * team is at most 7)
-      float4 *buf = reinterpret_cast<float4 *>(merge);
 #pragma unroll
-      for (int i0 = 0; i0 < KS; i0 += 4) {
-        if (sub > 0)
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            buf[(((sub - 1) * team + hr) * 4 + k) * 32 + lane] = make_float4(o[i0 + k][0], o[i0 + k][1], o[i0 + k][2], o[i0 + k][3]);
-        head_barrier(active);
-        if (sub == 0)
-          for (int w = 1; w < wph; ++w)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float4 x = buf[(((w - 1) * team + hr) * 4 + k) * 32 + lane];
-              o[i0 + k][0] += x.x;
-              o[i0 + k][1] += x.y;
-              o[i0 + k][2] += x.z;
-              o[i0 + k][3] += x.w;
-            }
-        head_barrier(active);
+      for (int i = 0; i < M; ++i) {
+        const float4 x = take[i * 32];
+        o[i][0] = o[i][0] * a[0] + x.x * b[0];
+        o[i][1] = o[i][1] * a[1] + x.y * b[1];
+        o[i][2] = o[i][2] * a[0] + x.z * b[0];
+        o[i][3] = o[i][3] * a[1] + x.w * b[1];
       }
-    }
-    if (sub == 0) {
-      if (seg.ts == 0 && seg.te == seg.nt) {          // the whole segment: write it out
+      if (upper) base += H;
+      if (H == 0) mine_to_write = !upper;
+    };
+    const bool whole = seg.ts == 0 && seg.te == seg.nt;
+    auto write = [&](auto count) {
+      constexpr int N = decltype(count)::value;
+      if (whole) {                                    // the whole segment: its output
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int r = rg * 8 + t4 * 2 + e;
           if (r >= P.group) continue;
           const int64_t row = static_cast<int64_t>(seg.b) * P.hq + head * P.group + r;
           const float inv = l[e] == 0.f ? 0.f : 1.f / l[e];
-          if (P.lse && g8 == 0) P.lse[row] = (m[e] + log2f(l[e])) * 0.6931471805599453f;
+          if (P.lse && g8 == 0 && base == 0) P.lse[row] = (m[e] + log2f(l[e])) * 0.6931471805599453f;
 #pragma unroll
-          for (int i = 0; i < KS; ++i)
+          for (int i = 0; i < N; ++i)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const int64_t at = row * D + i * 16 + h * 8 + g8;
+              const int64_t at = row * D + (base + i) * 16 + h * 8 + g8;
               const float x = o[i][e + 2 * h] * inv;
               if (P.out_fp32)
                 static_cast<float *>(P.out)[at] = x;
@@ -641,20 +680,36 @@ __global__ void __launch_bounds__(kThreads, 1)
       } else {
         const int slot = 2 * cta + (first_seg ? 0 : 1);
         const int64_t at = ((static_cast<int64_t>(slot) * P.heads_cta + hw) << rg_log) + rg;
-        if (g8 == 0) {
+        if (g8 == 0 && base == 0) {
           P.ml[at * 8 + t4 * 2] = make_float2(m[0], l[0]);
           P.ml[at * 8 + t4 * 2 + 1] = make_float2(m[1], l[1]);
         }
-        float4 *pp = reinterpret_cast<float4 *>(P.part) + at * KS * 32 + lane;
+        float4 *pp = reinterpret_cast<float4 *>(P.part) + (at * KS + base) * 32 + lane;
 #pragma unroll
-        for (int i = 0; i < KS; ++i) pp[i * 32] = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
-        if (threadIdx.x == 0 && seg.ts == 0) {
-          // this share starts the segment; the one that holds its last tile ends it
-          const int64_t end = u0 - cost + seg.first + seg.nt;      // unit behind the last tile, without the list's first cost
-          const int c_end = quotient(end * C + W - 1, W) - 1;
-          P.info[cta] = make_int4(seg.b, seg.g, c_end - cta + 1, slot);
-        }
+        for (int i = 0; i < N; ++i) pp[i * 32] = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
       }
+    };
+    if (wph == 1) {
+      write(std::integral_constant<int, KS>());
+    } else {
+      halve(std::integral_constant<int, KS / 2>(), wph / 2);
+      if (wph == 2) {
+        write(std::integral_constant<int, KS / 2>());
+      } else {
+        halve(std::integral_constant<int, KS / 4>(), wph / 4);
+        if (wph == 8) halve(std::integral_constant<int, KS / 8>(), 1);
+        // (D = 64: one m-tile each from here on)
+        if (wph == 4)
+          write(std::integral_constant<int, KS / 4>());
+        else if (mine_to_write)
+          write(std::integral_constant<int, KS / 8 ? KS / 8 : 1>());
+      }
+    }
+    if (threadIdx.x == 0 && seg.ts == 0 && !whole) {
+      // this share starts the segment; the one that holds its last tile ends it
+      const int64_t end = u0 - cost + seg.first + seg.nt;      // unit behind the last tile, without the list's first cost
+      const int c_end = quotient(end * C + W - 1, W) - 1;
+      P.info[cta] = make_int4(seg.b, seg.g, c_end - cta + 1, 2 * cta + (first_seg ? 0 : 1));
     }
     first_seg = 0;
     if (!go_on) break;
@@ -924,6 +979,7 @@ apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_
   std::memset(&P, 0, sizeof(P));
   P.pool = pool_view(cache, layer);
   P.seqlens = seqlens;
+  P.wide_lengths = (reinterpret_cast<uintptr_t>(seqlens) & 15) == 0;
   P.q = static_cast<const uint8_t *>(q);
   P.q_stride = q_token_stride;
   P.hq = num_q_heads;
