@@ -627,7 +627,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       constexpr int H = decltype(half)::value;        // 0: one m-tile each, which the lower of the two keeps
       constexpr int M = H ? H : 1;
       const bool upper = sub & bit;
-      const int other = warp ^ (bit * team);
+      const int other = upper ? warp - bit * team : warp + bit * team;   // (team is no power of two for 3 heads)
       float4 *give = reinterpret_cast<float4 *>(merge) + warp * (KS / 2) * 32 + lane;
       const float4 *take = reinterpret_cast<float4 *>(merge) + other * (KS / 2) * 32 + lane;
       team_barrier(hr, wph);                          // the last exchange's halves have been read

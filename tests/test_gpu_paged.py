@@ -308,6 +308,16 @@ def test_paged_attention(ap, lens, hq, hkv, dim, tokens, dtype, order, out_dtype
     check_attention(ap, rng, lens, hq, hkv, dim, tokens, dtype, order, out_dtype, layers=2, layer=1)
 
 
+@pytest.mark.parametrize("group", [1, 3, 9])
+@pytest.mark.parametrize("hkv", [1, 3, 5, 6, 7, 9, 12, 24])
+def test_paged_attention_head_counts(ap, hkv, group):
+    """Head counts that are no powers of two share a CTA's warps in other ways: what the warps of a head hold is summed
+    among them, whichever warps they are."""
+    rng = np.random.default_rng(100 * hkv + group)
+    check_attention(ap, rng, [5, 130, 0, 47, 700], group * hkv, hkv, 128, 16, "bf16", out_dtype="fp32")
+    check_attention(ap, rng, [60] * 20, group * hkv, hkv, 64, 5, "fp16")
+
+
 def test_paged_attention_of_many_sequences(ap):
     rng = np.random.default_rng(8)
     lens = [int(x) for x in rng.integers(0, 60, 300)]
