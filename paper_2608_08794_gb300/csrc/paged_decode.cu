@@ -10,8 +10,8 @@
 // Split over the cache's length.  The work is the list of all (sequence, head group, tile) in that order; every CTA
 // takes an equal contiguous share of it and finds its start from the lengths on the device, so that the launch does
 // not depend on them (a captured call follows growing caches).  Within a CTA a KV head has wph ring buffers of TMA
-// stages, each for every wph-th tile of the share; a ring is read by one warp, or with more than 8 query rows per KV
-// head by 2 or 4 warps of 8 rows each.  Its first warp refills a stage as soon as it has been used.  At the end of a
+// stages, each for every wph-th tile of the share; a ring is read by one warp of 8 or 16 query rows, or with more than 16
+// rows per KV head by 2 warps of 16.  Its first warp refills a stage as soon as it has been used.  At the end of a
 // (sequence, head group) the warps of a head merge through shared memory; what a share holds whole is written out,
 // what it holds in part goes to the workspace, and a second kernel merges those parts in order.
 //
@@ -59,7 +59,7 @@ struct PdPlan {
   int64_t q_stride;                  // bytes between sequences
   int32_t hq, group;                 // query heads, per KV head
   int32_t heads_cta, groups;         // KV heads of a CTA, head groups
-  int32_t wph_log, rg_log;           // log2 of the rings per head, and of the warps (groups of 8 query rows) per ring
+  int32_t wph_log, rg_log;           // log2 of the rings per head, and of the groups of 8 query rows
   int32_t box_tokens, boxes;         // tokens of one TMA box, boxes of a tile
   int32_t max_rows;
   int32_t wide_lengths;              // seqlens can be read four at a time
@@ -203,9 +203,12 @@ struct Walk {
   }
 };
 
-// SHARED: a ring has 2 or 4 warps (1 << rg_log); as a template, because the one-warp rings of most models are 1.5 %
-// faster without the other case's registers and branches.
-template <class T, int D, bool SHARED>
+// NG: groups of 8 query rows of a warp, which share its reads of K and V from shared memory.  SHARED: a ring is read by 2
+// warps; as templates, because the one-warp rings of most models are 1.5 % faster without the other case's registers and
+// branches.  60,000 tokens of 4 KV heads of 128: 29.4 us with 7 query heads each, 30.0 with 16, 34.3 with 24 or 32 (46.6
+// with 4 warps of one group per ring: every warp reads the whole tile, 4 times the traffic that fills it); 16 query heads
+// as 2 warps of one group each 30.0 too, 29.6 against 30.2 on 64 caches of 100 to 2,000 tokens: one variant less.
+template <class T, int D, int NG, bool SHARED>
 __global__ void __launch_bounds__(kThreads, 1)
     paged_chunk_kernel(const __grid_constant__ PdPlan P, const __grid_constant__ CUtensorMap kmap,
                        const __grid_constant__ CUtensorMap vmap) {
@@ -220,13 +223,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t *bars = reinterpret_cast<uint64_t *>(stat + kWarps * 8);       // full, then empty, of all stages
   int *window = reinterpret_cast<int *>(bars + 2 * kMaxStages);           // [warp][kWindow]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  // warp = (ring of the head, row group, head)
-  const int rg_log = SHARED ? P.rg_log : 0, wph = 1 << P.wph_log, readers = 1 << rg_log;
-  const int hw = warp % P.heads_cta, rg = SHARED ? (warp / P.heads_cta) & (readers - 1) : 0, sub = (warp / P.heads_cta) >> rg_log;
-  const int ring_id = sub * P.heads_cta + hw, stages = SHARED ? (kMaxStages / kWarps) << rg_log : kMaxStages / kWarps;
+  // warp = (ring of the head, reader of the ring, head)
+  constexpr int readers = SHARED ? 2 : 1;
+  const int wph = 1 << P.wph_log;
+  const int hw = warp % P.heads_cta, rd = SHARED ? (warp / P.heads_cta) & 1 : 0, sub = warp / P.heads_cta / readers;
+  const int ring_id = sub * P.heads_cta + hw, stages = kMaxStages / kWarps * readers;
   uint64_t *full = bars + ring_id * stages, *empty = full + kMaxStages;
   const uint32_t ring = smem_u32(smem) + ring_id * stages * kStageBytes;
-  if (sub < wph && rg == 0 && lane == 0) {
+  if (sub < wph && rd == 0 && lane == 0) {
     for (int i = 0; i < stages; ++i) {
       mbar_init(&full[i], 1);
       mbar_init(&empty[i], readers);
@@ -459,7 +463,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     ++issued;
   };
-  if (rg == 0)
+  if (rd == 0)
     for (int i = 0; i < stages; ++i) issue();
 
   // ---- consumer
@@ -470,15 +474,18 @@ __global__ void __launch_bounds__(kThreads, 1)
   bool dead = false;                                  // a wait gave up: no more loads are issued or waited for
   int first_seg = 1;
   // query fragments; the next segment's are loaded during this one
-  using QFrag = uint32_t[KS][2];
+  using QFrag = uint32_t[NG][KS][2];
   auto load_q = [&](const Walk<kTile> &w, QFrag &f) {
-    const int r = rg * 8 + g8;
-    const uint8_t *qb = P.q + w.b * P.q_stride + (static_cast<int64_t>(w.g * P.heads_cta + hw) * P.group + r) * D * 2;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
+    for (int ng = 0; ng < NG; ++ng) {
+      const int r = (rd * NG + ng) * 8 + g8;
+      const uint8_t *qb = P.q + w.b * P.q_stride + (static_cast<int64_t>(w.g * P.heads_cta + hw) * P.group + r) * D * 2;
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
-        f[ks][e] = r < P.group ? __ldg(reinterpret_cast<const uint32_t *>(qb + (ks * 16 + e * 8 + t4 * 2) * 2)) : 0u;
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          f[ng][ks][e] = r < P.group ? __ldg(reinterpret_cast<const uint32_t *>(qb + (ks * 16 + e * 8 + t4 * 2) * 2)) : 0u;
+    }
   };
   QFrag qf, q_next;
   load_q(seg, qf);
@@ -488,9 +495,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (go_on) load_q(after, q_next);
     const int head = seg.g * P.heads_cta + hw;
     // m: reference, log2 units; limit: of q.k, beyond which it grows; l and m of query rows 2 t4 and 2 t4 + 1
-    float o[KS][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, limit[2] = {-INFINITY, -INFINITY};
+    // (of each group of 8)
+    float o[NG][KS][4], m[NG][2], l[NG][2], limit[NG][2];
 #pragma unroll
-    for (int i = 0; i < KS; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+    for (int ng = 0; ng < NG; ++ng) {
+      m[ng][0] = m[ng][1] = limit[ng][0] = limit[ng][1] = -INFINITY;
+      l[ng][0] = l[ng][1] = 0.f;
+#pragma unroll
+      for (int i = 0; i < KS; ++i) o[ng][i][0] = o[ng][i][1] = o[ng][i][2] = o[ng][i][3] = 0.f;
+    }
     for (int t = seg.ts + sub; t < seg.te && !dead; t += wph) {
       if (!__all_sync(0xffffffffu, mbar_wait(&full[use_slot], use_phase, kWaitLimitNs))) {
         if (lane == 0) raise_device_error(P.err, APACK_ETIMEOUT, 83, cta, warp);
@@ -516,9 +529,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         fence_proxy_async_smem();                     // before TMA writes the slot again
         __syncwarp();
       }
-      float s[KM][4];
+      float s[NG][KM][4];
 #pragma unroll
-      for (int km = 0; km < KM; ++km) s[km][0] = s[km][1] = s[km][2] = s[km][3] = 0.f;
+      for (int ng = 0; ng < NG; ++ng)
+#pragma unroll
+        for (int km = 0; km < KM; ++km) s[ng][km][0] = s[ng][km][1] = s[ng][km][2] = s[ng][km][3] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
@@ -526,7 +541,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           uint32_t a[4];
           const uint32_t ch = ks * 2 + kchunk;
           ldmatrix4(kb + (ch >> 3) * kBlk + (km * 16 + krow) * 128 + (((ch & 7) ^ (krow & 7)) << 4), a);
-          Half16<T>::mma(s[km], a, qf[ks][0], qf[ks][1]);
+#pragma unroll
+          for (int ng = 0; ng < NG; ++ng) Half16<T>::mma(s[ng][km], a, qf[ng][ks][0], qf[ng][ks][1]);
         }
       // lane: keys g8 and g8 + 8 of 16, query rows 2 t4 and 2 t4 + 1
       if (valid < kTile)
@@ -534,51 +550,61 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int km = 0; km < KM; ++km)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (km * 16 + g8 + (i >> 1) * 8 >= valid) s[km][i] = -INFINITY;
-      // (a NaN logit leaves the maximum to the others, and its probability NaN)
-      float top[2];
+            if (km * 16 + g8 + (i >> 1) * 8 >= valid)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        top[e] = fmaxf(s[0][e], s[0][e + 2]);
-        if (KM > 1) top[e] = fmaxf(top[e], fmaxf(s[KM - 1][e], s[KM - 1][e + 2]));
-      }
-      if (__any_sync(0xffffffffu, !(top[0] <= limit[0] && top[1] <= limit[1]))) {
+              for (int ng = 0; ng < NG; ++ng) s[ng][km][i] = -INFINITY;
+      // (a NaN logit leaves the maximum to the others, and its probability NaN)
+      float top[NG][2];
+      bool grows = false;
+#pragma unroll
+      for (int ng = 0; ng < NG; ++ng)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float x = top[e];
-          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-          const float mn = fmaxf(m[e], fmaf(x, P.scale2, -Half16<T>::kShift));
-          const float f = mn == -INFINITY ? 1.f : ex2_approx(m[e] - mn);
-          m[e] = mn;
-          limit[e] = fmaxf(limit[e], x + P.grow);
-          l[e] *= f;
-#pragma unroll
-          for (int i = 0; i < KS; ++i) {
-            o[i][e] *= f;
-            o[i][e + 2] *= f;
-          }
+          top[ng][e] = fmaxf(s[ng][0][e], s[ng][0][e + 2]);
+          if (KM > 1) top[ng][e] = fmaxf(top[ng][e], fmaxf(s[ng][KM - 1][e], s[ng][KM - 1][e + 2]));
+          grows |= !(top[ng][e] <= limit[ng][e]);
         }
+      if (__any_sync(0xffffffffu, grows)) {
+#pragma unroll
+        for (int ng = 0; ng < NG; ++ng)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float x = top[ng][e];
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+            const float mn = fmaxf(m[ng][e], fmaf(x, P.scale2, -Half16<T>::kShift));
+            const float f = mn == -INFINITY ? 1.f : ex2_approx(m[ng][e] - mn);
+            m[ng][e] = mn;
+            limit[ng][e] = fmaxf(limit[ng][e], x + P.grow);
+            l[ng][e] *= f;
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+              o[ng][i][e] *= f;
+              o[ng][i][e + 2] *= f;
+            }
+          }
       }
       // P as the sum of two 16-bit numbers (2^-17 of it are left out in bf16, 2^-22 or 2^-36 of the largest in fp16; one
       // alone would cost 2^-9), transposed into B fragments
-      uint32_t hi[KM][2], lo[KM][2];
+      uint32_t hi[NG][KM][2], lo[NG][KM][2];
 #pragma unroll
-      for (int km = 0; km < KM; ++km) {
-        float p[4];
+      for (int ng = 0; ng < NG; ++ng)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = ex2_approx(fmaf(s[km][i], P.scale2, -m[i & 1]));
-        l[0] += p[0] + p[2];
-        l[1] += p[1] + p[3];
+        for (int km = 0; km < KM; ++km) {
+          float p[4];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint32_t h = Half16<T>::pack(p[2 * e], p[2 * e + 1]);
-          const float2 hf = Half16<T>::unpack(h);
-          hi[km][e] = transpose8x8(h);
-          lo[km][e] = transpose8x8(Half16<T>::pack(p[2 * e] - hf.x, p[2 * e + 1] - hf.y));
+          for (int i = 0; i < 4; ++i) p[i] = ex2_approx(fmaf(s[ng][km][i], P.scale2, -m[ng][i & 1]));
+          l[ng][0] += p[0] + p[2];
+          l[ng][1] += p[1] + p[3];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t h = Half16<T>::pack(p[2 * e], p[2 * e + 1]);
+            const float2 hf = Half16<T>::unpack(h);
+            hi[ng][km][e] = transpose8x8(h);
+            lo[ng][km][e] = transpose8x8(Half16<T>::pack(p[2 * e] - hf.x, p[2 * e + 1] - hf.y));
+          }
         }
-      }
 #pragma unroll
       for (int km = 0; km < KM; ++km)
 #pragma unroll
@@ -586,8 +612,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           uint32_t a[4];
           const uint32_t ch = i * 2 + vchunk;
           ldmatrix4_trans(vb + (ch >> 3) * kBlk + (km * 16 + vrow) * 128 + (((ch & 7) ^ (vrow & 7)) << 4), a);
-          Half16<T>::mma(o[i], a, hi[km][0], hi[km][1]);
-          Half16<T>::mma(o[i], a, lo[km][0], lo[km][1]);
+#pragma unroll
+          for (int ng = 0; ng < NG; ++ng) {
+            Half16<T>::mma(o[ng][i], a, hi[ng][km][0], hi[ng][km][1]);
+            Half16<T>::mma(o[ng][i], a, lo[ng][km][0], lo[ng][km][1]);
+          }
         }
       __syncwarp();                                   // every lane has read the stage
       if (!SHARED) {
@@ -595,7 +624,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       } else {
         if (lane == 0) mbar_arrive(&empty[slot]);
         // the stage before this one, which the ring's other warps have most likely left by now
-        if (rg == 0 && used >= 2 && (issued < queued || head_ok)) {
+        if (rd == 0 && used >= 2 && (issued < queued || head_ok)) {
           if (!__all_sync(0xffffffffu, mbar_wait(&empty[free_slot], free_phase, kWaitLimitNs))) {
             if (lane == 0) raise_device_error(P.err, APACK_ETIMEOUT, 84, cta, warp);
             dead = true;
@@ -610,112 +639,117 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
 
-    // ---- end of the segment: the warps of each head and row group merge
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      float x = l[e];
-      x += __shfl_xor_sync(0xffffffffu, x, 4);
-      x += __shfl_xor_sync(0xffffffffu, x, 8);
-      x += __shfl_xor_sync(0xffffffffu, x, 16);
-      l[e] = x;
-    }
-    // Pairs of them exchange halves of their m-tiles until each holds its own of the sums, o[0] on from m-tile `base`
-    const int hr = rg * P.heads_cta + hw, team = P.heads_cta << rg_log;   // warp = sub * team + hr
-    int base = 0;
-    bool mine_to_write = true;
-    auto halve = [&](auto half, int bit) {
-      constexpr int H = decltype(half)::value;        // 0: one m-tile each, which the lower of the two keeps
-      constexpr int M = H ? H : 1;
-      const bool upper = sub & bit;
-      const int other = upper ? warp - bit * team : warp + bit * team;   // (team is no power of two for 3 heads)
-      float4 *give = reinterpret_cast<float4 *>(merge) + warp * (KS / 2) * 32 + lane;
-      const float4 *take = reinterpret_cast<float4 *>(merge) + other * (KS / 2) * 32 + lane;
-      team_barrier(hr, wph);                          // the last exchange's halves have been read
-#pragma unroll
-      for (int i = 0; i < M; ++i) {
-        float(&x)[4] = o[i], (&y)[4] = o[i + H];
-        give[i * 32] = upper && H ? make_float4(x[0], x[1], x[2], x[3]) : make_float4(y[0], y[1], y[2], y[3]);
-        if (H)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) x[k] = upper ? y[k] : x[k];
-      }
-      if (g8 == 0) {
-        stat[warp * 8 + t4 * 2] = make_float2(m[0], l[0]);
-        stat[warp * 8 + t4 * 2 + 1] = make_float2(m[1], l[1]);
-      }
-      team_barrier(hr, wph);
-      float a[2], b[2];
+    // ---- end of the segment: the warps of each head and reader number merge, one group of 8 query rows after the other
+    const bool whole = seg.ts == 0 && seg.te == seg.nt;
+    auto merge_and_write = [&](float(&o)[KS][4], float(&m)[2], float(&l)[2], int rg) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float2 x = stat[other * 8 + t4 * 2 + e];
-        const float top = fmaxf(m[e], x.x);
-        a[e] = m[e] == top ? 1.f : ex2_approx(m[e] - top);
-        b[e] = x.x == top ? 1.f : ex2_approx(x.x - top);
-        l[e] = l[e] * a[e] + x.y * b[e];
-        m[e] = top;
+        float x = l[e];
+        x += __shfl_xor_sync(0xffffffffu, x, 4);
+        x += __shfl_xor_sync(0xffffffffu, x, 8);
+        x += __shfl_xor_sync(0xffffffffu, x, 16);
+        l[e] = x;
       }
+      // Pairs of them exchange halves of their m-tiles until each holds its own of the sums, o[0] on from m-tile `base`
+      const int hr = rd * P.heads_cta + hw, team = P.heads_cta * readers;   // warp = sub * team + hr
+      int base = 0;
+      bool mine_to_write = true;
+      auto halve = [&](auto half, int bit) {
+        constexpr int H = decltype(half)::value;        // 0: one m-tile each, which the lower of the two keeps
+        constexpr int M = H ? H : 1;
+        const bool upper = sub & bit;
+        const int other = upper ? warp - bit * team : warp + bit * team;   // (team is no power of two for 3 heads)
+        float4 *give = reinterpret_cast<float4 *>(merge) + warp * (KS / 2) * 32 + lane;
+        const float4 *take = reinterpret_cast<float4 *>(merge) + other * (KS / 2) * 32 + lane;
+        team_barrier(hr, wph);                          // the last exchange's halves have been read
 #pragma unroll
-      for (int i = 0; i < M; ++i) {
-        const float4 x = take[i * 32];
-        o[i][0] = o[i][0] * a[0] + x.x * b[0];
-        o[i][1] = o[i][1] * a[1] + x.y * b[1];
-        o[i][2] = o[i][2] * a[0] + x.z * b[0];
-        o[i][3] = o[i][3] * a[1] + x.w * b[1];
-      }
-      if (upper) base += H;
-      if (H == 0) mine_to_write = !upper;
-    };
-    const bool whole = seg.ts == 0 && seg.te == seg.nt;
-    auto write = [&](auto count) {
-      constexpr int N = decltype(count)::value;
-      if (whole) {                                    // the whole segment: its output
+        for (int i = 0; i < M; ++i) {
+          float(&x)[4] = o[i], (&y)[4] = o[i + H];
+          give[i * 32] = upper && H ? make_float4(x[0], x[1], x[2], x[3]) : make_float4(y[0], y[1], y[2], y[3]);
+          if (H)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[k] = upper ? y[k] : x[k];
+        }
+        if (g8 == 0) {
+          stat[warp * 8 + t4 * 2] = make_float2(m[0], l[0]);
+          stat[warp * 8 + t4 * 2 + 1] = make_float2(m[1], l[1]);
+        }
+        team_barrier(hr, wph);
+        float a[2], b[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const int r = rg * 8 + t4 * 2 + e;
-          if (r >= P.group) continue;
-          const int64_t row = static_cast<int64_t>(seg.b) * P.hq + head * P.group + r;
-          const float inv = l[e] == 0.f ? 0.f : 1.f / l[e];
-          if (P.lse && g8 == 0 && base == 0) P.lse[row] = (m[e] + log2f(l[e])) * 0.6931471805599453f;
-#pragma unroll
-          for (int i = 0; i < N; ++i)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const int64_t at = row * D + (base + i) * 16 + h * 8 + g8;
-              const float x = o[i][e + 2 * h] * inv;
-              if (P.out_fp32)
-                static_cast<float *>(P.out)[at] = x;
-              else
-                static_cast<T *>(P.out)[at] = static_cast<T>(x);
-            }
+          const float2 x = stat[other * 8 + t4 * 2 + e];
+          const float top = fmaxf(m[e], x.x);
+          a[e] = m[e] == top ? 1.f : ex2_approx(m[e] - top);
+          b[e] = x.x == top ? 1.f : ex2_approx(x.x - top);
+          l[e] = l[e] * a[e] + x.y * b[e];
+          m[e] = top;
         }
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+          const float4 x = take[i * 32];
+          o[i][0] = o[i][0] * a[0] + x.x * b[0];
+          o[i][1] = o[i][1] * a[1] + x.y * b[1];
+          o[i][2] = o[i][2] * a[0] + x.z * b[0];
+          o[i][3] = o[i][3] * a[1] + x.w * b[1];
+        }
+        if (upper) base += H;
+        if (H == 0) mine_to_write = !upper;
+      };
+      auto write = [&](auto count) {
+        constexpr int N = decltype(count)::value;
+        if (whole) {                                    // the whole segment: its output
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int r = rg * 8 + t4 * 2 + e;
+            if (r >= P.group) continue;
+            const int64_t row = static_cast<int64_t>(seg.b) * P.hq + head * P.group + r;
+            const float inv = l[e] == 0.f ? 0.f : 1.f / l[e];
+            if (P.lse && g8 == 0 && base == 0) P.lse[row] = (m[e] + log2f(l[e])) * 0.6931471805599453f;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const int64_t at = row * D + (base + i) * 16 + h * 8 + g8;
+                const float x = o[i][e + 2 * h] * inv;
+                if (P.out_fp32)
+                  static_cast<float *>(P.out)[at] = x;
+                else
+                  static_cast<T *>(P.out)[at] = static_cast<T>(x);
+              }
+          }
+        } else {
+          const int slot = 2 * cta + (first_seg ? 0 : 1);
+          const int64_t at = ((static_cast<int64_t>(slot) * P.heads_cta + hw) << P.rg_log) + rg;
+          if (g8 == 0 && base == 0) {
+            P.ml[at * 8 + t4 * 2] = make_float2(m[0], l[0]);
+            P.ml[at * 8 + t4 * 2 + 1] = make_float2(m[1], l[1]);
+          }
+          float4 *pp = reinterpret_cast<float4 *>(P.part) + (at * KS + base) * 32 + lane;
+#pragma unroll
+          for (int i = 0; i < N; ++i) pp[i * 32] = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
+        }
+      };
+      if (wph == 1) {
+        write(std::integral_constant<int, KS>());
       } else {
-        const int slot = 2 * cta + (first_seg ? 0 : 1);
-        const int64_t at = ((static_cast<int64_t>(slot) * P.heads_cta + hw) << rg_log) + rg;
-        if (g8 == 0 && base == 0) {
-          P.ml[at * 8 + t4 * 2] = make_float2(m[0], l[0]);
-          P.ml[at * 8 + t4 * 2 + 1] = make_float2(m[1], l[1]);
+        halve(std::integral_constant<int, KS / 2>(), wph / 2);
+        if (wph == 2) {
+          write(std::integral_constant<int, KS / 2>());
+        } else {
+          halve(std::integral_constant<int, KS / 4>(), wph / 4);
+          if (wph == 8) halve(std::integral_constant<int, KS / 8>(), 1);
+          // (D = 64: one m-tile each from here on)
+          if (wph == 4)
+            write(std::integral_constant<int, KS / 4>());
+          else if (mine_to_write)
+            write(std::integral_constant<int, KS / 8 ? KS / 8 : 1>());
         }
-        float4 *pp = reinterpret_cast<float4 *>(P.part) + (at * KS + base) * 32 + lane;
-#pragma unroll
-        for (int i = 0; i < N; ++i) pp[i * 32] = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
       }
     };
-    if (wph == 1) {
-      write(std::integral_constant<int, KS>());
-    } else {
-      halve(std::integral_constant<int, KS / 2>(), wph / 2);
-      if (wph == 2) {
-        write(std::integral_constant<int, KS / 2>());
-      } else {
-        halve(std::integral_constant<int, KS / 4>(), wph / 4);
-        if (wph == 8) halve(std::integral_constant<int, KS / 8>(), 1);
-        // (D = 64: one m-tile each from here on)
-        if (wph == 4)
-          write(std::integral_constant<int, KS / 4>());
-        else if (mine_to_write)
-          write(std::integral_constant<int, KS / 8 ? KS / 8 : 1>());
-      }
-    }
+#pragma unroll
+    for (int ng = 0; ng < NG; ++ng)
+      if ((rd * NG + ng) * 8 < P.group) merge_and_write(o[ng], m[ng], l[ng], rd * NG + ng);
     if (threadIdx.x == 0 && seg.ts == 0 && !whole) {
       // this share starts the segment; the one that holds its last tile ends it
       const int64_t end = u0 - cost + seg.first + seg.nt;      // unit behind the last tile, without the list's first cost
@@ -726,10 +760,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (!go_on) break;
     seg = after;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      qf[ks][0] = q_next[ks][0];
-      qf[ks][1] = q_next[ks][1];
-    }
+    for (int ng = 0; ng < NG; ++ng)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        qf[ng][ks][0] = q_next[ng][ks][0];
+        qf[ng][ks][1] = q_next[ng][ks][1];
+      }
   }
   if (dead)   // loads of the stages that were issued and not used may still be in flight
     for (int k = used; k < issued; ++k) mbar_wait(&full[k % stages], (k / stages) & 1u, kWaitLimitNs / 4);
@@ -908,12 +944,13 @@ apack_status plan_shape(const apack_paged_cache *c, int32_t hq, PdShape *s) {
   s->group = hq / c->num_kv_heads;
   if (s->group > 32) return APACK_EUNSUPPORTED;
   s->rg_log = s->group > 16 ? 2 : s->group > 8 ? 1 : 0;
+  const int readers_log = s->rg_log > 1;
   // KV heads of a CTA: the largest divisor of their number that its warps cover; the other warps split the tiles
   s->heads_cta = 1;
-  for (int h = 1; h <= kWarps >> s->rg_log; ++h)
+  for (int h = 1; h <= kWarps >> readers_log; ++h)
     if (c->num_kv_heads % h == 0) s->heads_cta = h;
   s->wph_log = 0;
-  while ((s->heads_cta << (s->rg_log + s->wph_log + 1)) <= kWarps) ++s->wph_log;
+  while ((s->heads_cta << (readers_log + s->wph_log + 1)) <= kWarps) ++s->wph_log;
   s->groups = c->num_kv_heads / s->heads_cta;
   s->grid = std::min(device_sm_count(), kMaxGrid);
   auto up = [](size_t x) { return (x + 255) & ~static_cast<size_t>(255); };
@@ -928,22 +965,23 @@ apack_status plan_shape(const apack_paged_cache *c, int32_t hq, PdShape *s) {
 constexpr size_t kSmem = kStageBytesCta + kMergeFloats * sizeof(float) + kWarps * 8 * sizeof(float2) +
                          2 * kMaxStages * sizeof(uint64_t) + kWarps * kWindow * sizeof(int);
 
-template <class T, int D, bool SHARED>
+template <class T, int D, int NG, bool SHARED>
 cudaError_t launch_chunk(const PdPlan &P, const CUtensorMap &kmap, const CUtensorMap &vmap, int grid, cudaStream_t stream) {
   static std::atomic<uint64_t> attr{0};
   const cudaError_t e = once_per_device(attr, [] {
-    return cudaFuncSetAttribute(paged_chunk_kernel<T, D, SHARED>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    return cudaFuncSetAttribute(paged_chunk_kernel<T, D, NG, SHARED>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 static_cast<int>(kSmem));
   });
   if (e != cudaSuccess) return e;
-  return launch_pdl(paged_chunk_kernel<T, D, SHARED>, dim3(grid), dim3(kThreads), kSmem, stream, P, kmap, vmap);
+  return launch_pdl(paged_chunk_kernel<T, D, NG, SHARED>, dim3(grid), dim3(kThreads), kSmem, stream, P, kmap, vmap);
 }
 
 template <class T, int D>
 cudaError_t launch_paged(const PdPlan &P, const CUtensorMap &kmap, const CUtensorMap &vmap, int grid,
                          cudaStream_t stream) {
-  cudaError_t e = P.rg_log ? launch_chunk<T, D, true>(P, kmap, vmap, grid, stream)
-                           : launch_chunk<T, D, false>(P, kmap, vmap, grid, stream);
+  cudaError_t e = P.rg_log == 0   ? launch_chunk<T, D, 1, false>(P, kmap, vmap, grid, stream)
+                  : P.rg_log == 1 ? launch_chunk<T, D, 2, false>(P, kmap, vmap, grid, stream)
+                                  : launch_chunk<T, D, 2, true>(P, kmap, vmap, grid, stream);
   if (e != cudaSuccess) return e;
   count_launches(1);
   e = launch_pdl(paged_combine_kernel<T, D>, dim3(grid), dim3(32 * kCombineWarps), 0, stream, P, grid);
