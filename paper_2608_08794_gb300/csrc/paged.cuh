@@ -27,8 +27,19 @@ struct PoolView {
   int32_t num_pages, num_seqs, max_pages;
   FastDiv page_tokens;
 
-  // Byte offset of row `row` of sequence `seq` within a layer (head 0), or -1: a negative row, a row
-  // behind the table or a page outside the pool.
+  // The page of row `row` of sequence `seq`, or -1: a negative row, or one behind the table.
+  __device__ __forceinline__ int32_t page_of(uint32_t seq, int32_t row) const {
+    if (row < 0) return -1;
+    const uint32_t p = page_tokens.div(static_cast<uint32_t>(row));
+    return p < static_cast<uint32_t>(max_pages) ? __ldg(table + static_cast<int64_t>(seq) * table_stride + p) : -1;
+  }
+  // Byte offset of the row in that page within a layer (head 0), or -1: a page outside the pool.
+  __device__ __forceinline__ int64_t offset_in(int32_t page, int32_t row) const {
+    if (static_cast<uint32_t>(page) >= static_cast<uint32_t>(num_pages)) return -1;
+    const uint32_t r = static_cast<uint32_t>(row);
+    return page * page_stride + static_cast<int64_t>(r - page_tokens.div(r) * page_tokens.d) * token_stride;
+  }
+  // Both in one (with one division), or -1.
   __device__ __forceinline__ int64_t row_offset(uint32_t seq, int32_t row) const {
     if (row < 0) return -1;
     const uint32_t p = page_tokens.div(static_cast<uint32_t>(row));

@@ -11,6 +11,7 @@
 #include <cstring>
 
 #include "paged.cuh"
+#include "ptx.cuh"
 
 namespace apack {
 namespace {
@@ -133,17 +134,22 @@ __global__ void __launch_bounds__(kMoveThreads, 4) move_rows_kernel(const __grid
 }
 
 // In place: output row j of a sequence reads row from(j) >= j of the same sequence, from ascending.  A warp owns
-// W 16-byte pieces of every row of one plane of one sequence and walks the rows upwards, kStep at a time; the rows a step
-// reads are loaded whole before it writes, and no later step reads a row below those this step writes.  So no
-// warp waits for another.  A step costs one trip to memory: the addresses of the next one are found meanwhile, from
-// indices read two steps ahead.  24 layers of 27,144 rows to 11,844: 2300 us with addresses found in the step and 32
-// rows in each.
-constexpr int kStep = 64;
+// W 16-byte pieces of every row of one plane of one sequence and walks the rows upwards, kStep at a time; the rows that a
+// step reads have all arrived before it writes, and no later step reads a row below those this step writes.  So no
+// warp waits for another, and the loads of kDepth steps are in flight (into the warp's ring in shared memory); addresses
+// are found a step before their loads, from page numbers read two and indices read three steps before.  A step costs
+// about one trip to L2 for those.  24 layers of 27,144 rows to 11,844, 4 heads of 128: 275 us, 4.2 TB/s (514 with
+// the loads of one step of 64 rows in registers; here 306 with 64 rows, 267 with 3 steps of 128, which lose on batches);
+// 8 caches of 9,000 rows, half of them kept: 589 us, 6.0 TB/s (989 before, 706 with 3 steps).
+constexpr int kStep = 128, kDepth = 2, kPlaceWarps = 2;
+constexpr int place_bytes(int w) { return kPlaceWarps * kDepth * kStep * (w * 16 + 8); }
 template <int W>
-__global__ void __launch_bounds__(128) move_in_place_kernel(const __grid_constant__ MovePlan P, int segs, int64_t units) {
+__global__ void __launch_bounds__(32 * kPlaceWarps)
+    move_in_place_kernel(const __grid_constant__ MovePlan P, int segs, int64_t units) {
+  extern __shared__ __align__(16) uint8_t place_smem[];
   pdl_wait_and_release();
-  const int lane = threadIdx.x & 31;
-  const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * kPlaceWarps + warp;
   if (unit >= units) return;
   const int seg = static_cast<int>(unit % segs);
   const int64_t rest = unit / segs;
@@ -152,25 +158,37 @@ __global__ void __launch_bounds__(128) move_in_place_kernel(const __grid_constan
   const uint8_t *src;
   uint8_t *dst;
   plane_bases(P, plane, &src, &dst);
-  constexpr int kRowsAtOnce = 32 / W, kLoads = kStep / kRowsAtOnce;
+  constexpr int kRowsAtOnce = 32 / W, kLoads = kStep / kRowsAtOnce, kRows = kStep / 32;
   const int c = seg * W + lane % W;
   const bool mine = c < P.pieces;
   const int32_t base = P.cu_src ? __ldg(P.cu_src + b) : 0;
-  // lane i finds the addresses of rows i and i + 32 of a step
-  int32_t keep[2];
-  int64_t from[2], to[2];
+  uint4 *ring = reinterpret_cast<uint4 *>(place_smem) + warp * kDepth * kStep * W;
+  int64_t *ring_to = reinterpret_cast<int64_t *>(place_smem + kPlaceWarps * kDepth * kStep * W * 16) + warp * kDepth * kStep;
+  // lane i finds the addresses of rows i, i + 32, ... of a step: its index, the pages of both rows, the offsets
+  int32_t keep[kRows], row[kRows], from_page[kRows], to_page[kRows];
+  int64_t from[kRows], to[kRows];
   auto read_keep = [&](int64_t j) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < kRows; ++h)
       if (j + h * 32 + lane < j1) keep[h] = __ldg(P.keep_idx + j + h * 32 + lane);
+  };
+  auto read_pages = [&](int64_t j) {
+#pragma unroll
+    for (int h = 0; h < kRows; ++h) {
+      const int64_t r = j + h * 32 + lane;
+      if (r >= j1) continue;
+      row[h] = keep[h] - base;
+      from_page[h] = P.src.page_of(b, row[h]);
+      to_page[h] = P.dst.page_of(b, static_cast<int32_t>(r - j0));
+    }
   };
   auto find = [&](int64_t j) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < kRows; ++h) {
       const int64_t r = j + h * 32 + lane;
       from[h] = to[h] = -1;
       if (r >= j1) continue;
-      const int64_t s = P.src.row_offset(b, keep[h] - base), d = P.dst.row_offset(b, static_cast<int32_t>(r - j0));
+      const int64_t s = P.src.offset_in(from_page[h], row[h]), d = P.dst.offset_in(to_page[h], static_cast<int32_t>(r - j0));
       if (s >= 0 && d >= 0) {
         from[h] = s;
         to[h] = d;
@@ -179,27 +197,57 @@ __global__ void __launch_bounds__(128) move_in_place_kernel(const __grid_constan
       }
     }
   };
-  read_keep(j0);
-  find(j0);
-  read_keep(j0 + kStep);
-  for (int64_t j = j0; j < j1; j += kStep) {
-    uint4 x[kLoads];
-    int64_t at[2] = {to[0], to[1]};                    // of this step, in the lanes that found them
+  // a lane writes what it has loaded itself
+  auto load = [&](int slot) {
+#pragma unroll
+    for (int h = 0; h < kRows; ++h) ring_to[slot * kStep + h * 32 + lane] = to[h];
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) {
       const int64_t s = __shfl_sync(0xffffffffu, from[u / W], u % W * kRowsAtOnce + lane / W);
-      if (s >= 0 && mine) x[u] = *reinterpret_cast<const uint4 *>(src + s + c * 16);
+      if (s >= 0 && mine) cp_async_16(smem_u32(ring + (slot * kLoads + u) * 32 + lane), src + s + c * 16);
     }
-    find(j + kStep);
-    read_keep(j + 2 * kStep);
+    cp_async_commit();
+  };
+  int64_t ahead = j0;                                  // the step that is loaded next
+  read_keep(ahead);
+  read_pages(ahead);
+  read_keep(ahead + kStep);
+  find(ahead);
+  read_pages(ahead + kStep);
+  read_keep(ahead + 2 * kStep);
+  auto advance = [&](int slot) {
+    load(slot);
+    ahead += kStep;
+    find(ahead);
+    read_pages(ahead + kStep);
+    read_keep(ahead + 2 * kStep);
+  };
+#pragma unroll
+  for (int slot = 0; slot < kDepth; ++slot) advance(slot);
+  int slot = 0;
+  for (int64_t j = j0; j < j1; j += kStep) {
+    cp_async_wait<kDepth - 1>();
     __syncwarp();                                      // every row of the step has been read
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) {
-      const int64_t d = __shfl_sync(0xffffffffu, at[u / W], u % W * kRowsAtOnce + lane / W);
-      if (d >= 0 && mine) *reinterpret_cast<uint4 *>(dst + d + c * 16) = x[u];
+      const int64_t d = ring_to[slot * kStep + u * kRowsAtOnce + lane / W];
+      if (d >= 0 && mine) *reinterpret_cast<uint4 *>(dst + d + c * 16) = ring[(slot * kLoads + u) * 32 + lane];
     }
     __syncwarp();
+    advance(slot);
+    slot = slot + 1 == kDepth ? 0 : slot + 1;
   }
+  cp_async_wait<0>();
+}
+
+template <int W>
+cudaError_t launch_in_place(const MovePlan &P, int segs, int64_t units, unsigned grid, cudaStream_t stream) {
+  static std::atomic<uint64_t> attr{0};
+  const cudaError_t e = once_per_device(attr, [] {
+    return cudaFuncSetAttribute(move_in_place_kernel<W>, cudaFuncAttributeMaxDynamicSharedMemorySize, place_bytes(W));
+  });
+  if (e != cudaSuccess) return e;
+  return launch_pdl(move_in_place_kernel<W>, dim3(grid), dim3(32 * kPlaceWarps), place_bytes(W), stream, P, segs, units);
 }
 
 // Heads of a token back to back: one plane per layer and tensor.
@@ -214,14 +262,18 @@ apack_status launch_move(MovePlan &P, const apack_paged_cache *a, const apack_pa
   P.piece_div = fast_div(P.pieces);
   P.planes = 2 * layers * P.heads;
   if (in_place) {
-    // 128 bytes of a row per warp; fewer where that leaves SMs with less than 8 warps (a warp's pace is its latency)
+    // 128 bytes of a row per warp; fewer where that leaves SMs with less than 4 warps (the prompt's prune 292 us with 2,
+    // 278 with 4; with 8, and so 32 bytes, no more)
     int w = 8;
-    auto units_of = [&](int width) { return static_cast<int64_t>(P.num_seqs) * P.planes * ((P.pieces + width - 1) / width); };
-    while (w > 2 && units_of(w) < 8 * static_cast<int64_t>(device_sm_count())) w /= 2;
-    const int64_t units = units_of(w), grid = (units + 3) / 4;
+    auto segs = [&](int width) { return (P.pieces + width - 1) / width; };
+    auto units_of = [&](int width) { return static_cast<int64_t>(P.num_seqs) * P.planes * segs(width); };
+    while (w > 2 && units_of(w) < 4 * static_cast<int64_t>(device_sm_count())) w /= 2;
+    const int64_t units = units_of(w), grid = (units + kPlaceWarps - 1) / kPlaceWarps;
     if (grid > INT32_MAX) return APACK_EUNSUPPORTED;
-    auto *kernel = w == 8 ? move_in_place_kernel<8> : w == 4 ? move_in_place_kernel<4> : move_in_place_kernel<2>;
-    if (check_cuda(launch_pdl(kernel, dim3(static_cast<unsigned>(grid)), dim3(128), 0, stream, P, (P.pieces + w - 1) / w, units)) != APACK_OK)
+    const unsigned g = static_cast<unsigned>(grid);
+    if (check_cuda(w == 8   ? launch_in_place<8>(P, segs(8), units, g, stream)
+                   : w == 4 ? launch_in_place<4>(P, segs(4), units, g, stream)
+                            : launch_in_place<2>(P, segs(2), units, g, stream)) != APACK_OK)
       return APACK_ECUDA;
     count_launches(1);
     return APACK_OK;

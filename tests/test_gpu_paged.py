@@ -496,6 +496,17 @@ def test_paged_compact(ap, lens, heads, dim, dtype, src, dst, indexed):
 ])
 @pytest.mark.parametrize("ratio", [0.02, 0.5, 0.97, 1.0])
 def test_paged_compact_in_place(ap, lens, heads, dim, tokens, order, ratio):
+    check_in_place(ap, lens, heads, dim, tokens, order, ratio)
+
+
+def test_paged_compact_in_place_of_batches(ap):
+    """Batches large enough for 64 and 128 bytes of a row per warp, sequences of several steps."""
+    check_in_place(ap, [400, 270] * 20, 4, 128, 16, "nhd", 0.9)
+    check_in_place(ap, [300, 1000] * 10, 4, 128, 16, "nhd", 0.6)
+    check_in_place(ap, [500] * 22, 5, 64, 7, "hnd", 0.95)
+
+
+def check_in_place(ap, lens, heads, dim, tokens, order, ratio):
     rng = np.random.default_rng(sum(lens) + heads)
     kept = [int(round(n * ratio)) for n in lens]
     cu_src, cu_dst = (np.concatenate([[0], np.cumsum(x)]) for x in (lens, kept))
