@@ -471,7 +471,7 @@ apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_
    and strides may differ.  Slots of dst that no j names keep what they hold.
    Out of place (another pool, other pages of the same one by another table, or other layers), no page that is
    written may be read by the same call.  In place: src and dst name the same pool, table and layers; keep_idx is
-   then given and ascending within each sequence, and each sequence's pages are its own; rows move towards the
+   then given and strictly ascending within each sequence, and each sequence's pages are its own; rows move towards the
    front of their sequence.
    ws: NULL, or a workspace whose error word receives APACK_EDEVICE when a row lies behind a page table or a
    page number outside its pool; such a row is not copied, with or without ws. */
