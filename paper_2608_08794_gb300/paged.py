@@ -7,7 +7,7 @@ and ``apack_paged_compact`` where pages have to move.  A fork shares its parent'
 copied when a sequence first writes behind its last row.
 
 All device work is queued on torch's current stream; a pool's calls belong on one stream (a page that is freed
-may be handed out again by the next call).  Every method checks that it can be carried out (pages, rows) before
+may be handed out again by the next call) and are not captured (a graph reads the tables that they change).  Every method checks that it can be carried out (pages, rows) before
 it changes anything.
 """
 
@@ -38,7 +38,8 @@ class PagePool:
         self._refs = np.zeros(num_pages, np.int64)
         self._free = list(range(num_pages - 1, -1, -1))
         self._pages = [None] * max_seqs          # page list of a sequence, None where the row is unused
-        self._len = np.zeros(max_seqs, np.int64)
+        self._len = np.zeros(max_seqs, np.int64)  # ceil(length / page_tokens) pages are held
+        self._shared = 0                         # sum over the pages of the holders beyond the first
 
     # ------------------------------------------------------------ host state
 
@@ -78,25 +79,42 @@ class PagePool:
         return got
 
     def _drop(self, pages):
-        for p in pages:
-            self._refs[p] -= 1
-            if self._refs[p] == 0:
-                self._free.append(p)
+        at = np.asarray(pages, np.int64)         # distinct
+        self._refs[at] -= 1
+        gone = at[self._refs[at] == 0]
+        self._free += gone.tolist()
+        self._shared -= len(at) - len(gone)
+
+    def _device(self, values):
+        """An array on the device, without waiting for the stream: through pinned memory, which torch does not hand
+        out again before it has been read."""
+        host = torch.from_numpy(values)
+        return (host.pin_memory() if self.k.is_cuda else host).to(self.device, non_blocking=True)
+
+    def _write(self, at, length, entries, more=(), clear=False):
+        """Lengths of the sequences `at` and, pairs of (place in the flat table, page), their entries, on the device;
+        returns `more` there.  One copy for all of them.  clear: -1 in all other entries of the sequences."""
+        n, m = len(at), len(entries)
+        both = np.array(entries, np.int64).reshape(m, 2)
+        wide = self._device(np.concatenate([at, both[:, 0], length, both[:, 1], more]).astype(np.int64))
+        narrow = wide[n + m:].to(torch.int32)
+        if n:
+            self.lengths.index_copy_(0, wide[:n], narrow[:n])
+        if clear:
+            self.page_table.index_fill_(0, wide[:n], -1)
+        if m:
+            self.page_table.view(-1).index_copy_(0, wide[n:n + m], narrow[n:n + m])
+        return narrow[n + m:]
 
     def _upload(self, seqs):
-        """The rows of these sequences in the device's tables."""
+        """The rows of these sequences in the device's tables, whole."""
         if not len(seqs):
             return
-        table = np.full((len(seqs), self.max_pages), -1, np.int32)
-        for i, s in enumerate(seqs):
-            pages = self._pages[s] or []
-            table[i, :len(pages)] = pages
-        at = torch.tensor(list(seqs), dtype=torch.int64, device=self.device)
-        self.page_table.index_copy_(0, at, torch.from_numpy(table).to(self.device))
-        self.lengths.index_copy_(0, at, torch.tensor([int(self._len[s]) for s in seqs], dtype=torch.int32, device=self.device))
+        self._write(np.asarray(seqs), self._len[list(seqs)],
+                    [(s * self.max_pages + i, p) for s in seqs for i, p in enumerate(self._pages[s])], clear=True)
 
     def _ints(self, values):
-        return torch.tensor(np.asarray(values, np.int32), device=self.device)
+        return self._device(np.asarray(values, np.int32))
 
     # ------------------------------------------------------------ sequences
 
@@ -113,8 +131,10 @@ class PagePool:
         pages = self._held(seq)
         new, = self._room(0, 1)
         self._refs[pages] += 1
+        self._shared += len(pages)
         self._pages[new], self._len[new] = list(pages), self._len[seq]
-        self._upload([new])
+        self.page_table[new].copy_(self.page_table[seq])
+        self.lengths[new].copy_(self.lengths[seq])
         return new
 
     def extend(self, seqs, rows=1):
@@ -122,41 +142,44 @@ class PagePool:
         them.  Returns the first new row of each (int32, on the device)."""
         if rows < 0 or len(set(seqs)) != len(seqs):
             raise ValueError("rows >= 0 and distinct sequences expected")
-        copied, wanted, shared = set(), 0, dict()
-        for s in seqs:
-            held, used = self._held(s), int(self._len[s])
-            wanted += self._need(used + rows) - len(held)
-            if rows and used % self.page_tokens:
-                last = held[used // self.page_tokens]
+        held = [self._held(s) for s in seqs]
+        used = self._len[list(seqs)]
+        total = used + rows
+        if len(seqs):
+            self._need(total.max())
+        grow = -(-total // self.page_tokens) + -used // self.page_tokens
+        copied, left = [], {}
+        if rows and self._shared:
+            for i in np.flatnonzero(used % self.page_tokens):
+                last = held[i][-1]
                 # of the sequences that share it, all but the last holder need a copy
-                left = shared.get(last, int(self._refs[last]))
-                if left > 1:
-                    copied.add(s)
-                    wanted += 1
-                    shared[last] = left - 1
-        self._room(wanted)
-        pairs, first = [], []
-        for s in seqs:
-            held, used = self._pages[s], int(self._len[s])
-            if s in copied:
-                i = used // self.page_tokens
-                own, = self._take(1)
-                pairs.append((held[i], own))
-                self._drop([held[i]])
-                held[i] = own
-            held += self._take(self._need(used + rows) - len(held))
-            first.append(used)
-            self._len[s] = used + rows
+                left.setdefault(last, self._refs[last])
+                if left[last] > 1:
+                    left[last] -= 1
+                    copied.append(i)
+        self._room(int(grow.sum()) + len(copied))
+        pairs, entries = [], []
+        for i in copied:
+            own, = self._take(1)
+            pairs.append((held[i][-1], own))
+            self._drop(held[i][-1:])
+            held[i][-1] = own
+            entries.append((seqs[i] * self.max_pages + len(held[i]) - 1, own))
+        for i in np.flatnonzero(grow):
+            new = self._take(grow[i])
+            entries += [(seqs[i] * self.max_pages + len(held[i]) + j, p) for j, p in enumerate(new)]
+            held[i] += new
+        self._len[list(seqs)] = total
         if pairs:
             apack_copy_pages(self.cache, self._ints(pairs))
-        self._upload(seqs)
-        return self._ints(first)
+        return self._write(np.asarray(seqs, np.int64), total, entries, used)
 
     def free(self, seq):
         """Gives up a sequence; pages that no other one shares become free."""
         self._drop(self._held(seq))
         self._pages[seq], self._len[seq] = None, 0
-        self._upload([seq])
+        self.page_table[seq].fill_(-1)
+        self.lengths[seq].fill_(0)
 
     # ------------------------------------------------------------ pruning
 

@@ -152,3 +152,32 @@ def test_refusals_change_nothing(pools):
         pool.free(b)
     pool.free(a)
     assert pool.free_pages == 3 and int(pool.lengths.sum()) == 0 and int(pool.page_table.max()) == -1
+
+
+def test_device_tables_follow_the_host(pools):
+    """After every call the device's table holds a sequence's pages and -1 behind them, and its length."""
+    pool = make(pools)
+
+    def check():
+        for s, pages in enumerate(pool._pages):
+            pages = pages or []
+            assert pool.page_table[s].tolist() == pages + [-1] * (pool.max_pages - len(pages))
+        assert pool.lengths.tolist() == pool._len.tolist() and pool.lengths.dtype == torch.int32
+
+    a, b = pool.add(9), pool.add(0)
+    check()
+    c = pool.fork(a)
+    check()
+    assert pool.extend([]).tolist() == []
+    assert pool.extend((c, b, a), 11).tolist() == [9, 0, 9]       # a copy, new pages of three sequences
+    check()
+    assert pool.extend(np.array([b]), 0).tolist() == [11]
+    pool.prune([a, b], torch.arange(31, dtype=torch.int32)[[0, 19, 20, 30]], [2, 2])
+    check()
+    pool.prune([c], torch.tensor([3, 4], dtype=torch.int32), [2], in_place=True)
+    check()
+    pool.free(a)
+    pool.free(b)
+    pool.free(c)
+    check()
+    assert pool.free_pages == 40 and pool._shared == 0
