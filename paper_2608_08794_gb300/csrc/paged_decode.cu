@@ -1023,6 +1023,9 @@ apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_
       (reinterpret_cast<uintptr_t>(out) & 15) || (reinterpret_cast<uintptr_t>(ws) & 255) ||
       ((reinterpret_cast<uintptr_t>(seqlens) | reinterpret_cast<uintptr_t>(lse)) & 3))
     return APACK_EINVAL;
+  const uintptr_t q0 = reinterpret_cast<uintptr_t>(q), q1 = q0 + (cache->num_seqs - 1) * q_token_stride + row;
+  const uintptr_t o0 = reinterpret_cast<uintptr_t>(out), o1 = o0 + cache->num_seqs * row * (out_dtype == APACK_FP32 ? 2 : 1);
+  if (q0 < o1 && o0 < q1) return APACK_EINVAL;
   if (ws_bytes < s.total) return APACK_EWORKSPACE;
   if (!on_current_device(cache->k) || !on_current_device(cache->v)) return APACK_EINVAL;   // read by TMA
   PdPlan P;

@@ -428,6 +428,23 @@ def test_paged_attention_bad_lengths_and_pages(ap):
     assert run([32, 0])[1] == ap.APACK_OK
 
 
+def test_paged_attention_refuses_an_output_over_its_queries(ap):
+    rng = np.random.default_rng(14)
+    k, v = (normal(rng, (1, 3, 16, 2, 64), torch.bfloat16) for _ in range(2))
+    both = normal(rng, (5, 4, 64), torch.bfloat16)
+    cache = ap.PagedCache(k, v, i32([[0, 1], [2, 2]]))
+    ws = workspace(ap.apack_paged_decode_workspace_size(cache, 4))
+    for q, out in ((both[:2], both[:2]), (both[:2], both[1:3]), (both[1:3], both[:2]), (both[::2][:2], both[1:3])):
+        with pytest.raises(ap.ApackError) as e:
+            ap.apack_paged_decode_attention(cache, 0, i32([20, 3]), q, out, ws)
+        assert e.value.status == ap.APACK_EINVAL
+    want, q = torch.empty(2, 4, 64, device="cuda").bfloat16(), both[:2].clone()
+    ap.apack_paged_decode_attention(cache, 0, i32([20, 3]), q, want, ws)
+    for out in (both[2:4], both[3:5]):                  # beside them
+        ap.apack_paged_decode_attention(cache, 0, i32([20, 3]), both[:2], out, ws)
+        assert torch.equal(out, want)
+
+
 def test_paged_attention_agrees_with_the_contiguous_call(ap):
     """One page that holds the whole packed cache of a sequence: the numbers of apack_decode_attention."""
     rng = np.random.default_rng(13)
