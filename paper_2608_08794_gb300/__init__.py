@@ -456,14 +456,20 @@ def _dtype_code(dtype):
 
 
 _cuda = None                      # (current device, current stream of a device), looked up once CUDA is there
+_int32_type = None                # torch.int32, likewise
+
+
+# The calls of a decode step take the host longer than the device.  So their wrappers test what is usual in a few plain
+# comparisons, and leave what is not (the unusual that is right, and the messages) to the functions below.
 
 
 def _on_device(tensors, stream):
     """The calls run on the current device: tensors elsewhere are refused (without a device the library's own checks
     answer).  Returns the address of the stream, the device's current one when None."""
-    global _cuda
+    global _cuda, _int32_type
     if _cuda is None:
         import torch
+        _int32_type = torch.int32
         if torch.cuda.is_initialized() or torch.cuda.is_available():
             torch.cuda.current_device()              # initialises
             try:
@@ -577,42 +583,93 @@ class Rotary:
 
 def apack_rotary(rotary, x, positions, out, transpose=False, stream=None):
     """Rotary positions of x [tokens, heads, D] into out (out is x: in place); transpose: the gradient."""
-    stream = _on_device((x, positions, out), stream)
-    size = x.element_size()
-    xs = size * _head_rows(x, "x")
-    n, heads, dim = x.shape
-    outs = xs if out is x else size * _head_rows(out, "out", x.dtype, x.shape)
-    axis = rotary._positions(positions, n)
-    _check(_lib.apack_rotary(rotary._address, _dtype_code(x.dtype), n, heads, dim, x.data_ptr(), xs, out.data_ptr(),
-                             outs, positions.data_ptr(), axis, 1 if transpose else 0, stream), "apack_rotary")
+    if _cuda is None:
+        stream = _on_device((x, positions, out), stream)
+    else:
+        dev = _cuda[0]()
+        if x.get_device() != dev or positions.get_device() != dev or out.get_device() != dev:
+            _on_device((x, positions, out), stream)
+        stream = _cuda[1](dev) if stream is None else _stream(stream)
+    dtype, shape, xs = x.dtype, x.shape, x.stride()
+    code = _CODES.get(dtype)
+    if code is None:
+        code = _dtype_code(dtype)
+    if len(shape) != 3 or xs[2] != 1 or xs[1] != shape[2]:
+        xs = (_head_rows(x, "x"),)
+    n, heads, dim = shape
+    xs = xs[0] if n > 1 else heads * dim
+    if out is x:
+        outs = xs
+    else:
+        outs = out.stride()
+        if out.dtype is not dtype or out.shape != shape or outs[2] != 1 or outs[1] != dim:
+            outs = (_head_rows(out, "out", dtype, shape),)
+        outs = outs[0] if n > 1 else heads * dim
+    axes, axis = rotary.num_axes, positions.stride()
+    if positions.dtype is _int32_type and positions.shape == ((axes, n) if axes > 1 else (n,)) and axis[-1] == 1:
+        axis = axis[0] if axes > 1 else n
+    else:
+        axis = rotary._positions(positions, n)
+    size = 4 if code == APACK_FP32 else 2
+    status = _lib.apack_rotary(rotary._address, code, n, heads, dim, x.data_ptr(), size * xs, out.data_ptr(), size * outs,
+                               positions.data_ptr(), axis, 1 if transpose else 0, stream)
+    if status:
+        raise ApackError(status, "apack_rotary")
 
 
 def apack_rotary_append(rotary, cache, layer, q, k, v, q_out, positions, rows, seqs=None, ws=None, stream=None):
     """Rotates new tokens' queries into q_out and their keys into the pages of `layer`, with their values.
     rotary None: no rotation; q (and q_out) None: keys and values alone."""
-    stream = _on_device((cache, q, k, v, q_out, positions, rows, seqs, ws), stream)
+    if _cuda is None:
+        stream = _on_device((cache, k, v, rows, q, q_out, positions, seqs, ws), stream)
+    else:
+        dev = _cuda[0]()
+        if (cache._device != dev or k.get_device() != dev or v.get_device() != dev or rows.get_device() != dev or
+                (q is not None and q.get_device() != dev) or (q_out is not None and q_out.get_device() != dev) or
+                (positions is not None and positions.get_device() != dev) or
+                (seqs is not None and seqs.get_device() != dev) or (ws is not None and ws.get_device() != dev)):
+            _on_device((cache, k, v, rows, q, q_out, positions, seqs, ws), stream)
+        stream = _cuda[1](dev) if stream is None else _stream(stream)
     n = k.shape[0]
     dtype, dim = cache.dtype, cache.head_dim
     shape = (n, cache.num_kv_heads, dim)
-    ks, vs = _head_rows(k, "k", dtype, shape), _head_rows(v, "v", dtype, shape)
-    qs = qos = heads = 0
+    ks, vs = k.stride(), v.stride()
+    if k.dtype is not dtype or k.shape != shape or ks[1] != dim or ks[2] != 1:
+        ks = (_head_rows(k, "k", dtype, shape),)
+    if v.dtype is not dtype or v.shape != shape or vs[1] != dim or vs[2] != 1:
+        vs = (_head_rows(v, "v", dtype, shape),)
+    ks, vs = (ks[0], vs[0]) if n > 1 else (shape[1] * dim, shape[1] * dim)
+    q_at = q_out_at = spec = pos_at = None
+    qs = qos = heads = axis = 0
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out: both or neither expected")
     if q is not None:
         heads = q.shape[1]
         shape = (n, heads, dim)
-        qs = _head_rows(q, "q", dtype, shape)
-        qos = qs if q_out is q else _head_rows(q_out, "q_out", dtype, shape)
-    axis = 0
+        qs, qos = q.stride(), q_out.stride()
+        if q.dtype is not dtype or q.shape != shape or qs[1] != dim or qs[2] != 1:
+            qs = (_head_rows(q, "q", dtype, shape),)
+        if q_out.dtype is not dtype or q_out.shape != shape or qos[1] != dim or qos[2] != 1:
+            qos = (_head_rows(q_out, "q_out", dtype, shape),)
+        qs, qos = (qs[0], qos[0]) if n > 1 else (heads * dim, heads * dim)
+        q_at, q_out_at = q.data_ptr(), q_out.data_ptr()
     if rotary is not None:
-        axis = rotary._positions(positions, n)
-    _int32(rows, "rows", (n,))
-    if seqs is not None:
+        axes, axis = rotary.num_axes, positions.stride()
+        if positions.dtype is _int32_type and positions.shape == ((axes, n) if axes > 1 else (n,)) and axis[-1] == 1:
+            axis = axis[0] if axes > 1 else n
+        else:
+            axis = rotary._positions(positions, n)
+        spec, pos_at = rotary._address, positions.data_ptr()
+    if not (rows.dtype is _int32_type and rows.shape == (n,) and rows.is_contiguous()):
+        _int32(rows, "rows", (n,))
+    if seqs is not None and not (seqs.dtype is _int32_type and seqs.shape == (n,) and seqs.is_contiguous()):
         _int32(seqs, "seqs", (n,))
-    _check(_lib.apack_rotary_append(None if rotary is None else rotary._address, cache._address, int(layer), n,
-                                    _ptr(q), 2 * qs, _ptr(q_out), 2 * qos, heads, k.data_ptr(), 2 * ks, v.data_ptr(),
-                                    2 * vs, None if rotary is None else positions.data_ptr(), axis, rows.data_ptr(),
-                                    _ptr(seqs), _ptr(ws), stream), "apack_rotary_append")
+    status = _lib.apack_rotary_append(
+        spec, cache._address, int(layer), n, q_at, 2 * qs, q_out_at, 2 * qos, heads, k.data_ptr(), 2 * ks, v.data_ptr(),
+        2 * vs, pos_at, axis, rows.data_ptr(), None if seqs is None else seqs.data_ptr(),
+        None if ws is None else ws.data_ptr(), stream)
+    if status:
+        raise ApackError(status, "apack_rotary_append")
 
 
 def apack_paged_decode_workspace_size(cache, num_q_heads):
@@ -625,19 +682,33 @@ def apack_paged_decode_workspace_size(cache, num_q_heads):
 def apack_paged_decode_attention(cache, layer, seqlens, q, out, ws, scale=None, lse=None, stream=None):
     """Attention of one decode token per sequence over its pages; seqlens: int32 [num_seqs] on the device.
     q [num_seqs, Hq, D]; out: the same shape, contiguous, of q's type or float32; lse: float32 [num_seqs, Hq]."""
-    stream = _on_device((cache, seqlens, q, out, ws, lse), stream)
+    if _cuda is None:
+        stream = _on_device((cache, seqlens, q, out, ws, lse), stream)
+    else:
+        dev = _cuda[0]()
+        if (cache._device != dev or seqlens.get_device() != dev or q.get_device() != dev or out.get_device() != dev or
+                ws.get_device() != dev or (lse is not None and lse.get_device() != dev)):
+            _on_device((cache, seqlens, q, out, ws, lse), stream)
+        stream = _cuda[1](dev) if stream is None else _stream(stream)
+    seqs, dim, dtype, qs = cache.num_seqs, cache.head_dim, cache.dtype, q.stride()
     heads = q.shape[1]
-    shape = (cache.num_seqs, heads, cache.head_dim)
-    qs = _head_rows(q, "q", cache.dtype, shape)
-    _int32(seqlens, "seqlens", shape[:1])
+    shape = (seqs, heads, dim)
+    if q.dtype is not dtype or q.shape != shape or qs[1] != dim or qs[2] != 1:
+        qs = (_head_rows(q, "q", dtype, shape),)
+    qs = qs[0] if seqs > 1 else heads * dim
+    if not (seqlens.dtype is _int32_type and seqlens.shape == (seqs,) and seqlens.is_contiguous()):
+        _int32(seqlens, "seqlens", (seqs,))
     if out.shape != shape or not out.is_contiguous():
         raise ValueError(f"out: contiguous {shape} expected")
-    if lse is not None and (str(lse.dtype) != "torch.float32" or lse.shape != shape[:2] or not lse.is_contiguous()):
+    if lse is not None and (str(lse.dtype) != "torch.float32" or lse.shape != (seqs, heads) or not lse.is_contiguous()):
         raise ValueError(f"lse: contiguous float32 {shape[:2]} expected")
-    _check(_lib.apack_paged_decode_attention(
+    code = _CODES.get(out.dtype)
+    status = _lib.apack_paged_decode_attention(
         cache._address, int(layer), seqlens.data_ptr(), q.data_ptr(), 2 * qs, heads,
-        cache._scale if scale is None else scale, out.data_ptr(), _dtype_code(out.dtype),
-        _ptr(lse), ws.data_ptr(), ws.nbytes, stream), "apack_paged_decode_attention")
+        cache._scale if scale is None else scale, out.data_ptr(), _dtype_code(out.dtype) if code is None else code,
+        None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.nbytes, stream)
+    if status:
+        raise ApackError(status, "apack_paged_decode_attention")
 
 
 def apack_paged_compact(src, dst, cu_dst, n_out, keep_idx=None, cu_src=None, src_layer=0, dst_layer=0,
@@ -661,10 +732,19 @@ def apack_paged_compact(src, dst, cu_dst, n_out, keep_idx=None, cu_src=None, src
 
 def apack_copy_pages(cache, pairs, ws=None, stream=None):
     """Copies page pairs[i, 0] to page pairs[i, 1] in every layer; pairs: int32 [n, 2] on the device."""
-    stream = _on_device((cache, pairs, ws), stream)
-    _int32(pairs, "pairs", (pairs.shape[0], 2))
-    _check(_lib.apack_copy_pages(cache._address, pairs.data_ptr(), pairs.shape[0], _ptr(ws), stream),
-           "apack_copy_pages")
+    if _cuda is None:
+        stream = _on_device((cache, pairs, ws), stream)
+    else:
+        dev = _cuda[0]()
+        if cache._device != dev or pairs.get_device() != dev or (ws is not None and ws.get_device() != dev):
+            _on_device((cache, pairs, ws), stream)
+        stream = _cuda[1](dev) if stream is None else _stream(stream)
+    n = pairs.shape[0]
+    if not (pairs.dtype is _int32_type and pairs.shape == (n, 2) and pairs.is_contiguous()):
+        _int32(pairs, "pairs", (n, 2))
+    status = _lib.apack_copy_pages(cache._address, pairs.data_ptr(), n, None if ws is None else ws.data_ptr(), stream)
+    if status:
+        raise ApackError(status, "apack_copy_pages")
 
 
 def apack_device_error(ws, stream=None, clear=True):
