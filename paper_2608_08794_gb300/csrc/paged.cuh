@@ -58,8 +58,7 @@ PoolView pool_view(const apack_paged_cache *c, int32_t layer);
 bool on_current_device(const void *p);
 
 // 5-D TMA map of one layer's K (or V): {64 features, token in page, 64-feature block, head, page}, boxes of
-// box_tokens tokens and box_blocks blocks of one head, 128-byte swizzle; pages outside the pool read as zeros.
-bool make_page_map(CUtensorMap *map, const apack_paged_cache *c, const void *layer_base, uint32_t box_tokens,
-                   uint32_t box_blocks);
+// box_tokens tokens of one head, 128-byte swizzle; pages outside the pool read as zeros.
+bool make_page_map(CUtensorMap *map, const apack_paged_cache *c, const void *layer_base, uint32_t box_tokens);
 
 }  // namespace apack

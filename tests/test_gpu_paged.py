@@ -428,6 +428,35 @@ def test_paged_attention_bad_lengths_and_pages(ap):
     assert run([32, 0])[1] == ap.APACK_OK
 
 
+@pytest.mark.parametrize("dim,tokens,group", [(128, 1, 2), (64, 5, 2), (128, 8, 12), (64, 2, 20)])
+def test_paged_attention_bad_pages_of_few_tokens(ap, dim, tokens, group):
+    """A page outside the pool is a page of zeros here too, for the rows of it that the sequence has, and is reported."""
+    rng = np.random.default_rng(15)
+    lens = [43, 17]
+    table, pages = make_table(rng, lens, tokens)
+    k, v = (normal(rng, (1, pages + 1, tokens, 2, dim), torch.bfloat16) for _ in range(2))
+    k[0, pages], v[0, pages] = 0, 0
+    q = normal(rng, (2, 2 * group, dim), torch.bfloat16)
+
+    def run(t):
+        cache = ap.PagedCache(k, v, i32(t))
+        ws = workspace(ap.apack_paged_decode_workspace_size(cache, 2 * group))
+        out, lse = torch.empty(2, 2 * group, dim, device="cuda"), torch.empty(2, 2 * group, device="cuda")
+        ap.apack_paged_decode_attention(cache, 0, i32(lens), q, out, ws, lse=lse)
+        return out, lse, ap.apack_device_error(ws)
+
+    for at in ((0, 0), (0, 42 // tokens), (1, 1)):
+        zeros = table.copy()
+        zeros[at] = pages
+        want, want_lse, code = run(zeros)
+        assert code == ap.APACK_OK and torch.isfinite(want).all()
+        for page in (-1, pages + 1, 2 ** 31 - 1, -2 ** 31):
+            bad = table.copy()
+            bad[at] = page
+            out, lse, code = run(bad)
+            assert code == ap.APACK_EDEVICE and torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
 def test_paged_attention_refuses_an_output_over_its_queries(ap):
     rng = np.random.default_rng(14)
     k, v = (normal(rng, (1, 3, 16, 2, 64), torch.bfloat16) for _ in range(2))
