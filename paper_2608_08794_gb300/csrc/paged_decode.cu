@@ -10,10 +10,11 @@
 // Split over the cache's length.  The work is the list of all (sequence, head group, tile) in that order; every CTA
 // takes an equal contiguous share of it and finds its start from the lengths on the device, so that the launch does
 // not depend on them (a captured call follows growing caches).  Within a CTA a KV head has wph ring buffers of stages
-// (filled by TMA from pages of a multiple of 16 tokens), each for every wph-th tile of the share; a ring is read by one warp of 8 or 16 query rows, or with more than 16
-// rows per KV head by 2 warps of 16.  Its first warp refills a stage as soon as it has been used.  At the end of a
-// (sequence, head group) the warps of a head merge through shared memory; what a share holds whole is written out,
-// what it holds in part goes to the workspace, and a second kernel merges those parts in order.
+// (filled by TMA from pages of a multiple of 16 tokens), each for every wph-th tile of the share; a ring is read by
+// one warp of 8 or 16 query rows, or with more than 16 rows per KV head by 2 warps of 16.  Its first warp refills a
+// stage as soon as it has been used.  At the end of a (sequence, head group) the warps of a head merge through shared
+// memory; what a share holds whole is written out, what it holds in part goes to the workspace, and a second kernel
+// merges those parts in order.
 //
 // Warp-level instructions, not tcgen05: that needs M = 128 keys, TMEM and a hand-over between warps for every tile of the
 // same 8 rows, and the tensor work is far below what the read allows either way (on contiguous caches the tcgen05

@@ -7,8 +7,8 @@ and ``apack_paged_compact`` where pages have to move.  A fork shares its parent'
 copied when a sequence first writes behind its last row.
 
 All device work is queued on torch's current stream; a pool's calls belong on one stream (a page that is freed
-may be handed out again by the next call) and are not captured (a graph reads the tables that they change).  Every method checks that it can be carried out (pages, rows) before
-it changes anything.
+may be handed out again by the next call) and are not captured (a graph reads the tables that they change).
+Every method checks that it can be carried out (pages, rows) before it changes anything.
 """
 
 import numpy as np
