@@ -20,8 +20,8 @@
 // same 8 rows, and the tensor work is far below what the read allows either way (on contiguous caches the tcgen05
 // kernel of decode_tc.cu takes 50.6 us for the ten-minute cache).
 //
-// Measured (28/4 heads of 128, bf16, 16-token pages, calls in a row): 135,272 tokens 50.3 us, 5.5 TB/s, 0.81 of the
-// copy rate, of which the chunk kernel 45 us (0.9); 16 caches of 600 to 12,000 tokens 33.7 us; 473 tokens 7.8 us.
+// Measured (28/4 heads of 128, bf16, 16-token pages, calls in a row): 135,272 tokens (64-token pages) 50.4 us, 5.5 TB/s, 0.81 of
+// the copy rate, of which the chunk kernel 45 us (0.9); 16 caches of 600 to 12,000 tokens 34.1 us; 473 tokens 8.3 us.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -81,11 +81,17 @@ struct PdPlan {
 // tiles need one vote instead of a reduction and rescaled accumulators.  bf16 has the range of fp32.  fp16 ends at
 // 2^16 and loses what lies below 2^-25: with probabilities of up to 2^15 (kShift + kGrow) the tail is kept down to
 // 2^-36 of the maximum; up to 1, a hundred thousand keys 17 below the maximum would be lost, 2^-8 of the sum.
+// kParts: a probability enters the value product as a sum of that many 16-bit numbers, so that it keeps the 24 bits that
+// the row's sum is made of: three of bf16 (8 bits each: what is left out is below 2^-26), two of fp16 (11 bits and a sign
+// each: 2^-23).  The third bf16 number costs 0.2 us of 50 or 34 (ten minutes, 16 caches), 0.5 of 31 with 16 query heads per
+// KV head and 3.7 of 38 with 32, which the matrix instructions bound (the same calls in fp16: 34.6); without it fp32 outputs
+// were 2e-6 off.
 template <class T>
 struct Half16;
 template <>
 struct Half16<__nv_bfloat16> {
   static constexpr float kGrow = 8.f, kShift = 0.f;
+  static constexpr int kParts = 3;
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<uint32_t *>(&v);
@@ -102,6 +108,7 @@ struct Half16<__nv_bfloat16> {
 template <>
 struct Half16<__half> {
   static constexpr float kGrow = 4.f, kShift = 11.f;
+  static constexpr int kParts = 2;
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     __half2 v = __floats2half2_rn(a, b);
     return *reinterpret_cast<uint32_t *>(&v);
@@ -206,9 +213,10 @@ struct Walk {
 
 // NG: groups of 8 query rows of a warp, which share its reads of K and V from shared memory.  SHARED: a ring is read by 2
 // warps; as templates, because the one-warp rings of most models are 1.5 % faster without the other case's registers and
-// branches.  60,000 tokens of 4 KV heads of 128: 29.4 us with 7 query heads each, 30.0 with 16, 34.3 with 24 or 32 (46.6
-// with 4 warps of one group per ring: every warp reads the whole tile, 4 times the traffic that fills it); 16 query heads
-// as 2 warps of one group each 30.0 too, 29.6 against 30.2 on 64 caches of 100 to 2,000 tokens: one variant less.
+// branches.  60,000 tokens of 4 KV heads of 128, bf16, 16-token pages: 28.5 us with 7 query heads each, 31.1 with 16, 38.1
+// with 24 or 32.  With two 16-bit numbers per probability the last took 34.3, and 46.6 with 4 warps of one group per ring
+// (every warp reads the whole tile, 4 times the traffic that fills it); 16 query heads as 2 warps of one group each the
+// same as here, 29.6 against 30.2 on 64 caches of 100 to 2,000 tokens: one variant less.
 template <class T, int D, int NG, bool SHARED>
 __global__ void __launch_bounds__(kThreads, 1)
     paged_chunk_kernel(const __grid_constant__ PdPlan P, const __grid_constant__ CUtensorMap kmap,
@@ -602,9 +610,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
       }
-      // P as the sum of two 16-bit numbers (2^-17 of it are left out in bf16, 2^-22 or 2^-36 of the largest in fp16; one
-      // alone would cost 2^-9), transposed into B fragments
-      uint32_t hi[NG][KM][2], lo[NG][KM][2];
+      // P as the sum of kParts 16-bit numbers, each the rounding of what those before it leave, transposed into B fragments
+      constexpr int kParts = Half16<T>::kParts;
+      uint32_t pf[NG][KM][kParts][2];
 #pragma unroll
       for (int ng = 0; ng < NG; ++ng)
 #pragma unroll
@@ -615,12 +623,15 @@ __global__ void __launch_bounds__(kThreads, 1)
           l[ng][0] += p[0] + p[2];
           l[ng][1] += p[1] + p[3];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const uint32_t h = Half16<T>::pack(p[2 * e], p[2 * e + 1]);
-            const float2 hf = Half16<T>::unpack(h);
-            hi[ng][km][e] = transpose8x8(h);
-            lo[ng][km][e] = transpose8x8(Half16<T>::pack(p[2 * e] - hf.x, p[2 * e + 1] - hf.y));
-          }
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int part = 0; part < kParts; ++part) {
+              const uint32_t h = Half16<T>::pack(p[2 * e], p[2 * e + 1]);
+              pf[ng][km][part][e] = transpose8x8(h);
+              const float2 hf = Half16<T>::unpack(h);
+              p[2 * e] -= hf.x;
+              p[2 * e + 1] -= hf.y;
+            }
         }
 #pragma unroll
       for (int km = 0; km < KM; ++km)
@@ -630,10 +641,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint32_t ch = i * 2 + vchunk;
           ldmatrix4_trans(vb + (ch >> 3) * kBlk + (km * 16 + vrow) * 128 + (((ch & 7) ^ (vrow & 7)) << 4), a);
 #pragma unroll
-          for (int ng = 0; ng < NG; ++ng) {
-            Half16<T>::mma(o[ng][i], a, hi[ng][km][0], hi[ng][km][1]);
-            Half16<T>::mma(o[ng][i], a, lo[ng][km][0], lo[ng][km][1]);
-          }
+          for (int ng = 0; ng < NG; ++ng)
+#pragma unroll
+            for (int part = 0; part < kParts; ++part) Half16<T>::mma(o[ng][i], a, pf[ng][km][part][0], pf[ng][km][part][1]);
         }
       __syncwarp();                                   // every lane has read the stage
       if (!SHARED) {
