@@ -8,7 +8,9 @@ copied when a sequence first writes behind its last row.
 
 All device work is queued on torch's current stream; a pool's calls belong on one stream (a page that is freed
 may be handed out again by the next call) and are not captured (a graph reads the tables that they change).
-Every method checks that it can be carried out (pages, rows) before it changes anything.
+Every method checks that it can be carried out (pages, rows) before it changes anything, and changes what the host
+keeps only after its device calls have been queued: one that raises (an allocation, a pool on another device than
+the current one) leaves every sequence as it was.
 """
 
 import numpy as np
@@ -73,10 +75,14 @@ class PagePool:
             raise MemoryError(f"{seqs} sequences wanted, {len(rows)} rows of the page table free")
         return rows[:seqs]
 
+    def _spare(self, n):
+        """The pages that the next _take(n) takes."""
+        return self._free[len(self._free) - n:][::-1]
+
     def _take(self, n):
-        got = [self._free.pop() for _ in range(n)]
+        got = self._spare(n)
+        del self._free[len(self._free) - n:]
         self._refs[got] = 1
-        return got
 
     def _drop(self, pages):
         at = np.asarray(pages, np.int64)         # distinct
@@ -91,27 +97,29 @@ class PagePool:
         host = torch.from_numpy(values)
         return (host.pin_memory() if self.k.is_cuda else host).to(self.device, non_blocking=True)
 
-    def _write(self, at, length, entries, more=(), clear=False):
-        """Lengths of the sequences `at` and, pairs of (place in the flat table, page), their entries, on the device;
-        returns `more` there.  One copy for all of them.  clear: -1 in all other entries of the sequences."""
+    def _stage(self, at, length, entries, more=()):
+        """What _write needs of an update, on the device; nothing is changed.  Lengths of the sequences `at` and, pairs of
+        (place in the flat table, page), their entries; `more` for the caller.  One copy for all of them."""
         n, m = len(at), len(entries)
         both = np.array(entries, np.int64).reshape(m, 2)
         wide = self._device(np.concatenate([at, both[:, 0], length, both[:, 1], more]).astype(np.int64))
-        narrow = wide[n + m:].to(torch.int32)
-        if n:
-            self.lengths.index_copy_(0, wide[:n], narrow[:n])
+        return n, m, wide, wide[n + m:].to(torch.int32)
+
+    def _stage_rows(self, seqs, lists, length):
+        """The same for these sequences' whole rows."""
+        return self._stage(np.asarray(seqs, np.int64), length,
+                           [(s * self.max_pages + i, p) for s, pages in zip(seqs, lists) for i, p in enumerate(pages)])
+
+    def _write(self, staged, clear=False):
+        """A staged update of the device's tables; returns its `more`.  clear: -1 in all other entries of the sequences."""
+        n, m, wide, narrow = staged
         if clear:
             self.page_table.index_fill_(0, wide[:n], -1)
         if m:
             self.page_table.view(-1).index_copy_(0, wide[n:n + m], narrow[n:n + m])
+        if n:
+            self.lengths.index_copy_(0, wide[:n], narrow[:n])
         return narrow[n + m:]
-
-    def _upload(self, seqs):
-        """The rows of these sequences in the device's tables, whole."""
-        if not len(seqs):
-            return
-        self._write(np.asarray(seqs), self._len[list(seqs)],
-                    [(s * self.max_pages + i, p) for s in seqs for i, p in enumerate(self._pages[s])], clear=True)
 
     def _ints(self, values):
         return self._device(np.asarray(values, np.int32))
@@ -122,19 +130,21 @@ class PagePool:
         """A new sequence with pages for `rows` rows, which the caller writes; returns its number."""
         n = self._need(rows)
         seq, = self._room(n, 1)
-        self._pages[seq], self._len[seq] = self._take(n), rows
-        self._upload([seq])
+        pages = self._spare(n)
+        self._write(self._stage_rows([seq], [pages], [rows]), clear=True)
+        self._take(n)
+        self._pages[seq], self._len[seq] = pages, rows
         return seq
 
     def fork(self, seq):
         """A new sequence that shares the pages of `seq`; returns its number."""
         pages = self._held(seq)
         new, = self._room(0, 1)
+        self.page_table[new].copy_(self.page_table[seq])
+        self.lengths[new].copy_(self.lengths[seq])
         self._refs[pages] += 1
         self._shared += len(pages)
         self._pages[new], self._len[new] = list(pages), self._len[seq]
-        self.page_table[new].copy_(self.page_table[seq])
-        self.lengths[new].copy_(self.lengths[seq])
         return new
 
     def extend(self, seqs, rows=1):
@@ -157,29 +167,33 @@ class PagePool:
                 if left[last] > 1:
                     left[last] -= 1
                     copied.append(i)
-        self._room(int(grow.sum()) + len(copied))
-        pairs, entries = [], []
-        for i in copied:
-            own, = self._take(1)
-            pairs.append((held[i][-1], own))
+        wanted = int(grow.sum()) + len(copied)
+        self._room(wanted)
+        spare = iter(self._spare(wanted))
+        own = [(i, next(spare)) for i in copied]                   # in the place of a shared last page
+        new = [(i, [next(spare) for _ in range(grow[i])]) for i in np.flatnonzero(grow)]
+        entries = [(seqs[i] * self.max_pages + len(held[i]) - 1, p) for i, p in own]
+        entries += [(seqs[i] * self.max_pages + len(held[i]) + j, p) for i, pages in new for j, p in enumerate(pages)]
+        staged = self._stage(np.asarray(seqs, np.int64), total, entries, used)
+        if own:
+            apack_copy_pages(self.cache, self._ints([(held[i][-1], p) for i, p in own]))
+        first = self._write(staged)
+        self._take(wanted)
+        for i, p in own:
             self._drop(held[i][-1:])
-            held[i][-1] = own
-            entries.append((seqs[i] * self.max_pages + len(held[i]) - 1, own))
-        for i in np.flatnonzero(grow):
-            new = self._take(grow[i])
-            entries += [(seqs[i] * self.max_pages + len(held[i]) + j, p) for j, p in enumerate(new)]
-            held[i] += new
+            held[i][-1] = p
+        for i, pages in new:
+            held[i] += pages
         self._len[list(seqs)] = total
-        if pairs:
-            apack_copy_pages(self.cache, self._ints(pairs))
-        return self._write(np.asarray(seqs, np.int64), total, entries, used)
+        return first
 
     def free(self, seq):
         """Gives up a sequence; pages that no other one shares become free."""
-        self._drop(self._held(seq))
-        self._pages[seq], self._len[seq] = None, 0
-        self.page_table[seq].fill_(-1)
+        pages = self._held(seq)
         self.lengths[seq].fill_(0)
+        self.page_table[seq].fill_(-1)
+        self._drop(pages)
+        self._pages[seq], self._len[seq] = None, 0
 
     # ------------------------------------------------------------ pruning
 
@@ -189,16 +203,10 @@ class PagePool:
             table[i, :len(pages)] = pages
         return PagedCache(self.k, self.v, self._ints(table))
 
-    def _moved(self, need, src, cu_dst, n_out, **how):
-        """Rows of src in new pages, need[i] of them for the i-th sequence; returns the page lists."""
-        new = [self._take(n) for n in need]
-        try:
-            apack_paged_compact(src, self._cache_of(new), cu_dst, n_out, **how)
-        except Exception:
-            for pages in new:
-                self._drop(pages)
-            raise
-        return new
+    def _split(self, need):
+        """Free pages in lists of these lengths (they stay free)."""
+        spare = iter(self._spare(sum(need)))
+        return [[next(spare) for _ in range(n)] for n in need]
 
     def prune(self, seqs, keep_idx, kept, in_place=None, ws=None):
         """Keeps kept[i] rows of seqs[i] (distinct): keep_idx holds them, packed over the sequences in this order
@@ -220,20 +228,23 @@ class PagePool:
         own = all(self._refs[p] == 1 for pages in lists for p in pages)
         if in_place and not own:
             raise ValueError("in place: a page is shared with another sequence")
-        if in_place or (in_place is None and own and sum(need) > len(self._free)):
-            apack_paged_compact(src, src, cu_dst, n_out, keep_idx=keep_idx, cu_src=cu_src, ws=ws)
-            for s, n, pages in zip(seqs, need, lists):
-                self._drop(pages[n:])
-                self._pages[s] = pages[:n]
+        if in_place is None:
+            in_place = own and sum(need) > len(self._free)
+        if in_place:
+            new = [pages[:n] for n, pages in zip(need, lists)]
+            dst = src
         else:
             self._room(sum(need))
-            new = self._moved(need, src, cu_dst, n_out, keep_idx=keep_idx, cu_src=cu_src, ws=ws)
-            for s, pages, own in zip(seqs, lists, new):
-                self._drop(pages)
-                self._pages[s] = own
-        for s, m in zip(seqs, kept):
-            self._len[s] = int(m)
-        self._upload(seqs)
+            new = self._split(need)
+            dst = self._cache_of(new)
+        staged = self._stage_rows(seqs, new, kept)
+        apack_paged_compact(src, dst, cu_dst, n_out, keep_idx=keep_idx, cu_src=cu_src, ws=ws)
+        self._write(staged, clear=True)
+        if not in_place:
+            self._take(sum(need))
+        for s, m, n, pages, now in zip(seqs, kept, need, lists, new):
+            self._drop(pages[n:] if in_place else pages)
+            self._pages[s], self._len[s] = now, int(m)
 
     def take(self, src, kept, keep_idx=None, cu_src=None, src_layer=0, dst_layer=0, num_layers=None, ws=None):
         """New sequences from the kept rows of another PagedCache (a prefill's contiguous caches, say: one page of
@@ -243,9 +254,12 @@ class PagePool:
         need = [self._need(m) for m in kept]
         rows = self._room(sum(need), len(kept))
         cu_dst = self._ints(np.concatenate([[0], np.cumsum(kept)]))
-        new = self._moved(need, src, cu_dst, int(sum(int(m) for m in kept)), keep_idx=keep_idx, cu_src=cu_src,
-                          src_layer=src_layer, dst_layer=dst_layer, num_layers=num_layers, ws=ws)
+        new = self._split(need)
+        staged = self._stage_rows(rows, new, kept)
+        apack_paged_compact(src, self._cache_of(new), cu_dst, int(sum(int(m) for m in kept)), keep_idx=keep_idx, cu_src=cu_src,
+                            src_layer=src_layer, dst_layer=dst_layer, num_layers=num_layers, ws=ws)
+        self._write(staged, clear=True)
+        self._take(sum(need))
         for s, pages, m in zip(rows, new, kept):
             self._pages[s], self._len[s] = pages, int(m)
-        self._upload(rows)
         return rows
