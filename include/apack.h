@@ -468,8 +468,9 @@ apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_
      keep_idx[j]               where cu_src is NULL (one page that holds the packed batch)
      j - cu_dst[b]             where keep_idx is NULL (every sequence's first rows; cu_src must be NULL)
    of src's sequence b, for j in [cu_dst[b], cu_dst[b+1]); cu_dst: device [B+1], apack_select's new_cu_seqlens.
-   n_out: cu_dst[B], or an upper bound of it.  B = num_seqs of both pools; heads, D and dtype equal; page sizes
-   and strides may differ.  Slots of dst that no j names keep what they hold.
+   n_out: cu_dst[B], or an upper bound of it (keep_idx is read below cu_dst[B] alone).  B = num_seqs of both
+   pools; heads, D and dtype equal; page sizes and strides may differ.  Slots of dst that no j names keep what
+   they hold.
    Out of place (another pool, other pages of the same one by another table, or other layers), no page that is
    written may be read by the same call.  In place: src and dst name the same pool, table and layers; keep_idx is
    then given and strictly ascending within each sequence, and each sequence's pages are its own; rows move towards the

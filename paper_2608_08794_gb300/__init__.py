@@ -714,7 +714,8 @@ def apack_paged_decode_attention(cache, layer, seqlens, q, out, ws, scale=None, 
 def apack_paged_compact(src, dst, cu_dst, n_out, keep_idx=None, cu_src=None, src_layer=0, dst_layer=0,
                         num_layers=None, ws=None, stream=None):
     """The kept rows of every sequence of pool src, in order, to the first rows of its pages in dst (src is dst:
-    in place).  cu_dst, cu_src: int32 [num_seqs + 1] on the device; num_layers: all that both have by default."""
+    in place).  cu_dst, cu_src: int32 [num_seqs + 1] on the device; keep_idx: n_out entries at least (the call cannot
+    see cu_dst); num_layers: all that both have by default."""
     stream = _on_device((src, dst, cu_dst, keep_idx, cu_src, ws), stream)
     _int32(cu_dst, "cu_dst", (dst.num_seqs + 1,))
     if cu_src is not None:

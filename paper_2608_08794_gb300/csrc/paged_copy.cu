@@ -97,7 +97,9 @@ __global__ void __launch_bounds__(kMoveThreads, 4) move_rows_kernel(const __grid
   const int64_t j = static_cast<int64_t>(blockIdx.x) * P.rows_cta + threadIdx.x;
   const int32_t *cu = P.cu_dst;
   int32_t keep = 0;
-  if (P.keep_idx && threadIdx.x < P.rows_cta && j < P.n_rows) keep = __ldg(P.keep_idx + j);
+  // n_rows may be more than cu_dst[B]; keep_idx ends there
+  if (P.keep_idx && threadIdx.x < P.rows_cta && j < min(P.n_rows, static_cast<int64_t>(__ldg(P.cu_dst + P.num_seqs))))
+    keep = __ldg(P.keep_idx + j);
   if (!P.pairs && P.num_seqs <= kStagedSeqs) {
     for (int b = threadIdx.x; b <= P.num_seqs; b += kMoveThreads) cu_s[b] = __ldg(P.cu_dst + b);
     __syncthreads();

@@ -1,0 +1,54 @@
+"""Calls at the edges of what the paged-cache entry points allow, on the GPU."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged_oracle as po
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ap():
+    import __graft_entry__
+    __graft_entry__.build()
+    import paper_2608_08794_gb300 as ap
+    return ap
+
+
+def i32(a):
+    return torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")
+
+
+def workspace(n=0):
+    raw = torch.zeros(max(n, 1024) + 256, dtype=torch.uint8, device="cuda")
+    return raw[(-raw.data_ptr()) % 256:][:max(n, 1024)]
+
+
+@pytest.mark.parametrize("lens,kept", [([40, 0, 25], [11, 0, 25]), ([300], [200]), ([5] * 1500, [3] * 1500)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_rows_bound_above_the_offsets(ap, lens, kept, in_place):
+    """n_out above cu_dst[B], with an index that ends there: what lies behind it names no row, and is not used."""
+    rng = np.random.default_rng(len(lens))
+    tokens, layers, spare = 8, 2, 700
+    cu_src, cu_dst = (np.concatenate([[0], np.cumsum(x)]) for x in (lens, kept))
+    keep = np.concatenate([np.sort(rng.permutation(n)[:m]) + o for n, m, o in zip(lens, kept, cu_src)])
+    need = [-(-n // tokens) for n in lens]
+    perm, at = rng.permutation(sum(need)), 0
+    table = np.full((len(lens), max(need)), -1)
+    for b, n in enumerate(need):
+        table[b, :n] = perm[at:at + n]
+        at += n
+    k, v = (torch.randn(layers, sum(need), tokens, 2, 64, device="cuda").bfloat16() for _ in range(2))
+    src = ap.PagedCache(k, v, i32(table))
+    dst = src if in_place else ap.PagedCache(torch.zeros_like(k), torch.zeros_like(v), i32(table))
+    want = [po.move_rows(a.double().cpu().numpy(), b.double().cpu().numpy(), table, table, cu_dst, keep, cu_src)
+            for a, b in ((k, dst.k), (v, dst.v))]
+    longer = i32(np.concatenate([keep, rng.choice([-5, 2 ** 31 - 1, -2 ** 31, 10 ** 6], spare)]))
+    ws, cu_src, cu_dst = workspace(), i32(cu_src), i32(cu_dst)
+    status = ap._lib.apack_paged_compact(src._address, dst._address, 0, 0, layers, longer.data_ptr(), cu_src.data_ptr(),
+                                         cu_dst.data_ptr(), len(keep) + spare, ws.data_ptr(), None)
+    assert status == ap.APACK_OK and ap.apack_device_error(ws) == ap.APACK_OK
+    torch.cuda.synchronize()
+    assert np.array_equal(dst.k.double().cpu().numpy(), want[0]) and np.array_equal(dst.v.double().cpu().numpy(), want[1])
