@@ -386,8 +386,8 @@ typedef struct apack_paged_cache {
    elements from rotary_dim on pass unchanged.  With num_axes 2 or 3 (time, height and width of a visual
    token) the first section[0] pairs take their position from axis 0, the next section[1] from axis 1 and so
    on; the sections add up to rotary_dim/2.  Angles are reduced modulo one turn in 64-bit fixed point, so
-   that far positions keep them to 2^-24 of a turn, whatever int32 the position is; arithmetic in fp32, one
-   rounding. */
+   that far positions keep them to 2^-24 of a turn, whatever int32 the position is and for frequencies of up to
+   2^40 radians (twice as far off for each doubling beyond); arithmetic in fp32, one rounding. */
 enum { APACK_ROTARY_HALF = 0, APACK_ROTARY_PAIRS = 1 };
 typedef struct apack_rotary_spec {
   int32_t layout;               /* APACK_ROTARY_* */

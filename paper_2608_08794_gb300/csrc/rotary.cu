@@ -276,6 +276,19 @@ cudaError_t launch_rotary(RotPlan &P, bool pairs_layout, bool wide, float sign, 
   return e;
 }
 
+// f radians in turns, modulo one turn, in units of 2^-64.  A position multiplies its error by up to 2^31, so 53 bits are
+// too few: 1/(2 pi) is taken as a sum of two doubles and the product with the first one whole (its rounding from an fma).
+// Off by at most 2 units for |f| up to 2^40; a negative frequency is the two's complement of its opposite.
+uint64_t turns_of(double f) {
+  constexpr double kHigh = 0.15915494309189535, kLow = -9.839338337591243e-18;
+  const double a = std::fabs(f), high = a * kHigh;
+  double low = std::fma(a, kLow, std::fma(a, kHigh, -high));
+  low -= std::floor(low + 0.5);
+  const uint64_t turns = static_cast<uint64_t>(std::ldexp(high - std::floor(high), 64)) +
+                         static_cast<uint64_t>(std::llrint(std::ldexp(low, 64)));
+  return f < 0 ? ~turns + 1 : turns;
+}
+
 apack_status plan_spec(const apack_rotary_spec *s, int32_t head_dim, RotPlan &P) {
   if (s->layout != APACK_ROTARY_HALF && s->layout != APACK_ROTARY_PAIRS) return APACK_EINVAL;
   if (s->rotary_dim < 2 || s->rotary_dim > head_dim || (s->rotary_dim & 1) || !s->freq_h) return APACK_EINVAL;
@@ -294,11 +307,8 @@ apack_status plan_spec(const apack_rotary_spec *s, int32_t head_dim, RotPlan &P)
   }
   P.magnitude = s->magnitude;
   for (int i = 0; i < P.pairs; ++i) {
-    const double f = s->freq_h[i] / 6.283185307179586476925286766559;
-    if (!std::isfinite(f)) return APACK_EINVAL;
-    double turns = f - std::floor(f);                       // in [0, 1]
-    if (turns >= 1.0) turns = 0.0;
-    P.freq[i] = static_cast<uint64_t>(std::ldexp(turns, 64));
+    if (!std::isfinite(s->freq_h[i])) return APACK_EINVAL;
+    P.freq[i] = turns_of(s->freq_h[i]);
   }
   return APACK_OK;
 }

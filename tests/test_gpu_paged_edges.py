@@ -1,5 +1,8 @@
 """Calls at the edges of what the paged-cache entry points allow, on the GPU."""
 
+from fractions import Fraction
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -52,3 +55,27 @@ def test_rows_bound_above_the_offsets(ap, lens, kept, in_place):
     assert status == ap.APACK_OK and ap.apack_device_error(ws) == ap.APACK_OK
     torch.cuda.synchronize()
     assert np.array_equal(dst.k.double().cpu().numpy(), want[0]) and np.array_equal(dst.v.double().cpu().numpy(), want[1])
+
+
+PI = Fraction(31415926535897932384626433832795028841971693993751, 10 ** 49)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_angles_of_any_frequency(ap, interleaved):
+    """cos and sin of position * frequency (the pair (1, 0), fp32) against exact reductions: the angle to 2^-24 of a turn,
+    sincospif to 2 ulp below 1 (2^-23), and products with 1 and 0 that are exact."""
+    freq = np.array([0.3, 1.0, 3.0, 5.0, 2 * math.pi, -0.1, -1.0, -1e-12, 1e-7, 1000.0, 1e5, -12345.678, 2.0 ** 40, 0.0, 0.9, -2.9])
+    pos = [2 ** 31 - 1, -2 ** 31, 2 ** 31 - 7, 2 ** 30 + 12345, -2 ** 30 - 99, 10 ** 6, 1, 0, -1] + [2 ** 31 - 1 - 1000 * i for i in range(55)]
+    pairs, n = len(freq), len(pos)
+    x = torch.zeros(n, 1, 2 * pairs, device="cuda")
+    lo = slice(0, None, 2) if interleaved else slice(0, pairs)
+    hi = slice(1, None, 2) if interleaved else slice(pairs, None)
+    x[:, :, lo] = 1
+    out = torch.empty_like(x)
+    ap.apack_rotary(ap.Rotary(2 * pairs, interleaved=interleaved, frequencies=freq), x, i32(pos), out)
+    turns = [[float(p * Fraction(f) / (2 * PI) - math.floor(p * Fraction(f) / (2 * PI))) for f in freq.tolist()] for p in pos]
+    angle = 2 * math.pi * np.array(turns)
+    tol = 2 * math.pi * 2.0 ** -24 + 2.0 ** -23
+    got = out.double().cpu().numpy()[:, 0]
+    assert float(np.abs(got[:, lo] - np.cos(angle)).max()) <= tol
+    assert float(np.abs(got[:, hi] - np.sin(angle)).max()) <= tol
