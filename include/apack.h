@@ -450,8 +450,11 @@ apack_status apack_rotary_append(const apack_rotary_spec *spec, const apack_page
    [num_seqs][Hq] or NULL, ln sum_r exp(scale q.k).  Hq / Hkv <= 32 (APACK_EUNSUPPORTED otherwise), Hq <= 1024.
    fp32 softmax and accumulation; the sums' order depends on the lengths alone (deterministic).
    A length below 0 or above max_pages*page_tokens is read as the nearest of the two, and a page number outside
-   the pool as a page of zeros; both record APACK_EDEVICE in the error word of ws.  So do lengths that add up to more
-   than some 1e10 tokens (shared pages), and nothing is computed.
+   the pool as a page of zeros; both record APACK_EDEVICE in the error word of ws.  So do lengths (over shared pages)
+   whose list of work passes 2^31 - 1025 entries, and the outputs of sequences that are not empty are left as they are.
+   With h the largest divisor of Hkv up to 8 (up to 4 if Hq / Hkv > 16), a sequence of n > 0 tokens has
+   Hkv / h * (ceil(n D / 2048) + 24 / h) entries (24 / h rounded down), and the first 24 / h are not counted: some 3.4e10
+   tokens for D = 128 and Hkv up to 8, 1.4e8 for 251 KV heads.
    ws: 256-byte aligned, apack_paged_decode_workspace_size bytes (for this pool and Hq, whatever the lengths;
    query it on the device that runs the call), its error word (first 16 bytes) zeroed once by the caller.
    Two captured graphs may share a workspace as long as they do not overlap.  Two kernel launches. */

@@ -79,3 +79,28 @@ def test_angles_of_any_frequency(ap, interleaved):
     got = out.double().cpu().numpy()[:, 0]
     assert float(np.abs(got[:, lo] - np.cos(angle)).max()) <= tol
     assert float(np.abs(got[:, hi] - np.sin(angle)).max()) <= tol
+
+
+@pytest.mark.parametrize("hq,hkv,h", [(251, 251, 1), (244, 244, 4), (5 * 47, 5 * 47, 5), (17 * 60, 60, 4)])
+def test_work_beyond_the_list_is_reported(ap, hq, hkv, h):
+    """4096 sequences over one shared page, one tile beyond 2^31 - 1025 entries by the formula of the header: nothing is
+    computed but the empty sequence's zeros.  (One tile below the limit would be work of seconds.)"""
+    B, tokens, tile, limit = 4096, 2048, 32, 2 ** 31 - 1025
+    cost, groups = 24 // h, hkv // h
+    full = B - 2                                              # sequences of as many tiles, one shorter, one empty
+    tiles = (limit + cost) // groups // (full + 1) - cost
+    lens = np.full(B, tiles * tile)
+    lens[7] = 0
+    rest = (limit + cost) // groups - full * (tiles + cost)   # entries per group left for the last sequence
+    lens[-1] = (rest + 1 - cost) * tile
+    total = sum(groups * (-(-int(n) // tile) + cost) for n in lens if n) - cost
+    assert 0 <= limit - (total - groups) < groups and total > limit
+    columns = -(-int(lens.max()) // tokens)
+    k = torch.zeros(1, 1, tokens, hkv, 64, dtype=torch.bfloat16, device="cuda")
+    cache = ap.PagedCache(k, k.clone(), torch.zeros(B, columns, dtype=torch.int32, device="cuda"))
+    q = torch.zeros(B, hq, 64, dtype=torch.bfloat16, device="cuda")
+    out = torch.full((B, hq, 64), 3.5, dtype=torch.bfloat16, device="cuda")
+    ws = workspace(ap.apack_paged_decode_workspace_size(cache, hq))
+    ap.apack_paged_decode_attention(cache, 0, i32(lens), q, out, ws)
+    assert ap.apack_device_error(ws) == ap.APACK_EDEVICE
+    assert not out[7].any() and bool((out[:7] == 3.5).all()) and bool((out[8:] == 3.5).all())
