@@ -412,8 +412,8 @@ apack_status apack_rotary_frequencies(int32_t rotary_dim, double base, int32_t s
                                       float *magnitude_h);
 
 /* Rotates num_heads heads of D elements in each of n_tokens rows.  x: token t's heads, back to back, at
-   x + t*x_token_stride bytes; out likewise; out == x with equal strides rotates in place, and the two must not
-   overlap otherwise.  positions: int32, axis a's position of token t at positions[a*pos_axis_stride + t].
+   x + t*x_token_stride bytes; out likewise; out == x with equal strides rotates in place, and no row of out may
+   overlap one of x otherwise (APACK_EINVAL).  positions: int32, axis a's position of token t at positions[a*pos_axis_stride + t].
    transpose non-zero: the transposed map, the gradient with respect to x of a rotation (it turns back by the
    same angles and keeps the magnitude).  dtype: APACK_BF16, APACK_FP16 or APACK_FP32.  head_dim: 2 .. 256,
    even.  x and out aligned to the element; 16-byte aligned rows and rotary_dim, head_dim multiples of 16 take
@@ -427,7 +427,7 @@ apack_status apack_rotary(const apack_rotary_spec *spec, int32_t dtype, int64_t 
    sequence t, n_tokens <= num_seqs); a negative row writes neither key nor value (padding of a captured batch;
    its query is rotated all the same).  No two tokens of a call may name one slot.  q [n][num_q_heads][D] (at
    any token stride, as k and v: slices of one projection's output), q_out likewise (q_out == q with equal strides in
-   place), k and v [n][num_kv_heads][D]; dtype and D of the cache; every pointer and stride a multiple of 16
+   place; otherwise no row of it may overlap one of q, k or v, APACK_EINVAL), k and v [n][num_kv_heads][D]; dtype and D of the cache; every pointer and stride a multiple of 16
    bytes.  spec NULL: nothing is rotated.  num_q_heads 0 .. 1024; with 0, q and q_out are NULL (keys and values
    alone).
    ws: NULL, or a workspace whose error word (its first 16 bytes) receives APACK_EDEVICE when a row lies behind

@@ -320,6 +320,25 @@ bool aligned16(std::initializer_list<int64_t> v) {
 }
 int64_t addr(const void *p) { return static_cast<int64_t>(reinterpret_cast<uintptr_t>(p)); }
 
+// Whether any of n rows of `row_a` bytes, stride_a apart from a on, shares a byte with any of n rows at b.
+bool rows_overlap(int64_t n, int64_t a, int64_t stride_a, int64_t row_a, int64_t b, int64_t stride_b, int64_t row_b) {
+  if (n == 1) stride_a = stride_b = 0;
+  if (a + (n - 1) * stride_a + row_a <= b || b + (n - 1) * stride_b + row_b <= a) return false;
+  if (n == 1) return true;
+  if (stride_a == stride_b) {            // rows i and j: -row_b < b - a + (j - i) stride < row_a
+    const int64_t d = b - a + row_b;     // the least j - i above -d / stride
+    const int64_t least = d >= 0 ? -((d - 1 + stride_a) / stride_a) + 1 : -d / stride_a + 1;
+    const int64_t m = std::max(least, 1 - n);
+    return m < n && b - a + m * stride_a < row_a;
+  }
+  for (int64_t i = std::max<int64_t>(0, (b - a - row_a) / stride_a); i < n && a + i * stride_a < b + (n - 1) * stride_b + row_b; ++i) {
+    const int64_t at = a + i * stride_a, d = at - b - row_b;   // the first row of b that ends behind `at`
+    const int64_t j = d < 0 ? 0 : d / stride_b + 1;
+    if (j < n && b + j * stride_b < at + row_a) return true;
+  }
+  return false;
+}
+
 // Chunks of 16 bytes fit the rotated part, its halves and the rest of the head.
 bool wide_heads(int32_t rotary_dim, int32_t head_dim, int size) {
   const int w = 16 / size;
@@ -378,7 +397,9 @@ apack_status apack_rotary(const apack_rotary_spec *spec, int32_t dtype, int64_t 
   if (n_tokens == 0) return APACK_OK;
   if (!x || !out || !positions || addr(x) % size || addr(out) % size || (addr(positions) & 3)) return APACK_EINVAL;
   if (spec->num_axes > 1 && pos_axis_stride < n_tokens) return APACK_EINVAL;
-  if (x == out && x_token_stride != out_token_stride && n_tokens > 1) return APACK_EINVAL;
+  if (!(x == out && (n_tokens == 1 || x_token_stride == out_token_stride)) &&
+      rows_overlap(n_tokens, addr(x), x_token_stride, row, addr(out), out_token_stride, row))
+    return APACK_EINVAL;
   P.heads = P.rot_heads = P.q_heads = num_heads;
   P.head_dim = head_dim;
   P.n_tokens = n_tokens;
@@ -427,7 +448,13 @@ apack_status apack_rotary_append(const apack_rotary_spec *spec, const apack_page
       ((addr(rows) | addr(seqs) | addr(positions) | addr(ws)) & 3))
     return APACK_EINVAL;
   if (n_tokens > 1 && ((q && (q_token_stride < qrow || q_out_token_stride < qrow)) || k_token_stride < kvrow ||
-                       v_token_stride < kvrow || (q && q == q_out && q_token_stride != q_out_token_stride)))
+                       v_token_stride < kvrow))
+    return APACK_EINVAL;
+  auto q_out_over = [&](const void *p, int64_t stride, int64_t bytes) {
+    return rows_overlap(n_tokens, addr(q_out), q_out_token_stride, qrow, addr(p), stride, bytes);
+  };
+  if (q && ((!(q == q_out && (n_tokens == 1 || q_token_stride == q_out_token_stride)) && q_out_over(q, q_token_stride, qrow)) ||
+            q_out_over(k, k_token_stride, kvrow) || q_out_over(v, v_token_stride, kvrow)))
     return APACK_EINVAL;
   if (spec && spec->num_axes > 1 && pos_axis_stride < n_tokens) return APACK_EINVAL;
   P.q_heads = num_q_heads;

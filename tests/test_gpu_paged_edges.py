@@ -104,3 +104,35 @@ def test_work_beyond_the_list_is_reported(ap, hq, hkv, h):
     ap.apack_paged_decode_attention(cache, 0, i32(lens), q, out, ws)
     assert ap.apack_device_error(ws) == ap.APACK_EDEVICE
     assert not out[7].any() and bool((out[:7] == 3.5).all()) and bool((out[8:] == 3.5).all())
+
+
+def test_outputs_between_the_rows_that_are_read(ap):
+    """Slices of one buffer that share no byte, although their ranges do: as written elsewhere."""
+    torch.manual_seed(0)
+    n, rot, pos = 37, ap.Rotary(64), i32(np.arange(37) * 977)
+    wide = torch.randn(n, 12, 64, device="cuda").bfloat16()
+    x, want = wide[:, 2:6], torch.empty(n, 4, 64, dtype=torch.bfloat16, device="cuda")
+    ap.apack_rotary(rot, x, pos, want)
+    for out in (wide[:, 6:10], wide[:, 8:12]):
+        before = wide.clone()
+        ap.apack_rotary(rot, x, pos, out)
+        assert torch.equal(out, want)
+        out.copy_(before[:, out.storage_offset() // 64:][:, :4])
+        assert torch.equal(wide, before)
+    # behind the last row read, with another stride
+    flat = torch.randn(4000 + n * 64, device="cuda").bfloat16()
+    x, out = flat[:13 * 300].view(13, 300)[:, :64].view(13, 1, 64), flat[13 * 300 - 236:][:13 * 64].view(13, 1, 64)
+    want = torch.empty(13, 1, 64, dtype=torch.bfloat16, device="cuda")
+    ap.apack_rotary(rot, x, pos[:13], want)
+    ap.apack_rotary(rot, x, pos[:13], out)
+    assert torch.equal(out, want)
+    # the append: queries into the heads behind the values, and one token's queries in place under another stride
+    k, v = (torch.zeros(1, n, 1, 2, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    cache = ap.PagedCache(k, v, torch.arange(n, dtype=torch.int32, device="cuda").view(n, 1))
+    zeros = torch.zeros(n, dtype=torch.int32, device="cuda")
+    q_want = torch.empty(n, 4, 64, dtype=torch.bfloat16, device="cuda")
+    ap.apack_rotary_append(rot, cache, 0, wide[:, :4], wide[:, 4:6], wide[:, 6:8], q_want, pos, zeros)
+    k_want, v_want = k.clone(), wide[:, 6:8].clone()
+    k.zero_(), v.zero_()
+    ap.apack_rotary_append(rot, cache, 0, wide[:, :4], wide[:, 4:6], wide[:, 6:8], wide[:, 8:], pos, zeros)
+    assert torch.equal(wide[:, 8:], q_want) and torch.equal(k, k_want) and torch.equal(v.flatten(0, 2), v_want)
