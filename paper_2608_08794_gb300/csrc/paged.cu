@@ -1,4 +1,6 @@
 // paged.cu -- host side of the paged key-value cache: descriptor checks and TMA maps.
+#include <algorithm>
+
 #include "paged.cuh"
 
 namespace apack {
@@ -30,6 +32,24 @@ bool on_current_device(const void *p) {
     return false;
   }
   return at.type == cudaMemoryTypeManaged || (at.type == cudaMemoryTypeDevice && at.device == dev);
+}
+
+bool rows_overlap(int64_t n, int64_t a, int64_t stride_a, int64_t row_a, int64_t b, int64_t stride_b, int64_t row_b) {
+  if (n == 1) stride_a = stride_b = 0;
+  if (a + (n - 1) * stride_a + row_a <= b || b + (n - 1) * stride_b + row_b <= a) return false;
+  if (n == 1) return true;
+  if (stride_a == stride_b) {            // rows i and j: -row_b < b - a + (j - i) stride < row_a
+    const int64_t d = b - a + row_b;     // the least j - i above -d / stride
+    const int64_t least = d >= 0 ? -((d - 1 + stride_a) / stride_a) + 1 : -d / stride_a + 1;
+    const int64_t m = std::max(least, 1 - n);
+    return m < n && b - a + m * stride_a < row_a;
+  }
+  for (int64_t i = std::max<int64_t>(0, (b - a - row_a) / stride_a); i < n && a + i * stride_a < b + (n - 1) * stride_b + row_b; ++i) {
+    const int64_t at = a + i * stride_a, d = at - b - row_b;   // the first row of b that ends behind `at`
+    const int64_t j = d < 0 ? 0 : d / stride_b + 1;
+    if (j < n && b + j * stride_b < at + row_a) return true;
+  }
+  return false;
 }
 
 apack_status validate_pool(const apack_paged_cache *c, bool table) {

@@ -54,6 +54,8 @@ struct PoolView {
 // page table.
 apack_status validate_pool(const apack_paged_cache *c, bool table);
 PoolView pool_view(const apack_paged_cache *c, int32_t layer);
+// Whether any of n rows of `row_a` bytes, stride_a apart from a on, shares a byte with any of n rows at b.
+bool rows_overlap(int64_t n, int64_t a, int64_t stride_a, int64_t row_a, int64_t b, int64_t stride_b, int64_t row_b);
 // Whether p is device memory of the current device (or managed memory).
 bool on_current_device(const void *p);
 

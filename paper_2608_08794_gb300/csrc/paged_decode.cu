@@ -20,8 +20,8 @@
 // same 8 rows, and the tensor work is far below what the read allows either way (on contiguous caches the tcgen05
 // kernel of decode_tc.cu takes 50.6 us for the ten-minute cache).
 //
-// Measured (28/4 heads of 128, bf16, 16-token pages, calls in a row): 135,272 tokens (64-token pages) 50.4 us, 5.5 TB/s, 0.81 of
-// the copy rate, of which the chunk kernel 45 us (0.9); 16 caches of 600 to 12,000 tokens 34.1 us; 473 tokens 8.3 us.
+// Measured (28/4 heads of 128, bf16, 16-token pages, calls in a row): 135,272 tokens (64-token pages) 50.4 us, 5.5 TB/s,
+// 0.81 of the copy rate, of which the chunk kernel 45 us (0.9); 16 caches of 600 to 12,000 tokens 34.1 us; 473 tokens 8.3 us.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -1050,9 +1050,10 @@ apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_
       (reinterpret_cast<uintptr_t>(out) & 15) || (reinterpret_cast<uintptr_t>(ws) & 255) ||
       ((reinterpret_cast<uintptr_t>(seqlens) | reinterpret_cast<uintptr_t>(lse)) & 3))
     return APACK_EINVAL;
-  const uintptr_t q0 = reinterpret_cast<uintptr_t>(q), q1 = q0 + (cache->num_seqs - 1) * q_token_stride + row;
-  const uintptr_t o0 = reinterpret_cast<uintptr_t>(out), o1 = o0 + cache->num_seqs * row * (out_dtype == APACK_FP32 ? 2 : 1);
-  if (q0 < o1 && o0 < q1) return APACK_EINVAL;
+  const int64_t out_row = row * (out_dtype == APACK_FP32 ? 2 : 1);
+  if (rows_overlap(cache->num_seqs, static_cast<int64_t>(reinterpret_cast<uintptr_t>(q)), q_token_stride, row,
+                   static_cast<int64_t>(reinterpret_cast<uintptr_t>(out)), out_row, out_row))
+    return APACK_EINVAL;
   if (ws_bytes < s.total) return APACK_EWORKSPACE;
   if (!on_current_device(cache->k) || !on_current_device(cache->v)) return APACK_EINVAL;   // read by TMA
   PdPlan P;

@@ -136,3 +136,29 @@ def test_outputs_between_the_rows_that_are_read(ap):
     k.zero_(), v.zero_()
     ap.apack_rotary_append(rot, cache, 0, wide[:, :4], wide[:, 4:6], wide[:, 6:8], wide[:, 8:], pos, zeros)
     assert torch.equal(wide[:, 8:], q_want) and torch.equal(k, k_want) and torch.equal(v.flatten(0, 2), v_want)
+
+
+@pytest.mark.parametrize("out_dtype", [torch.bfloat16, torch.float32])
+def test_attention_output_between_query_rows(ap, out_dtype):
+    """Query rows far apart, the contiguous output in a gap between them: no byte is shared, and the call is taken."""
+    torch.manual_seed(1)
+    k, v = (torch.randn(1, 4, 16, 2, 64, device="cuda").bfloat16() for _ in range(2))
+    cache = ap.PagedCache(k, v, i32([[0, 1], [2, 3]]))
+    rows = torch.randn(12, 4, 64, device="cuda").bfloat16()
+    q = rows[::7][:2]                                           # rows 0 and 7
+    ws = workspace(ap.apack_paged_decode_workspace_size(cache, 4))
+    want = torch.empty(2, 4, 64, dtype=out_dtype, device="cuda")
+    ap.apack_paged_decode_attention(cache, 0, i32([20, 31]), q, want, ws)
+    size = 2 if out_dtype == torch.bfloat16 else 4
+    for first in (1, 7 - size, 8):
+        before = rows.clone()
+        out = rows[first:first + size].view(out_dtype).reshape(-1).view(2, 4, 64)
+        ap.apack_paged_decode_attention(cache, 0, i32([20, 31]), q, out, ws)
+        assert torch.equal(out, want)
+        rows[first:first + size] = before[first:first + size]
+        assert torch.equal(rows, before)
+    for first in (0, 7 - size + 1, 7):
+        out = rows[first:first + size].view(out_dtype).reshape(-1).view(2, 4, 64)
+        with pytest.raises(ap.ApackError) as e:
+            ap.apack_paged_decode_attention(cache, 0, i32([20, 31]), q, out, ws)
+        assert e.value.status == ap.APACK_EINVAL
