@@ -413,7 +413,8 @@ apack_status apack_rotary_frequencies(int32_t rotary_dim, double base, int32_t s
 
 /* Rotates num_heads heads of D elements in each of n_tokens rows.  x: token t's heads, back to back, at
    x + t*x_token_stride bytes; out likewise; out == x with equal strides rotates in place, and no row of out may
-   overlap one of x otherwise (APACK_EINVAL).  positions: int32, axis a's position of token t at positions[a*pos_axis_stride + t].
+   overlap one of x otherwise (APACK_EINVAL).  positions: int32, axis a's position of token t at
+   positions[a*pos_axis_stride + t]; pos_axis_stride >= n_tokens, or 0: one position for all axes (a text token).
    transpose non-zero: the transposed map, the gradient with respect to x of a rotation (it turns back by the
    same angles and keeps the magnitude).  dtype: APACK_BF16, APACK_FP16 or APACK_FP32.  head_dim: 2 .. 256,
    even.  x and out aligned to the element; 16-byte aligned rows and rotary_dim, head_dim multiples of 16 take

@@ -573,11 +573,12 @@ class Rotary:
         self._address = ctypes.addressof(self.struct)
 
     def _positions(self, positions, n):
-        """Checks int32 [n] or [axes, n]; returns the stride between axes."""
+        """Checks int32 [n] or [axes, n] (expanded from one axis, where all share it); returns the stride between axes."""
         dims, stride = positions.shape, positions.stride()
         if str(positions.dtype) != "torch.int32" or not (
                 dims == (self.num_axes, n) or (self.num_axes == 1 and dims == (n,))) or (stride[-1] != 1 and n > 1):
-            raise ValueError(f"positions: int32 [{self.num_axes}, {n}] expected, not {positions.dtype} {tuple(dims)}")
+            raise ValueError(f"positions: int32 [{self.num_axes}, {n}], tokens contiguous, expected, not "
+                             f"{positions.dtype} {tuple(dims)}")
         return stride[0] if self.num_axes > 1 else n
 
 
@@ -654,6 +655,8 @@ def apack_rotary_append(rotary, cache, layer, q, k, v, q_out, positions, rows, s
         qs, qos = (qs[0], qos[0]) if n > 1 else (heads * dim, heads * dim)
         q_at, q_out_at = q.data_ptr(), q_out.data_ptr()
     if rotary is not None:
+        if positions is None:
+            raise ValueError("positions: expected with a rotation")
         axes, axis = rotary.num_axes, positions.stride()
         if positions.dtype is _int32_type and positions.shape == ((axes, n) if axes > 1 else (n,)) and axis[-1] == 1:
             axis = axis[0] if axes > 1 else n

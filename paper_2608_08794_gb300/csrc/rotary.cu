@@ -377,7 +377,7 @@ apack_status apack_rotary(const apack_rotary_spec *spec, int32_t dtype, int64_t 
     return APACK_EINVAL;
   if (n_tokens == 0) return APACK_OK;
   if (!x || !out || !positions || addr(x) % size || addr(out) % size || (addr(positions) & 3)) return APACK_EINVAL;
-  if (spec->num_axes > 1 && pos_axis_stride < n_tokens) return APACK_EINVAL;
+  if (spec->num_axes > 1 && pos_axis_stride != 0 && pos_axis_stride < n_tokens) return APACK_EINVAL;
   if (!(x == out && (n_tokens == 1 || x_token_stride == out_token_stride)) &&
       rows_overlap(n_tokens, addr(x), x_token_stride, row, addr(out), out_token_stride, row))
     return APACK_EINVAL;
@@ -437,7 +437,7 @@ apack_status apack_rotary_append(const apack_rotary_spec *spec, const apack_page
   if (q && ((!(q == q_out && (n_tokens == 1 || q_token_stride == q_out_token_stride)) && q_out_over(q, q_token_stride, qrow)) ||
             q_out_over(k, k_token_stride, kvrow) || q_out_over(v, v_token_stride, kvrow)))
     return APACK_EINVAL;
-  if (spec && spec->num_axes > 1 && pos_axis_stride < n_tokens) return APACK_EINVAL;
+  if (spec && spec->num_axes > 1 && pos_axis_stride != 0 && pos_axis_stride < n_tokens) return APACK_EINVAL;
   P.q_heads = num_q_heads;
   P.kv_heads = cache->num_kv_heads;
   P.heads = num_q_heads + 2 * cache->num_kv_heads;

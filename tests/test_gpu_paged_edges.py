@@ -162,3 +162,25 @@ def test_attention_output_between_query_rows(ap, out_dtype):
         with pytest.raises(ap.ApackError) as e:
             ap.apack_paged_decode_attention(cache, 0, i32([20, 31]), q, out, ws)
         assert e.value.status == ap.APACK_EINVAL
+
+
+@pytest.mark.parametrize("n", [1, 5, 700])
+def test_positions_that_the_axes_share(ap, n):
+    """One row of positions expanded over three axes: what three equal rows give."""
+    torch.manual_seed(n)
+    rot = ap.Rotary(128, sections=[16, 24, 24])
+    x = torch.randn(n, 8, 128, device="cuda").bfloat16()
+    pos = torch.randint(0, 2 ** 30, (n,), dtype=torch.int32, device="cuda")
+    outs = []
+    for p in (pos.expand(3, n).contiguous(), pos.expand(3, n), pos.view(1, n).expand(3, n)):
+        out = torch.empty_like(x)
+        ap.apack_rotary(rot, x, p, out)
+        k, v = (torch.zeros(1, n, 1, 2, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        cache = ap.PagedCache(k, v, torch.arange(n, dtype=torch.int32, device="cuda").view(1, n))
+        q = torch.empty_like(x[:, :4])
+        ap.apack_rotary_append(rot, cache, 0, x[:, :4], x[:, 4:6], x[:, 6:], q, p,
+                               torch.arange(n, dtype=torch.int32, device="cuda"), seqs=torch.zeros(n, dtype=torch.int32, device="cuda"))
+        outs.append((out, q, k, v))
+    for other in outs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(outs[0], other))
+    assert torch.equal(outs[0][0][:, :4], outs[0][1]) and torch.equal(outs[0][2].flatten(0, 2), outs[0][0][:, 4:6])

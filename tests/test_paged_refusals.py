@@ -1,4 +1,5 @@
-"""Outputs of the rotary calls over rows that the same call reads are refused (on the CPU: before anything is launched)."""
+"""Refusals of the rotary calls (on the CPU: before anything is launched): outputs over rows that the call reads, and
+missing positions."""
 
 import numpy as np
 import pytest
@@ -82,3 +83,11 @@ def test_overlap_of_strided_rows_against_all_bytes(ap):
                                     pos.data_ptr(), 64, 0, None)
         assert (code == ap.APACK_EINVAL) == refused, (n, heads, dim, x0, sx, o0, so)
     assert min(seen) > 30
+
+
+def test_append_without_positions_is_a_value_error(ap):
+    cache = ap.PagedCache(*(torch.zeros(1, 4, 16, 2, 64, dtype=torch.bfloat16) for _ in range(2)),
+                          torch.zeros(3, 2, dtype=torch.int32))
+    x, n = torch.zeros(3, 2, 64, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    with pytest.raises(ValueError, match="positions"):
+        ap.apack_rotary_append(ap.Rotary(64), cache, 0, x, x, x, x.clone(), None, n, stream=0)
