@@ -516,7 +516,7 @@ class PagedCache:
             raise ValueError("page_table: int32 [sequences, pages] with contiguous rows expected")
         if not k.get_device() == v.get_device() == page_table.get_device():
             raise ValueError("k, v and page_table: one device expected")
-        self.k, self.v, self.page_table = k, v, page_table
+        self._tensors = k, v, page_table
         self.dtype, self._device = k.dtype, k.get_device()
         size = k.element_size()
         layers, pages, tokens, heads, dim = k.shape
@@ -532,6 +532,11 @@ class PagedCache:
             table_stride=page_table.stride(0) if seqs > 1 else columns, num_seqs=seqs, max_pages=columns)
         self._address = ctypes.addressof(self.struct)
 
+    # struct holds their addresses: other tensors take another PagedCache
+    k = property(lambda self: self._tensors[0])
+    v = property(lambda self: self._tensors[1])
+    page_table = property(lambda self: self._tensors[2])
+
     def get_device(self):
         return self._device
 
@@ -541,7 +546,8 @@ class Rotary:
 
     scaling: "none", "linear", "ntk" or "yarn" (see apack_rotary_frequencies); frequencies: radians per position
     of the rotary_dim / 2 pairs, in the place of base and scaling.  sections: pairs per position axis (2 or 3
-    axes).  interleaved: pairs of neighbouring elements, else of the two halves."""
+    axes).  interleaved: pairs of neighbouring elements, else of the two halves.  The attributes that say what it was
+    made with are read-only."""
 
     def __init__(self, rotary_dim, base=10000.0, interleaved=False, scaling="none", factor=1.0, original_len=0,
                  beta_fast=32.0, beta_slow=1.0, sections=None, magnitude=None, frequencies=None):
@@ -552,25 +558,31 @@ class Rotary:
         pairs = max(1, int(rotary_dim) // 2)
         m = ctypes.c_float(1.0)
         if frequencies is None:
-            self.frequencies = np.zeros(pairs, np.float64)
+            frequencies = np.zeros(pairs, np.float64)
             _check(_lib.apack_rotary_frequencies(int(rotary_dim), float(base), modes[scaling], float(factor),
                                                  int(original_len), float(beta_fast), float(beta_slow),
-                                                 _host(self.frequencies), ctypes.byref(m)), "apack_rotary_frequencies")
+                                                 _host(frequencies), ctypes.byref(m)), "apack_rotary_frequencies")
         else:
-            self.frequencies = np.array(frequencies, np.float64)
-            if self.frequencies.shape != (pairs,):
+            frequencies = np.array(frequencies, np.float64)
+            if frequencies.shape != (pairs,):
                 raise ValueError(f"frequencies: {pairs} expected")
-        self.rotary_dim = int(rotary_dim)
-        self.magnitude = float(m.value if magnitude is None else magnitude)
+        self._frequencies = frequencies          # struct holds its address
         sec = [] if sections is None else [int(x) for x in sections]
         if len(sec) > 3:
             raise ValueError("sections: at most three axes")
-        self.num_axes = max(1, len(sec))
+        self._magnitude = float(m.value if magnitude is None else magnitude)
         self.struct = apack_rotary_spec(
-            layout=APACK_ROTARY_PAIRS if interleaved else APACK_ROTARY_HALF, rotary_dim=self.rotary_dim,
-            num_axes=self.num_axes, section=(ctypes.c_int32 * 3)(*(sec + [0] * (3 - len(sec)))),
-            magnitude=self.magnitude, freq_h=self.frequencies.ctypes.data_as(ctypes.POINTER(ctypes.c_double)))
+            layout=APACK_ROTARY_PAIRS if interleaved else APACK_ROTARY_HALF, rotary_dim=int(rotary_dim),
+            num_axes=max(1, len(sec)), section=(ctypes.c_int32 * 3)(*(sec + [0] * (3 - len(sec)))),
+            magnitude=self._magnitude,
+            freq_h=frequencies.ctypes.data_as(ctypes.POINTER(ctypes.c_double)))
+        self._axes = self.struct.num_axes
         self._address = ctypes.addressof(self.struct)
+
+    frequencies = property(lambda self: self._frequencies)
+    rotary_dim = property(lambda self: self.struct.rotary_dim)
+    magnitude = property(lambda self: self._magnitude)
+    num_axes = property(lambda self: self._axes)
 
     def _positions(self, positions, n):
         """Checks int32 [n] or [axes, n] (expanded from one axis, where all share it); returns the stride between axes."""
@@ -606,7 +618,7 @@ def apack_rotary(rotary, x, positions, out, transpose=False, stream=None):
         if out.dtype is not dtype or out.shape != shape or outs[2] != 1 or outs[1] != dim:
             outs = (_head_rows(out, "out", dtype, shape),)
         outs = outs[0] if n > 1 else heads * dim
-    axes, axis = rotary.num_axes, positions.stride()
+    axes, axis = rotary._axes, positions.stride()
     if positions.dtype is _int32_type and positions.shape == ((axes, n) if axes > 1 else (n,)) and axis[-1] == 1:
         axis = axis[0] if axes > 1 else n
     else:
@@ -657,7 +669,7 @@ def apack_rotary_append(rotary, cache, layer, q, k, v, q_out, positions, rows, s
     if rotary is not None:
         if positions is None:
             raise ValueError("positions: expected with a rotation")
-        axes, axis = rotary.num_axes, positions.stride()
+        axes, axis = rotary._axes, positions.stride()
         if positions.dtype is _int32_type and positions.shape == ((axes, n) if axes > 1 else (n,)) and axis[-1] == 1:
             axis = axis[0] if axes > 1 else n
         else:

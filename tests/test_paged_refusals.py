@@ -91,3 +91,20 @@ def test_append_without_positions_is_a_value_error(ap):
     x, n = torch.zeros(3, 2, 64, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
     with pytest.raises(ValueError, match="positions"):
         ap.apack_rotary_append(ap.Rotary(64), cache, 0, x, x, x, x.clone(), None, n, stream=0)
+
+
+def test_handles_keep_what_they_were_made_with(ap):
+    """The structures hold addresses of the arrays and tensors: nothing else can take their place."""
+    rot = ap.Rotary(128, frequencies=np.arange(64.0))
+    cache = ap.PagedCache(*(torch.zeros(1, 4, 16, 2, 64, dtype=torch.bfloat16) for _ in range(2)),
+                          torch.zeros(3, 2, dtype=torch.int32))
+    for handle, names in ((rot, ("frequencies", "rotary_dim", "magnitude", "num_axes")), (cache, ("k", "v", "page_table"))):
+        for name in names:
+            with pytest.raises(AttributeError):
+                setattr(handle, name, getattr(handle, name))
+    junk = [np.full(64, 7.5) for _ in range(300)]
+    assert [rot.struct.freq_h[i] for i in range(64)] == list(range(64)) and len(junk) == 300
+    assert (cache.struct.k, cache.struct.v, cache.struct.page_table) == (
+        cache.k.data_ptr(), cache.v.data_ptr(), cache.page_table.data_ptr())
+    assert (rot.rotary_dim, rot.magnitude, rot.num_axes) == (128, 1.0, 1)
+    assert ap.Rotary(128, sections=[16, 24, 24], magnitude=1.1).num_axes == 3
