@@ -445,7 +445,8 @@ apack_status apack_rotary_append(const apack_rotary_spec *spec, const apack_page
    the lengths on the DEVICE, so that a captured call follows growing caches.  An empty sequence gives zeros
    and an lse of -infinity; what lies behind a sequence's last row (infinities and NaN too) has no influence.
    A NaN or infinity among the rows themselves makes what it enters NaN (an infinite value: infinite or NaN).
-   q: [num_seqs][Hq][D] at q_token_stride bytes, cache dtype, 16-byte aligned; scale > 0 (1/sqrt(D) is usual).
+   q: [num_seqs][Hq][D] at q_token_stride bytes, cache dtype, 16-byte aligned; scale > 0, finite times log2(e)
+   too (1/sqrt(D) is usual).
    out: [num_seqs][Hq][D], contiguous, 16-byte aligned, out_dtype the cache's or APACK_FP32; it must not overlap q
    (APACK_EINVAL).  lse: fp32
    [num_seqs][Hq] or NULL, ln sum_r exp(scale q.k).  Hq / Hkv <= 32 (APACK_EUNSUPPORTED otherwise), Hq <= 1024.

@@ -1042,7 +1042,8 @@ apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_
   PdShape s;
   st = plan_shape(cache, num_q_heads, &s);
   if (st != APACK_OK) return st;
-  if (layer < 0 || layer >= cache->num_layers || !seqlens || !q || !out || !ws || !(scale > 0.f) || !std::isfinite(scale))
+  if (layer < 0 || layer >= cache->num_layers || !seqlens || !q || !out || !ws || !(scale > 0.f) ||
+      !std::isfinite(scale * 1.4426950408889634f))
     return APACK_EINVAL;
   if (out_dtype != cache->dtype && out_dtype != APACK_FP32) return APACK_EINVAL;
   const int64_t row = static_cast<int64_t>(num_q_heads) * cache->head_dim * 2;

@@ -184,3 +184,26 @@ def test_positions_that_the_axes_share(ap, n):
     for other in outs[1:]:
         assert all(torch.equal(a, b) for a, b in zip(outs[0], other))
     assert torch.equal(outs[0][0][:, :4], outs[0][1]) and torch.equal(outs[0][2].flatten(0, 2), outs[0][0][:, 4:6])
+
+
+def test_scales_at_the_ends_of_fp32(ap):
+    """The kernel works with scale * log2(e): what overflows there is refused, and the largest and smallest scales that do
+    not give logits of any size (here 0 and ln 2: the softmax is 1/3 and 2/3)."""
+    k = torch.zeros(1, 1, 16, 1, 64, dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    v[0, 0, 1] = 3
+    cache = ap.PagedCache(k, v, i32([[0]]))
+    ws = workspace(ap.apack_paged_decode_workspace_size(cache, 1))
+    q, out = torch.zeros(1, 1, 64, dtype=torch.bfloat16, device="cuda"), torch.empty(1, 1, 64, device="cuda")
+    for scale in (3e38, 2.4e38):
+        with pytest.raises(ap.ApackError) as e:
+            ap.apack_paged_decode_attention(cache, 0, i32([2]), q, out, ws, scale=scale)
+        assert e.value.status == ap.APACK_EINVAL
+    for scale in (2.0 ** 127, 2.0 ** -100, 1.0):
+        # ln 2 = scale q k for a power of two of the scale, q k a bf16 number: 0.69140625 of it
+        e = -round(math.log2(scale))
+        k[0, 0, 1, 0, 0] = 0.69140625 * 2.0 ** (e // 2)
+        q[0, 0, 0] = 2.0 ** (e - e // 2)
+        ap.apack_paged_decode_attention(cache, 0, i32([2]), q, out, ws, scale=scale)
+        p = math.exp(0.69140625)
+        assert abs(float(out[0, 0, 0]) - 3 * p / (1 + p)) <= 2.0 ** -19 * 3
