@@ -91,7 +91,8 @@ PoolView pool_view(const apack_paged_cache *c, int32_t layer) {
   return p;
 }
 
-bool make_page_map(CUtensorMap *map, const apack_paged_cache *c, const void *layer_base, uint32_t box_tokens) {
+bool make_page_map(CUtensorMap *map, const apack_paged_cache *c, const void *layer_base, uint32_t box_tokens,
+                   uint32_t box_blocks) {
   const EncodeTiledFn fn = encode_tiled_fn();
   if (!fn) return false;
   const cuuint64_t dims[5] = {64, static_cast<cuuint64_t>(c->page_tokens), static_cast<cuuint64_t>(c->head_dim / 64),
@@ -100,7 +101,7 @@ bool make_page_map(CUtensorMap *map, const apack_paged_cache *c, const void *lay
   const cuuint64_t strides[4] = {static_cast<cuuint64_t>(c->page_tokens > 1 ? c->token_stride : 128), 128,
                                  static_cast<cuuint64_t>(c->num_kv_heads > 1 ? c->head_stride : 128),
                                  static_cast<cuuint64_t>(c->num_pages > 1 ? c->page_stride : 128)};
-  const cuuint32_t box[5] = {64, box_tokens, static_cast<cuuint32_t>(c->head_dim / 64), 1, 1};
+  const cuuint32_t box[5] = {64, box_tokens, box_blocks, 1, 1};
   const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 5, const_cast<void *>(layer_base), dims, strides, box, estr,
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,

@@ -60,7 +60,8 @@ bool rows_overlap(int64_t n, int64_t a, int64_t stride_a, int64_t row_a, int64_t
 bool on_current_device(const void *p);
 
 // 5-D TMA map of one layer's K (or V): {64 features, token in page, 64-feature block, head, page}, boxes of
-// box_tokens tokens of one head, 128-byte swizzle; pages outside the pool read as zeros.
-bool make_page_map(CUtensorMap *map, const apack_paged_cache *c, const void *layer_base, uint32_t box_tokens);
+// box_tokens tokens and box_blocks blocks of one head, 128-byte swizzle; pages outside the pool read as zeros.
+bool make_page_map(CUtensorMap *map, const apack_paged_cache *c, const void *layer_base, uint32_t box_tokens,
+                   uint32_t box_blocks);
 
 }  // namespace apack

@@ -10,7 +10,7 @@
 // Split over the cache's length.  The work is the list of all (sequence, head group, tile) in that order; every CTA
 // takes an equal contiguous share of it and finds its start from the lengths on the device, so that the launch does
 // not depend on them (a captured call follows growing caches).  Within a CTA a KV head has wph ring buffers of stages
-// (filled by TMA from pages of a multiple of 16 tokens), each for every wph-th tile of the share; a ring is read by
+// (filled by TMA from pages of a multiple of 8 or 16 tokens), each for every wph-th tile of the share; a ring is read by
 // one warp of 8 or 16 query rows, or with more than 16 rows per KV head by 2 warps of 16.  Its first warp refills a
 // stage as soon as it has been used.  At the end of a (sequence, head group) the warps of a head merge through shared
 // memory; what a share holds whole is written out, what it holds in part goes to the workspace, and a second kernel
@@ -61,7 +61,7 @@ struct PdPlan {
   int32_t hq, group;                 // query heads, per KV head
   int32_t heads_cta, groups;         // KV heads of a CTA, head groups
   int32_t wph_log, rg_log;           // log2 of the rings per head, and of the groups of 8 query rows
-  int32_t boxes;                     // TMA boxes of a tile, 1 or 2; 0: its rows are copied by the lanes
+  int32_t boxes;                     // TMA boxes of a tile: of 16 or 32 tokens, or (NG 1) of 8; 0: its rows are copied by the lanes
   int32_t max_rows;
   int32_t wide_lengths;              // seqlens can be read four at a time
   int32_t seg_cost;                  // what a segment costs beyond its tiles, in tiles
@@ -411,7 +411,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       q_t = t;
       q_len = w.len;
       q_head = w.g * P.heads_cta + hw;
-      if (P.boxes) {
+      if (P.boxes && P.boxes <= KM) {
         const uint32_t p = P.pool.page_tokens.div(t * kTile);
         const int32_t *row = P.pool.table + w.b * P.pool.table_stride + p;
         q_in = t * kTile - p * P.pool.page_tokens.d;
@@ -431,14 +431,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     head_t = __shfl_sync(0xffffffffu, t, 31) + wph;
   };
   // One TMA box pair; a page outside the pool reads as zeros (the map ends there).
-  auto load_box = [&](int slot, int32_t page, uint32_t in_page, int head, int b, uint32_t offset) {
+  auto load_box = [&](int slot, int32_t page, uint32_t in_page, int head, int b, int block, uint32_t offset) {
     if (static_cast<uint32_t>(page) >= static_cast<uint32_t>(P.pool.num_pages)) {
       raise_device_error(P.err, APACK_EDEVICE, 82, b, page);
       page = P.pool.num_pages;
     }
     const uint32_t dst = ring + slot * kStageBytes + offset;
-    tma_load_5d(dst, &kmap, &full[slot], in_page, 0, head, page);
-    tma_load_5d(dst + kHalf, &vmap, &full[slot], in_page, 0, head, page);
+    tma_load_5d(dst, &kmap, &full[slot], in_page, block, head, page);
+    tma_load_5d(dst + kHalf, &vmap, &full[slot], in_page, block, head, page);
   };
   // Tile number `issued` of the warp, if there is one.
   auto issue = [&] {
@@ -449,20 +449,38 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     const int slot = issue_slot, owner = issued & 31;
     issue_slot = slot + 1 == stages ? 0 : slot + 1;
-    if (P.boxes) {
+    if (P.boxes && P.boxes <= KM) {
       if (lane == owner) {
         const bool second = KM > 1 && P.boxes > 1 && q_t * kTile + 16 < q_len;
         mbar_arrive_expect_tx(&full[slot], KM > 1 && P.boxes > 1 && !second ? kHalf : 2 * kHalf);
-        load_box(slot, q_page[0], q_in, q_head, q_b, 0);
-        if (second) load_box(slot, q_page[KM - 1], q_in + 16 >= P.pool.page_tokens.d ? 0 : q_in + 16, q_head, q_b, 2048);
+        load_box(slot, q_page[0], q_in, q_head, q_b, 0, 0);
+        if (second) load_box(slot, q_page[KM - 1], q_in + 16 >= P.pool.page_tokens.d ? 0 : q_in + 16, q_head, q_b, 0, 2048);
+      }
+      ++issued;
+      return;
+    }
+    const int t = __shfl_sync(0xffffffffu, q_t, owner), b = __shfl_sync(0xffffffffu, q_b, owner);
+    const int head = __shfl_sync(0xffffffffu, q_head, owner), len = __shfl_sync(0xffffffffu, q_len, owner);
+    const int rows = min(kTile, len - t * kTile);
+    if (NG == 1 && P.boxes) {
+      // Pages of a multiple of 8 tokens: a box of 8 per lane (and 64-feature block), those that hold a row of the sequence.
+      // Against copies by the lanes, 60,000 tokens of 4 heads of 128 in pages of 24 or 1,000: 28.9 and 29.7 us, of 8 29.5 and
+      // 30.0; 120,000 of heads of 64: 28.6 and 29.3, in pages of 8 31.0 and 30.4 (96 short caches 22.6 and 23.9).
+      // Not with two groups of rows per warp: 16-token pages would lose 1.5 to 2 % by the registers (31.1 -> 31.8, 38.3 ->
+      // 39.1 us with 16 and 32 query heads per KV head), pages of 8 gain up to 6 % (46.5 -> 43.7).
+      const int nbox = (rows + 7) / 8;
+      if (lane == 0) mbar_arrive_expect_tx(&full[slot], nbox * 8 * D * 4);
+      __syncwarp();
+      if (lane < nbox) {
+        const uint32_t row = t * kTile + lane * 8, p = P.pool.page_tokens.div(row);
+        const int32_t page = __ldg(P.pool.table + b * P.pool.table_stride + p);
+#pragma unroll
+        for (int blk = 0; blk < D / 64; ++blk)
+          load_box(slot, page, row - p * P.pool.page_tokens.d, head, b, blk, blk * kBlk + lane * 1024);
       }
     } else {
-      // Pages of no multiple of 16 tokens: rows copied by the lanes, 16 bytes at a time, to where a box would put them.
-      // A box per page is as fast down to 8 tokens (60,000 tokens: 29.5 us either way), but boxes of a row or two
-      // are bound by their number (pages of 2: 37.5 against 30.5, of 1: 50.5 against 31.3).
-      const int t = __shfl_sync(0xffffffffu, q_t, owner), b = __shfl_sync(0xffffffffu, q_b, owner);
-      const int head = __shfl_sync(0xffffffffu, q_head, owner), len = __shfl_sync(0xffffffffu, q_len, owner);
-      const int rows = min(kTile, len - t * kTile);
+      // Other pages: rows copied by the lanes, 16 bytes at a time, to where a box would put them.  Smaller boxes are bound by
+      // their number: 60,000 tokens of 4 heads of 128 in pages of 4 31.4 against 30.5 us, of 1 50.5 against 31.6.
       int64_t off = -1;
       if (lane < rows) {
         const int row = t * kTile + lane;
@@ -1072,7 +1090,7 @@ apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_
   P.groups = s.groups;
   const int tile = tile_tokens(cache->head_dim);
   const int box_tokens = std::gcd(cache->page_tokens, tile);
-  P.boxes = box_tokens < 16 ? 0 : tile / box_tokens;
+  P.boxes = box_tokens < (s.rg_log > 0 ? 16 : 8) ? 0 : tile / box_tokens;
   P.max_rows = static_cast<int32_t>(
       std::min<int64_t>(INT32_MAX - tile, static_cast<int64_t>(cache->max_pages) * cache->page_tokens));
   P.seg_cost = std::max(1, kSegBytes / (tile * s.heads_cta * cache->head_dim * 4));
@@ -1089,7 +1107,9 @@ apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_
   CUtensorMap kmap, vmap;
   std::memset(&kmap, 0, sizeof(kmap));
   std::memset(&vmap, 0, sizeof(vmap));
-  if (P.boxes && (!make_page_map(&kmap, cache, P.pool.k, box_tokens) || !make_page_map(&vmap, cache, P.pool.v, box_tokens)))
+  const uint32_t blocks = box_tokens < 16 ? 1 : cache->head_dim / 64;   // tiles keep their blocks apart
+  if (P.boxes && (!make_page_map(&kmap, cache, P.pool.k, box_tokens, blocks) ||
+                  !make_page_map(&vmap, cache, P.pool.v, box_tokens, blocks)))
     return APACK_ECUDA;
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
   if (cache->dtype == APACK_BF16)

@@ -8,6 +8,7 @@ import pytest
 import torch
 
 from oracle import paged_oracle as po
+import test_gpu_paged as base
 
 pytestmark = pytest.mark.gpu
 
@@ -207,3 +208,42 @@ def test_scales_at_the_ends_of_fp32(ap):
         ap.apack_paged_decode_attention(cache, 0, i32([2]), q, out, ws, scale=scale)
         p = math.exp(0.69140625)
         assert abs(float(out[0, 0, 0]) - 3 * p / (1 + p)) <= 2.0 ** -19 * 3
+
+
+@pytest.mark.parametrize("dim,tokens,group", [(64, 8, 2), (64, 24, 5), (128, 24, 7), (64, 40, 20), (128, 8, 32)])
+def test_bad_pages_in_boxes_of_eight_tokens(ap, dim, tokens, group):
+    """A page outside the pool is read as zeros, for the rows of it that the sequence has, and is reported."""
+    rng = np.random.default_rng(15)
+    lens = [3 * tokens - 5, tokens + 1]
+    table, pages = base.make_table(rng, lens, tokens)
+    k, v = (base.normal(rng, (1, pages + 1, tokens, 2, dim), torch.bfloat16) for _ in range(2))
+    k[0, pages], v[0, pages] = 0, 0
+    q = base.normal(rng, (2, 2 * group, dim), torch.bfloat16)
+
+    def run(t):
+        cache = ap.PagedCache(k, v, i32(t))
+        ws = workspace(ap.apack_paged_decode_workspace_size(cache, 2 * group))
+        out, lse = torch.empty(2, 2 * group, dim, device="cuda"), torch.empty(2, 2 * group, device="cuda")
+        ap.apack_paged_decode_attention(cache, 0, i32(lens), q, out, ws, lse=lse)
+        return out, lse, ap.apack_device_error(ws)
+
+    for at in ((0, 0), (0, 1), (0, 2), (1, 1)):
+        zeros = table.copy()
+        zeros[at] = pages
+        want, want_lse, code = run(zeros)
+        assert code == ap.APACK_OK and torch.isfinite(want).all()
+        for page in (-1, pages + 1, 2 ** 31 - 1, -2 ** 31):
+            bad = table.copy()
+            bad[at] = page
+            out, lse, code = run(bad)
+            assert code == ap.APACK_EDEVICE and torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("tokens", [8, 24, 56, 104])
+def test_attention_over_pages_of_eight_tokens(ap, dim, tokens):
+    """Sequences that end anywhere in a box, a page or a tile, behind which NaN and infinities lie."""
+    rng = np.random.default_rng(dim + tokens)
+    lens = list(range(1, 42)) + [tokens * i + j for i in (1, 2, 5) for j in (-1, 0, 1)] + [0, 777]
+    base.check_attention(ap, rng, lens, 12, 4, dim, tokens, "bf16", "hnd", "fp32")
+    base.check_attention(ap, rng, lens[::3], 40, 2, dim, tokens, "fp16", "nhd")
