@@ -42,7 +42,7 @@ struct RotPlan {
   int64_t whole, units;                 // tokens that a warp takes whole, and units of work in all
   int32_t splits, unit_heads;           // parts of the other tokens' heads, and heads of a part
   int32_t heads, rot_heads, q_heads;    // heads in all; the first rot_heads are rotated; q_heads of them are q
-  int32_t kv_heads, head_dim;
+  int32_t head_dim;
   int64_t n_tokens;
   const uint8_t *x, *k, *v;
   uint8_t *out;
@@ -439,7 +439,6 @@ apack_status apack_rotary_append(const apack_rotary_spec *spec, const apack_page
     return APACK_EINVAL;
   if (spec && spec->num_axes > 1 && pos_axis_stride != 0 && pos_axis_stride < n_tokens) return APACK_EINVAL;
   P.q_heads = num_q_heads;
-  P.kv_heads = cache->num_kv_heads;
   P.heads = num_q_heads + 2 * cache->num_kv_heads;
   P.rot_heads = num_q_heads + cache->num_kv_heads;
   P.head_dim = cache->head_dim;

@@ -23,6 +23,9 @@ class PagePool:
     """Pools ``k`` and ``v`` [layers, pages, page_tokens, Hkv, D], ``page_table`` [max_seqs, max_pages] and
     ``lengths`` [max_seqs] on the device, and ``cache``, the PagedCache of all of it.
 
+    A sequence has one length and one list of pages for all layers.  Layers that keep different rows (the levels of
+    a progressive schedule) take a pool each.
+
     heads_first: the heads of a page outermost in memory ([layers, pages, Hkv, page_tokens, D])."""
 
     def __init__(self, num_layers, num_pages, page_tokens, num_kv_heads, head_dim, max_seqs, max_pages=None,
@@ -248,7 +251,10 @@ class PagePool:
 
     def take(self, src, kept, keep_idx=None, cu_src=None, src_layer=0, dst_layer=0, num_layers=None, ws=None):
         """New sequences from the kept rows of another PagedCache (a prefill's contiguous caches, say: one page of
-        all tokens), kept[i] rows of its sequence i; the arguments as in apack_paged_compact.  Returns their numbers."""
+        all tokens), kept[i] rows of its sequence i; the arguments as in apack_paged_compact.  Returns their numbers.
+        Layers of the pool outside dst_layer .. dst_layer + num_layers - 1 hold what the pages held before: the caller
+        writes them (apack_paged_compact from their source, into a PagedCache of the pool and the new sequences' pages)
+        before they are read."""
         if len(kept) != src.num_seqs:
             raise ValueError(f"kept: {src.num_seqs} numbers expected")
         need = [self._need(m) for m in kept]
