@@ -284,8 +284,9 @@ uint64_t turns_of(double f) {
   const double a = std::fabs(f), high = a * kHigh;
   double low = std::fma(a, kLow, std::fma(a, kHigh, -high));
   low -= std::floor(low + 0.5);
-  const uint64_t turns = static_cast<uint64_t>(std::ldexp(high - std::floor(high), 64)) +
-                         static_cast<uint64_t>(std::llrint(std::ldexp(low, 64)));
+  constexpr double kUnit = 18446744073709551616.0;                       // 2^64
+  double whole;                                                          // (modf: no difference that could become an fma)
+  const uint64_t turns = static_cast<uint64_t>(std::modf(high, &whole) * kUnit) + static_cast<uint64_t>(std::llrint(low * kUnit));
   return f < 0 ? ~turns + 1 : turns;
 }
 
