@@ -5,7 +5,7 @@
 // token's heads are not back to back).  A CTA resolves the page of each row of its run once and then moves those
 // rows in several planes.  Measured: 24 layers of a contiguous cache, 27,144 rows to 11,844 in pages, 172.6 us, 6.7
 // TB/s, 0.99 of the copy rate; 257 pages of 28 layers 71.2 us (0.98); 13 caches of 512-byte rows, pages to pages,
-// 42.4 us (0.92); one page of 28 layers 2.2 us.
+// 42.6 us (0.91); one page of 28 layers 2.3 us.
 #include <algorithm>
 #include <cstdlib>
 #include <cstring>
@@ -140,9 +140,10 @@ __global__ void __launch_bounds__(kMoveThreads, 4) move_rows_kernel(const __grid
 // step reads have all arrived before it writes, and no later step reads a row below those this step writes.  So no
 // warp waits for another, and the loads of kDepth steps are in flight (into the warp's ring in shared memory); addresses
 // are found a step before their loads, from page numbers read two and indices read three steps before.  A step costs
-// about one trip to L2 for those.  24 layers of 27,144 rows to 11,844, 4 heads of 128: 275 us, 4.2 TB/s (514 with
-// the loads of one step of 64 rows in registers; here 306 with 64 rows, 267 with 3 steps of 128, which lose on batches);
-// 8 caches of 9,000 rows, half of them kept: 589 us, 6.0 TB/s (989 before, 706 with 3 steps).
+// about one trip to L2 for those.  24 layers of 27,144 rows to 11,844, 4 heads of 128, calls in a row: 266 us in pages of
+// 16 tokens (4.4 TB/s), 260 of 64, 221 in one page, 368 of 1; 8 caches of 9,000 rows, half of them kept, 16-token pages: 582
+// us, 6.1 TB/s.  When it was chosen (266 was 275, 582 was 589): 514 and 989 with the loads of one step of 64 rows in
+// registers, 306 and 632 or less with steps of 64 in the ring, 267 and 706 with 3 steps of 128.
 constexpr int kStep = 128, kDepth = 2, kPlaceWarps = 2;
 constexpr int place_bytes(int w) { return kPlaceWarps * kDepth * kStep * (w * 16 + 8); }
 template <int W>

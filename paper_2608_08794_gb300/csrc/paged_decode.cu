@@ -84,8 +84,8 @@ struct PdPlan {
 // kParts: a probability enters the value product as a sum of that many 16-bit numbers, so that it keeps the 24 bits that
 // the row's sum is made of: three of bf16 (8 bits each: what is left out is below 2^-26), two of fp16 (11 bits and a sign
 // each: 2^-23).  The third bf16 number costs 0.2 us of 50 or 34 (ten minutes, 16 caches), 0.5 of 31 with 16 query heads per
-// KV head and 3.7 of 38 with 32, which the matrix instructions bound (the same calls in fp16: 34.6); without it fp32 outputs
-// were 2e-6 off.
+// KV head and 3.7 of 38 with 32, where a warp's chain of instructions is the bound (0.28 issued per clock and scheduler; the
+// same call in fp16: 34.5); without it fp32 outputs were 2e-6 off.
 template <class T>
 struct Half16;
 template <>

@@ -13,8 +13,10 @@
 // Behind it comes instruction issue (2 loads, 2 stores and about 60 instructions per 16 elements), so a lane owns
 // one 16-byte chunk position of a head (both halves of its pairs) and keeps its (cos, sin) in registers over the
 // heads it walks through.  Few tokens are bound by latency: position -> angle -> product.
-// Measured: 27,144 tokens of 28/4 heads of 128 with append 80.8 us, 6.2 TB/s, 0.91 of the copy rate; 8,780 rows of 18
-// heads 17.8 us (4.5 TB/s); 61 tokens 3.3 us.
+// Measured: 27,144 tokens of 28/4 heads of 128 with append 80.8 us, 6.2 TB/s, 0.91 of the copy rate; 27,144 rows of 32
+// heads 78.1 us (0.84), fp32 144.4 (0.91); 8,780 rows of 18 heads 17.8 us (0.67), fp32 29.3 (0.82); 61 tokens 3.4 us.
+// Narrow accesses (rows or halves that are no whole 16-byte pieces) are bound by issue: the 8,780 rows 30.4 us, 27,144 of 32
+// heads with 36 of 128 elements rotated 243.
 #include <algorithm>
 #include <cmath>
 #include <cstring>

@@ -215,8 +215,8 @@ class PagePool:
         """Keeps kept[i] rows of seqs[i] (distinct): keep_idx holds them, packed over the sequences in this order
         as apack_select writes it (row r of seqs[i] is the sum of the lengths before it + r), ascending.  The kept rows
         go to new pages and the old ones are given up, or, in place, to the first of the sequences' own pages (no
-        page of which may be shared) and only the pages behind them are given up: slower (275 against 173 us for a
-        two-minute prompt's 24 layers), but no page is needed.  in_place None: in place only where there are too few
+        page of which may be shared) and only the pages behind them are given up: slower (266 against 173 us for a
+        two-minute prompt's 24 layers in 16-token pages), but no page is needed.  in_place None: in place only where there are too few
         free pages for the other way."""
         if not len(seqs) or len(set(seqs)) != len(seqs) or len(kept) != len(seqs):
             raise ValueError("distinct sequences and a number of kept rows for each expected")
