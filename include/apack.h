@@ -466,6 +466,48 @@ apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_
                                           void *out, int32_t out_dtype, float *lse, void *ws, size_t ws_bytes,
                                           void *stream);
 
+/* ---- Attention over shared rows.
+   Sequences that were forked from one (questions about one video) hold the same first pages, and one decode token each is
+   not all that a step brings: a question's tokens enter together, and so does a part of a long prompt.
+   apack_paged_group_plan lays out a step's work from lengths and groups on the DEVICE, once for all layers;
+   apack_paged_group_attention runs it on a layer:
+     out[t][h] = sum_r softmax_r(scale q[t][h] . k[r][g]) v[r][g],  g = h / (Hq / Hkv),  r <= position of token t,
+   for the new tokens t of every sequence of the batch, whose keys and values are in the cache already.
+
+   The batch: n_seqs entries (1 .. APACK_MAX_SEQS); entry e is sequence seqs[e] of the cache (device [n_seqs]; NULL:
+   sequence e), with seqlens[seqs[e]] rows (device [num_seqs]; 0 .. min(max_pages * page_tokens, 2^30)).  Its new tokens are
+   the last of them: token cu_q[e] + i (device [n_seqs + 1], rising from 0; NULL: one token each, n_q = n_seqs) is row
+   seqlens - m + i, of m = cu_q[e+1] - cu_q[e].  q has n_q tokens, cu_q[n_seqs] <= n_q; what lies behind them is neither
+   read nor written (padding of a captured batch).  A token that sees no row gives zeros and an lse of -infinity.
+   Groups: group i is entries cu_groups[i] .. cu_groups[i+1] - 1 (device [n_groups + 1], rising, 0 .. n_seqs; entries outside
+   share nothing; n_groups 0: none).  The caller says with prefix[i] (device [n_groups]) that the first prefix[i] rows of all
+   of them are the same; they are read once, through the first entry's row of the page table (its length at least
+   prefix[i]).  Which rows are read together changes the result by rounding only.
+   An entry or a group that these words do not allow records APACK_EDEVICE in the error word of ws: a length or a prefix out
+   of range is read as the nearest in range, tokens before a sequence's first row see nothing, an entry outside the cache
+   gives zeros; offsets that do not rise leave no plan, and the attention calls then record APACK_EDEVICE and write nothing.
+   So do calls that do not match the plan's n_q, heads, D or cache geometry.
+
+   q: [n_q][Hq][D] at q_token_stride bytes, cache dtype, 16-byte aligned; scale as in apack_paged_decode_attention; out:
+   [n_q][Hq][D], contiguous, cache dtype, 16-byte aligned, not over q; lse: fp32 [n_q][Hq] or NULL, ln sum_r exp(scale q.k).
+   Hq <= 1024, any Hq / Hkv; n_q * Hq <= 2^28, n_q <= 2^24.  fp32 softmax and accumulation; deterministic.
+   A page number outside the pool is read as a page of zeros and recorded.  What a token does not see (rows behind it,
+   behind the sequence's last, NaN and infinities too) has no influence on it; a NaN or infinity among the rows that
+   it sees makes what it enters NaN (an infinite value: infinite or NaN).
+   ws: 256-byte aligned, apack_paged_group_workspace_size bytes (for at most n_seqs entries and n_q tokens; query it on the
+   device that runs the calls), its error word (first 16 bytes) zeroed once by the caller.  The plan and the parts of unfinished
+   sums live in it: calls of one plan follow each other on one stream, and another plan in the same workspace ends the
+   first.  One launch for a plan, two for a layer. */
+apack_status apack_paged_group_workspace_size(const apack_paged_cache *cache, int32_t num_q_heads, int32_t n_seqs,
+                                              int64_t n_q, size_t *bytes);
+apack_status apack_paged_group_plan(const apack_paged_cache *cache, const int32_t *seqlens, int32_t num_q_heads,
+                                    int32_t n_seqs, const int32_t *seqs, const int32_t *cu_q, int64_t n_q,
+                                    int32_t n_groups, const int32_t *cu_groups, const int32_t *prefix, void *ws,
+                                    size_t ws_bytes, void *stream);
+apack_status apack_paged_group_attention(const apack_paged_cache *cache, int32_t layer, int64_t n_q, const void *q,
+                                         int64_t q_token_stride, int32_t num_q_heads, float scale, void *out, float *lse,
+                                         void *ws, size_t ws_bytes, void *stream);
+
 /* apack_compact between pools: row j - cu_dst[b] of dst's sequence b receives, for K and V of num_layers
    layers (src_layer and dst_layer on), bit for bit, row
      keep_idx[j] - cu_src[b]   (keep_idx as apack_select writes it, packed over the batch; cu_src: the packed
@@ -492,6 +534,57 @@ apack_status apack_paged_compact(const apack_paged_cache *src, const apack_paged
    ws as in apack_paged_compact; a pair with a page outside the pool is not copied. */
 apack_status apack_copy_pages(const apack_paged_cache *cache, const int32_t *pairs, int64_t n_pairs, void *ws,
                               void *stream);
+
+/* ---- Page tables kept on the device.
+   Who holds which page: the page tables and lengths of up to num_seqs sequences, how many sequences hold each page
+   (refs; 0: a free page), and a stack of the free pages (free_list[0 .. *free_count - 1], the last on top).  The calls
+   below change them with kernels, from device arrays, so that a captured step of a server (new tokens, questions that
+   come and go) needs neither the host nor fixed lengths.  All are int32 device memory of the caller's, 4-byte aligned;
+   page_table and lengths are those that apack_paged_cache and the attention calls read.  Start: lengths 0, refs 0,
+   free_list all pages, *free_count num_pages.  One call at a time may change them (calls on one stream).
+   In every call: n entries, 0 .. APACK_MAX_SEQS; seqs (device [n]): the sequence of an entry, NULL: entry i is sequence i
+   (n <= num_seqs); no sequence twice.  An entry that cannot be carried out (a sequence outside the table or named twice,
+   rows or pages that it does not have, pages that are wanted and not free, a page of the table that nobody holds)
+   leaves everything as it was, and records APACK_EDEVICE in the error word of ws (NULL, or a 16-byte aligned workspace)
+   for the whole call.  Which pages a call takes and leaves depends on its arguments and the state alone
+   (deterministic).  n = 0 does nothing, except that apack_pages_extend writes its maps. */
+typedef struct apack_page_tables {
+  int32_t *page_table;          /* [num_seqs][max_pages]; -1 where a sequence has no page */
+  int64_t table_stride;         /* int32 entries between its rows, >= max_pages */
+  int32_t *lengths;             /* [num_seqs] rows of each sequence; ceil(rows / page_tokens) pages are held */
+  int32_t *refs;                /* [num_pages] */
+  int32_t *free_list;           /* [num_pages] */
+  int32_t *free_count;          /* [1] */
+  int32_t num_seqs;             /* 1 .. APACK_MAX_SEQS */
+  int32_t max_pages;            /* columns of page_table, >= 1 */
+  int32_t num_pages;            /* >= 1 */
+  int32_t page_tokens;          /* 1 .. 2^30 */
+} apack_page_tables;
+
+/* Every entry keeps its first keep_rows[i] rows (device [n], 0 .. its length; 0: the sequence ends).  The pages behind them
+   are given up; those that no other sequence holds become free, the call's first on top of the stack (in the order of
+   entries, then of rows), so that an extension by as many pages takes the same ones to the same places. */
+apack_status apack_pages_release(const apack_page_tables *tables, int32_t n, const int32_t *seqs, const int32_t *keep_rows,
+                                 void *ws, void *stream);
+
+/* Entry i's sequence, which must be empty, shares the pages and takes the length of sequence parents[i] (device [n]; a parent
+   may be named often).  seqs is not NULL. */
+apack_status apack_pages_fork(const apack_page_tables *tables, int32_t n, const int32_t *parents, const int32_t *seqs,
+                              void *ws, void *stream);
+
+/* Room for new_rows[i] >= 0 more rows behind each entry's, in pages from the top of the stack (in the order of entries, then of
+   rows).  A partly filled last page that other sequences hold too is not written to: the entry gets a page of its own in its
+   place, first of its pages, and pairs[i] = (old, new) for apack_copy_pages, (0, 0) elsewhere, which copies nothing (int32
+   [n][2], 8-byte aligned, or NULL where no page is shared).  Of the sequences that share it, all that the call extends
+   get their own but the last holder.
+   The map of the new rows, packed over the entries: cu_new (int32 [n+1]) their offsets; rows[j] (int32 [max_rows]) the row in
+   its sequence, row_seqs[j] (int32 [max_rows] or NULL) that sequence, as apack_rotary_append takes them; slots[j] (int64
+   [max_rows], 8-byte aligned, or NULL) page * page_tokens + slot in the page.  Behind the last new row, and all of them in
+   a call that cannot be carried out: -1 (padding of a captured batch), cu_new 0 in the latter.  More than max_rows new rows cannot be
+   carried out.  One kernel launch, two with max_rows above 8192. */
+apack_status apack_pages_extend(const apack_page_tables *tables, int32_t n, const int32_t *seqs, const int32_t *new_rows,
+                                int32_t *cu_new, int64_t max_rows, int32_t *rows, int32_t *row_seqs, int64_t *slots,
+                                int32_t *pairs, void *ws, void *stream);
 
 /* Synchronises `stream`, then reads the device error word of `ws` into
    *code_out (APACK_OK, APACK_ETIMEOUT or APACK_EDEVICE) and clears it when

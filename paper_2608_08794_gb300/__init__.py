@@ -36,7 +36,9 @@ EXPORTED = ("apack_workspace_size", "apack_keep_counts", "apack_score", "apack_s
             "apack_decode_workspace_size", "apack_decode_attention", "apack_prune_schedule",
             "apack_prune_schedule_graph", "apack_graph_launch", "apack_graph_destroy",
             "apack_rotary_frequencies", "apack_rotary", "apack_rotary_append", "apack_paged_decode_workspace_size",
-            "apack_paged_decode_attention", "apack_paged_compact", "apack_copy_pages")
+            "apack_paged_decode_attention", "apack_paged_compact", "apack_copy_pages",
+            "apack_paged_group_workspace_size", "apack_paged_group_plan", "apack_paged_group_attention",
+            "apack_pages_release", "apack_pages_fork", "apack_pages_extend")
 
 
 class ApackError(RuntimeError):
@@ -84,6 +86,13 @@ class apack_paged_cache(ctypes.Structure):
                 ("max_pages", ctypes.c_int32)]
 
 
+class apack_page_tables(ctypes.Structure):
+    _fields_ = [("page_table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("lengths", ctypes.c_void_p),
+                ("refs", ctypes.c_void_p), ("free_list", ctypes.c_void_p), ("free_count", ctypes.c_void_p),
+                ("num_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("page_tokens", ctypes.c_int32)]
+
+
 class apack_rotary_spec(ctypes.Structure):
     _fields_ = [("layout", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("num_axes", ctypes.c_int32),
                 ("section", ctypes.c_int32 * 3), ("magnitude", ctypes.c_float),
@@ -126,6 +135,12 @@ def _load():
     lib.apack_paged_decode_attention.argtypes = [VP, I32, VP, VP, I64, I32, F32, VP, I32, VP, VP, SZ, VP]
     lib.apack_paged_compact.argtypes = [VP, VP, I32, I32, I32, VP, VP, VP, I64, VP, VP]
     lib.apack_copy_pages.argtypes = [VP, VP, I64, VP, VP]
+    lib.apack_paged_group_workspace_size.argtypes = [VP, I32, I32, I64, P(SZ)]
+    lib.apack_paged_group_plan.argtypes = [VP, VP, I32, I32, VP, VP, I64, I32, VP, VP, VP, SZ, VP]
+    lib.apack_paged_group_attention.argtypes = [VP, I32, I64, VP, I64, I32, F32, VP, VP, VP, SZ, VP]
+    lib.apack_pages_release.argtypes = [VP, I32, VP, VP, VP, VP]
+    lib.apack_pages_fork.argtypes = [VP, I32, VP, VP, VP, VP]
+    lib.apack_pages_extend.argtypes = [VP, I32, VP, VP, VP, I64, VP, VP, VP, VP, VP, VP]
     lib.apack_launch_count.argtypes = []
     lib.apack_launch_count.restype = ctypes.c_uint64
     lib.apack_status_string.argtypes = [I32]
@@ -761,6 +776,167 @@ def apack_copy_pages(cache, pairs, ws=None, stream=None):
     status = _lib.apack_copy_pages(cache._address, pairs.data_ptr(), n, None if ws is None else ws.data_ptr(), stream)
     if status:
         raise ApackError(status, "apack_copy_pages")
+
+
+def apack_paged_group_workspace_size(cache, num_q_heads, n_seqs, n_q):
+    """Bytes that apack_paged_group_plan and apack_paged_group_attention need for up to n_seqs sequences and n_q tokens."""
+    n = ctypes.c_size_t(0)
+    _check(_lib.apack_paged_group_workspace_size(cache._address, int(num_q_heads), int(n_seqs), int(n_q), ctypes.byref(n)),
+           "apack_paged_group_workspace_size")
+    return n.value
+
+
+def apack_paged_group_plan(cache, seqlens, num_q_heads, n_q, ws, cu_q=None, seqs=None, cu_groups=None, prefix=None,
+                           stream=None):
+    """The work of apack_paged_group_attention for one step, into ws, from lengths and groups on the device: once for all
+    layers.  seqlens: int32 [num_seqs] of the cache.  The batch's sequences: seqs (int32 [n]; None: all of the cache's, in
+    order), their n_q new tokens packed, cu_q int32 [n + 1] (None: one each); groups of them that share their first rows:
+    cu_groups int32 [groups + 1] and prefix int32 [groups] (None: none do)."""
+    stream = _on_device((cache, seqlens, ws, cu_q, seqs, cu_groups, prefix), stream)
+    _int32(seqlens, "seqlens", (cache.num_seqs,))
+    n = cache.num_seqs
+    if seqs is not None:
+        n = seqs.numel()
+        _int32(seqs, "seqs", (n,))
+    if cu_q is not None:
+        _int32(cu_q, "cu_q", (n + 1,))
+    if (cu_groups is None) != (prefix is None):
+        raise ValueError("cu_groups and prefix: both or neither expected")
+    groups = 0
+    if prefix is not None:
+        groups = prefix.numel()
+        _int32(prefix, "prefix", (groups,))
+        _int32(cu_groups, "cu_groups", (groups + 1,))
+    _check(_lib.apack_paged_group_plan(cache._address, seqlens.data_ptr(), int(num_q_heads), n, _ptr(seqs), _ptr(cu_q),
+                                       int(n_q), groups, _ptr(cu_groups), _ptr(prefix), ws.data_ptr(), ws.nbytes,
+                                       stream), "apack_paged_group_plan")
+
+
+def apack_paged_group_attention(cache, layer, q, out, ws, scale=None, lse=None, stream=None):
+    """Attention of the planned batch's new tokens in one layer.  q [n_q, Hq, D]; out: the same shape and type, contiguous;
+    lse: float32 [n_q, Hq]."""
+    if _cuda is None:
+        stream = _on_device((cache, q, out, ws, lse), stream)
+    else:
+        dev = _cuda[0]()
+        if (cache._device != dev or q.get_device() != dev or out.get_device() != dev or ws.get_device() != dev or
+                (lse is not None and lse.get_device() != dev)):
+            _on_device((cache, q, out, ws, lse), stream)
+        stream = _cuda[1](dev) if stream is None else _stream(stream)
+    dim, dtype, shape, qs = cache.head_dim, cache.dtype, q.shape, q.stride()
+    if len(shape) != 3 or shape[2] != dim:
+        raise ValueError(f"q: [tokens, heads, {dim}] expected, not {tuple(shape)}")
+    n, heads = shape[0], shape[1]
+    if q.dtype is not dtype or qs[1] != dim or qs[2] != 1:
+        qs = (_head_rows(q, "q", dtype),)
+    qs = qs[0] if n > 1 else heads * dim
+    if out.dtype is not dtype or out.shape != shape or not out.is_contiguous():
+        raise ValueError(f"out: contiguous {dtype} {tuple(shape)} expected")
+    if lse is not None and (str(lse.dtype) != "torch.float32" or lse.shape != shape[:2] or not lse.is_contiguous()):
+        raise ValueError(f"lse: contiguous float32 {tuple(shape[:2])} expected")
+    status = _lib.apack_paged_group_attention(
+        cache._address, int(layer), n, q.data_ptr(), 2 * qs, heads, cache._scale if scale is None else scale,
+        out.data_ptr(), None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.nbytes, stream)
+    if status:
+        raise ApackError(status, "apack_paged_group_attention")
+
+
+# ---------------------------------------------------------------- page tables on the device
+
+
+class PageTables:
+    """Page tables, lengths, reference counts and free pages on the device (apack_page_tables).
+
+    page_table: int32 [num_seqs, max_pages]; lengths [num_seqs]; refs and free_list [num_pages]; free_count [1].
+    PageTables.new makes them for an empty pool.  Holds the tensors."""
+
+    def __init__(self, page_table, lengths, refs, free_list, free_count, page_tokens):
+        import torch
+        if page_table.dtype != torch.int32 or page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+            raise ValueError("page_table: int32 [sequences, pages] with contiguous rows expected")
+        seqs, columns = page_table.shape
+        _int32(lengths, "lengths", (seqs,))
+        _int32(refs, "refs")
+        _int32(free_list, "free_list", refs.shape)
+        _int32(free_count, "free_count", (1,))
+        if refs.dim() != 1:
+            raise ValueError("refs and free_list: [pages] expected")
+        if len({t.get_device() for t in (page_table, lengths, refs, free_list, free_count)}) > 1:
+            raise ValueError("page_table, lengths, refs, free_list and free_count: one device expected")
+        self._tensors = page_table, lengths, refs, free_list, free_count
+        self._device, self.num_seqs = page_table.get_device(), seqs
+        self.struct = apack_page_tables(
+            page_table=page_table.data_ptr(), table_stride=page_table.stride(0) if seqs > 1 else columns,
+            lengths=lengths.data_ptr(), refs=refs.data_ptr(), free_list=free_list.data_ptr(),
+            free_count=free_count.data_ptr(), num_seqs=seqs, max_pages=columns, num_pages=refs.numel(),
+            page_tokens=int(page_tokens))
+        self._address = ctypes.addressof(self.struct)
+
+    @classmethod
+    def new(cls, num_seqs, max_pages, num_pages, page_tokens, device="cuda"):
+        import torch
+        def full(shape, value):
+            return torch.full(shape, value, dtype=torch.int32, device=device)
+        return cls(full((num_seqs, max_pages), -1), full((num_seqs,), 0), full((num_pages,), 0),
+                   torch.arange(num_pages - 1, -1, -1, dtype=torch.int32, device=device), full((1,), num_pages), page_tokens)
+
+    page_table = property(lambda self: self._tensors[0])
+    lengths = property(lambda self: self._tensors[1])
+    refs = property(lambda self: self._tensors[2])
+    free_list = property(lambda self: self._tensors[3])
+    free_count = property(lambda self: self._tensors[4])
+    page_tokens = property(lambda self: self.struct.page_tokens)
+
+    def get_device(self):
+        return self._device
+
+
+def _entries(tables, values, what, seqs):
+    """Checks the entries of a call on page tables; returns their number."""
+    if not (values.dtype is _int32_type and values.dim() == 1 and values.is_contiguous()):
+        _int32(values, what, (values.numel(),))
+    n = values.numel()
+    if seqs is not None and not (seqs.dtype is _int32_type and seqs.shape == (n,) and seqs.is_contiguous()):
+        _int32(seqs, "seqs", (n,))
+    return n
+
+
+def apack_pages_release(tables, keep_rows, seqs=None, ws=None, stream=None):
+    """Keeps the first keep_rows[i] rows of sequence seqs[i] (None: i) and gives up the pages behind them."""
+    stream = _on_device((tables, keep_rows, seqs, ws), stream)
+    n = _entries(tables, keep_rows, "keep_rows", seqs)
+    _check(_lib.apack_pages_release(tables._address, n, None if seqs is None else seqs.data_ptr(), keep_rows.data_ptr(),
+                                    _ptr(ws), stream), "apack_pages_release")
+
+
+def apack_pages_fork(tables, parents, seqs, ws=None, stream=None):
+    """Empty sequence seqs[i] shares the pages of sequence parents[i]."""
+    stream = _on_device((tables, parents, seqs, ws), stream)
+    n = _entries(tables, parents, "parents", seqs)
+    _check(_lib.apack_pages_fork(tables._address, n, parents.data_ptr(), seqs.data_ptr(), _ptr(ws), stream),
+           "apack_pages_fork")
+
+
+def apack_pages_extend(tables, new_rows, cu_new, rows, seqs=None, row_seqs=None, slots=None, pairs=None, ws=None,
+                       stream=None):
+    """Room for new_rows[i] more rows behind sequence seqs[i] (None: i).  cu_new int32 [n + 1], rows and row_seqs int32
+    [max_rows] and slots int64 [max_rows] receive the map of the new rows, pairs int32 [n, 2] the pages to copy
+    (apack_copy_pages) before they are written."""
+    stream = _on_device((tables, new_rows, cu_new, rows, seqs, row_seqs, slots, pairs, ws), stream)
+    n = _entries(tables, new_rows, "new_rows", seqs)
+    _int32(cu_new, "cu_new", (n + 1,))
+    if rows.dim() != 1:
+        raise ValueError("rows: [max_rows] expected")
+    _int32(rows, "rows")
+    if row_seqs is not None:
+        _int32(row_seqs, "row_seqs", rows.shape)
+    if slots is not None and (str(slots.dtype) != "torch.int64" or slots.shape != rows.shape or not slots.is_contiguous()):
+        raise ValueError(f"slots: contiguous int64 {tuple(rows.shape)} expected")
+    if pairs is not None:
+        _int32(pairs, "pairs", (n, 2))
+    _check(_lib.apack_pages_extend(tables._address, n, None if seqs is None else seqs.data_ptr(), new_rows.data_ptr(),
+                                   cu_new.data_ptr(), rows.numel(), rows.data_ptr(), _ptr(row_seqs), _ptr(slots),
+                                   _ptr(pairs), _ptr(ws), stream), "apack_pages_extend")
 
 
 def apack_device_error(ws, stream=None, clear=True):

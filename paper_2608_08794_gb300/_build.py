@@ -76,7 +76,7 @@ def build_apack():
     headers = [os.path.join(INCLUDE, "apack.h")] + [
         os.path.join(csrc, h) for h in os.listdir(csrc) if h.endswith((".cuh", ".h"))]
     return _build_lib(csrc, ["apack.cu", "score.cu", "score_narrow.cu", "score_narrow_tc.cu", "select.cu", "compact.cu", "compact_tma.cu", "compact_inplace.cu", "score_static.cu", "prellm.cu", "decode.cu", "decode_tc.cu", "schedule.cu",
-                               "paged.cu", "rotary.cu", "paged_decode.cu", "paged_copy.cu"], headers,
+                               "paged.cu", "rotary.cu", "paged_decode.cu", "paged_copy.cu", "pages.cu", "group_plan.cu", "group_attention.cu"], headers,
                       os.path.join(HERE, "_lib"), "libapack.so")
 
 

@@ -1,0 +1,430 @@
+// group_plan.cu -- the work of attention over shared rows, laid out on the device from lengths and groups.
+//
+// A step's plan serves all its layers, and lengths stay on the device, so that a captured step follows growing caches.  One
+// CTA: it finds each sequence's group (a search among the groups' bounds in shared memory), how many rows of its keys are
+// the group's, how long the runs of keys should be, and writes items, segments and what each token sees.
+//
+// Bound by latency (block barriers and trips to L2, some 8 us for 64 sequences): once per step, not per layer.
+//
+// The length of a run.  A segment of c tiles costs about c + kSegCost tiles of one SM; n segments on S SMs end after
+// max(sum of all / S, ceil(long ones / S) * (c + kSegCost)) at the least, and every part's row is written and read once
+// more.  32 warps try a run length each over all items, twice (spread over the logarithm, then around the best), and
+// the least estimate wins.
+#include <algorithm>
+#include <cstring>
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "group.cuh"
+
+namespace apack {
+namespace {
+
+constexpr int kThreads = 1024;
+constexpr int kWarps = 32;
+constexpr int kPer = APACK_MAX_SEQS / kThreads;
+constexpr float kSegCost = 2.5f;               // tiles: queries, first loads, parts
+constexpr float kRowCost = 1056.f / 65536.f;   // tiles: a part's row written and read, against a tile of K and V
+
+struct PlanArgs {
+  const int32_t *seqlens, *seqs, *cu_q, *cu_groups, *prefix;
+  uint8_t *ws;
+  int32_t n, groups, n_q, hq, hkv, group, head_dim;
+  int32_t num_seqs, max_pages, page_tokens, num_pages, max_rows;
+  int32_t align;                     // shared rows are cut to a multiple of this
+  int32_t sms, halves;
+  int64_t cap_rows, cap_segs;
+  int64_t tok_off, item_off, seg_off, ml_off, part_off, total;
+  DeviceError *err;
+};
+
+struct PlanShared {
+  int32_t cu_q[APACK_MAX_SEQS + 1], cu_g[APACK_MAX_SEQS + 1];
+  int32_t rows[2 * APACK_MAX_SEQS], tiles[2 * APACK_MAX_SEQS];      // of the items: groups, then sequences
+  int32_t seg0[2 * APACK_MAX_SEQS + 1];
+  float est[kWarps];
+  int32_t cand[kWarps];
+  int64_t warp_sum[kWarps];
+  int32_t bad, longest, chunk, causal;
+};
+
+__device__ __forceinline__ int runs_of(int rows) { return (rows + kGRows - 1) / kGRows; }
+__device__ __forceinline__ int sub_of(const PlanArgs &P, int rows) {
+  const int last = rows - (runs_of(rows) - 1) * kGRows;
+  return P.halves && rows <= 4 * kGRows && last <= kGSlot ? 2 : 1;
+}
+
+__device__ int64_t scan(int64_t v, PlanShared &s, int64_t *total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int64_t x = v;
+#pragma unroll
+  for (int o = 1; o < 32; o *= 2) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();
+  if (lane == 31) s.warp_sum[warp] = x;
+  __syncthreads();
+  int64_t w = s.warp_sum[lane];
+#pragma unroll
+  for (int o = 1; o < 32; o *= 2) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, w, o);
+    if (lane >= o) w += y;
+  }
+  *total = __shfl_sync(0xffffffffu, w, 31);
+  const int64_t before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
+  return x - v + (warp ? before : 0);
+}
+
+// The last i < n with at[i] <= j.
+__device__ __forceinline__ int last_at(const int32_t *at, int n, int j) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (at[mid] <= j)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  return lo;
+}
+
+// Estimated time of run length c, in tiles of one SM; infinite where the workspace does not hold it.  By one warp.
+__device__ float estimate(const PlanArgs &P, const PlanShared &s, int items, int c) {
+  const int lane = threadIdx.x & 31;
+  float work = 0.f, segs = 0.f, rows = 0.f, big = 0.f, most = 0.f;
+  for (int i = lane; i < items; i += 32) {
+    if (s.rows[i] == 0) continue;
+    const int splits = (s.tiles[i] + c - 1) / c, chunk = (s.tiles[i] + splits - 1) / splits;
+    const float heads = static_cast<float>(P.hkv) * runs_of(s.rows[i]);
+    work += heads * s.tiles[i];
+    segs += heads * splits;
+    rows += static_cast<float>(s.rows[i]) * P.hkv * splits * sub_of(P, s.rows[i]);
+    if (2 * chunk > c) {
+      big += heads * splits;
+      most = fmaxf(most, chunk);
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    work += __shfl_xor_sync(0xffffffffu, work, o);
+    segs += __shfl_xor_sync(0xffffffffu, segs, o);
+    rows += __shfl_xor_sync(0xffffffffu, rows, o);
+    big += __shfl_xor_sync(0xffffffffu, big, o);
+    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+  }
+  if (rows > 0.99f * P.cap_rows || segs > 0.99f * P.cap_segs) return INFINITY;
+  const float even = (work + segs * kSegCost) / P.sms;
+  const float rounds = ceilf(big / P.sms) * (most + kSegCost);
+  return fmaxf(even, rounds) + rows * kRowCost / P.sms;
+}
+
+__global__ void __launch_bounds__(kThreads, 1) group_plan_kernel(const __grid_constant__ PlanArgs P) {
+  extern __shared__ uint8_t raw[];
+  PlanShared &s = *reinterpret_cast<PlanShared *>(raw);
+  GroupHead *head = reinterpret_cast<GroupHead *>(P.ws + kGHeadOff);
+  GroupItem *items = reinterpret_cast<GroupItem *>(P.ws + P.item_off);
+  GroupTok *tok = reinterpret_cast<GroupTok *>(P.ws + P.tok_off);
+  GroupSeg *segs = reinterpret_cast<GroupSeg *>(P.ws + P.seg_off);
+  const int warp = threadIdx.x >> 5, n = P.n, ng = P.groups, G = P.group;
+  if (threadIdx.x == 0) s.bad = s.longest = s.causal = 0;
+  pdl_wait_and_release();
+  for (int i = threadIdx.x; i <= n; i += kThreads) s.cu_q[i] = P.cu_q ? P.cu_q[i] : i;
+  for (int i = threadIdx.x; i <= ng; i += kThreads) s.cu_g[i] = ng ? P.cu_groups[i] : 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i <= n; i += kThreads) {
+    const int at = s.cu_q[i];
+    if (at < (i ? s.cu_q[i - 1] : 0) || at > P.n_q || (i == 0 && at != 0)) {
+      raise_device_error(P.err, APACK_EDEVICE, 141, i, at);
+      s.bad = 1;
+    }
+  }
+  for (int i = threadIdx.x; i <= ng && ng; i += kThreads) {
+    const int at = s.cu_g[i];
+    if (at < (i ? s.cu_g[i - 1] : 0) || at > n) {
+      raise_device_error(P.err, APACK_EDEVICE, 142, i, at);
+      s.bad = 1;
+    }
+  }
+  auto sequence = [&](int e, int *len) {           // of entry e; -1: none
+    const int b = P.seqs ? P.seqs[e] : e;
+    if (static_cast<uint32_t>(b) >= static_cast<uint32_t>(P.num_seqs)) {
+      raise_device_error(P.err, APACK_EDEVICE, 143, e, b);
+      *len = 0;
+      return -1;
+    }
+    const int x = P.seqlens[b];
+    *len = min(max(x, 0), P.max_rows);
+    if (*len != x) raise_device_error(P.err, APACK_EDEVICE, 144, b, x);
+    return b;
+  };
+  __syncthreads();
+  const bool bad = s.bad;
+  const int total_items = ng + n;
+  // ---- items: groups
+  for (int g = threadIdx.x; g < ng; g += kThreads) {
+    s.rows[g] = s.tiles[g] = 0;
+    if (bad) continue;
+    const int e0 = s.cu_g[g], e1 = s.cu_g[g + 1];
+    GroupItem it = {};
+    if (e1 - e0 > 1) {
+      int len;
+      const int b = sequence(e0, &len), shared = P.prefix[g];
+      if (shared < 0 || shared > len) raise_device_error(P.err, APACK_EDEVICE, 145, g, shared);
+      const int common = min(max(shared, 0), len), cut = common - common % P.align;
+      const int rows = (s.cu_q[e1] - s.cu_q[e0]) * G;
+      if (b >= 0 && cut > 0 && rows > 0) {
+        it.seq = b;
+        it.key1 = cut;
+        it.row0 = s.cu_q[e0] * G;
+        it.rows = s.rows[g] = rows;
+        s.tiles[g] = (cut + kGTile - 1) / kGTile;
+        atomicMax(&s.longest, s.tiles[g]);
+      }
+    }
+    items[g] = it;
+  }
+  __syncthreads();
+  // ---- items: sequences
+  for (int e = threadIdx.x; e < n; e += kThreads) {
+    s.rows[ng + e] = s.tiles[ng + e] = 0;
+    if (bad) continue;
+    GroupItem it = {};
+    int len;
+    const int b = sequence(e, &len), m = s.cu_q[e + 1] - s.cu_q[e];
+    int g = -1, cut = 0;
+    if (ng && e >= s.cu_g[0] && e < s.cu_g[ng]) {
+      g = last_at(s.cu_g, ng, e);
+      if (s.rows[g]) cut = items[g].key1;
+    }
+    if (m > len) raise_device_error(P.err, APACK_EDEVICE, 146, e, len);
+    if (m > 0 && b >= 0 && cut < len) {
+      it.seq = b;
+      it.key0 = cut;
+      it.key1 = len;
+      it.row0 = s.cu_q[e] * G;
+      it.rows = s.rows[ng + e] = m * G;
+      it.causal = m > 1;
+      s.tiles[ng + e] = (len - cut + kGTile - 1) / kGTile;
+      atomicMax(&s.longest, s.tiles[ng + e]);
+      if (m > 1) s.causal = 1;
+    }
+    items[ng + e] = it;
+    if (cut > len - m + 1) s.causal = 1;           // a token that does not see all of the shared rows
+    for (int t = s.cu_q[e], i = 1; i <= m && m <= 32; ++t, ++i)
+      tok[t] = GroupTok{max(len - m + i, 0), cut > 0 ? g : -1, s.rows[ng + e] ? ng + e : -1, 1};
+  }
+  __syncthreads();
+  const int n_tok = bad ? 0 : s.cu_q[n];
+  for (int t = threadIdx.x; t < P.n_q; t += kThreads) {
+    if (t >= n_tok) {
+      tok[t] = GroupTok{0, -1, -1, 0};
+      continue;
+    }
+    const int e = last_at(s.cu_q, n, t), m = s.cu_q[e + 1] - s.cu_q[e];
+    if (m <= 32) continue;                         // written above
+    int len;
+    sequence(e, &len);
+    int g = -1;
+    if (ng && e >= s.cu_g[0] && e < s.cu_g[ng]) {
+      g = last_at(s.cu_g, ng, e);
+      if (!s.rows[g]) g = -1;
+    }
+    tok[t] = GroupTok{max(len - m + 1 + t - s.cu_q[e], 0), g, s.rows[ng + e] ? ng + e : -1, 1};
+  }
+  // ---- the run length
+  const int longest = max(s.longest, 1);
+  int lo = 1, hi = longest;
+  for (int round = 0; round < 2; ++round) {
+    const float f = static_cast<float>(warp + 1) / kWarps;
+    int c = round == 0 ? static_cast<int>(exp2f(log2f(static_cast<float>(longest)) * f) + 0.5f)
+                       : lo + static_cast<int>((hi - lo) * (f - 1.f / kWarps) * (kWarps / (kWarps - 1.f)) + 0.5f);
+    c = warp == kWarps - 1 ? (round == 0 ? longest : hi) : min(max(c, 1), longest);
+    const float est = estimate(P, s, total_items, c);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) {
+      s.est[warp] = est;
+      s.cand[warp] = c;
+    }
+    __syncthreads();
+    int best = 0;
+    for (int w = 1; w < kWarps; ++w)
+      if (s.est[w] <= s.est[best]) best = w;       // of equals the longest runs
+    if (threadIdx.x == 0) s.chunk = s.est[best] < INFINITY ? s.cand[best] : longest;
+    lo = s.cand[max(best - 1, 0)];
+    hi = s.cand[min(best + 1, kWarps - 1)];
+  }
+  __syncthreads();
+  const int chunk = s.chunk;
+  // ---- places of segments and parts
+  int64_t seg_at = 0, part_at = 0;
+  for (int i0 = 0; i0 < total_items; i0 += kThreads) {
+    const int i = i0 + threadIdx.x;
+    int splits = 0, sub = 1;
+    if (i < total_items && s.rows[i]) {
+      splits = (s.tiles[i] + chunk - 1) / chunk;
+      sub = sub_of(P, s.rows[i]);
+    }
+    const int64_t here = splits ? static_cast<int64_t>(splits) * P.hkv * runs_of(s.rows[i]) : 0;
+    const int64_t part = splits ? static_cast<int64_t>(splits) * sub * P.hkv * s.rows[i] : 0;
+    int64_t all_segs, all_parts;
+    const int64_t seg = seg_at + scan(here, s, &all_segs), row = part_at + scan(part, s, &all_parts);
+    if (i < total_items) {
+      s.seg0[i] = static_cast<int32_t>(min(seg, static_cast<int64_t>(INT32_MAX)));
+      if (splits) {
+        items[i].splits = splits;
+        items[i].chunk = (s.tiles[i] + splits - 1) / splits;
+        items[i].sub = sub;
+        items[i].part = static_cast<int32_t>(min(row, static_cast<int64_t>(INT32_MAX)));
+      }
+    }
+    seg_at += all_segs;
+    part_at += all_parts;
+  }
+  const bool fits = seg_at <= P.cap_segs && part_at <= P.cap_rows;
+  if (!fits && threadIdx.x == 0) raise_device_error(P.err, APACK_EDEVICE, 147, static_cast<int>(seg_at), static_cast<int>(part_at));
+  __syncthreads();
+  const int count = bad || !fits ? 0 : static_cast<int>(seg_at);
+  for (int j = threadIdx.x; j < count; j += kThreads) {
+    const int i = last_at(s.seg0, total_items, j), runs = runs_of(s.rows[i]);
+    const GroupItem it = items[i];
+    int x = j - s.seg0[i];
+    const int run = x % runs;
+    x /= runs;
+    const int h = x % P.hkv, split = x / P.hkv;
+    GroupSeg g;
+    g.seq = it.seq;
+    g.head = h;
+    g.row0 = it.row0 + run * kGRows;
+    g.rows = min(kGRows, it.rows - run * kGRows);
+    g.key0 = it.key0 + split * it.chunk * kGTile;
+    g.key1 = min(it.key1, g.key0 + it.chunk * kGTile);
+    if (it.causal) g.key1 = min(g.key1, tok[(g.row0 + g.rows - 1) / G].limit);
+    g.part = it.part + (split * it.sub * P.hkv + h) * it.rows + run * kGRows;
+    g.step = it.sub == 2 && g.rows <= kGSlot ? P.hkv * it.rows : 0;
+    segs[j] = g;
+  }
+  if (threadIdx.x == 0) {
+    GroupHead h = {};
+    h.magic = bad || !fits ? 0 : kGMagic;          // without a plan the attention calls record an error and write nothing
+    h.n_q = P.n_q;
+    h.hq = P.hq;
+    h.hkv = P.hkv;
+    h.head_dim = P.head_dim;
+    h.num_seqs = P.num_seqs;
+    h.max_pages = P.max_pages;
+    h.page_tokens = P.page_tokens;
+    h.num_pages = P.num_pages;
+    h.segs = count;
+    h.causal_any = s.causal;
+    h.tok_off = P.tok_off;
+    h.item_off = P.item_off;
+    h.seg_off = P.seg_off;
+    h.ml_off = P.ml_off;
+    h.part_off = P.part_off;
+    h.total = P.total;
+    *head = h;
+    *reinterpret_cast<uint32_t *>(P.ws + kGClaimOff) = 0;
+  }
+}
+
+}  // namespace
+
+apack_status group_shape(const apack_paged_cache *c, int32_t hq, int32_t n_seqs, int64_t n_q, GroupShape *s) {
+  if (hq < 1 || hq > 1024 || hq % c->num_kv_heads != 0) return APACK_EINVAL;
+  if (n_seqs < 1 || n_seqs > APACK_MAX_SEQS || n_q < 0 || n_q > (1 << 24) || n_q * hq > (1 << 28)) return APACK_EINVAL;
+  s->group = hq / c->num_kv_heads;
+  const int64_t rows = n_q * hq, packed = n_q * s->group, sms = device_sm_count();
+  // every item once (shared and own rows; twice in halves), and what runs of keys add for all SMs
+  s->halves = packed <= 8192;
+  s->cap_rows = rows * (s->halves ? 4 : 2) + std::min(rows * sms, sms * 4 * kGRows) + 64;
+  s->cap_segs = c->num_kv_heads * (2 * (packed / kGRows) + 2 * static_cast<int64_t>(n_seqs)) + 8 * sms + 64;
+  auto up = [](int64_t x) { return static_cast<size_t>((x + 255) & ~int64_t{255}); };
+  s->tok_off = kGFixed;
+  s->item_off = up(s->tok_off + n_q * sizeof(GroupTok));
+  s->seg_off = up(s->item_off + 2 * static_cast<int64_t>(n_seqs) * sizeof(GroupItem));
+  s->ml_off = up(s->seg_off + s->cap_segs * sizeof(GroupSeg));
+  s->part_off = up(s->ml_off + s->cap_rows * sizeof(float2));
+  s->total = up(s->part_off + s->cap_rows * c->head_dim * sizeof(float));
+  return APACK_OK;
+}
+
+}  // namespace apack
+
+using namespace apack;
+
+extern "C" {
+
+apack_status apack_paged_group_workspace_size(const apack_paged_cache *cache, int32_t num_q_heads, int32_t n_seqs,
+                                              int64_t n_q, size_t *bytes) {
+  if (!bytes) return APACK_EINVAL;
+  apack_status st = validate_pool(cache, true);
+  if (st != APACK_OK) return st;
+  GroupShape s;
+  st = group_shape(cache, num_q_heads, n_seqs, n_q, &s);
+  if (st == APACK_OK) *bytes = s.total;
+  return st;
+}
+
+apack_status apack_paged_group_plan(const apack_paged_cache *cache, const int32_t *seqlens, int32_t num_q_heads,
+                                    int32_t n_seqs, const int32_t *seqs, const int32_t *cu_q, int64_t n_q,
+                                    int32_t n_groups, const int32_t *cu_groups, const int32_t *prefix, void *ws,
+                                    size_t ws_bytes, void *stream) {
+  apack_status st = validate_pool(cache, true);
+  if (st != APACK_OK) return st;
+  GroupShape s;
+  st = group_shape(cache, num_q_heads, n_seqs, n_q, &s);
+  if (st != APACK_OK) return st;
+  if (!seqlens || !ws || (!seqs && n_seqs > cache->num_seqs) || (!cu_q && n_q != n_seqs)) return APACK_EINVAL;
+  if (n_groups < 0 || n_groups > n_seqs || (n_groups > 0 && (!cu_groups || !prefix))) return APACK_EINVAL;
+  if (((reinterpret_cast<uintptr_t>(seqlens) | reinterpret_cast<uintptr_t>(seqs) | reinterpret_cast<uintptr_t>(cu_q) |
+        reinterpret_cast<uintptr_t>(cu_groups) | reinterpret_cast<uintptr_t>(prefix)) & 3) ||
+      (reinterpret_cast<uintptr_t>(ws) & 255))
+    return APACK_EINVAL;
+  if (ws_bytes < s.total) return APACK_EWORKSPACE;
+  PlanArgs P;
+  std::memset(&P, 0, sizeof(P));
+  P.seqlens = seqlens;
+  P.seqs = seqs;
+  P.cu_q = cu_q;
+  P.cu_groups = cu_groups;
+  P.prefix = prefix;
+  P.ws = static_cast<uint8_t *>(ws);
+  P.n = n_seqs;
+  P.groups = n_groups;
+  P.n_q = static_cast<int32_t>(n_q);
+  P.hq = num_q_heads;
+  P.hkv = cache->num_kv_heads;
+  P.group = s.group;
+  P.head_dim = cache->head_dim;
+  P.num_seqs = cache->num_seqs;
+  P.max_pages = cache->max_pages;
+  P.page_tokens = cache->page_tokens;
+  P.num_pages = cache->num_pages;
+  P.max_rows = static_cast<int32_t>(
+      std::min<int64_t>(1 << 30, static_cast<int64_t>(cache->max_pages) * cache->page_tokens));
+  P.align = std::max(1, group_box(cache->page_tokens));
+  P.sms = device_sm_count();
+  P.halves = s.halves;
+  P.cap_rows = s.cap_rows;
+  P.cap_segs = s.cap_segs;
+  P.tok_off = s.tok_off;
+  P.item_off = s.item_off;
+  P.seg_off = s.seg_off;
+  P.ml_off = s.ml_off;
+  P.part_off = s.part_off;
+  P.total = s.total;
+  P.err = static_cast<DeviceError *>(ws);
+  static std::atomic<uint64_t> attr{0};
+  cudaError_t e = once_per_device(attr, [] {
+    return cudaFuncSetAttribute(group_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                static_cast<int>(sizeof(PlanShared)));
+  });
+  if (e == cudaSuccess)
+    e = launch_pdl(group_plan_kernel, dim3(1), dim3(kThreads), sizeof(PlanShared), static_cast<cudaStream_t>(stream), P);
+  if (e == cudaSuccess) count_launches(1);
+  return check_cuda(e);
+}
+
+}  // extern "C"
