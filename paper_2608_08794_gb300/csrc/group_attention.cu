@@ -1,4 +1,37 @@
 // group_attention.cu -- attention of new tokens over paged caches, the shared rows of a group of sequences read once.
+//
+//   out[t, h] = sum_r softmax_r(scale q[t, h] . k[r, g(h)]) v[r, g(h)],  r <= position of t
+//
+// What makes it fast.  64 conversations about one video read the same cache; token by token that is 64 reads of it, and one
+// here.  All query rows of a KV head (tokens of all sequences that share the keys, times the query heads of the KV head) are rows
+// of one matrix product, 256 of them per segment, so that the tensor cores do what several reads did: with 256 rows a tile of
+// 128 keys takes 2 x 128 x 128 x D x 4 flops against 512 D bytes, and the tensor pipe, not HBM, is the bound above some 160 rows.
+//
+// A segment (group_plan.cu) is 256 query rows of a KV head against a run of 128-key tiles.  CTAs (one per SM) take segments from
+// a counter, long ones first; every segment's result is a part (max, sum, unnormalised values) of its own, and the merge
+// adds a row's parts in the order of their keys, so that the result does not depend on who took what.
+//   warps 0..3, 4..7   softmax of accumulators 0 and 1, a query row per thread (TMEM lane): scores S read whole, P written over
+//                      them as 16-bit pairs (the A operand of the second product comes from TMEM), O left in TMEM for the whole
+//                      segment.  The row's reference maximum is set anew only when it has grown by more than 2^8 (2^4 in fp16):
+//                      then the warp rescales its rows of O.
+//   warp 8             the tensor products, one thread issuing: S = Q K^T and O += P V for accumulators 0 and 1 in turn, so that
+//                      one softmax runs while the other's products do.  S of the operation after next is issued
+//                      right behind O of this one (same accumulator; products run in the order of issue).
+//   warps 9..11        loads: K and V tiles in a ring of 5 (8 with heads of 64), by TMA boxes of up to 128 tokens (warp 9, a box per lane), or
+//                      16 bytes at a time where pages are no multiple of 8 tokens (all three)
+// A segment of more than 128 rows gives each accumulator half of the rows; one of fewer gives them the even and the odd tiles,
+// and writes two parts.  Operations alternate between the accumulators across segments too, so that short segments overlap.
+//
+// P enters the second product as one 16-bit number per probability: 2^-9 (bf16) or 2^-12 (fp16) of each at most, on average
+// less than the output's own rounding, where a second number would take half as much tensor time again; the row's sum
+// is taken of the unrounded probabilities in fp32, so the lse keeps 32 bits.
+//
+// What a token must not see: keys behind its own are masked in S; values there enter as 0 times a number, so rows behind the
+// segment's last key become zeros in shared memory, and where that is not enough (another token's key whose value is NaN or
+// infinite: 0 times it is NaN) the merge computes the row anew, key by key.
+//
+// Every wait is bounded (2 s); one that gives up records APACK_ETIMEOUT, and the CTA leaves with its copies and products done.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 
@@ -7,44 +40,698 @@
 namespace apack {
 namespace {
 
-// A warp per query row.
+constexpr int kThreads = 384;
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kLoadWarps = 3;
+constexpr int kHalfBytes = kGTile * 128;                       // 64 features of 128 rows
+constexpr int kRecs = 16;
+constexpr uint32_t kTmemCols = 512;                            // S 0, S 1, O 0, O 1, 128 columns each
+
+template <int D>
+struct Lay {
+  static constexpr int kTileBytes = kGTile * D * 2;
+  static constexpr int kRing = D == 128 ? 5 : 8;               // K and V tiles
+  static constexpr uint32_t kOffRing = 2 * kGSlot * D * 2;     // behind the two query tiles
+  static constexpr uint32_t kOffBars = kOffRing + kRing * kTileBytes;
+  static constexpr uint32_t kBytes = kOffBars + 1536;
+};
+
+struct __align__(16) Bars {
+  GroupSeg rec[kRecs];                                         // the CTA's segments in turn; seq -1: no more
+  uint64_t full[8], empty[8];
+  uint64_t rec_full[kRecs];
+  uint64_t q_full[2], s_full[2], p_full[2], o_full[2], drain;
+  uint32_t tmem;
+  volatile int32_t abort;
+};
+static_assert(sizeof(Bars) <= 1536, "barrier block");
+
+// 16-bit types of K, V and P.  The reference is kShift below the row's maximum when it was set; see paged_decode.cu for the
+// range of fp16 (a long tail far below one key).
+template <class T>
+struct Type;
+template <>
+struct Type<__nv_bfloat16> {
+  static constexpr float kGrow = 8.f, kShift = 0.f;
+  static constexpr uint32_t kFormat = (1u << 7) | (1u << 10);
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<uint32_t *>(&v);
+  }
+};
+template <>
+struct Type<__half> {
+  static constexpr float kGrow = 4.f, kShift = 11.f;
+  static constexpr uint32_t kFormat = 0;
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    __half2 v = __floats2half2_rn(a, b);
+    return *reinterpret_cast<uint32_t *>(&v);
+  }
+};
+
+template <class T>
+constexpr uint32_t idesc(int n, bool b_mn_major) {
+  return (1u << 4) | Type<T>::kFormat | (b_mn_major ? 1u << 16 : 0u) | (static_cast<uint32_t>(n >> 3) << 17) |
+         (static_cast<uint32_t>(kGSlot >> 4) << 24);
+}
+
+// D[tmem] (+)= A[tmem] * B[smem]^T
+__device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void store8(float *p, const uint32_t *r) {       // 32 bytes, aligned
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+               "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+__device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap *map, uint64_t *bar, int32_t token, int32_t block,
+                                        int32_t head, int32_t page) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], "
+      "[%2];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(0), "r"(token), "r"(block), "r"(head), "r"(page)
+      : "memory");
+}
+
+// Bounded; false when it gave up or another role of the CTA has.
+__device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, Bars *b, DeviceError *err, int where) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = globaltimer_ns();
+  for (;;) {
+    for (int i = 0; i < 32; ++i)
+      if (mbar_try_wait(bar, parity)) return true;
+    if (b->abort) return false;
+    if (globaltimer_ns() - t0 > kWaitLimitNs) {
+      b->abort = 1;
+      raise_device_error(err, APACK_ETIMEOUT, where, blockIdx.x, threadIdx.x);
+      return false;
+    }
+  }
+}
+// The same for a whole warp, which goes on or leaves together.
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, Bars *b, DeviceError *err, int where) {
+  return __all_sync(0xffffffffu, wait(bar, parity, b, err, where));
+}
+
+// A role's walk over the CTA's segments.  An operation is an accumulator's products with a tile: two per tile (pair: each
+// accumulator its half of the rows), or one (the accumulators take the tiles in turn).
+struct Seg {
+  GroupSeg g;
+  int tiles;
+  bool pair;
+};
+__device__ __forceinline__ bool read_rec(Bars *b, int n, Seg &s, DeviceError *err, int where) {
+  if (!warp_wait(&b->rec_full[n % kRecs], (n / kRecs) & 1u, b, err, where)) return false;
+  s.g = b->rec[n % kRecs];
+  s.tiles = (s.g.key1 - s.g.key0 + kGTile - 1) / kGTile;
+  s.pair = s.g.step == 0;
+  return s.g.seq >= 0;
+}
+struct Ops {
+  Seg s;
+  int rec = 0, tile = 0, half = 0, all_tiles = 0, count = 0;   // count: operations so far; the accumulator is its parity
+  bool ok;
+  __device__ __forceinline__ void start(Bars *b, DeviceError *err) { ok = read_rec(b, 0, s, err, 161); }
+  __device__ __forceinline__ int slot() const { return count & 1; }
+  __device__ __forceinline__ bool first() const { return s.pair ? tile == 0 : tile <= 1; }          // of its accumulator
+  __device__ __forceinline__ bool last() const { return s.pair ? tile == s.tiles - 1 : tile >= s.tiles - 2; }
+  __device__ __forceinline__ bool opens() const { return !s.pair || half == 0; }                      // of its tile
+  __device__ __forceinline__ bool closes() const { return !s.pair || half == 1; }
+  __device__ __forceinline__ void next(Bars *b, DeviceError *err) {
+    ++count;
+    if (s.pair && half == 0) {
+      half = 1;
+      return;
+    }
+    half = 0;
+    ++all_tiles;
+    if (++tile == s.tiles) {
+      tile = 0;
+      ok = read_rec(b, ++rec, s, err, 161);
+    }
+  }
+};
+
 template <class T, int D>
-__global__ void __launch_bounds__(256) group_rows_kernel(const __grid_constant__ GroupArgs A) {
-  constexpr int kF = D / 32;
-  __shared__ float qs[8][D];
-  pdl_wait_and_release();
-  GroupHead h;
-  if (!group_head(A, h)) {
-    if (threadIdx.x == 0 && blockIdx.x == 0) raise_device_error(A.err, APACK_EDEVICE, 150);
+__global__ void __launch_bounds__(kThreads, 1)
+    group_tc_kernel(const __grid_constant__ GroupArgs A, const __grid_constant__ FastDiv group,
+                    const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
+  using L = Lay<D>;
+  constexpr int kRing = L::kRing, kBlocks = D / 64;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  Bars *b = reinterpret_cast<Bars *>(smem + L::kOffBars);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if ((smem_u32(smem) & 1023u) != 0) {
+    if (threadIdx.x == 0) raise_device_error(A.err, APACK_EDEVICE, 160);
     return;
   }
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kRing; ++i) {
+      mbar_init(&b->full[i], A.box ? 1 : kLoadWarps * 32);
+      mbar_init(&b->empty[i], 1);
+    }
+    for (int i = 0; i < kRecs; ++i) mbar_init(&b->rec_full[i], 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&b->q_full[i], 4);
+      mbar_init(&b->s_full[i], 1);
+      mbar_init(&b->p_full[i], 4);
+      mbar_init(&b->o_full[i], 1);
+    }
+    mbar_init(&b->drain, 1);
+    b->abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == kMmaWarp) {
+    tmem_alloc(&b->tmem, kTmemCols);
+    tc_fence_before();
+  }
+  if (threadIdx.x == kLoadWarp * 32 && A.box) {
+    tma_prefetch_desc(&kmap);
+    tma_prefetch_desc(&vmap);
+  }
+  __syncthreads();
+  tc_fence_after();
+  pdl_wait_and_release();
+  const uint32_t tmem = b->tmem;
+  GroupHead h;
+  const bool planned = group_head(A, h);
+  int item = 0;                                                   // tiles issued by a load warp
+  if (!planned) {
+    if (threadIdx.x == 0 && blockIdx.x == 0) raise_device_error(A.err, APACK_EDEVICE, 150);
+  } else if (warp >= kLoadWarp) {
+    // ------------------------------------------------------------ loads
+    const GroupSeg *segs = reinterpret_cast<const GroupSeg *>(A.ws + h.seg_off);
+    unsigned int *claims = reinterpret_cast<unsigned int *>(A.ws + kGClaimOff);
+    const uint32_t ring = smem_u32(smem) + L::kOffRing;
+    if (A.box && warp == kLoadWarp) {
+      const int box = A.box;
+      // the lane's box of a tile: its page, known one tile ahead
+      const int blk = lane % kBlocks, bx = lane / kBlocks;
+      auto claim = [&] {
+        unsigned c = 0;
+        if (lane == 0) c = gridDim.x + atomicAdd(claims, 1u);
+        return c;
+      };
+      auto fetch = [&](unsigned &claimed, GroupSeg &g) {          // the next segment with work; seq -1: none
+        for (;;) {
+          const unsigned i = __shfl_sync(0xffffffffu, claimed, 0);
+          g.seq = -1;
+          if (i >= static_cast<unsigned>(h.segs)) return;
+          g = segs[i];
+          claimed = claim();
+          if (g.key0 < g.key1) return;
+        }
+      };
+      auto page_of = [&](const GroupSeg &g, int tile) {
+        const int row = g.key0 + tile * kGTile + bx * box;
+        if (g.seq < 0 || bx * box >= kGTile || row >= g.key1) return -1;
+        const int p = A.pool.page_tokens.div(row);
+        const int32_t page = __ldg(A.pool.table + g.seq * A.pool.table_stride + p);
+        if (static_cast<uint32_t>(page) < static_cast<uint32_t>(A.pool.num_pages)) return static_cast<int>(page);
+        raise_device_error(A.err, APACK_EDEVICE, 140, g.seq, page);
+        return A.pool.num_pages;                                  // behind the map's end: zeros
+      };
+      unsigned claimed = blockIdx.x;
+      GroupSeg g, next;
+      fetch(claimed, g);
+      int page = page_of(g, 0);
+      bool ok = true;
+      for (int rec = 0; ok; ++rec) {
+        if (lane == 0) {
+          b->rec[rec % kRecs] = g;
+          mbar_arrive(&b->rec_full[rec % kRecs]);
+        }
+        if (g.seq < 0) break;
+        const int tiles = (g.key1 - g.key0 + kGTile - 1) / kGTile;
+        for (int t = 0; t < tiles && ok; ++t) {
+          if (t == 0) fetch(claimed, next);
+          const int row = g.key0 + t * kGTile, valid = min(kGTile, g.key1 - row);
+          const int boxes = (valid + box - 1) / box;
+          const int mine = page;
+          const bool has = bx < boxes && bx * box < kGTile;
+          const int in = row + bx * box - A.pool.page_tokens.div(row + bx * box) * A.pool.page_tokens.d;
+          page = t + 1 < tiles ? page_of(g, t + 1) : page_of(next, 0);
+          for (int v = 0; v < 2; ++v, ++item) {
+            const int slot = item % kRing;
+            if (item >= kRing && !warp_wait(&b->empty[slot], ((item / kRing) - 1) & 1u, b, A.err, 162)) {
+              ok = false;
+              break;
+            }
+            if (lane == 0) mbar_arrive_expect_tx(&b->full[slot], boxes * box * D * 2);
+            __syncwarp();
+            if (has)
+              tma_box(ring + slot * L::kTileBytes + blk * kHalfBytes + bx * box * 128, v ? &vmap : &kmap, &b->full[slot], in,
+                      blk, g.head, mine);
+          }
+        }
+        g = next;
+      }
+    } else if (!A.box) {
+      // rows by the lanes.  A copy is seen by the tensor cores only behind a fence of the thread that made it, so a tile's
+      // arrival is signalled when the tile after next has been issued and its own copies have landed.
+      constexpr int kChunks = D / 8, kAtOnce = 32 / kChunks, kBehind = 2;
+      const int w = warp - kLoadWarp, ch = lane % kChunks;
+      unsigned claimed = blockIdx.x;
+      int signalled = 0;
+      bool ok = true;
+      auto signal = [&](int upto) {
+        fence_proxy_async_smem();
+        for (; signalled < upto; ++signalled) mbar_arrive(&b->full[signalled % kRing]);
+      };
+      for (int rec = 0; ok; ++rec) {
+        Seg s;
+        if (w == 0) {
+          GroupSeg g;
+          for (;;) {
+            const unsigned i = __shfl_sync(0xffffffffu, claimed, 0);
+            g.seq = -1;
+            if (i >= static_cast<unsigned>(h.segs)) break;
+            g = segs[i];
+            if (lane == 0) claimed = gridDim.x + atomicAdd(claims, 1u);
+            if (g.key0 < g.key1) break;
+          }
+          if (lane == 0) {
+            b->rec[rec % kRecs] = g;
+            mbar_arrive(&b->rec_full[rec % kRecs]);
+          }
+          __syncwarp();
+        }
+        if (!read_rec(b, rec, s, A.err, 163)) break;
+        for (int t = 0; t < s.tiles && ok; ++t) {
+          const int row = s.g.key0 + t * kGTile, valid = min(kGTile, s.g.key1 - row);
+          int64_t off[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            off[i] = -1;
+            const int r = i * 32 + lane;
+            if (r >= valid) continue;
+            const int32_t page = A.pool.page_of(s.g.seq, row + r);
+            off[i] = A.pool.offset_in(page, row + r);
+            if (off[i] < 0) raise_device_error(A.err, APACK_EDEVICE, 140, s.g.seq, page);
+            off[i] += off[i] < 0 ? 0 : s.g.head * A.pool.head_stride;
+          }
+          for (int v = 0; v < 2; ++v, ++item) {
+            const int slot = item % kRing;
+            if (item >= kRing && !warp_wait(&b->empty[slot], ((item / kRing) - 1) & 1u, b, A.err, 162)) {
+              ok = false;
+              break;
+            }
+            const uint8_t *base = v ? A.pool.v : A.pool.k;
+            const uint32_t dst = ring + slot * L::kTileBytes + (ch >> 3) * kHalfBytes;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll 4
+              for (int j = w; j < 32 / kAtOnce; j += kLoadWarps) {
+                const int rr = j * kAtOnce + lane / kChunks, r = i * 32 + rr;
+                const int64_t o = __shfl_sync(0xffffffffu, off[i], rr);
+                if (r < valid)
+                  cp_async_16_or_zero(dst + r * 128 + (((ch & 7) ^ (r & 7)) << 4), base + (o < 0 ? 0 : o) + ch * 16, o >= 0);
+              }
+            cp_async_commit();
+            cp_async_wait<kBehind>();
+            if (item + 1 > kBehind) signal(item + 1 - kBehind);
+          }
+        }
+      }
+      cp_async_wait<0>();
+      signal(item);
+    }
+  } else if (warp == kMmaWarp) {
+    // ------------------------------------------------------------ products
+    const uint32_t q_base = smem_u32(smem), ring = q_base + L::kOffRing;
+    constexpr uint32_t kIdS = idesc<T>(kGTile, false), kIdO = idesc<T>(D, true);
+    uint32_t q_par[2] = {0, 0}, p_par[2] = {0, 0};
+    bool issued = false;
+    auto scores = [&](const Ops &o) {
+      const int s = o.slot(), n = 2 * o.all_tiles, slot = n % kRing;
+      if (o.first()) {
+        if (!warp_wait(&b->q_full[s], s ? q_par[1] : q_par[0], b, A.err, 164)) return false;
+        if (s)
+          q_par[1] ^= 1;
+        else
+          q_par[0] ^= 1;
+      }
+      if (o.opens() && !warp_wait(&b->full[slot], (n / kRing) & 1u, b, A.err, 165)) return false;
+      tc_fence_after();
+      if (lane == 0) {
+        const uint32_t a = q_base + s * (kGSlot * D * 2), k = ring + slot * L::kTileBytes;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+          const uint32_t off = (i >> 2) * kHalfBytes + (i & 3) * 32;
+          tc_mma_bf16(tmem + s * kGTile, smem_desc_sw128(a + off), smem_desc_sw128(k + off), kIdS, i > 0);
+        }
+        tc_commit(&b->s_full[s]);
+        if (o.closes()) tc_commit(&b->empty[slot]);
+      }
+      issued = true;
+      __syncwarp();
+      return true;
+    };
+    Ops ahead, now;
+    ahead.start(b, A.err);
+    now = ahead;
+    bool ok = true;
+    for (int i = 0; i < 2 && ok && ahead.ok; ++i) {
+      ok = scores(ahead);
+      ahead.next(b, A.err);
+    }
+    while (ok && now.ok) {
+      const int s = now.slot(), n = 2 * now.all_tiles + 1, slot = n % kRing;
+      if (!warp_wait(&b->p_full[s], s ? p_par[1] : p_par[0], b, A.err, 166)) break;
+      if (s)
+        p_par[1] ^= 1;
+      else
+        p_par[0] ^= 1;
+      const uint32_t v = ring + slot * L::kTileBytes;
+      if (now.opens()) {
+        if (!warp_wait(&b->full[slot], (n / kRing) & 1u, b, A.err, 167)) break;
+        const int valid = now.s.g.key1 - now.s.g.key0 - now.tile * kGTile;
+        if (valid < kGTile) {
+          // behind the last key: zeros, whatever lies there (0 times a stale infinity would be NaN)
+          for (int i = lane; i < (kGTile - valid) * (D / 8); i += 32) {
+            const int r = valid + i / (D / 8), ch = i % (D / 8);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v + (ch >> 3) * kHalfBytes + r * 128 + (ch & 7) * 16),
+                         "r"(0)
+                         : "memory");
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+      }
+      tc_fence_after();
+      if (lane == 0) {
+#pragma unroll
+        for (int i = 0; i < kGTile / 16; ++i)
+          tc_mma_ts(tmem + 256 + s * 128, tmem + s * kGTile + i * 8, smem_desc_sw128_mn(v + i * 2048, kHalfBytes, 1024), kIdO,
+                    (!now.first() || i > 0) ? 1u : 0u);
+        if (now.closes()) tc_commit(&b->empty[slot]);
+        if (now.last()) tc_commit(&b->o_full[s]);
+      }
+      __syncwarp();
+      now.next(b, A.err);
+      if (ahead.ok) {
+        ok = scores(ahead);
+        ahead.next(b, A.err);
+      }
+    }
+    if (issued && lane == 0) {                                    // every product done before the CTA leaves
+      tc_commit(&b->drain);
+      mbar_wait(&b->drain, 0, kWaitLimitNs / 4);
+    }
+    __syncwarp();
+  } else {
+    // ------------------------------------------------------------ softmax, a query row per thread
+    const int s = warp >> 2, row = threadIdx.x & 127;
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t sc = tmem + lanes + s * kGTile, oc = tmem + lanes + 256 + s * 128;
+    const GroupTok *toks = reinterpret_cast<const GroupTok *>(A.ws + h.tok_off);
+    float2 *ml = reinterpret_cast<float2 *>(A.ws + h.ml_off);
+    float *parts = reinterpret_cast<float *>(A.ws + h.part_off);
+    uint8_t *qs = smem + s * (kGSlot * D * 2);
+    uint32_t s_par = 0, o_par = 0, par = 0;
+    Seg seg;
+    for (int rec = 0; read_rec(b, rec, seg, A.err, 168); ++rec) {
+      const int which = s ^ par;                                  // half of the rows, or first tile
+      if (!seg.pair) par ^= seg.tiles & 1;
+      if (!seg.pair && which >= seg.tiles) continue;
+      const int r = (seg.pair ? which * kGSlot : 0) + row;
+      const bool real = r < seg.g.rows;
+      int limit = 0;
+      {
+        const uint32_t packed = seg.g.row0 + (real ? r : 0), t = group.div(packed);
+        const uint4 *src = reinterpret_cast<const uint4 *>(
+            A.q + t * A.q_stride + (static_cast<int64_t>(seg.g.head) * A.group + (packed - t * A.group)) * (D * 2));
+        if (real) limit = min(toks[t].limit, seg.g.key1);
+#pragma unroll
+        for (int i0 = 0; i0 < D / 8; i0 += 8) {
+          uint4 x[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = real ? __ldg(src + i0 + i) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            *reinterpret_cast<uint4 *>(qs + (i0 >> 3) * kHalfBytes + row * 128 + ((i ^ (row & 7)) << 4)) = x[i];
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&b->q_full[s]);
+      float m = -INFINITY, l = 0.f;
+      bool ok = true, first = true;
+      for (int t = seg.pair ? 0 : which; t < seg.tiles; t += seg.pair ? 1 : 2) {
+        ok = warp_wait(&b->s_full[s], s_par, b, A.err, 169);
+        if (!ok) break;
+        s_par ^= 1;
+        tc_fence_after();
+        uint32_t x[4][32];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tmem_ld32(sc + i * 32, x[i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tmem_wait32(x[i]);
+        const int seen = limit - seg.g.key0 - t * kGTile;
+        if (__any_sync(0xffffffffu, seen < kGTile)) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (i * 32 + j >= seen) x[i][j] = 0xFF800000u;      // -infinity
+        }
+        float top[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          top[i] = __uint_as_float(x[i][0]);
+#pragma unroll
+          for (int j = 1; j < 32; ++j) top[i] = fmaxf(top[i], __uint_as_float(x[i][j]));
+        }
+        const float mn = fmaf(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), A.scale2, -Type<T>::kShift);
+        const bool grows = mn > m + Type<T>::kGrow;               // (also every finite logit against -infinity)
+        if (__any_sync(0xffffffffu, grows)) {
+          const float f = grows ? ex2_approx(m - mn) : 1.f;
+          if (grows) m = mn;
+          l *= f;
+          if (!first) {
+#pragma unroll
+            for (int c = 0; c < D; c += 16) {
+              uint32_t o[16];
+              tmem_ld16_wait(oc + c, o);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+              tmem_st16(oc + c, o);
+            }
+          }
+        }
+        const float2 neg = m == -INFINITY ? make_float2(0.f, 0.f) : make_float2(-m, -m);
+        const float2 scale = make_float2(A.scale2, A.scale2);
+        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t p[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const float2 y = ffma2(make_float2(__uint_as_float(x[i][2 * j]), __uint_as_float(x[i][2 * j + 1])), scale, neg);
+            const float2 e = make_float2(ex2_approx(y.x), ex2_approx(y.y));
+            sum[j & 1] = fadd2(sum[j & 1], e);
+            p[j] = Type<T>::pack(e.x, e.y);
+          }
+          tmem_st16(sc + i * 16, p);
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&b->p_full[s]);
+        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+        first = false;
+      }
+      ok = ok && warp_wait(&b->o_full[s], o_par, b, A.err, 170);
+      if (!ok) break;
+      o_par ^= 1;
+      tc_fence_after();
+      const int64_t at = static_cast<int64_t>(seg.g.part) + (seg.pair ? r : static_cast<int64_t>(which) * seg.g.step + row);
+      if (real) ml[at] = make_float2(m, l);
+#pragma unroll
+      for (int c = 0; c < D; c += 32) {
+        uint32_t o[32];
+        tmem_ld32(oc + c, o);
+        tmem_wait32(o);
+        if (real)
+#pragma unroll
+          for (int j = 0; j < 32; j += 8) store8(parts + at * D + c + j, o + j);
+      }
+      tc_fence_before();
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (b->abort && A.box && warp == kLoadWarp && lane == 0)        // copies that nobody waited for
+    for (int i = max(0, item - kRing); i < item; ++i) mbar_wait(&b->full[i % kRing], (i / kRing) & 1u, kWaitLimitNs / 4);
+  if (warp == kMmaWarp) tmem_dealloc(tmem, kTmemCols);
+}
+
+// ---------------------------------------------------------------- merge
+
+constexpr int kBatch = 8;                // parts whose loads a warp has in flight
+
+template <int D>
+struct Row {                             // of a warp: max, sum, D / 32 values on from lane * D / 32
+  float m, l, o[D / 32];
+};
+
+template <int D>
+__device__ __forceinline__ void load_values(float (&o)[D / 32], const float *p) {
+  if (D == 128) {
+    const float4 x = *reinterpret_cast<const float4 *>(p);
+    o[0] = x.x, o[1] = x.y, o[2 % (D / 32)] = x.z, o[3 % (D / 32)] = x.w;
+  } else {
+    const float2 x = *reinterpret_cast<const float2 *>(p);
+    o[0] = x.x, o[1] = x.y;
+  }
+}
+
+// A row's parts of one item: those from number `from` on, every `step`th, added to a.
+template <int D>
+__device__ __forceinline__ void merge_item(const GroupArgs &A, const GroupHead &h, const GroupTok *toks, const GroupItem &it,
+                                           int head, int packed, int from, int step, Row<D> &a) {
+  constexpr int kF = D / 32;
+  const int lane = threadIdx.x & 31, rr = packed - it.row0, run = rr / kGRows;
+  const int rows = min(kGRows, it.rows - run * kGRows);
+  const bool two = it.sub == 2 && rows <= kGSlot;
+  int key1 = it.key1;
+  if (it.causal) key1 = min(key1, toks[(it.row0 + run * kGRows + rows - 1) / A.group].limit);
+  const int tiles = (key1 - it.key0 + kGTile - 1) / kGTile, splits = (tiles + it.chunk - 1) / it.chunk;
+  const int n = splits * (two ? 2 : 1);
+  const float2 *ml = reinterpret_cast<const float2 *>(A.ws + h.ml_off);
+  const float *parts = reinterpret_cast<const float *>(A.ws + h.part_off);
+  for (int k = from; k < n; k += kBatch * step) {
+    float2 st[kBatch];
+    float x[kBatch][kF];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int j = k + i * step, split = two ? j >> 1 : j, u = two ? j & 1 : 0;
+      st[i] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int e = 0; e < kF; ++e) x[i][e] = 0.f;
+      if (j < n && (u == 0 || tiles - split * it.chunk > 1) && !(u == 1 && it.chunk < 2)) {
+        const int64_t at = static_cast<int64_t>(it.part) + static_cast<int64_t>((split * it.sub + u) * A.hkv + head) * it.rows + rr;
+        st[i] = ml[at];
+        load_values<D>(x[i], parts + at * D + lane * kF);
+      }
+    }
+    float top = a.m;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) top = fmaxf(top, st[i].x);
+    const float f = a.m == top ? 1.f : ex2_approx(a.m - top);
+    a.m = top;
+    a.l *= f;
+#pragma unroll
+    for (int e = 0; e < kF; ++e) a.o[e] *= f;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      // (a part whose row saw nothing has sum 0, and a NaN maximum none)
+      const float w = st[i].x == top ? 1.f : ex2_approx(st[i].x - top);
+      a.l += st[i].y * w;
+#pragma unroll
+      for (int e = 0; e < kF; ++e) a.o[e] += x[i][e] * w;
+    }
+  }
+}
+
+// W: warps of a row (a CTA of 8 warps takes 8 / W rows).
+template <class T, int D, int W>
+__global__ void __launch_bounds__(256) group_merge_kernel(const __grid_constant__ GroupArgs A) {
+  constexpr int kF = D / 32;
+  __shared__ float qs[8][D];
+  __shared__ float2 stat[8];
+  pdl_wait_and_release();
+  GroupHead h;
+  if (!group_head(A, h)) return;                       // recorded by the kernel before
+  if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<unsigned int *>(A.ws + kGClaimOff) = 0;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t u = blockIdx.x * 8ll + warp;
+  const int64_t u = blockIdx.x * (8ll / W) + warp / W;
   if (u >= static_cast<int64_t>(A.n_q) * A.hq) return;
   const int t = static_cast<int>(u / A.hq), hd = static_cast<int>(u - static_cast<int64_t>(t) * A.hq);
-  const GroupTok tok = reinterpret_cast<const GroupTok *>(A.ws + h.tok_off)[t];
+  const GroupTok *toks = reinterpret_cast<const GroupTok *>(A.ws + h.tok_off);
+  const GroupTok tok = toks[t];
   if (!tok.real) return;
-  const T *q = reinterpret_cast<const T *>(A.q + t * A.q_stride) + hd * D;
-  for (int i = lane; i < D; i += 32) qs[warp][i] = static_cast<float>(q[i]);
-  __syncwarp();
-  float m = -INFINITY, l = 0.f, o[kF] = {};
   const GroupItem *items = reinterpret_cast<const GroupItem *>(A.ws + h.item_off);
-#pragma unroll 1
-  for (int part = 0; part < 2; ++part) {
-    const int i = part ? tok.own : tok.prefix;
-    if (i < 0) continue;
-    group_row<T, D>(A, items[i].seq, hd / A.group, items[i].key0, min(items[i].key1, tok.limit), qs[warp], m, l, o);
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int head = hd / A.group, packed = t * A.group + hd - head * A.group;
+  Row<D> a = {-INFINITY, 0.f, {}};
+  if (tok.prefix >= 0) merge_item<D>(A, h, toks, items[tok.prefix], head, packed, warp % W, W, a);
+  if (tok.own >= 0) merge_item<D>(A, h, toks, items[tok.own], head, packed, warp % W, W, a);
+  if (W > 1) {
+    stat[warp] = make_float2(a.m, a.l);
 #pragma unroll
-  for (int e = 0; e < kF; ++e) reinterpret_cast<T *>(A.out)[u * D + lane * kF + e] = static_cast<T>(o[e] * inv);
-  if (A.lse && lane == 0) A.lse[u] = (m + log2f(l)) * 0.6931471805599453f;
+    for (int e = 0; e < kF; ++e) qs[warp][lane * kF + e] = a.o[e];
+    __syncthreads();
+    if (warp != 0) return;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < W; ++w) top = fmaxf(top, stat[w].x);
+    a = {top, 0.f, {}};
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const float f = stat[w].x == top ? 1.f : ex2_approx(stat[w].x - top);
+      a.l += stat[w].y * f;
+#pragma unroll
+      for (int e = 0; e < kF; ++e) a.o[e] += qs[w][lane * kF + e] * f;
+    }
+    __syncwarp();
+  }
+  bool nan = a.l != a.l;
+#pragma unroll
+  for (int e = 0; e < kF; ++e) nan |= a.o[e] != a.o[e];
+  if (h.causal_any && __any_sync(0xffffffffu, nan)) {
+    // perhaps of a value that the row does not see (0 times NaN): key by key
+    const T *q = reinterpret_cast<const T *>(A.q + t * A.q_stride) + hd * D;
+    for (int i = lane; i < D; i += 32) qs[warp][i] = static_cast<float>(q[i]);
+    __syncwarp();
+    a = {-INFINITY, 0.f, {}};
+#pragma unroll 1
+    for (int part = 0; part < 2; ++part) {
+      const int i = part ? tok.own : tok.prefix;
+      if (i >= 0) group_row<T, D>(A, items[i].seq, head, items[i].key0, min(items[i].key1, tok.limit), qs[warp], a.m, a.l, a.o);
+    }
+  }
+  const float inv = a.l == 0.f ? 0.f : 1.f / a.l;
+  uint32_t w[kF / 2];
+#pragma unroll
+  for (int e = 0; e < kF / 2; ++e) w[e] = Type<T>::pack(a.o[2 * e] * inv, a.o[2 * e + 1] * inv);
+  uint8_t *out = A.out + (u * D + lane * kF) * 2;
+  if (D == 128)
+    *reinterpret_cast<uint2 *>(out) = make_uint2(w[0], w[kF / 2 - 1]);
+  else
+    *reinterpret_cast<uint32_t *>(out) = w[0];
+  if (A.lse && lane == 0) A.lse[u] = (a.m + log2f(a.l)) * 0.6931471805599453f;
 }
 
 template <class T, int D>
-cudaError_t launch_rows(const GroupArgs &A, cudaStream_t stream) {
+cudaError_t launch_group(const GroupArgs &A, const CUtensorMap &kmap, const CUtensorMap &vmap, cudaStream_t stream) {
+  static std::atomic<uint64_t> attr{0};
+  cudaError_t e = once_per_device(attr, [] {
+    return cudaFuncSetAttribute(group_tc_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                static_cast<int>(Lay<D>::kBytes));
+  });
+  if (e != cudaSuccess) return e;
+  const int sms = device_sm_count();
+  e = launch_pdl(group_tc_kernel<T, D>, dim3(sms), dim3(kThreads), Lay<D>::kBytes, stream, A,
+                 fast_div(static_cast<uint32_t>(A.group)), kmap, vmap);
+  if (e != cudaSuccess) return e;
+  count_launches(1);
   const int64_t rows = static_cast<int64_t>(A.n_q) * A.hq;
-  const cudaError_t e = launch_pdl(group_rows_kernel<T, D>, dim3(static_cast<unsigned>((rows + 7) / 8)), dim3(256), 0, stream, A);
+  // few rows have many parts: eight warps each
+  e = rows <= 8 * sms ? launch_pdl(group_merge_kernel<T, D, 8>, dim3(static_cast<unsigned>(rows)), dim3(256), 0, stream, A)
+                      : launch_pdl(group_merge_kernel<T, D, 1>, dim3(static_cast<unsigned>((rows + 7) / 8)), dim3(256), 0, stream, A);
   if (e == cudaSuccess) count_launches(1);
   return e;
 }
@@ -94,7 +781,14 @@ extern "C" apack_status apack_paged_group_attention(const apack_paged_cache *cac
   A.box = group_box(cache->page_tokens);
   A.err = static_cast<DeviceError *>(ws);
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  CUtensorMap kmap, vmap;
+  std::memset(&kmap, 0, sizeof(kmap));
+  std::memset(&vmap, 0, sizeof(vmap));
+  if (A.box && (!make_page_map(&kmap, cache, A.pool.k, A.box, 1) || !make_page_map(&vmap, cache, A.pool.v, A.box, 1)))
+    return APACK_ECUDA;
   if (cache->dtype == APACK_BF16)
-    return check_cuda(cache->head_dim == 128 ? launch_rows<__nv_bfloat16, 128>(A, cs) : launch_rows<__nv_bfloat16, 64>(A, cs));
-  return check_cuda(cache->head_dim == 128 ? launch_rows<__half, 128>(A, cs) : launch_rows<__half, 64>(A, cs));
+    return check_cuda(cache->head_dim == 128 ? launch_group<__nv_bfloat16, 128>(A, kmap, vmap, cs)
+                                             : launch_group<__nv_bfloat16, 64>(A, kmap, vmap, cs));
+  return check_cuda(cache->head_dim == 128 ? launch_group<__half, 128>(A, kmap, vmap, cs)
+                                           : launch_group<__half, 64>(A, kmap, vmap, cs));
 }
