@@ -43,7 +43,7 @@ namespace {
 constexpr int kThreads = 384;
 constexpr int kMmaWarp = 8, kLoadWarp = 9, kLoadWarps = 3;
 constexpr int kHalfBytes = kGTile * 128;                       // 64 features of 128 rows
-constexpr int kRecs = 16;
+constexpr int kRecs = 16, kTails = 4;
 constexpr uint32_t kTmemCols = 512;                            // S 0, S 1, O 0, O 1, 128 columns each
 
 template <int D>
@@ -60,6 +60,7 @@ struct __align__(16) Bars {
   uint64_t full[8], empty[8];
   uint64_t rec_full[kRecs];
   uint64_t q_full[2], s_full[2], p_full[2], o_full[2], drain;
+  uint64_t tail_asked[kTails], tail_done[kTails];               // in turn; asked for at most 3 operations ahead of its product
   uint32_t tmem;
   volatile int32_t abort;
 };
@@ -110,6 +111,14 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
+// One thread of the warp.  What it issues to the tensor cores inside this branch takes one instruction each; inside
+// "lane == 0" the compiler cannot tell that a single thread is there (8 products issued in 580 clocks, here 520, of which
+// 512 are the products).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+  return one != 0;
+}
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void store8(float *p, const uint32_t *r) {       // 32 bytes, aligned
   asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
@@ -127,10 +136,11 @@ __device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap *map, ui
 
 // Bounded; false when it gave up or another role of the CTA has.
 __device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, Bars *b, DeviceError *err, int where) {
-  if (mbar_try_wait(bar, parity)) return true;
+  for (int i = 0; i < 64; ++i)                                    // most end here, without a look at the clock
+    if (mbar_try_wait(bar, parity)) return true;
   const uint64_t t0 = globaltimer_ns();
   for (;;) {
-    for (int i = 0; i < 32; ++i)
+    for (int i = 0; i < 64; ++i)
       if (mbar_try_wait(bar, parity)) return true;
     if (b->abort) return false;
     if (globaltimer_ns() - t0 > kWaitLimitNs) {
@@ -152,8 +162,11 @@ struct Seg {
   int tiles;
   bool pair;
 };
+template <bool WARP = true>
 __device__ __forceinline__ bool read_rec(Bars *b, int n, Seg &s, DeviceError *err, int where) {
-  if (!warp_wait(&b->rec_full[n % kRecs], (n / kRecs) & 1u, b, err, where)) return false;
+  uint64_t *bar = &b->rec_full[n % kRecs];
+  const uint32_t parity = (n / kRecs) & 1u;
+  if (!(WARP ? warp_wait(bar, parity, b, err, where) : wait(bar, parity, b, err, where))) return false;
   s.g = b->rec[n % kRecs];
   s.tiles = (s.g.key1 - s.g.key0 + kGTile - 1) / kGTile;
   s.pair = s.g.step == 0;
@@ -163,7 +176,7 @@ struct Ops {
   Seg s;
   int rec = 0, tile = 0, half = 0, all_tiles = 0, count = 0;   // count: operations so far; the accumulator is its parity
   bool ok;
-  __device__ __forceinline__ void start(Bars *b, DeviceError *err) { ok = read_rec(b, 0, s, err, 161); }
+  __device__ __forceinline__ void start(Bars *b, DeviceError *err) { ok = read_rec<false>(b, 0, s, err, 161); }
   __device__ __forceinline__ int slot() const { return count & 1; }
   __device__ __forceinline__ bool first() const { return s.pair ? tile == 0 : tile <= 1; }          // of its accumulator
   __device__ __forceinline__ bool last() const { return s.pair ? tile == s.tiles - 1 : tile >= s.tiles - 2; }
@@ -179,7 +192,7 @@ struct Ops {
     ++all_tiles;
     if (++tile == s.tiles) {
       tile = 0;
-      ok = read_rec(b, ++rec, s, err, 161);
+      ok = read_rec<false>(b, ++rec, s, err, 161);
     }
   }
 };
@@ -208,6 +221,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&b->s_full[i], 1);
       mbar_init(&b->p_full[i], 4);
       mbar_init(&b->o_full[i], 1);
+    }
+    for (int i = 0; i < kTails; ++i) {
+      mbar_init(&b->tail_asked[i], 1);
+      mbar_init(&b->tail_done[i], 1);
     }
     mbar_init(&b->drain, 1);
     b->abort = 0;
@@ -298,6 +315,31 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         g = next;
       }
+    } else if (A.box && warp == kLoadWarp + 1) {
+      // behind a segment's last key: zeros in V, whatever lies there (0 times a stale infinity would be NaN).  Asked for when the
+      // scores of that tile are issued: its V is then the next tile to land in its place, or has.
+      Seg s;
+      int n = 1, tails = 0;                                       // n: the V tile's place among the tiles
+      for (int rec = 0; read_rec(b, rec, s, A.err, 172); ++rec) {
+        n += 2 * (s.tiles - 1);
+        const int valid = s.g.key1 - s.g.key0 - (s.tiles - 1) * kGTile, slot = n % kRing;
+        if (valid < kGTile) {
+          if (!warp_wait(&b->tail_asked[tails % kTails], (tails / kTails) & 1u, b, A.err, 174)) break;
+          if (!warp_wait(&b->full[slot], (n / kRing) & 1u, b, A.err, 173)) break;
+          const uint32_t v = ring + slot * L::kTileBytes;
+          for (int i = lane; i < (kGTile - valid) * (D / 8); i += 32) {
+            const int r = valid + i / (D / 8), ch = i % (D / 8);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v + (ch >> 3) * kHalfBytes + r * 128 + (ch & 7) * 16),
+                         "r"(0)
+                         : "memory");
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&b->tail_done[tails % kTails]);
+          ++tails;
+        }
+        n += 2;
+      }
     } else if (!A.box) {
       // rows by the lanes.  A copy is seen by the tensor cores only behind a fence of the thread that made it, so a tile's
       // arrival is signalled when the tile after next has been issued and its own copies have landed.
@@ -356,7 +398,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               for (int j = w; j < 32 / kAtOnce; j += kLoadWarps) {
                 const int rr = j * kAtOnce + lane / kChunks, r = i * 32 + rr;
                 const int64_t o = __shfl_sync(0xffffffffu, off[i], rr);
-                if (r < valid)
+                if (r < valid || v)                               // (values behind the last key: zeros)
                   cp_async_16_or_zero(dst + r * 128 + (((ch & 7) ^ (r & 7)) << 4), base + (o < 0 ? 0 : o) + ch * 16, o >= 0);
               }
             cp_async_commit();
@@ -369,86 +411,70 @@ __global__ void __launch_bounds__(kThreads, 1)
       signal(item);
     }
   } else if (warp == kMmaWarp) {
-    // ------------------------------------------------------------ products
-    const uint32_t q_base = smem_u32(smem), ring = q_base + L::kOffRing;
-    constexpr uint32_t kIdS = idesc<T>(kGTile, false), kIdO = idesc<T>(D, true);
-    uint32_t q_par[2] = {0, 0}, p_par[2] = {0, 0};
-    bool issued = false;
-    auto scores = [&](const Ops &o) {
-      const int s = o.slot(), n = 2 * o.all_tiles, slot = n % kRing;
-      if (o.first()) {
-        if (!warp_wait(&b->q_full[s], s ? q_par[1] : q_par[0], b, A.err, 164)) return false;
-        if (s)
-          q_par[1] ^= 1;
-        else
-          q_par[0] ^= 1;
-      }
-      if (o.opens() && !warp_wait(&b->full[slot], (n / kRing) & 1u, b, A.err, 165)) return false;
-      tc_fence_after();
-      if (lane == 0) {
-        const uint32_t a = q_base + s * (kGSlot * D * 2), k = ring + slot * L::kTileBytes;
+    // ------------------------------------------------------------ products, by one thread
+    if (elect_one()) {
+      const uint32_t q_base = smem_u32(smem), ring = q_base + L::kOffRing;
+      constexpr uint32_t kIdS = idesc<T>(kGTile, false), kIdO = idesc<T>(D, true);
+      uint32_t q_par = 0, p_par = 0;                              // a bit per accumulator
+      int asked = 0, tails = 0;
+      auto ragged = [&](const Ops &o) {                           // the tile has places behind the last key
+        return A.box && o.opens() && o.s.g.key1 - o.s.g.key0 - o.tile * kGTile < kGTile;
+      };
+      bool issued = false;
+      auto scores = [&](const Ops &o) {
+        const int s = o.slot(), n = 2 * o.all_tiles, slot = n % kRing;
+        if (o.first()) {
+          if (!wait(&b->q_full[s], q_par >> s & 1u, b, A.err, 164)) return false;
+          q_par ^= 1u << s;
+        }
+        if (o.opens() && !wait(&b->full[slot], (n / kRing) & 1u, b, A.err, 165)) return false;
+        if (ragged(o)) mbar_arrive(&b->tail_asked[asked++ % kTails]);
+        tc_fence_after();
+        const uint64_t q = smem_desc_sw128(q_base + s * (kGSlot * D * 2)), k = smem_desc_sw128(ring + slot * L::kTileBytes);
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
-          const uint32_t off = (i >> 2) * kHalfBytes + (i & 3) * 32;
-          tc_mma_bf16(tmem + s * kGTile, smem_desc_sw128(a + off), smem_desc_sw128(k + off), kIdS, i > 0);
+          const uint32_t off = ((i >> 2) * kHalfBytes + (i & 3) * 32) >> 4;      // (addresses are below 2^18: no carry)
+          tc_mma_bf16(tmem + s * kGTile, q + off, k + off, kIdS, i > 0);
         }
         tc_commit(&b->s_full[s]);
         if (o.closes()) tc_commit(&b->empty[slot]);
-      }
-      issued = true;
-      __syncwarp();
-      return true;
-    };
-    Ops ahead, now;
-    ahead.start(b, A.err);
-    now = ahead;
-    bool ok = true;
-    for (int i = 0; i < 2 && ok && ahead.ok; ++i) {
-      ok = scores(ahead);
-      ahead.next(b, A.err);
-    }
-    while (ok && now.ok) {
-      const int s = now.slot(), n = 2 * now.all_tiles + 1, slot = n % kRing;
-      if (!warp_wait(&b->p_full[s], s ? p_par[1] : p_par[0], b, A.err, 166)) break;
-      if (s)
-        p_par[1] ^= 1;
-      else
-        p_par[0] ^= 1;
-      const uint32_t v = ring + slot * L::kTileBytes;
-      if (now.opens()) {
-        if (!warp_wait(&b->full[slot], (n / kRing) & 1u, b, A.err, 167)) break;
-        const int valid = now.s.g.key1 - now.s.g.key0 - now.tile * kGTile;
-        if (valid < kGTile) {
-          // behind the last key: zeros, whatever lies there (0 times a stale infinity would be NaN)
-          for (int i = lane; i < (kGTile - valid) * (D / 8); i += 32) {
-            const int r = valid + i / (D / 8), ch = i % (D / 8);
-            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v + (ch >> 3) * kHalfBytes + r * 128 + (ch & 7) * 16),
-                         "r"(0)
-                         : "memory");
-          }
-          fence_proxy_async_smem();
-          __syncwarp();
-        }
-      }
-      tc_fence_after();
-      if (lane == 0) {
-#pragma unroll
-        for (int i = 0; i < kGTile / 16; ++i)
-          tc_mma_ts(tmem + 256 + s * 128, tmem + s * kGTile + i * 8, smem_desc_sw128_mn(v + i * 2048, kHalfBytes, 1024), kIdO,
-                    (!now.first() || i > 0) ? 1u : 0u);
-        if (now.closes()) tc_commit(&b->empty[slot]);
-        if (now.last()) tc_commit(&b->o_full[s]);
-      }
-      __syncwarp();
-      now.next(b, A.err);
-      if (ahead.ok) {
+        issued = true;
+        return true;
+      };
+      Ops ahead, now;
+      ahead.start(b, A.err);
+      now = ahead;
+      bool ok = true;
+      for (int i = 0; i < 2 && ok && ahead.ok; ++i) {
         ok = scores(ahead);
         ahead.next(b, A.err);
       }
-    }
-    if (issued && lane == 0) {                                    // every product done before the CTA leaves
-      tc_commit(&b->drain);
-      mbar_wait(&b->drain, 0, kWaitLimitNs / 4);
+      while (ok && now.ok) {
+        const int s = now.slot(), n = 2 * now.all_tiles + 1, slot = n % kRing;
+        if (!wait(&b->p_full[s], p_par >> s & 1u, b, A.err, 166)) break;
+        p_par ^= 1u << s;
+        if (now.opens() && !wait(&b->full[slot], (n / kRing) & 1u, b, A.err, 167)) break;
+        if (ragged(now)) {
+          if (!wait(&b->tail_done[tails % kTails], (tails / kTails) & 1u, b, A.err, 171)) break;
+          ++tails;
+        }
+        tc_fence_after();
+        const uint64_t v = smem_desc_sw128_mn(ring + slot * L::kTileBytes, kHalfBytes, 1024);
+#pragma unroll
+        for (int i = 0; i < kGTile / 16; ++i)
+          tc_mma_ts(tmem + 256 + s * 128, tmem + s * kGTile + i * 8, v + (i * 2048 >> 4), kIdO, (i > 0 || !now.first()) ? 1u : 0u);
+        if (now.closes()) tc_commit(&b->empty[slot]);
+        if (now.last()) tc_commit(&b->o_full[s]);
+        now.next(b, A.err);
+        if (ahead.ok) {
+          ok = scores(ahead);
+          ahead.next(b, A.err);
+        }
+      }
+      if (issued) {                                               // every product done before the CTA leaves
+        tc_commit(&b->drain);
+        mbar_wait(&b->drain, 0, kWaitLimitNs / 4);
+      }
     }
     __syncwarp();
   } else {
