@@ -10,15 +10,15 @@
 // A segment (group_plan.cu) is 256 query rows of a KV head against a run of 128-key tiles.  CTAs (one per SM) take segments from
 // a counter, long ones first; every segment's result is a part (max, sum, unnormalised values) of its own, and the merge
 // adds a row's parts in the order of their keys, so that the result does not depend on who took what.
-//   warps 0..3, 4..7   softmax of accumulators 0 and 1, a query row per thread (TMEM lane): scores S read whole, P written over
-//                      them as 16-bit pairs (the A operand of the second product comes from TMEM), O left in TMEM for the whole
-//                      segment.  The row's reference maximum is set anew only when it has grown by more than 2^8 (2^4 in fp16):
-//                      then the warp rescales its rows of O.
-//   warp 8             the tensor products, one thread issuing: S = Q K^T and O += P V for accumulators 0 and 1 in turn, so that
-//                      one softmax runs while the other's products do.  S of the operation after next is issued
-//                      right behind O of this one (same accumulator; products run in the order of issue).
-//   warps 9..11        loads: K and V tiles in a ring of 5 (8 with heads of 64), by TMA boxes of up to 128 tokens (warp 9, a box per lane), or
-//                      16 bytes at a time where pages are no multiple of 8 tokens (all three)
+//   warps 0..3, 4..7   softmax of accumulators 0 and 1, a query row per thread (TMEM lane): P is written over S as 16-bit pairs (the
+//                      A operand of the second product comes from TMEM), O stays in TMEM for the whole segment.  A row's
+//                      reference maximum is set anew only when it has grown by more than 2^8 (2^4 in fp16): then its warp
+//                      rescales its O.
+//   warp 8             the tensor products, one thread issuing: S = Q K^T and O += P V of accumulators 0 and 1 in turn, so that
+//                      one softmax runs while the other's products do.  S of an accumulator's next tile is issued right
+//                      behind O of this one (products run in the order of issue).
+//   warps 9..11        loads: K and V tiles in a ring of 5 (8 with heads of 64), by TMA boxes of up to 128 tokens (a warp for K, one
+//                      for V, a box per lane), or 16 bytes at a time where pages are no multiple of 8 tokens (all three)
 // A segment of more than 128 rows gives each accumulator half of the rows; one of fewer gives them the even and the odd tiles,
 // and writes two parts.  Operations alternate between the accumulators across segments too, so that short segments overlap.
 //
@@ -43,7 +43,7 @@ namespace {
 constexpr int kThreads = 384;
 constexpr int kMmaWarp = 8, kLoadWarp = 9, kLoadWarps = 3;
 constexpr int kHalfBytes = kGTile * 128;                       // 64 features of 128 rows
-constexpr int kRecs = 16, kTails = 4;
+constexpr int kRecs = 16;
 constexpr uint32_t kTmemCols = 512;                            // S 0, S 1, O 0, O 1, 128 columns each
 
 template <int D>
@@ -60,7 +60,6 @@ struct __align__(16) Bars {
   uint64_t full[8], empty[8];
   uint64_t rec_full[kRecs];
   uint64_t q_full[2], s_full[2], p_full[2], o_full[2], drain;
-  uint64_t tail_asked[kTails], tail_done[kTails];               // in turn; asked for at most 3 operations ahead of its product
   uint32_t tmem;
   volatile int32_t abort;
 };
@@ -155,8 +154,8 @@ __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, Bars *
   return __all_sync(0xffffffffu, wait(bar, parity, b, err, where));
 }
 
-// A role's walk over the CTA's segments.  An operation is an accumulator's products with a tile: two per tile (pair: each
-// accumulator its half of the rows), or one (the accumulators take the tiles in turn).
+// A segment of the CTA as its roles read it.  pair: each accumulator takes half of the rows and every tile; else the
+// accumulators take the tiles in turn.
 struct Seg {
   GroupSeg g;
   int tiles;
@@ -172,27 +171,188 @@ __device__ __forceinline__ bool read_rec(Bars *b, int n, Seg &s, DeviceError *er
   s.pair = s.g.step == 0;
   return s.g.seq >= 0;
 }
-struct Ops {
-  Seg s;
-  int rec = 0, tile = 0, half = 0, all_tiles = 0, count = 0;   // count: operations so far; the accumulator is its parity
-  bool ok;
-  __device__ __forceinline__ void start(Bars *b, DeviceError *err) { ok = read_rec<false>(b, 0, s, err, 161); }
-  __device__ __forceinline__ int slot() const { return count & 1; }
-  __device__ __forceinline__ bool first() const { return s.pair ? tile == 0 : tile <= 1; }          // of its accumulator
-  __device__ __forceinline__ bool last() const { return s.pair ? tile == s.tiles - 1 : tile >= s.tiles - 2; }
-  __device__ __forceinline__ bool opens() const { return !s.pair || half == 0; }                      // of its tile
-  __device__ __forceinline__ bool closes() const { return !s.pair || half == 1; }
-  __device__ __forceinline__ void next(Bars *b, DeviceError *err) {
-    ++count;
-    if (s.pair && half == 0) {
-      half = 1;
-      return;
+// A tile's places in the ring: K, and V behind it.
+template <int RING>
+struct Place {
+  int k = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ int v() const { return k + 1 == RING ? 0 : k + 1; }
+  __device__ __forceinline__ uint32_t v_phase() const { return k + 1 == RING ? phase ^ 1u : phase; }
+  __device__ __forceinline__ void next() {
+    k += 2;
+    if (k >= RING) {
+      k -= RING;
+      phase ^= 1u;
     }
-    half = 0;
-    ++all_tiles;
-    if (++tile == s.tiles) {
-      tile = 0;
-      ok = read_rec<false>(b, ++rec, s, err, 161);
+  }
+  __device__ __forceinline__ void skip(int tiles) {
+    const int at = k + 2 * tiles;
+    phase ^= (at / RING) & 1;
+    k = at % RING;
+  }
+};
+
+__device__ __forceinline__ bool passed(uint64_t *bar, uint32_t parity) {      // without waiting
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
+// Bounded, and asked for again and again: for what comes within a tile's time.
+__device__ __forceinline__ bool hot_wait(uint64_t *bar, uint32_t parity, Bars *b, DeviceError *err, int where) {
+  for (int i = 0; i < 1024; ++i)
+    if (passed(bar, parity)) return true;
+  return wait(bar, parity, b, err, where);
+}
+
+// The products of the CTA's segments, by one thread.  What it does between a softmax's signal and the products that wait for
+// it is on the critical path of an accumulator, and takes some ten clocks per instruction: so a tile's places, phases and
+// descriptors are ready before, and the next tile's scores follow the values with nothing but their issue in between.
+template <class T, int D>
+struct Products {
+  using L = Lay<D>;
+  Bars *b;
+  DeviceError *err;
+  uint32_t base, tmem;
+  Place<L::kRing> at;                                            // of the tile whose scores come next
+  uint32_t q_par = 0, p_par = 0;                                 // a bit per accumulator
+
+  __device__ __forceinline__ uint64_t keys_desc(int slot) const { return smem_desc_sw128(base + L::kOffRing + slot * L::kTileBytes); }
+  __device__ __forceinline__ uint64_t values_desc(int slot) const {
+    return smem_desc_sw128_mn(base + L::kOffRing + slot * L::kTileBytes, kHalfBytes, 1024);
+  }
+  template <int S>
+  __device__ __forceinline__ void scores(uint64_t k) const {
+    const uint64_t q = smem_desc_sw128(base + S * (kGSlot * D * 2));
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      const uint32_t off = ((i >> 2) * kHalfBytes + (i & 3) * 32) >> 4;      // (addresses are below 2^18: no carry)
+      tc_mma_bf16(tmem + S * kGTile, q + off, k + off, idesc<T>(kGTile, false), i > 0);
+    }
+  }
+  template <int S>
+  __device__ __forceinline__ void values(uint64_t v, uint32_t accumulate) const {
+#pragma unroll
+    for (int i = 0; i < kGTile / 16; ++i)
+      tc_mma_ts(tmem + 256 + S * 128, tmem + S * kGTile + i * 8, v + (i * 2048 >> 4), idesc<T>(D, true), i > 0 ? 1u : accumulate);
+  }
+  template <int S>
+  __device__ __forceinline__ bool queries() {
+    if (!wait(&b->q_full[S], q_par >> S & 1u, b, err, 165)) return false;
+    q_par ^= 1u << S;
+    return true;
+  }
+  template <int S>
+  __device__ __forceinline__ bool weights() {
+    if (!hot_wait(&b->p_full[S], p_par >> S & 1u, b, err, 166)) return false;
+    p_par ^= 1u << S;
+    tc_fence_after();
+    return true;
+  }
+  __device__ __forceinline__ bool tile(const Place<L::kRing> &p) {
+    return wait(&b->full[p.k], p.phase, b, err, 167) && wait(&b->full[p.v()], p.v_phase(), b, err, 167);
+  }
+
+  // Both accumulators, F first, each its rows: every tile.
+  template <int F>
+  __device__ __forceinline__ bool rows(int tiles) {
+    if (!queries<F>() || !wait(&b->full[at.k], at.phase, b, err, 168)) return false;
+    tc_fence_after();
+    uint64_t k = keys_desc(at.k);
+    scores<F>(k);
+    tc_commit(&b->s_full[F]);
+    if (!queries<1 - F>()) return false;
+    tc_fence_after();
+    scores<1 - F>(k);
+    tc_commit(&b->s_full[1 - F]);
+    tc_commit(&b->empty[at.k]);
+    for (int t = 0; t < tiles; ++t) {
+      Place<L::kRing> then = at;
+      then.next();
+      const bool more = t + 1 < tiles;
+      const int vs = at.v();
+      const uint64_t v = values_desc(vs);
+      k = keys_desc(then.k);
+      const uint32_t accumulate = t > 0;
+      if (!wait(&b->full[vs], at.v_phase(), b, err, 167) || (more && !wait(&b->full[then.k], then.phase, b, err, 168))) return false;
+      if (!weights<F>()) return false;
+      values<F>(v, accumulate);
+      if (more) scores<F>(k);
+      tc_commit(more ? &b->s_full[F] : &b->o_full[F]);
+      if (!weights<1 - F>()) return false;
+      values<1 - F>(v, accumulate);
+      if (more) scores<1 - F>(k);
+      tc_commit(more ? &b->s_full[1 - F] : &b->o_full[1 - F]);
+      tc_commit(&b->empty[vs]);
+      if (more) tc_commit(&b->empty[then.k]);
+      at = then;
+    }
+    return true;
+  }
+  // Both accumulators, F first, the tiles in turn.
+  template <int F>
+  __device__ __forceinline__ bool turns(int tiles) {
+    Place<L::kRing> p[2] = {at, at};
+    p[1].next();
+    if (!queries<F>() || !wait(&b->full[p[0].k], p[0].phase, b, err, 168)) return false;
+    tc_fence_after();
+    scores<F>(keys_desc(p[0].k));
+    tc_commit(&b->s_full[F]);
+    tc_commit(&b->empty[p[0].k]);
+    if (tiles > 1) {
+      if (!queries<1 - F>() || !wait(&b->full[p[1].k], p[1].phase, b, err, 168)) return false;
+      tc_fence_after();
+      scores<1 - F>(keys_desc(p[1].k));
+      tc_commit(&b->s_full[1 - F]);
+      tc_commit(&b->empty[p[1].k]);
+    }
+    for (int t = 0; t < tiles; t += 2) {
+      if (!turn<F>(p[0], t, tiles)) return false;
+      if (t + 1 < tiles && !turn<1 - F>(p[1], t + 1, tiles)) return false;
+    }
+    at.skip(tiles);
+    return true;
+  }
+  template <int S>
+  __device__ __forceinline__ bool turn(Place<L::kRing> &p, int t, int tiles) {
+    Place<L::kRing> then = p;
+    then.next();
+    then.next();
+    const bool more = t + 2 < tiles;
+    const int vs = p.v();
+    const uint64_t v = values_desc(vs), k = keys_desc(then.k);
+    if (!wait(&b->full[vs], p.v_phase(), b, err, 167) || (more && !wait(&b->full[then.k], then.phase, b, err, 168))) return false;
+    if (!weights<S>()) return false;
+    values<S>(v, t > 1);
+    if (more) scores<S>(k);
+    tc_commit(more ? &b->s_full[S] : &b->o_full[S]);
+    tc_commit(&b->empty[vs]);
+    if (more) tc_commit(&b->empty[then.k]);
+    p = then;
+    return true;
+  }
+  __device__ __forceinline__ void run() {
+    uint32_t par = 0;
+    bool issued = false, ok = true;
+    Seg seg;
+    for (int rec = 0; ok && read_rec<false>(b, rec, seg, err, 161); ++rec) {
+      issued = true;
+      if (seg.pair) {
+        ok = par ? rows<1>(seg.tiles) : rows<0>(seg.tiles);
+      } else {
+        ok = par ? turns<1>(seg.tiles) : turns<0>(seg.tiles);
+        par ^= seg.tiles & 1;
+      }
+    }
+    if (issued) {                                               // every product done before the CTA leaves
+      tc_commit(&b->drain);
+      mbar_wait(&b->drain, 0, kWaitLimitNs / 4);
     }
   }
 };
@@ -222,10 +382,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&b->p_full[i], 4);
       mbar_init(&b->o_full[i], 1);
     }
-    for (int i = 0; i < kTails; ++i) {
-      mbar_init(&b->tail_asked[i], 1);
-      mbar_init(&b->tail_done[i], 1);
-    }
     mbar_init(&b->drain, 1);
     b->abort = 0;
     fence_mbar_init();
@@ -252,93 +408,79 @@ __global__ void __launch_bounds__(kThreads, 1)
     const GroupSeg *segs = reinterpret_cast<const GroupSeg *>(A.ws + h.seg_off);
     unsigned int *claims = reinterpret_cast<unsigned int *>(A.ws + kGClaimOff);
     const uint32_t ring = smem_u32(smem) + L::kOffRing;
-    if (A.box && warp == kLoadWarp) {
-      const int box = A.box;
-      // the lane's box of a tile: its page, known one tile ahead
+    if (A.box && warp < kLoadWarp + 2) {
+      // by TMA: K tiles by the first warp, which also takes the segments, V tiles by the second; a box per lane, whose page is
+      // known one tile ahead
+      const int box = A.box, v = warp - kLoadWarp;
       const int blk = lane % kBlocks, bx = lane / kBlocks;
-      auto claim = [&] {
-        unsigned c = 0;
-        if (lane == 0) c = gridDim.x + atomicAdd(claims, 1u);
-        return c;
-      };
-      auto fetch = [&](unsigned &claimed, GroupSeg &g) {          // the next segment with work; seq -1: none
-        for (;;) {
-          const unsigned i = __shfl_sync(0xffffffffu, claimed, 0);
-          g.seq = -1;
-          if (i >= static_cast<unsigned>(h.segs)) return;
-          g = segs[i];
-          claimed = claim();
-          if (g.key0 < g.key1) return;
-        }
-      };
+      const CUtensorMap *map = v ? &vmap : &kmap;
       auto page_of = [&](const GroupSeg &g, int tile) {
         const int row = g.key0 + tile * kGTile + bx * box;
         if (g.seq < 0 || bx * box >= kGTile || row >= g.key1) return -1;
         const int p = A.pool.page_tokens.div(row);
-        const int32_t page = __ldg(A.pool.table + g.seq * A.pool.table_stride + p);
-        if (static_cast<uint32_t>(page) < static_cast<uint32_t>(A.pool.num_pages)) return static_cast<int>(page);
-        raise_device_error(A.err, APACK_EDEVICE, 140, g.seq, page);
-        return A.pool.num_pages;                                  // behind the map's end: zeros
+        return __ldg(A.pool.table + g.seq * A.pool.table_stride + p);
       };
       unsigned claimed = blockIdx.x;
-      GroupSeg g, next;
-      fetch(claimed, g);
-      int page = page_of(g, 0);
-      bool ok = true;
-      for (int rec = 0; ok; ++rec) {
+      auto fetch = [&] {                                          // the next segment with work; seq -1: none
+        GroupSeg g;
+        for (;;) {
+          const unsigned i = __shfl_sync(0xffffffffu, claimed, 0);
+          g.seq = -1;
+          if (i >= static_cast<unsigned>(h.segs)) return g;
+          g = segs[i];
+          if (lane == 0) claimed = gridDim.x + atomicAdd(claims, 1u);
+          if (g.key0 < g.key1) return g;
+        }
+      };
+      auto publish = [&](int rec, const GroupSeg &g) {
         if (lane == 0) {
           b->rec[rec % kRecs] = g;
           mbar_arrive(&b->rec_full[rec % kRecs]);
         }
-        if (g.seq < 0) break;
+      };
+      auto segment = [&](int rec) {                               // number `rec` of the CTA, for the second warp
+        Seg s;
+        if (!read_rec(b, rec, s, A.err, 163)) s.g.seq = -1;
+        return s.g;
+      };
+      GroupSeg g, next;
+      if (v == 0) {
+        g = fetch();
+        publish(0, g);
+      } else {
+        g = segment(0);
+      }
+      int page = page_of(g, 0);
+      item = v;
+      bool ok = true;
+      for (int rec = 1; ok && g.seq >= 0; ++rec) {
         const int tiles = (g.key1 - g.key0 + kGTile - 1) / kGTile;
-        for (int t = 0; t < tiles && ok; ++t) {
-          if (t == 0) fetch(claimed, next);
-          const int row = g.key0 + t * kGTile, valid = min(kGTile, g.key1 - row);
-          const int boxes = (valid + box - 1) / box;
-          const int mine = page;
-          const bool has = bx < boxes && bx * box < kGTile;
-          const int in = row + bx * box - A.pool.page_tokens.div(row + bx * box) * A.pool.page_tokens.d;
-          page = t + 1 < tiles ? page_of(g, t + 1) : page_of(next, 0);
-          for (int v = 0; v < 2; ++v, ++item) {
-            const int slot = item % kRing;
-            if (item >= kRing && !warp_wait(&b->empty[slot], ((item / kRing) - 1) & 1u, b, A.err, 162)) {
-              ok = false;
-              break;
-            }
-            if (lane == 0) mbar_arrive_expect_tx(&b->full[slot], boxes * box * D * 2);
-            __syncwarp();
-            if (has)
-              tma_box(ring + slot * L::kTileBytes + blk * kHalfBytes + bx * box * 128, v ? &vmap : &kmap, &b->full[slot], in,
-                      blk, g.head, mine);
+        for (int t = 0; t < tiles; ++t, item += 2) {
+          if (t == 0 && v == 0) next = fetch();
+          if (t + 1 == tiles) {
+            if (v == 0)
+              publish(rec, next);
+            else
+              next = segment(rec);
           }
+          const int row = g.key0 + t * kGTile + bx * box, boxes = (min(kGTile, g.key1 - g.key0 - t * kGTile) + box - 1) / box;
+          const int in = row - A.pool.page_tokens.div(row) * A.pool.page_tokens.d, slot = item % kRing;
+          int mine = page;
+          page = t + 1 < tiles ? page_of(g, t + 1) : page_of(next, 0);
+          if (item >= kRing && !warp_wait(&b->empty[slot], ((item / kRing) - 1) & 1u, b, A.err, 162)) {
+            ok = false;
+            break;
+          }
+          if (lane == 0) mbar_arrive_expect_tx(&b->full[slot], boxes * box * D * 2);
+          __syncwarp();
+          if (bx < boxes && static_cast<uint32_t>(mine) >= static_cast<uint32_t>(A.pool.num_pages)) {
+            raise_device_error(A.err, APACK_EDEVICE, 140, g.seq, mine);
+            mine = A.pool.num_pages;                              // behind the map's end: zeros
+          }
+          if (bx < boxes)
+            tma_box(ring + slot * L::kTileBytes + blk * kHalfBytes + bx * box * 128, map, &b->full[slot], in, blk, g.head, mine);
         }
         g = next;
-      }
-    } else if (A.box && warp == kLoadWarp + 1) {
-      // behind a segment's last key: zeros in V, whatever lies there (0 times a stale infinity would be NaN).  Asked for when the
-      // scores of that tile are issued: its V is then the next tile to land in its place, or has.
-      Seg s;
-      int n = 1, tails = 0;                                       // n: the V tile's place among the tiles
-      for (int rec = 0; read_rec(b, rec, s, A.err, 172); ++rec) {
-        n += 2 * (s.tiles - 1);
-        const int valid = s.g.key1 - s.g.key0 - (s.tiles - 1) * kGTile, slot = n % kRing;
-        if (valid < kGTile) {
-          if (!warp_wait(&b->tail_asked[tails % kTails], (tails / kTails) & 1u, b, A.err, 174)) break;
-          if (!warp_wait(&b->full[slot], (n / kRing) & 1u, b, A.err, 173)) break;
-          const uint32_t v = ring + slot * L::kTileBytes;
-          for (int i = lane; i < (kGTile - valid) * (D / 8); i += 32) {
-            const int r = valid + i / (D / 8), ch = i % (D / 8);
-            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v + (ch >> 3) * kHalfBytes + r * 128 + (ch & 7) * 16),
-                         "r"(0)
-                         : "memory");
-          }
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&b->tail_done[tails % kTails]);
-          ++tails;
-        }
-        n += 2;
       }
     } else if (!A.box) {
       // rows by the lanes.  A copy is seen by the tensor cores only behind a fence of the thread that made it, so a tile's
@@ -411,70 +553,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       signal(item);
     }
   } else if (warp == kMmaWarp) {
-    // ------------------------------------------------------------ products, by one thread
+    // ------------------------------------------------------------ products, by one thread, the accumulators in turn
     if (elect_one()) {
-      const uint32_t q_base = smem_u32(smem), ring = q_base + L::kOffRing;
-      constexpr uint32_t kIdS = idesc<T>(kGTile, false), kIdO = idesc<T>(D, true);
-      uint32_t q_par = 0, p_par = 0;                              // a bit per accumulator
-      int asked = 0, tails = 0;
-      auto ragged = [&](const Ops &o) {                           // the tile has places behind the last key
-        return A.box && o.opens() && o.s.g.key1 - o.s.g.key0 - o.tile * kGTile < kGTile;
-      };
-      bool issued = false;
-      auto scores = [&](const Ops &o) {
-        const int s = o.slot(), n = 2 * o.all_tiles, slot = n % kRing;
-        if (o.first()) {
-          if (!wait(&b->q_full[s], q_par >> s & 1u, b, A.err, 164)) return false;
-          q_par ^= 1u << s;
-        }
-        if (o.opens() && !wait(&b->full[slot], (n / kRing) & 1u, b, A.err, 165)) return false;
-        if (ragged(o)) mbar_arrive(&b->tail_asked[asked++ % kTails]);
-        tc_fence_after();
-        const uint64_t q = smem_desc_sw128(q_base + s * (kGSlot * D * 2)), k = smem_desc_sw128(ring + slot * L::kTileBytes);
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-          const uint32_t off = ((i >> 2) * kHalfBytes + (i & 3) * 32) >> 4;      // (addresses are below 2^18: no carry)
-          tc_mma_bf16(tmem + s * kGTile, q + off, k + off, kIdS, i > 0);
-        }
-        tc_commit(&b->s_full[s]);
-        if (o.closes()) tc_commit(&b->empty[slot]);
-        issued = true;
-        return true;
-      };
-      Ops ahead, now;
-      ahead.start(b, A.err);
-      now = ahead;
-      bool ok = true;
-      for (int i = 0; i < 2 && ok && ahead.ok; ++i) {
-        ok = scores(ahead);
-        ahead.next(b, A.err);
-      }
-      while (ok && now.ok) {
-        const int s = now.slot(), n = 2 * now.all_tiles + 1, slot = n % kRing;
-        if (!wait(&b->p_full[s], p_par >> s & 1u, b, A.err, 166)) break;
-        p_par ^= 1u << s;
-        if (now.opens() && !wait(&b->full[slot], (n / kRing) & 1u, b, A.err, 167)) break;
-        if (ragged(now)) {
-          if (!wait(&b->tail_done[tails % kTails], (tails / kTails) & 1u, b, A.err, 171)) break;
-          ++tails;
-        }
-        tc_fence_after();
-        const uint64_t v = smem_desc_sw128_mn(ring + slot * L::kTileBytes, kHalfBytes, 1024);
-#pragma unroll
-        for (int i = 0; i < kGTile / 16; ++i)
-          tc_mma_ts(tmem + 256 + s * 128, tmem + s * kGTile + i * 8, v + (i * 2048 >> 4), kIdO, (i > 0 || !now.first()) ? 1u : 0u);
-        if (now.closes()) tc_commit(&b->empty[slot]);
-        if (now.last()) tc_commit(&b->o_full[s]);
-        now.next(b, A.err);
-        if (ahead.ok) {
-          ok = scores(ahead);
-          ahead.next(b, A.err);
-        }
-      }
-      if (issued) {                                               // every product done before the CTA leaves
-        tc_commit(&b->drain);
-        mbar_wait(&b->drain, 0, kWaitLimitNs / 4);
-      }
+      Products<T, D> products{b, A.err, smem_u32(smem), tmem};
+      products.run();
     }
     __syncwarp();
   } else {
@@ -485,10 +567,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     const GroupTok *toks = reinterpret_cast<const GroupTok *>(A.ws + h.tok_off);
     float2 *ml = reinterpret_cast<float2 *>(A.ws + h.ml_off);
     float *parts = reinterpret_cast<float *>(A.ws + h.part_off);
-    uint8_t *qs = smem + s * (kGSlot * D * 2);
+    uint8_t *qs = smem + s * (kGSlot * D * 2) + row * 128;
     uint32_t s_par = 0, o_par = 0, par = 0;
+    Place<kRing> place;                                           // of the segment's first tile
     Seg seg;
+    int before = 0;                                               // tiles of the segment before
     for (int rec = 0; read_rec(b, rec, seg, A.err, 168); ++rec) {
+      place.skip(before);
+      before = seg.tiles;
       const int which = s ^ par;                                  // half of the rows, or first tile
       if (!seg.pair) par ^= seg.tiles & 1;
       if (!seg.pair && which >= seg.tiles) continue;
@@ -499,16 +585,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t packed = seg.g.row0 + (real ? r : 0), t = group.div(packed);
         const uint4 *src = reinterpret_cast<const uint4 *>(
             A.q + t * A.q_stride + (static_cast<int64_t>(seg.g.head) * A.group + (packed - t * A.group)) * (D * 2));
-        if (real) limit = min(toks[t].limit, seg.g.key1);
+        if (real) limit = min(toks[t].limit, seg.g.key1) - seg.g.key0;
+        uint4 x[D / 8];
 #pragma unroll
-        for (int i0 = 0; i0 < D / 8; i0 += 8) {
-          uint4 x[8];
+        for (int i = 0; i < D / 8; ++i) x[i] = real ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = real ? __ldg(src + i0 + i) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            *reinterpret_cast<uint4 *>(qs + (i0 >> 3) * kHalfBytes + row * 128 + ((i ^ (row & 7)) << 4)) = x[i];
-        }
+        for (int i = 0; i < D / 8; ++i)
+          *reinterpret_cast<uint4 *>(qs + (i >> 3) * kHalfBytes + (((i & 7) ^ (row & 7)) << 4)) = x[i];
       }
       fence_proxy_async_smem();
       __syncwarp();
@@ -520,31 +603,47 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!ok) break;
         s_par ^= 1;
         tc_fence_after();
-        uint32_t x[4][32];
+        // Probabilities against the present reference, and the maximum beside them: the two use different units.  Where the
+        // reference turns out to be too low (always in a segment's first tile), both are taken again against a new one.
+        const int seen = limit - t * kGTile;
+        const bool cut = __any_sync(0xffffffffu, seen < kGTile);
+        uint32_t p[4][16];
+        float2 sum[2];
+        float top;
+        auto exponentials = [&] {
+          uint32_t x[4][32];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_ld32(sc + i * 32, x[i]);
+          for (int i = 0; i < 4; ++i) tmem_ld32(sc + i * 32, x[i]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_wait32(x[i]);
-        const int seen = limit - seg.g.key0 - t * kGTile;
-        if (__any_sync(0xffffffffu, seen < kGTile)) {
+          for (int i = 0; i < 4; ++i) tmem_wait32(x[i]);
+          if (cut)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                if (i * 32 + j >= seen) x[i][j] = 0xFF800000u;      // -infinity
+          const float2 neg = m == -INFINITY ? make_float2(0.f, 0.f) : make_float2(-m, -m);
+          const float2 scale = make_float2(A.scale2, A.scale2);
+          sum[0] = sum[1] = make_float2(0.f, 0.f);
+          float most[2] = {-INFINITY, -INFINITY};
 #pragma unroll
           for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (i * 32 + j >= seen) x[i][j] = 0xFF800000u;      // -infinity
-        }
-        float top[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          top[i] = __uint_as_float(x[i][0]);
-#pragma unroll
-          for (int j = 1; j < 32; ++j) top[i] = fmaxf(top[i], __uint_as_float(x[i][j]));
-        }
-        const float mn = fmaf(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), A.scale2, -Type<T>::kShift);
-        const bool grows = mn > m + Type<T>::kGrow;               // (also every finite logit against -infinity)
+            for (int j = 0; j < 16; ++j) {
+              const float2 v = make_float2(__uint_as_float(x[i][2 * j]), __uint_as_float(x[i][2 * j + 1]));
+              const float2 y = ffma2(v, scale, neg);
+              const float2 e = make_float2(ex2_approx(y.x), ex2_approx(y.y));
+              most[j & 1] = fmaxf(most[j & 1], fmaxf(v.x, v.y));
+              sum[j & 1] = fadd2(sum[j & 1], e);
+              p[i][j] = Type<T>::pack(e.x, e.y);
+            }
+          top = fmaf(fmaxf(most[0], most[1]), A.scale2, -Type<T>::kShift);
+        };
+        exponentials();
+        const bool grows = top > m + Type<T>::kGrow;              // (every finite score grows from -infinity)
         if (__any_sync(0xffffffffu, grows)) {
-          const float f = grows ? ex2_approx(m - mn) : 1.f;
-          if (grows) m = mn;
+          const float f = grows ? ex2_approx(m - top) : 1.f;
+          if (grows) m = top;
           l *= f;
           if (!first) {
 #pragma unroll
@@ -556,21 +655,26 @@ __global__ void __launch_bounds__(kThreads, 1)
               tmem_st16(oc + c, o);
             }
           }
+          exponentials();
         }
-        const float2 neg = m == -INFINITY ? make_float2(0.f, 0.f) : make_float2(-m, -m);
-        const float2 scale = make_float2(A.scale2, A.scale2);
-        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t p[16];
+        for (int i = 0; i < 4; ++i) tmem_st16(sc + i * 16, p[i]);
+        if (t == seg.tiles - 1 && A.box) {
+          // behind the segment's last key: zeros in V, whatever lies there (0 times a stale infinity would be NaN; where both
+          // accumulators read the tile, both write them)
+          const int valid = seg.g.key1 - seg.g.key0 - t * kGTile;
+          if (valid < kGTile) {
+            Place<kRing> at = place;
+            at.skip(t);
+            ok = warp_wait(&b->full[at.v()], at.v_phase(), b, A.err, 173);
+            if (!ok) break;
+            if (row >= valid)
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const float2 y = ffma2(make_float2(__uint_as_float(x[i][2 * j]), __uint_as_float(x[i][2 * j + 1])), scale, neg);
-            const float2 e = make_float2(ex2_approx(y.x), ex2_approx(y.y));
-            sum[j & 1] = fadd2(sum[j & 1], e);
-            p[j] = Type<T>::pack(e.x, e.y);
+              for (int i = 0; i < D / 8; ++i)
+                *reinterpret_cast<uint4 *>(smem + L::kOffRing + at.v() * L::kTileBytes + (i >> 3) * kHalfBytes + row * 128 +
+                                           (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+            fence_proxy_async_smem();
           }
-          tmem_st16(sc + i * 16, p);
         }
         tmem_wait_st();
         tc_fence_before();
@@ -600,8 +704,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (b->abort && A.box && warp == kLoadWarp && lane == 0)        // copies that nobody waited for
-    for (int i = max(0, item - kRing); i < item; ++i) mbar_wait(&b->full[i % kRing], (i / kRing) & 1u, kWaitLimitNs / 4);
+  if (b->abort && A.box && warp >= kLoadWarp && warp < kLoadWarp + 2 && lane == 0)        // copies that nobody waited for
+    for (int i = max(warp - kLoadWarp, item - 2 * kRing); i < item; i += 2)
+      mbar_wait(&b->full[i % kRing], (i / kRing) & 1u, kWaitLimitNs / 4);
   if (warp == kMmaWarp) tmem_dealloc(tmem, kTmemCols);
 }
 
