@@ -44,6 +44,7 @@ constexpr int kThreads = 384;
 constexpr int kMmaWarp = 8, kLoadWarp = 9, kLoadWarps = 3;
 constexpr int kHalfBytes = kGTile * 128;                       // 64 features of 128 rows
 constexpr int kRecs = 16;
+constexpr int kClaimAhead = 3;                                 // tiles before a segment's end at which the next is claimed
 constexpr uint32_t kTmemCols = 512;                            // S 0, S 1, O 0, O 1, 128 columns each
 
 template <int D>
@@ -456,7 +457,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int rec = 1; ok && g.seq >= 0; ++rec) {
         const int tiles = (g.key1 - g.key0 + kGTile - 1) / kGTile;
         for (int t = 0; t < tiles; ++t, item += 2) {
-          if (t == 0 && v == 0) next = fetch();
+          // (not sooner: a segment that is claimed early waits for a CTA that has a long one)
+          if (t == max(0, tiles - kClaimAhead) && v == 0) next = fetch();
           if (t + 1 == tiles) {
             if (v == 0)
               publish(rec, next);
@@ -567,7 +569,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const GroupTok *toks = reinterpret_cast<const GroupTok *>(A.ws + h.tok_off);
     float2 *ml = reinterpret_cast<float2 *>(A.ws + h.ml_off);
     float *parts = reinterpret_cast<float *>(A.ws + h.part_off);
-    uint8_t *qs = smem + s * (kGSlot * D * 2) + row * 128;
+    uint8_t *qs = smem + s * (kGSlot * D * 2);
     uint32_t s_par = 0, o_par = 0, par = 0;
     Place<kRing> place;                                           // of the segment's first tile
     Seg seg;
@@ -578,20 +580,36 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int which = s ^ par;                                  // half of the rows, or first tile
       if (!seg.pair) par ^= seg.tiles & 1;
       if (!seg.pair && which >= seg.tiles) continue;
-      const int r = (seg.pair ? which * kGSlot : 0) + row;
+      const int r0 = seg.pair ? which * kGSlot : 0, r = r0 + row;
       const bool real = r < seg.g.rows;
-      int limit = 0;
-      {
-        const uint32_t packed = seg.g.row0 + (real ? r : 0), t = group.div(packed);
-        const uint4 *src = reinterpret_cast<const uint4 *>(
-            A.q + t * A.q_stride + (static_cast<int64_t>(seg.g.head) * A.group + (packed - t * A.group)) * (D * 2));
-        if (real) limit = min(toks[t].limit, seg.g.key1) - seg.g.key0;
-        uint4 x[D / 8];
+      const bool idle = r0 + (warp & 3) * 32 >= seg.g.rows;       // no row of the warp is one: what it leaves in TMEM is not read
+      int limit = 1 << 30;                                        // (what is no row need not be masked: nothing of it is kept)
+      if (real) limit = min(toks[group.div(seg.g.row0 + r)].limit, seg.g.key1) - seg.g.key0;
+      if (!idle) {
+        // the warp's 32 rows, D / 8 lanes each: a row's 16-byte pieces side by side (a row per lane took 10,000 clocks)
+        constexpr int kLanes = D / 8, kRows = 32 / kLanes;
+        const int piece = lane % kLanes;
+        constexpr int kAtOnce = 8;
+#pragma unroll 1
+        for (int i0 = 0; i0 < kLanes && r0 + (warp & 3) * 32 + i0 * kRows < seg.g.rows; i0 += kAtOnce) {
+          uint4 x[kAtOnce];
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) x[i] = real ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
+          for (int i = 0; i < kAtOnce; ++i) {
+            const int q = (warp & 3) * 32 + (i0 + i) * kRows + lane / kLanes;
+            const uint32_t packed = seg.g.row0 + r0 + q, t = group.div(packed);
+            x[i] = make_uint4(0, 0, 0, 0);
+            if (r0 + q < seg.g.rows)
+              x[i] = __ldg(reinterpret_cast<const uint4 *>(A.q + t * A.q_stride +
+                                                           (static_cast<int64_t>(seg.g.head) * A.group + (packed - t * A.group)) *
+                                                               (D * 2)) +
+                           piece);
+          }
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i)
-          *reinterpret_cast<uint4 *>(qs + (i >> 3) * kHalfBytes + (((i & 7) ^ (row & 7)) << 4)) = x[i];
+          for (int i = 0; i < kAtOnce; ++i) {
+            const int q = (warp & 3) * 32 + (i0 + i) * kRows + lane / kLanes;
+            *reinterpret_cast<uint4 *>(qs + (piece >> 3) * kHalfBytes + q * 128 + (((piece & 7) ^ (q & 7)) << 4)) = x[i];
+          }
+        }
       }
       fence_proxy_async_smem();
       __syncwarp();
@@ -603,62 +621,85 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!ok) break;
         s_par ^= 1;
         tc_fence_after();
-        // Probabilities against the present reference, and the maximum beside them: the two use different units.  Where the
-        // reference turns out to be too low (always in a segment's first tile), both are taken again against a new one.
-        const int seen = limit - t * kGTile;
-        const bool cut = __any_sync(0xffffffffu, seen < kGTile);
-        uint32_t p[4][16];
-        float2 sum[2];
-        float top;
-        auto exponentials = [&] {
-          uint32_t x[4][32];
+        if (!idle) {
+          const int seen = limit - t * kGTile;
+          const float2 scale = make_float2(A.scale2, A.scale2);
+          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+          // Most tiles: probabilities against the present reference, and the maximum beside them, because the two use
+          // different units.  Only if the reference turns out to be high enough are they written over the scores.
+          bool done = false;
+          if (!__any_sync(0xffffffffu, first || seen < kGTile)) {
+            uint32_t x[4][32], p[4][16];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) tmem_ld32(sc + i * 32, x[i]);
+            for (int i = 0; i < 4; ++i) tmem_ld32(sc + i * 32, x[i]);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) tmem_wait32(x[i]);
-          if (cut)
+            for (int i = 0; i < 4; ++i) tmem_wait32(x[i]);
+            const float2 neg = m == -INFINITY ? make_float2(0.f, 0.f) : make_float2(-m, -m);
+            float most[2] = {-INFINITY, -INFINITY};
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (i * 32 + j >= seen) x[i][j] = 0xFF800000u;      // -infinity
-          const float2 neg = m == -INFINITY ? make_float2(0.f, 0.f) : make_float2(-m, -m);
-          const float2 scale = make_float2(A.scale2, A.scale2);
-          sum[0] = sum[1] = make_float2(0.f, 0.f);
-          float most[2] = {-INFINITY, -INFINITY};
+              for (int j = 0; j < 16; ++j) {
+                const float2 v = make_float2(__uint_as_float(x[i][2 * j]), __uint_as_float(x[i][2 * j + 1]));
+                const float2 y = ffma2(v, scale, neg);
+                const float2 e = make_float2(ex2_approx(y.x), ex2_approx(y.y));
+                most[j & 1] = fmaxf(most[j & 1], fmaxf(v.x, v.y));
+                sum[j & 1] = fadd2(sum[j & 1], e);
+                p[i][j] = Type<T>::pack(e.x, e.y);
+              }
+            const float top = fmaf(fmaxf(most[0], most[1]), A.scale2, -Type<T>::kShift);
+            done = !__any_sync(0xffffffffu, top > m + Type<T>::kGrow);
+            if (done)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+              for (int i = 0; i < 4; ++i) tmem_st16(sc + i * 16, p[i]);
+          }
+          if (!done) {
+            // A segment's first tile, one that a row does not see whole, or a new reference: 32 scores at a time, in loops (code
+            // that runs once per segment is read from far away)
+            float most = -INFINITY;
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {
+              uint32_t x[32];
+              tmem_ld32(sc + i * 32, x);
+              tmem_wait32(x);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              const float2 v = make_float2(__uint_as_float(x[i][2 * j]), __uint_as_float(x[i][2 * j + 1]));
-              const float2 y = ffma2(v, scale, neg);
-              const float2 e = make_float2(ex2_approx(y.x), ex2_approx(y.y));
-              most[j & 1] = fmaxf(most[j & 1], fmaxf(v.x, v.y));
-              sum[j & 1] = fadd2(sum[j & 1], e);
-              p[i][j] = Type<T>::pack(e.x, e.y);
+              for (int j = 0; j < 32; ++j) most = i * 32 + j < seen ? fmaxf(most, __uint_as_float(x[j])) : most;
             }
-          top = fmaf(fmaxf(most[0], most[1]), A.scale2, -Type<T>::kShift);
-        };
-        exponentials();
-        const bool grows = top > m + Type<T>::kGrow;              // (every finite score grows from -infinity)
-        if (__any_sync(0xffffffffu, grows)) {
-          const float f = grows ? ex2_approx(m - top) : 1.f;
-          if (grows) m = top;
-          l *= f;
-          if (!first) {
+            const float top = fmaf(most, A.scale2, -Type<T>::kShift);
+            const bool grows = top > m + Type<T>::kGrow;          // (also every finite score against -infinity)
+            const float f = grows ? ex2_approx(m - top) : 1.f;
+            if (grows) m = top;
+            l *= f;
+            if (!first && __any_sync(0xffffffffu, grows))
+#pragma unroll 1
+              for (int c = 0; c < D; c += 16) {
+                uint32_t o[16];
+                tmem_ld16_wait(oc + c, o);
 #pragma unroll
-            for (int c = 0; c < D; c += 16) {
-              uint32_t o[16];
-              tmem_ld16_wait(oc + c, o);
+                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                tmem_st16(oc + c, o);
+              }
+            first = false;
+            const float2 neg = m == -INFINITY ? make_float2(0.f, 0.f) : make_float2(-m, -m);
+            sum[0] = sum[1] = make_float2(0.f, 0.f);
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {                         // (P of 32 scores covers none that are still to come)
+              uint32_t x[32], p[16];
+              tmem_ld32(sc + i * 32, x);
+              tmem_wait32(x);
 #pragma unroll
-              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-              tmem_st16(oc + c, o);
+              for (int j = 0; j < 16; ++j) {
+                const float2 y = ffma2(make_float2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), scale, neg);
+                const float2 e = make_float2(i * 32 + 2 * j < seen ? ex2_approx(y.x) : 0.f,
+                                             i * 32 + 2 * j + 1 < seen ? ex2_approx(y.y) : 0.f);
+                sum[j & 1] = fadd2(sum[j & 1], e);
+                p[j] = Type<T>::pack(e.x, e.y);
+              }
+              tmem_st16(sc + i * 16, p);
             }
           }
-          exponentials();
+          l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_st16(sc + i * 16, p[i]);
         if (t == seg.tiles - 1 && A.box) {
           // behind the segment's last key: zeros in V, whatever lies there (0 times a stale infinity would be NaN; where both
           // accumulators read the tile, both write them)
@@ -668,11 +709,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             at.skip(t);
             ok = warp_wait(&b->full[at.v()], at.v_phase(), b, A.err, 173);
             if (!ok) break;
-            if (row >= valid)
-#pragma unroll
-              for (int i = 0; i < D / 8; ++i)
-                *reinterpret_cast<uint4 *>(smem + L::kOffRing + at.v() * L::kTileBytes + (i >> 3) * kHalfBytes + row * 128 +
-                                           (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+            for (int i = row; i < (kGTile - valid) * (D / 8); i += kGSlot) {
+              const int v = valid + i / (D / 8), ch = i % (D / 8);
+              *reinterpret_cast<uint4 *>(smem + L::kOffRing + at.v() * L::kTileBytes + (ch >> 3) * kHalfBytes + v * 128 +
+                                         (ch & 7) * 16) = make_uint4(0, 0, 0, 0);
+            }
             fence_proxy_async_smem();
           }
         }
@@ -680,8 +721,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&b->p_full[s]);
-        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-        first = false;
       }
       ok = ok && warp_wait(&b->o_full[s], o_par, b, A.err, 170);
       if (!ok) break;
@@ -689,15 +728,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc_fence_after();
       const int64_t at = static_cast<int64_t>(seg.g.part) + (seg.pair ? r : static_cast<int64_t>(which) * seg.g.step + row);
       if (real) ml[at] = make_float2(m, l);
+      if (!idle)
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+          uint32_t o[32];
+          tmem_ld32(oc + c, o);
+          tmem_wait32(o);
+          if (real)
 #pragma unroll
-      for (int c = 0; c < D; c += 32) {
-        uint32_t o[32];
-        tmem_ld32(oc + c, o);
-        tmem_wait32(o);
-        if (real)
-#pragma unroll
-          for (int j = 0; j < 32; j += 8) store8(parts + at * D + c + j, o + j);
-      }
+            for (int j = 0; j < 32; j += 8) store8(parts + at * D + c + j, o + j);
+        }
       tc_fence_before();
     }
   }
