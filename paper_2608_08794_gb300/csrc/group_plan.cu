@@ -8,8 +8,7 @@
 //
 // The length of a run.  A segment of c tiles costs about c + kSegCost tiles of one SM; n segments on S SMs end after
 // max(sum of all / S, ceil(long ones / S) * (c + kSegCost)) at the least, and every part's row is written and read once
-// more.  32 warps try a run length each over all items, twice (spread over the logarithm, then around the best), and
-// the least estimate wins.
+// more.  32 warps try two run lengths each over all items, and the least estimate wins.
 #include <algorithm>
 #include <cstring>
 
@@ -39,14 +38,21 @@ struct PlanArgs {
   DeviceError *err;
 };
 
+// Sequences of more new tokens have them written by all threads (the first kMany of them).
+constexpr int kFew = 32, kMany = 1024;
+
+struct Two {
+  int64_t a, b;
+};
 struct PlanShared {
   int32_t cu_q[APACK_MAX_SEQS + 1], cu_g[APACK_MAX_SEQS + 1];
   int32_t rows[2 * APACK_MAX_SEQS], tiles[2 * APACK_MAX_SEQS];      // of the items: groups, then sequences
   int32_t seg0[2 * APACK_MAX_SEQS + 1];
-  float est[kWarps];
-  int32_t cand[kWarps];
-  int64_t warp_sum[kWarps];
-  int32_t bad, longest, chunk, causal;
+  float est[2 * kWarps];
+  Two warp_sum[kWarps];
+  int32_t bad, longest, causal, many;
+  int32_t many_entry[kMany];
+  GroupTok many_tok[kMany];
 };
 
 __device__ __forceinline__ int runs_of(int rows) { return (rows + kGRows - 1) / kGRows; }
@@ -55,26 +61,25 @@ __device__ __forceinline__ int sub_of(const PlanArgs &P, int rows) {
   return P.halves && rows <= 4 * kGRows && last <= kGSlot ? 2 : 1;
 }
 
-__device__ int64_t scan(int64_t v, PlanShared &s, int64_t *total) {
+// Exclusive sums over the block's threads, and the totals, of two numbers each.
+__device__ Two scan(Two v, PlanShared &s, Two *total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int64_t x = v;
+  auto inclusive = [&](Two x) {
 #pragma unroll
-  for (int o = 1; o < 32; o *= 2) {
-    const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
-    if (lane >= o) x += y;
-  }
+    for (int o = 1; o < 32; o *= 2) {
+      const int64_t ya = __shfl_up_sync(0xffffffffu, x.a, o), yb = __shfl_up_sync(0xffffffffu, x.b, o);
+      if (lane >= o) x.a += ya, x.b += yb;
+    }
+    return x;
+  };
+  const Two x = inclusive(v);
   __syncthreads();
   if (lane == 31) s.warp_sum[warp] = x;
   __syncthreads();
-  int64_t w = s.warp_sum[lane];
-#pragma unroll
-  for (int o = 1; o < 32; o *= 2) {
-    const int64_t y = __shfl_up_sync(0xffffffffu, w, o);
-    if (lane >= o) w += y;
-  }
-  *total = __shfl_sync(0xffffffffu, w, 31);
-  const int64_t before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
-  return x - v + (warp ? before : 0);
+  const Two w = inclusive(s.warp_sum[lane]);
+  *total = Two{__shfl_sync(0xffffffffu, w.a, 31), __shfl_sync(0xffffffffu, w.b, 31)};
+  const int64_t ba = __shfl_sync(0xffffffffu, w.a, (warp + 31) & 31), bb = __shfl_sync(0xffffffffu, w.b, (warp + 31) & 31);
+  return Two{x.a - v.a + (warp ? ba : 0), x.b - v.b + (warp ? bb : 0)};
 }
 
 // The last i < n with at[i] <= j.
@@ -90,34 +95,51 @@ __device__ __forceinline__ int last_at(const int32_t *at, int n, int j) {
   return lo;
 }
 
-// Estimated time of run length c, in tiles of one SM; infinite where the workspace does not hold it.  By one warp.
-__device__ float estimate(const PlanArgs &P, const PlanShared &s, int items, int c) {
+// Run length number k of 64 that are tried: the longest item in 1 to 32 runs, then more of them, up to a tile each.
+__device__ __forceinline__ int candidate(int k, int longest) {
+  if (k < 32) return (longest + k) / (k + 1);
+  const float runs = 32.f * exp2f(log2f(longest * (1.f / 32.f)) * (k - 31) * (1.f / 32.f));
+  return max(1, min(longest, static_cast<int>(longest / fmaxf(runs, 1.f) + 0.999f)));
+}
+// Estimated time of two run lengths, in tiles of one SM; infinite where the workspace does not hold them.  By one warp.
+__device__ void estimate(const PlanArgs &P, const PlanShared &s, int items, const int (&c)[2], float (&est)[2]) {
   const int lane = threadIdx.x & 31;
-  float work = 0.f, segs = 0.f, rows = 0.f, big = 0.f, most = 0.f;
+  float work = 0.f, segs[2] = {}, rows[2] = {}, big[2] = {}, most[2] = {};
   for (int i = lane; i < items; i += 32) {
     if (s.rows[i] == 0) continue;
-    const int splits = (s.tiles[i] + c - 1) / c, chunk = (s.tiles[i] + splits - 1) / splits;
     const float heads = static_cast<float>(P.hkv) * runs_of(s.rows[i]);
+    const float part = static_cast<float>(s.rows[i]) * P.hkv * sub_of(P, s.rows[i]);
     work += heads * s.tiles[i];
-    segs += heads * splits;
-    rows += static_cast<float>(s.rows[i]) * P.hkv * splits * sub_of(P, s.rows[i]);
-    if (2 * chunk > c) {
-      big += heads * splits;
-      most = fmaxf(most, chunk);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int splits = (s.tiles[i] + c[j] - 1) / c[j];
+      const float chunk = __fdividef(s.tiles[i], splits);
+      segs[j] += heads * splits;
+      rows[j] += part * splits;
+      if (2.f * chunk > c[j]) {
+        big[j] += heads * splits;
+        most[j] = fmaxf(most[j], ceilf(chunk));
+      }
     }
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     work += __shfl_xor_sync(0xffffffffu, work, o);
-    segs += __shfl_xor_sync(0xffffffffu, segs, o);
-    rows += __shfl_xor_sync(0xffffffffu, rows, o);
-    big += __shfl_xor_sync(0xffffffffu, big, o);
-    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      segs[j] += __shfl_xor_sync(0xffffffffu, segs[j], o);
+      rows[j] += __shfl_xor_sync(0xffffffffu, rows[j], o);
+      big[j] += __shfl_xor_sync(0xffffffffu, big[j], o);
+      most[j] = fmaxf(most[j], __shfl_xor_sync(0xffffffffu, most[j], o));
+    }
   }
-  if (rows > 0.99f * P.cap_rows || segs > 0.99f * P.cap_segs) return INFINITY;
-  const float even = (work + segs * kSegCost) / P.sms;
-  const float rounds = ceilf(big / P.sms) * (most + kSegCost);
-  return fmaxf(even, rounds) + rows * kRowCost / P.sms;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const float even = (work + segs[j] * kSegCost) / P.sms, rounds = ceilf(big[j] / P.sms) * (most[j] + kSegCost);
+    est[j] = rows[j] > 0.99f * P.cap_rows || segs[j] > 0.99f * P.cap_segs
+                 ? INFINITY
+                 : fmaxf(even, rounds) + rows[j] * kRowCost / P.sms;
+  }
 }
 
 __global__ void __launch_bounds__(kThreads, 1) group_plan_kernel(const __grid_constant__ PlanArgs P) {
@@ -128,7 +150,7 @@ __global__ void __launch_bounds__(kThreads, 1) group_plan_kernel(const __grid_co
   GroupTok *tok = reinterpret_cast<GroupTok *>(P.ws + P.tok_off);
   GroupSeg *segs = reinterpret_cast<GroupSeg *>(P.ws + P.seg_off);
   const int warp = threadIdx.x >> 5, n = P.n, ng = P.groups, G = P.group;
-  if (threadIdx.x == 0) s.bad = s.longest = s.causal = 0;
+  if (threadIdx.x == 0) s.bad = s.longest = s.causal = s.many = 0;
   pdl_wait_and_release();
   for (int i = threadIdx.x; i <= n; i += kThreads) s.cu_q[i] = P.cu_q ? P.cu_q[i] : i;
   for (int i = threadIdx.x; i <= ng; i += kThreads) s.cu_g[i] = ng ? P.cu_groups[i] : 0;
@@ -147,59 +169,51 @@ __global__ void __launch_bounds__(kThreads, 1) group_plan_kernel(const __grid_co
       s.bad = 1;
     }
   }
-  auto sequence = [&](int e, int *len) {           // of entry e; -1: none
-    const int b = P.seqs ? P.seqs[e] : e;
-    if (static_cast<uint32_t>(b) >= static_cast<uint32_t>(P.num_seqs)) {
-      raise_device_error(P.err, APACK_EDEVICE, 143, e, b);
-      *len = 0;
-      return -1;
-    }
-    const int x = P.seqlens[b];
-    *len = min(max(x, 0), P.max_rows);
-    if (*len != x) raise_device_error(P.err, APACK_EDEVICE, 144, b, x);
-    return b;
-  };
   __syncthreads();
   const bool bad = s.bad;
   const int total_items = ng + n;
-  // ---- items: groups
-  for (int g = threadIdx.x; g < ng; g += kThreads) {
-    s.rows[g] = s.tiles[g] = 0;
-    if (bad) continue;
-    const int e0 = s.cu_g[g], e1 = s.cu_g[g + 1];
-    GroupItem it = {};
-    if (e1 - e0 > 1) {
-      int len;
-      const int b = sequence(e0, &len), shared = P.prefix[g];
-      if (shared < 0 || shared > len) raise_device_error(P.err, APACK_EDEVICE, 145, g, shared);
-      const int common = min(max(shared, 0), len), cut = common - common % P.align;
-      const int rows = (s.cu_q[e1] - s.cu_q[e0]) * G;
-      if (b >= 0 && cut > 0 && rows > 0) {
-        it.seq = b;
-        it.key1 = cut;
-        it.row0 = s.cu_q[e0] * G;
-        it.rows = s.rows[g] = rows;
-        s.tiles[g] = (cut + kGTile - 1) / kGTile;
-        atomicMax(&s.longest, s.tiles[g]);
-      }
-    }
-    items[g] = it;
-  }
+  // ---- items: every sequence finds its group's shared rows by itself, so that nothing waits between groups and sequences
+  for (int g = threadIdx.x; g < ng; g += kThreads) s.rows[g] = s.tiles[g] = 0;
   __syncthreads();
-  // ---- items: sequences
   for (int e = threadIdx.x; e < n; e += kThreads) {
     s.rows[ng + e] = s.tiles[ng + e] = 0;
     if (bad) continue;
-    GroupItem it = {};
-    int len;
-    const int b = sequence(e, &len), m = s.cu_q[e + 1] - s.cu_q[e];
-    int g = -1, cut = 0;
+    const int m = s.cu_q[e + 1] - s.cu_q[e];
+    int g = -1, first = e, shared = 0, count = 0;
     if (ng && e >= s.cu_g[0] && e < s.cu_g[ng]) {
       g = last_at(s.cu_g, ng, e);
-      if (s.rows[g]) cut = items[g].key1;
+      first = s.cu_g[g];
+      count = s.cu_g[g + 1] - first;
+      shared = P.prefix[g];
     }
+    const int b = P.seqs ? P.seqs[e] : e, b0 = P.seqs ? P.seqs[first] : first;
+    const bool in = static_cast<uint32_t>(b) < static_cast<uint32_t>(P.num_seqs);
+    const bool in0 = static_cast<uint32_t>(b0) < static_cast<uint32_t>(P.num_seqs);
+    const int x = in ? P.seqlens[b] : 0, x0 = in0 ? P.seqlens[b0] : 0;
+    const int len = min(max(x, 0), P.max_rows), len0 = min(max(x0, 0), P.max_rows);
+    if (!in) raise_device_error(P.err, APACK_EDEVICE, 143, e, b);
+    if (len != x) raise_device_error(P.err, APACK_EDEVICE, 144, b, x);
     if (m > len) raise_device_error(P.err, APACK_EDEVICE, 146, e, len);
-    if (m > 0 && b >= 0 && cut < len) {
+    int cut = 0;                                   // rows that are read with the group's
+    if (count > 1) {
+      if (e == first && (shared < 0 || shared > len0)) raise_device_error(P.err, APACK_EDEVICE, 145, g, shared);
+      cut = min(max(shared, 0), len0);
+      cut -= cut % P.align;
+      const int rows = (s.cu_q[first + count] - s.cu_q[first]) * G;
+      if (!in0 || rows == 0) cut = 0;
+      if (e == first && cut > 0) {
+        GroupItem it = {};
+        it.seq = b0;
+        it.key1 = cut;
+        it.row0 = s.cu_q[first] * G;
+        it.rows = s.rows[g] = rows;
+        s.tiles[g] = (cut + kGTile - 1) / kGTile;
+        atomicMax(&s.longest, s.tiles[g]);
+        items[g] = it;
+      }
+    }
+    if (m > 0 && in && cut < len) {
+      GroupItem it = {};
       it.seq = b;
       it.key0 = cut;
       it.key1 = len;
@@ -208,55 +222,45 @@ __global__ void __launch_bounds__(kThreads, 1) group_plan_kernel(const __grid_co
       it.causal = m > 1;
       s.tiles[ng + e] = (len - cut + kGTile - 1) / kGTile;
       atomicMax(&s.longest, s.tiles[ng + e]);
-      if (m > 1) s.causal = 1;
+      items[ng + e] = it;
     }
-    items[ng + e] = it;
-    if (cut > len - m + 1) s.causal = 1;           // a token that does not see all of the shared rows
-    for (int t = s.cu_q[e], i = 1; i <= m && m <= 32; ++t, ++i)
-      tok[t] = GroupTok{max(len - m + i, 0), cut > 0 ? g : -1, s.rows[ng + e] ? ng + e : -1, 1};
+    if (m > 1 || cut > len - m + 1) s.causal = 1;  // (the latter: a token that does not see all of the shared rows)
+    const GroupTok tk = {len - m + 1 - s.cu_q[e], cut > 0 ? g : -1, s.rows[ng + e] ? ng + e : -1, 1};
+    const int i = m > kFew ? atomicAdd(&s.many, 1) : kMany;      // by all threads, below (in any order)
+    if (i < kMany) {
+      s.many_entry[i] = e;
+      s.many_tok[i] = tk;
+    } else {
+      for (int t = s.cu_q[e]; t < s.cu_q[e + 1]; ++t) tok[t] = GroupTok{max(tk.limit + t, 0), tk.prefix, tk.own, 1};
+    }
   }
   __syncthreads();
-  const int n_tok = bad ? 0 : s.cu_q[n];
-  for (int t = threadIdx.x; t < P.n_q; t += kThreads) {
-    if (t >= n_tok) {
-      tok[t] = GroupTok{0, -1, -1, 0};
-      continue;
-    }
-    const int e = last_at(s.cu_q, n, t), m = s.cu_q[e + 1] - s.cu_q[e];
-    if (m <= 32) continue;                         // written above
-    int len;
-    sequence(e, &len);
-    int g = -1;
-    if (ng && e >= s.cu_g[0] && e < s.cu_g[ng]) {
-      g = last_at(s.cu_g, ng, e);
-      if (!s.rows[g]) g = -1;
-    }
-    tok[t] = GroupTok{max(len - m + 1 + t - s.cu_q[e], 0), g, s.rows[ng + e] ? ng + e : -1, 1};
+  const int n_tok = bad ? 0 : s.cu_q[n], many = min(s.many, kMany);
+  for (int i = 0; i < many; ++i) {
+    const int e = s.many_entry[i];
+    const GroupTok tk = s.many_tok[i];
+    for (int t = s.cu_q[e] + threadIdx.x; t < s.cu_q[e + 1]; t += kThreads)
+      tok[t] = GroupTok{max(tk.limit + t, 0), tk.prefix, tk.own, 1};
   }
+  for (int t = n_tok + threadIdx.x; t < P.n_q; t += kThreads) tok[t] = GroupTok{0, -1, -1, 0};
   // ---- the run length
-  const int longest = max(s.longest, 1);
-  int lo = 1, hi = longest;
-  for (int round = 0; round < 2; ++round) {
-    const float f = static_cast<float>(warp + 1) / kWarps;
-    int c = round == 0 ? static_cast<int>(exp2f(log2f(static_cast<float>(longest)) * f) + 0.5f)
-                       : lo + static_cast<int>((hi - lo) * (f - 1.f / kWarps) * (kWarps / (kWarps - 1.f)) + 0.5f);
-    c = warp == kWarps - 1 ? (round == 0 ? longest : hi) : min(max(c, 1), longest);
-    const float est = estimate(P, s, total_items, c);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) {
-      s.est[warp] = est;
-      s.cand[warp] = c;
+  const int longest = max(s.longest, 1), lane = threadIdx.x & 31;
+  {
+    const int c[2] = {candidate(warp, longest), candidate(warp + 32, longest)};
+    float est[2];
+    estimate(P, s, total_items, c, est);
+    if (lane == 0) {
+      s.est[warp] = est[0];
+      s.est[warp + 32] = est[1];
     }
-    __syncthreads();
-    int best = 0;
-    for (int w = 1; w < kWarps; ++w)
-      if (s.est[w] <= s.est[best]) best = w;       // of equals the longest runs
-    if (threadIdx.x == 0) s.chunk = s.est[best] < INFINITY ? s.cand[best] : longest;
-    lo = s.cand[max(best - 1, 0)];
-    hi = s.cand[min(best + 1, kWarps - 1)];
   }
   __syncthreads();
-  const int chunk = s.chunk;
+  // the least, of equals the longest runs; none is finite: one run each, which the workspace holds
+  float best = fminf(s.est[lane], s.est[lane + 32]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) best = fminf(best, __shfl_xor_sync(0xffffffffu, best, o));
+  const unsigned hit = __ballot_sync(0xffffffffu, s.est[lane] == best), later = __ballot_sync(0xffffffffu, s.est[lane + 32] == best);
+  const int chunk = best < INFINITY ? candidate(hit ? __ffs(hit) - 1 : 31 + __ffs(later), longest) : longest;
   // ---- places of segments and parts
   int64_t seg_at = 0, part_at = 0;
   for (int i0 = 0; i0 < total_items; i0 += kThreads) {
@@ -268,8 +272,9 @@ __global__ void __launch_bounds__(kThreads, 1) group_plan_kernel(const __grid_co
     }
     const int64_t here = splits ? static_cast<int64_t>(splits) * P.hkv * runs_of(s.rows[i]) : 0;
     const int64_t part = splits ? static_cast<int64_t>(splits) * sub * P.hkv * s.rows[i] : 0;
-    int64_t all_segs, all_parts;
-    const int64_t seg = seg_at + scan(here, s, &all_segs), row = part_at + scan(part, s, &all_parts);
+    Two all;
+    const Two before = scan(Two{here, part}, s, &all);
+    const int64_t seg = seg_at + before.a, row = part_at + before.b;
     if (i < total_items) {
       s.seg0[i] = static_cast<int32_t>(min(seg, static_cast<int64_t>(INT32_MAX)));
       if (splits) {
@@ -279,8 +284,8 @@ __global__ void __launch_bounds__(kThreads, 1) group_plan_kernel(const __grid_co
         items[i].part = static_cast<int32_t>(min(row, static_cast<int64_t>(INT32_MAX)));
       }
     }
-    seg_at += all_segs;
-    part_at += all_parts;
+    seg_at += all.a;
+    part_at += all.b;
   }
   const bool fits = seg_at <= P.cap_segs && part_at <= P.cap_rows;
   if (!fits && threadIdx.x == 0) raise_device_error(P.err, APACK_EDEVICE, 147, static_cast<int>(seg_at), static_cast<int>(part_at));
@@ -300,7 +305,8 @@ __global__ void __launch_bounds__(kThreads, 1) group_plan_kernel(const __grid_co
     g.rows = min(kGRows, it.rows - run * kGRows);
     g.key0 = it.key0 + split * it.chunk * kGTile;
     g.key1 = min(it.key1, g.key0 + it.chunk * kGTile);
-    if (it.causal) g.key1 = min(g.key1, tok[(g.row0 + g.rows - 1) / G].limit);
+    // (the last row's token sees the fewest rows too many: len - m + 1 + its number)
+    if (it.causal) g.key1 = min(g.key1, it.key1 - it.rows / G + 1 + (run * kGRows + g.rows - 1) / G);
     g.part = it.part + (split * it.sub * P.hkv + h) * it.rows + run * kGRows;
     g.step = it.sub == 2 && g.rows <= kGSlot ? P.hkv * it.rows : 0;
     segs[j] = g;
