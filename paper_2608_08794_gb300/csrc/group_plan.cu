@@ -22,7 +22,6 @@ namespace {
 
 constexpr int kThreads = 1024;
 constexpr int kWarps = 32;
-constexpr int kPer = APACK_MAX_SEQS / kThreads;
 constexpr float kSegCost = 2.5f;               // tiles: queries, first loads, parts
 constexpr float kRowCost = 1056.f / 65536.f;   // tiles: a part's row written and read, against a tile of K and V
 

@@ -13,6 +13,7 @@
 #include <cstring>
 
 #include "paged.cuh"
+#include "ptx.cuh"
 
 namespace apack {
 namespace {
@@ -20,6 +21,10 @@ namespace {
 constexpr int kThreads = 1024;
 constexpr int kWarps = kThreads / 32;
 constexpr int kPer = APACK_MAX_SEQS / kThreads;      // entries of a thread: kThreads apart, so that few entries take few steps
+// Calls that may move more pages than this take a cluster (a step of 61 sequences as one CTA, which saves 3 us; 45,000 pages of
+// 64 questions by one SM, that reads one of them per clock at best, take {ONE} us, by eight {EIGHT}).
+constexpr int kMaxCluster = 8;
+constexpr int64_t kClusterPages = 16384;
 // Rows of the slot map that the first kernel fills by itself.
 constexpr int kInlineRows = 8192;
 
@@ -48,7 +53,9 @@ struct Shared {
   int64_t warp_sum[kWarps];
   uint32_t seen[APACK_MAX_SEQS / 32];
   int32_t at[APACK_MAX_SEQS + 1];    // exclusive sums over the entries
-  int32_t bad;
+  int32_t bad;                       // an entry, as every CTA finds by itself
+  int32_t wrong, shared;             // a page; raised for the whole cluster, read behind its next barrier
+  int32_t freed[kMaxCluster];
 };
 
 __device__ __forceinline__ void report(const Call &C, int where, int a, int b) {
@@ -108,24 +115,67 @@ __device__ int entry_seq(const Call &C, Shared &s, int i) {
   return b;
 }
 
-// The last i with at[i] <= j.
-__device__ __forceinline__ int entry_of(const int32_t *at, int n, int j) {
-  int lo = 0, hi = n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (at[mid] <= j)
-      lo = mid;
-    else
-      hi = mid;
+__device__ __forceinline__ int32_t now(const int32_t *p) { return *const_cast<const volatile int32_t *>(p); }
+
+// The entries of kBatch places of the list (the last i with at[i] <= j), side by side: every pass over a list is bound by the
+// trips of its reads, so a thread has as many of them under way (64 questions that leave and come, 45,000 pages: {BEFORE} us
+// one by one, {AFTER} so).
+constexpr int kBatch = 8;
+__device__ __forceinline__ void entries_of(const int32_t *at, int n, const int (&j)[kBatch], int (&e)[kBatch]) {
+#pragma unroll
+  for (int k = 0; k < kBatch; ++k) e[k] = 0;
+  for (int step = n > 1 ? 1 << (31 - __clz(n - 1)) : 0; step > 0; step >>= 1)
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int c = e[k] + step;
+      if (c < n && at[c] <= j[k]) e[k] = c;
+    }
+}
+// For the thread's places of a list of `sum`, in batches: first `load` for all of a batch, then `more`, then `use`.
+template <int CL, class Load, class More, class Use>
+__device__ __forceinline__ void for_places(const int32_t *at, int n, int sum, Load &&load, More &&more, Use &&use) {
+  for (int j0 = (CL > 1 ? static_cast<int>(cluster_ctarank()) * kThreads : 0) + threadIdx.x; j0 < sum; j0 += kBatch * CL * kThreads) {
+    int j[kBatch], e[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) j[k] = min(j0 + k * CL * kThreads, sum - 1);
+    entries_of(at, n, j, e);
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) load(k, j[k], e[k]);
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) more(k);
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k)
+      if (j0 + k * CL * kThreads < sum) use(k, j[k], e[k]);
   }
-  return lo;
+}
+struct Nothing {
+  __device__ __forceinline__ void operator()(int) const {}
+};
+
+// CL: CTAs of the kernel's cluster, which share a list's places; every one of them looks at all entries by itself.
+template <int CL>
+__device__ __forceinline__ void sync_all() {
+  if (CL > 1)
+    cluster_sync();
+  else
+    __syncthreads();
+}
+template <int CL>
+__device__ __forceinline__ void raise_flag(int32_t *flag) {
+  if (CL == 1) {
+    *flag = 1;
+  } else if (*const_cast<volatile int32_t *>(flag) == 0) {
+    for (int r = 0; r < CL; ++r)
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_shared_rank(flag, r)), "r"(1) : "memory");
+  }
 }
 
+template <int CL>
 __device__ void begin(Shared &s) {
   for (int i = threadIdx.x; i < APACK_MAX_SEQS / 32; i += kThreads) s.seen[i] = 0;
-  if (threadIdx.x == 0) s.bad = 0;
+  if (threadIdx.x == 0) s.bad = s.wrong = s.shared = 0;
   pdl_wait_and_release();
-  __syncthreads();
+  sync_all<CL>();                     // (no CTA writes another's flags before they are cleared)
 }
 
 // ---------------------------------------------------------------- release
@@ -133,9 +183,10 @@ __device__ void begin(Shared &s) {
 // Every entry keeps its first rows[i] rows.  The pages behind them lose a holder; each that has none left goes to the
 // stack once, at its first place in the call's list: while the list is walked a count of 0 becomes the least place at which
 // the page is named (minus 2^31), which is found whatever the order of the threads.
+template <int CL>
 __global__ void __launch_bounds__(kThreads, 1) pages_release_kernel(const __grid_constant__ Call C) {
   __shared__ Shared s;
-  begin(s);
+  begin<CL>(s);
   const PagesView &t = C.t;
   int seq[kPer], keep[kPer], drop[kPer];
   const int count = *t.free_count;
@@ -169,59 +220,108 @@ __global__ void __launch_bounds__(kThreads, 1) pages_release_kernel(const __grid
   if (s.bad) return;                                        // nothing is changed
   // the pages are there, and held
   const int n = C.n, sum = static_cast<int>(total);
-  auto place_of = [&](int j, int *entry) {                  // the table's entry of the list's page j
-    const int e = entry_of(s.at, n, j);
-    *entry = e;
+  auto place_of = [&](int j, int e) {                       // the table's entry of the list's page j
     const int b = C.seqs ? __ldg(C.seqs + e) : e;
     return t.row(b) + t.pages_of(C.rows[e]) + (j - s.at[e]);
   };
-  int e;
-  for (int j = threadIdx.x; j < sum; j += kThreads) {
-    const int p = *place_of(j, &e);
-    if (static_cast<uint32_t>(p) >= static_cast<uint32_t>(t.num_pages) || t.refs[p] < 1) {
-      report(C, 124, e, p);
-      s.bad = 1;
+  int32_t *place[kBatch];
+  int p[kBatch], r[kBatch];
+  auto load = [&](int k, int j, int e) {
+    place[k] = place_of(j, e);
+    p[k] = now(place[k]);
+  };
+  auto holders = [&](int k) { r[k] = static_cast<uint32_t>(p[k]) < static_cast<uint32_t>(t.num_pages) ? now(t.refs + p[k]) : 0; };
+  for_places<CL>(s.at, n, sum, load, holders, [&](int k, int, int e) {
+    if (r[k] < 1) {
+      report(C, 124, e, p[k]);
+      raise_flag<CL>(&s.wrong);
     }
-  }
+    if (r[k] != 1) raise_flag<CL>(&s.shared);
+  });
   if (count < 0 || count > t.num_pages) {
     if (threadIdx.x == 0) report(C, 125, count, 0);
-    s.bad = 1;
+    raise_flag<CL>(&s.wrong);
   }
-  __syncthreads();
-  if (s.bad) return;
-  for (int j = threadIdx.x; j < sum; j += kThreads) atomicSub(t.refs + *place_of(j, &e), 1);
-  __syncthreads();
-  for (int j = threadIdx.x; j < sum; j += kThreads) {
-    const int p = *place_of(j, &e);
-    if (*const_cast<volatile int32_t *>(t.refs + p) <= 0) atomicMin(t.refs + p, j + INT32_MIN);
-  }
-  __syncthreads();
-  // the freed pages' places among themselves
-  const int per = (sum + kThreads - 1) / kThreads, j0 = threadIdx.x * per, j1 = min(sum, j0 + per);
-  int64_t freed = 0;
-  for (int j = j0; j < j1; ++j) freed += *const_cast<volatile int32_t *>(t.refs + *place_of(j, &e)) == j + INT32_MIN;
-  int64_t all;
-  int64_t rank = block_scan(freed, s, &all);
-  if (count + all > t.num_pages) {                          // more free pages than there are: the counts disagree
-    if (threadIdx.x == 0) report(C, 125, count, static_cast<int>(all));
-    all = max(t.num_pages - count, 0);
-  }
-  const int top = count + static_cast<int>(all);
-  for (int j = j0; j < j1; ++j) {
-    int32_t *place = place_of(j, &e);
-    const int p = *place;
-    if (*const_cast<volatile int32_t *>(t.refs + p) == j + INT32_MIN) {
-      if (rank < all) t.free_list[top - 1 - rank] = p;
-      ++rank;
+  sync_all<CL>();
+  if (s.wrong) return;
+  const int room = t.num_pages - count;
+  int top = count;
+  if (!s.shared) {
+    // every page was this sequence's alone: its place in the list is its place on the stack
+    top += min(sum, room);
+    if (sum > room && threadIdx.x == 0) report(C, 125, count, sum);   // more free pages than there are: the counts disagree
+    for_places<CL>(s.at, n, sum, load, Nothing(), [&](int k, int j, int) {
+      if (j < top - count) t.free_list[top - 1 - j] = p[k];
+      t.refs[p[k]] = 0;
+      *place[k] = -1;
+    });
+  } else {
+    for_places<CL>(s.at, n, sum, load, Nothing(), [&](int k, int, int) { atomicSub(t.refs + p[k], 1); });
+    sync_all<CL>();
+    for_places<CL>(s.at, n, sum, load, holders, [&](int k, int j, int) {
+      if (r[k] <= 0) atomicMin(t.refs + p[k], j + INT32_MIN);
+    });
+    sync_all<CL>();
+    // the freed pages' places among themselves: a run of the list per CTA, counted, then placed
+    const int rank = CL > 1 ? cluster_ctarank() : 0;
+    const int per = (sum + CL - 1) / CL, lo = min(rank * per, sum), hi = min(lo + per, sum);
+    int64_t here = 0, first = 0, all = 0;
+    auto run = [&](auto &&take) {                           // in the list's order
+      int64_t before = 0;
+      for (int j0 = lo; j0 < hi; j0 += kBatch * kThreads) {
+        int j[kBatch], e[kBatch], freed = 0;
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) j[k] = min(j0 + static_cast<int>(threadIdx.x) * kBatch + k, sum - 1);
+        entries_of(s.at, n, j, e);
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) load(k, j[k], e[k]);
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) holders(k);
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+          r[k] = j0 + static_cast<int>(threadIdx.x) * kBatch + k < hi && r[k] == j[k] + INT32_MIN;
+          freed += r[k];
+        }
+        int64_t total_here;
+        take(before + block_scan(freed, s, &total_here));
+        before += total_here;
+      }
+      return before;
+    };
+    if (CL > 1) {
+      here = run([](int64_t) {});
+      if (threadIdx.x < CL)
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_shared_rank(&s.freed[rank], threadIdx.x)), "r"(static_cast<int>(here))
+                     : "memory");
+      sync_all<CL>();
+      for (int i = 0; i < CL; ++i) {
+        if (i < rank) first += s.freed[i];
+        all += s.freed[i];
+      }
+    } else {
+      all = run([](int64_t) {});
     }
+    if (all > room) {
+      if (threadIdx.x == 0) report(C, 125, count, static_cast<int>(all));
+      all = room;
+    }
+    top += static_cast<int>(all);
+    run([&](int64_t at) {
+      at += first;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k)
+        if (r[k]) {
+          if (at < all) t.free_list[top - 1 - at] = p[k];
+          ++at;
+        }
+    });
+    sync_all<CL>();
+    for_places<CL>(s.at, n, sum, load, holders, [&](int k, int, int) {
+      if (r[k] < 0) atomicMax(t.refs + p[k], 0);
+      *place[k] = -1;
+    });
   }
-  __syncthreads();
-  for (int j = threadIdx.x; j < sum; j += kThreads) {
-    int32_t *place = place_of(j, &e);
-    const int p = *place;
-    if (*const_cast<volatile int32_t *>(t.refs + p) < 0) atomicMax(t.refs + p, 0);
-    *place = -1;
-  }
+  if (CL > 1 && cluster_ctarank() != 0) return;
   if (threadIdx.x == 0) *t.free_count = top;
 #pragma unroll
   for (int k = 0; k < kPer; ++k)
@@ -231,9 +331,10 @@ __global__ void __launch_bounds__(kThreads, 1) pages_release_kernel(const __grid
 // ---------------------------------------------------------------- fork
 
 // Entry i's sequence takes over its parent's table row and length; every page gets a holder more.
+template <int CL>
 __global__ void __launch_bounds__(kThreads, 1) pages_fork_kernel(const __grid_constant__ Call C) {
   __shared__ Shared s;
-  begin(s);
+  begin<CL>(s);
   const PagesView &t = C.t;
   int need[kPer], rows[kPer];
 #pragma unroll
@@ -264,22 +365,23 @@ __global__ void __launch_bounds__(kThreads, 1) pages_fork_kernel(const __grid_co
   __syncthreads();
   if (s.bad) return;
   const int n = C.n, sum = static_cast<int>(total);
-  for (int j = threadIdx.x; j < sum; j += kThreads) {
-    const int e = entry_of(s.at, n, j), p = t.row(C.rows[e])[j - s.at[e]];
-    // (a sequence that is a child here was empty: as a parent it has no pages to read)
-    if (static_cast<uint32_t>(p) >= static_cast<uint32_t>(t.num_pages) || t.refs[p] < 1) {
-      report(C, 124, e, p);
-      s.bad = 1;
+  int p[kBatch], r[kBatch];
+  // (a sequence that is a child here was empty: as a parent it has no pages to read)
+  auto load = [&](int k, int j, int e) { p[k] = now(t.row(C.rows[e]) + (j - s.at[e])); };
+  auto holders = [&](int k) { r[k] = static_cast<uint32_t>(p[k]) < static_cast<uint32_t>(t.num_pages) ? now(t.refs + p[k]) : 0; };
+  for_places<CL>(s.at, n, sum, load, holders, [&](int k, int, int e) {
+    if (r[k] < 1) {
+      report(C, 124, e, p[k]);
+      raise_flag<CL>(&s.wrong);
     }
-  }
-  __syncthreads();
-  if (s.bad) return;
-  for (int j = threadIdx.x; j < sum; j += kThreads) {
-    const int e = entry_of(s.at, n, j), c = j - s.at[e];
-    const int p = t.row(C.rows[e])[c];
-    atomicAdd(t.refs + p, 1);
-    t.row(C.seqs ? __ldg(C.seqs + e) : e)[c] = p;
-  }
+  });
+  sync_all<CL>();
+  if (s.wrong) return;
+  for_places<CL>(s.at, n, sum, load, Nothing(), [&](int k, int j, int e) {
+    atomicAdd(t.refs + p[k], 1);
+    t.row(C.seqs ? __ldg(C.seqs + e) : e)[j - s.at[e]] = p[k];
+  });
+  if (CL > 1 && cluster_ctarank() != 0) return;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const int i = k * kThreads + threadIdx.x;
@@ -296,30 +398,42 @@ struct Maps {
   int64_t max_rows;
 };
 
-// New row number j of the call: row, sequence and slot.
-__device__ __forceinline__ void write_map(const Call &C, const Maps &M, const int32_t *cu, int64_t j) {
-  int row = -1, b = -1;
-  int64_t slot = -1;
-  if (j < cu[C.n]) {
-    const int e = entry_of(cu, C.n, static_cast<int>(j));
-    b = C.seqs ? __ldg(C.seqs + e) : e;
-    row = C.t.lengths[b] - cu[e + 1] + static_cast<int>(j);
-    slot = static_cast<int64_t>(C.t.row(b)[C.t.page_tokens.div(row)]) * C.t.page_tokens.d + C.t.in_page(row);
+// New rows number j0, j0 + stride, ... of the call, kBatch of them: row, sequence and slot.
+__device__ __forceinline__ void write_maps(const Call &C, const Maps &M, const int32_t *cu, int64_t j0, int64_t stride) {
+  int j[kBatch], e[kBatch], b[kBatch], row[kBatch], page[kBatch];
+  const int last = cu[C.n] - 1;
+#pragma unroll
+  for (int k = 0; k < kBatch; ++k) j[k] = static_cast<int>(min(j0 + k * stride, static_cast<int64_t>(max(last, 0))));
+  if (last >= 0) {
+    entries_of(cu, C.n, j, e);
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) b[k] = C.seqs ? __ldg(C.seqs + e[k]) : e[k];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) row[k] = now(C.t.lengths + b[k]) - cu[e[k] + 1] + j[k];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) page[k] = now(C.t.row(b[k]) + C.t.page_tokens.div(row[k]));
   }
-  M.rows[j] = row;
-  if (M.row_seqs) M.row_seqs[j] = b;
-  if (M.slots) M.slots[j] = slot;
+#pragma unroll
+  for (int k = 0; k < kBatch; ++k) {
+    const int64_t at = j0 + k * stride;
+    if (at >= M.max_rows) break;
+    const bool real = at <= last;
+    M.rows[at] = real ? row[k] : -1;
+    if (M.row_seqs) M.row_seqs[at] = real ? b[k] : -1;
+    if (M.slots) M.slots[at] = real ? static_cast<int64_t>(page[k]) * C.t.page_tokens.d + C.t.in_page(row[k]) : -1;
+  }
 }
 
 // Entry i gets rows[i] more rows.  A last page that it shares and would write into is replaced by one of its own: of the
 // sequences that hold it, all that the call extends but the last holder; the pair (old, new) is left for apack_copy_pages.
+template <int CL>
 __global__ void __launch_bounds__(kThreads, 1)
     pages_extend_kernel(const __grid_constant__ Call C, const __grid_constant__ Maps M) {
   __shared__ Shared s;
   __shared__ int32_t sharing[APACK_MAX_SEQS];
   __shared__ int n_sharing;
   if (threadIdx.x == 0) n_sharing = 0;
-  begin(s);
+  begin<CL>(s);
   const PagesView &t = C.t;
   int seq[kPer], len[kPer], grow[kPer], take[kPer], last[kPer];
   const int count = *t.free_count;
@@ -382,15 +496,18 @@ __global__ void __launch_bounds__(kThreads, 1)
   const bool bad = s.bad;
   const int sum = bad ? 0 : static_cast<int>(total);
   __syncthreads();
-  for (int j = threadIdx.x; j < sum; j += kThreads) {
-    const int p = t.free_list[count - 1 - j];
-    if (static_cast<uint32_t>(p) >= static_cast<uint32_t>(t.num_pages) || t.refs[p] != 0) {
-      report(C, 129, count - 1 - j, p);
-      s.bad = 1;
+  int p[kBatch], r[kBatch];
+  auto load = [&](int k, int j, int) { p[k] = now(t.free_list + (count - 1 - j)); };
+  auto holders = [&](int k) { r[k] = static_cast<uint32_t>(p[k]) < static_cast<uint32_t>(t.num_pages) ? now(t.refs + p[k]) : -1; };
+  for_places<CL>(s.at, C.n, sum, load, holders, [&](int k, int j, int) {
+    if (r[k] != 0) {
+      report(C, 129, count - 1 - j, p[k]);
+      raise_flag<CL>(&s.wrong);
     }
-  }
-  __syncthreads();
-  if (s.bad) {                                              // nothing is changed, and nothing is there to be written
+  });
+  sync_all<CL>();
+  const bool leads = CL == 1 || cluster_ctarank() == 0;
+  if (bad || s.wrong) {                                     // nothing is changed, and nothing is there to be written
     for (int i = threadIdx.x; i <= C.n; i += kThreads) {
       M.cu[i] = 0;
       if (M.pairs && i < C.n) M.pairs[i] = make_int2(0, 0);
@@ -400,28 +517,28 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int k = 0; k < kPer; ++k) {
       const int i = k * kThreads + threadIdx.x;
       if (i >= C.n) continue;
+      sharing[i] = t.pages_of(len[k]) - (last[k] >= 0);     // the column of the first page that it takes
+      if (!leads) continue;
       int2 pair = make_int2(0, 0);
       if (last[k] >= 0) {
         pair = make_int2(last[k], t.free_list[count - 1 - s.at[i]]);
         atomicSub(t.refs + last[k], 1);
       }
       if (M.pairs) M.pairs[i] = pair;
-      sharing[i] = t.pages_of(len[k]) - (last[k] >= 0);     // the column of the first page that it takes
       t.lengths[seq[k]] = len[k] + grow[k];
     }
     __syncthreads();
-    for (int j = threadIdx.x; j < sum; j += kThreads) {
-      const int e = entry_of(s.at, C.n, j), p = t.free_list[count - 1 - j];
-      t.row(C.seqs ? __ldg(C.seqs + e) : e)[sharing[e] + j - s.at[e]] = p;
-      t.refs[p] = 1;
-    }
-    if (threadIdx.x == 0) *t.free_count = count - sum;
+    for_places<CL>(s.at, C.n, sum, load, Nothing(), [&](int k, int j, int e) {
+      t.row(C.seqs ? __ldg(C.seqs + e) : e)[sharing[e] + j - s.at[e]] = p[k];
+      t.refs[p[k]] = 1;
+    });
+    if (threadIdx.x == 0 && leads) *t.free_count = count - sum;
   }
   __syncthreads();
-  if (M.max_rows > kInlineRows) return;                     // the next kernel's
+  if (CL > 1 || M.max_rows > kInlineRows) return;           // the next kernel's
   for (int i = threadIdx.x; i <= C.n; i += kThreads) s.at[i] = M.cu[i];
   __syncthreads();
-  for (int64_t j = threadIdx.x; j < M.max_rows; j += kThreads) write_map(C, M, s.at, j);
+  for (int64_t j = threadIdx.x; j < M.max_rows; j += kBatch * kThreads) write_maps(C, M, s.at, j, kThreads);
 }
 
 __global__ void __launch_bounds__(256) pages_map_kernel(const __grid_constant__ Call C, const __grid_constant__ Maps M) {
@@ -429,7 +546,8 @@ __global__ void __launch_bounds__(256) pages_map_kernel(const __grid_constant__ 
   pdl_wait_and_release();
   for (int i = threadIdx.x; i <= C.n; i += 256) cu[i] = M.cu[i];
   __syncthreads();
-  for (int64_t j = blockIdx.x * 256ll + threadIdx.x; j < M.max_rows; j += gridDim.x * 256ll) write_map(C, M, cu, j);
+  for (int64_t j = blockIdx.x * 256ll + threadIdx.x; j < M.max_rows; j += kBatch * 256ll * gridDim.x)
+    write_maps(C, M, cu, j, 256ll * gridDim.x);
 }
 
 // ---------------------------------------------------------------- host side
@@ -463,6 +581,26 @@ apack_status make_call(const apack_page_tables *t, int32_t n, const int32_t *seq
   return APACK_OK;
 }
 
+// One CTA, or a cluster.
+template <class... K, class... A>
+cudaError_t launch_cluster(void (*kernel)(K...), int ctas, cudaStream_t stream, A &&...args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ctas);
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = stream;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = ctas;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = ctas > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<K>(args)...);
+}
+
+bool large(const Call &C) { return static_cast<int64_t>(C.n) * C.t.max_pages > kClusterPages; }
+
 apack_status launched(cudaError_t e) {
   if (e == cudaSuccess) count_launches(1);
   return check_cuda(e);
@@ -480,7 +618,9 @@ apack_status apack_pages_release(const apack_page_tables *tables, int32_t n, con
   Call C;
   const apack_status st = make_call(tables, n, seqs, keep_rows, ws, &C);
   if (st != APACK_OK || n == 0) return st;
-  return launched(launch_pdl(pages_release_kernel, dim3(1), dim3(kThreads), 0, static_cast<cudaStream_t>(stream), C));
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  return launched(large(C) ? launch_cluster(pages_release_kernel<kMaxCluster>, kMaxCluster, cs, C)
+                           : launch_cluster(pages_release_kernel<1>, 1, cs, C));
 }
 
 apack_status apack_pages_fork(const apack_page_tables *tables, int32_t n, const int32_t *parents, const int32_t *seqs,
@@ -490,7 +630,9 @@ apack_status apack_pages_fork(const apack_page_tables *tables, int32_t n, const 
   if (st != APACK_OK) return st;
   if (n > 0 && !seqs) return APACK_EINVAL;
   if (n == 0) return APACK_OK;
-  return launched(launch_pdl(pages_fork_kernel, dim3(1), dim3(kThreads), 0, static_cast<cudaStream_t>(stream), C));
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  return launched(large(C) ? launch_cluster(pages_fork_kernel<kMaxCluster>, kMaxCluster, cs, C)
+                           : launch_cluster(pages_fork_kernel<1>, 1, cs, C));
 }
 
 apack_status apack_pages_extend(const apack_page_tables *tables, int32_t n, const int32_t *seqs, const int32_t *new_rows,
@@ -505,9 +647,13 @@ apack_status apack_pages_extend(const apack_page_tables *tables, int32_t n, cons
     return APACK_EINVAL;
   Maps M{cu_new, rows, row_seqs, slots, reinterpret_cast<int2 *>(pairs), max_rows};
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
-  apack_status r = launched(launch_pdl(pages_extend_kernel, dim3(1), dim3(kThreads), 0, cs, C, M));
-  if (r != APACK_OK || max_rows <= kInlineRows) return r;
-  const int grid = static_cast<int>(std::min<int64_t>(4 * device_sm_count(), (max_rows + 1023) / 1024));
+  if (max_rows <= kInlineRows) return launched(launch_cluster(pages_extend_kernel<1>, 1, cs, C, M));
+  // (as many pages as the new rows need at most)
+  const bool many = std::min(max_rows / tables->page_tokens + 2 * static_cast<int64_t>(n), static_cast<int64_t>(C.t.num_pages)) > kClusterPages;
+  const apack_status r = launched(many ? launch_cluster(pages_extend_kernel<kMaxCluster>, kMaxCluster, cs, C, M)
+                                       : launch_cluster(pages_extend_kernel<1>, 1, cs, C, M));
+  if (r != APACK_OK) return r;
+  const int grid = static_cast<int>(std::min<int64_t>(4 * device_sm_count(), (max_rows + kBatch * 256 - 1) / (kBatch * 256)));
   return launched(launch_pdl(pages_map_kernel, dim3(grid), dim3(256), 0, cs, C, M));
 }
 
