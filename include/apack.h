@@ -530,7 +530,8 @@ apack_status apack_paged_compact(const apack_paged_cache *src, const apack_paged
 
 /* Copies page pairs[i][0] to page pairs[i][1] in every layer, K and V, i < n_pairs (device int32 [n_pairs][2]):
    the pages that a forked sequence needs of its own.  No page may be written twice, nor written and read by
-   the same call (a pair of one page with itself changes nothing).  page_table is not read and may be NULL.
+   the same call; a pair of one page with itself is padding, reads and writes nothing and may stand beside any other.
+   page_table is not read and may be NULL.
    ws as in apack_paged_compact; a pair with a page outside the pool is not copied. */
 apack_status apack_copy_pages(const apack_paged_cache *cache, const int32_t *pairs, int64_t n_pairs, void *ws,
                               void *stream);

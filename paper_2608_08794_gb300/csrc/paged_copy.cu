@@ -65,6 +65,7 @@ __device__ __forceinline__ void resolve(const MovePlan &P, const int32_t *cu, in
       if (P.err) raise_device_error(P.err, APACK_EDEVICE, 92, a, b);
       return;
     }
+    if (a == b) return;                // padding: not even written back, so that it may stand beside a pair that writes the page
     *src = a * P.src.page_stride + r * P.src.token_stride;
     *dst = b * P.src.page_stride + r * P.src.token_stride;
     return;

@@ -11,12 +11,16 @@ may be handed out again by the next call) and are not captured (a graph reads th
 Every method checks that it can be carried out (pages, rows) before it changes anything, and changes what the host
 keeps only after its device calls have been queued: one that raises (an allocation, a pool on another device than
 the current one) leaves every sequence as it was.
+
+``DevicePool`` keeps the same on the device instead: its calls take and leave device arrays, read nothing back, and can
+be captured; what a call cannot carry out leaves everything as it was and is recorded in the error word of ``ws``.
 """
 
 import numpy as np
 import torch
 
-from . import PagedCache, apack_copy_pages, apack_paged_compact
+from . import (PagedCache, PageTables, apack_copy_pages, apack_device_error, apack_paged_compact, apack_pages_extend,
+               apack_pages_fork, apack_pages_release)
 
 
 class PagePool:
@@ -198,6 +202,27 @@ class PagePool:
         self._drop(pages)
         self._pages[seq], self._len[seq] = None, 0
 
+    def groups(self, seqs):
+        """These sequences (distinct), those that share their first pages side by side, and their groups as
+        apack_paged_group_plan takes them: the numbers in that order (a list), cu_groups and prefix (int32, on the device)."""
+        if len(set(seqs)) != len(seqs):
+            raise ValueError("distinct sequences expected")
+        by = {}
+        for s in seqs:
+            pages = self._held(s)
+            by.setdefault(pages[0] if pages else -1 - s, []).append(s)
+        order, bounds, prefix = [], [0], []
+        for members in by.values():
+            lists = [self._pages[s] for s in members]
+            common = min(map(len, lists))
+            table = np.array([x[:common] for x in lists], np.int64)
+            same = (table == table[0]).all(0)
+            common = common if same.all() else int(same.argmin())
+            order += members
+            bounds.append(len(order))
+            prefix.append(min(common * self.page_tokens, *(int(self._len[s]) for s in members)) if len(members) > 1 else 0)
+        return order, self._ints(bounds), self._ints(prefix)
+
     # ------------------------------------------------------------ pruning
 
     def _cache_of(self, lists):
@@ -269,3 +294,47 @@ class PagePool:
         for s, pages, m in zip(rows, new, kept):
             self._pages[s], self._len[s] = pages, int(m)
         return rows
+
+
+class DevicePool:
+    """Pools ``k`` and ``v`` [layers, pages, page_tokens, Hkv, D], ``tables`` (PageTables) on the device and ``cache``, the
+    PagedCache of both.  Sequences are numbered 0 .. max_seqs - 1 by the caller; an empty one has length 0 and no page.
+
+    seqs, keep_rows, parents and new_rows are int32 device tensors; the calls are queued on torch's current stream, one
+    stream for a pool.  heads_first: the heads of a page outermost in memory ([layers, pages, Hkv, page_tokens, D])."""
+
+    def __init__(self, num_layers, num_pages, page_tokens, num_kv_heads, head_dim, max_seqs, max_pages=None,
+                 dtype=torch.bfloat16, device="cuda", heads_first=False):
+        shape = (num_layers, num_pages, num_kv_heads, page_tokens, head_dim) if heads_first else (
+            num_layers, num_pages, page_tokens, num_kv_heads, head_dim)
+        self.k, self.v = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
+        if heads_first:
+            self.k, self.v = self.k.permute(0, 1, 3, 2, 4), self.v.permute(0, 1, 3, 2, 4)
+        self.tables = PageTables.new(max_seqs, num_pages if max_pages is None else max_pages, num_pages, page_tokens, device)
+        self.cache = PagedCache(self.k, self.v, self.tables.page_table)
+        self.lengths, self.page_table = self.tables.lengths, self.tables.page_table
+        self.ws = torch.zeros(256, dtype=torch.uint8, device=device)      # the error word
+
+    def release(self, keep_rows, seqs=None):
+        """Keeps the first keep_rows[i] rows of sequence seqs[i] (None: i; 0: the sequence ends)."""
+        apack_pages_release(self.tables, keep_rows, seqs=seqs, ws=self.ws)
+
+    def fork(self, parents, seqs):
+        """Empty sequence seqs[i] shares the pages of parents[i]."""
+        apack_pages_fork(self.tables, parents, seqs, ws=self.ws)
+
+    def extend(self, new_rows, max_rows, seqs=None):
+        """Room for new_rows[i] more rows behind sequence seqs[i] (None: i), max_rows in all at most, which the caller writes; a
+        shared page that they would be written to is copied.  Returns cu_new [n + 1], rows and row_seqs [max_rows] as
+        apack_pages_extend leaves them."""
+        n, dev = new_rows.numel(), new_rows.device
+        cu, rows, owners = (torch.empty(m, dtype=torch.int32, device=dev) for m in (n + 1, max_rows, max_rows))
+        pairs = torch.empty(n, 2, dtype=torch.int32, device=dev)
+        apack_pages_extend(self.tables, new_rows, cu, rows, seqs=seqs, row_seqs=owners, pairs=pairs, ws=self.ws)
+        apack_copy_pages(self.cache, pairs, ws=self.ws)
+        return cu, rows, owners
+
+    def check(self):
+        """Raises if a call since the last check could not be carried out (waits for the stream)."""
+        if apack_device_error(self.ws):
+            raise RuntimeError("DevicePool: a call could not be carried out (rows, pages or sequences that are not there)")

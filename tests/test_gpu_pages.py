@@ -99,3 +99,117 @@ def test_many_entries_and_a_long_map(ap):
     p.same()
     p.extend(seqs[::-1], [1] * 4096)
     p.same()
+
+
+def test_many_shared_pages(ap):
+    """Lists of more pages than one CTA takes, with shared pages in them, given up in parts."""
+    rng = np.random.default_rng(8)
+    p = Pair(ap, 60, 400, 6000, 16)
+    p.extend([0, 1, 2], [5000, 6399, 4100])
+    p.same()
+    kids = list(range(3, 60))
+    parents = [int(x) for x in rng.integers(0, 3, len(kids))]
+    p.fork(parents, kids)
+    p.same()
+    p.extend(kids, [int(x) for x in rng.integers(0, 1, len(kids))])               # no rows: nothing is copied
+    p.same()
+    p.release(kids[::2], [int(rng.integers(0, p.ref.lengths[b] + 1)) for b in kids[::2]])
+    p.same()
+    p.extend(kids, [1 if p.ref.lengths[b] < 6400 else 0 for b in kids])
+    p.same()
+    p.release([0, 1, 2] + kids[1::2], [0, 17, 0] + [0] * len(kids[1::2]))           # the last holders of most pages
+    p.same()
+    p.release(list(range(60)), [0] * 60)
+    p.same()
+    assert int(p.t.free_count) == 6000
+
+
+def state(t):
+    return [x.clone() for x in (t.page_table, t.lengths, t.refs, t.free_list, t.free_count)]
+
+
+@pytest.mark.parametrize("seqs,width", [(6, 4), (60, 400)])                         # one CTA, a cluster
+def test_what_cannot_be_carried_out_changes_nothing(ap, seqs, width):
+    pages = 24
+    t = ap.PageTables.new(seqs, width, pages, 16)
+    w = ws()
+    cu, rows = i32([9] * 4), i32([9] * 200)
+    ap.apack_pages_extend(t, i32([40, 16, 1]), cu, rows, seqs=i32([0, 1, 2]), ws=w)
+    assert cu.tolist() == [0, 40, 56, 57] and ap.apack_device_error(w) == 0
+    before = state(t)
+
+    def unchanged(n=None):
+        assert ap.apack_device_error(w) == ap.APACK_EDEVICE
+        assert all(torch.equal(a, b) for a, b in zip(before, state(t)))
+        if n is not None:
+            assert cu.tolist() == [0] * (n + 1) and (rows == -1).all() and (pairs == 0).all()
+
+    for seq, grow in (([0, 1, 0], [1, 1, 1]),                    # named twice
+                      ([0, 1, seqs], [1, 1, 1]), ([0, -1, 2], [1, 1, 1]),
+                      ([0, 1, 2], [1, -1, 1]),
+                      ([0, 1, 2], [1, width * 16, 1]),            # more rows than its part of the table
+                      ([3, 4, 5], [60, 60, 81]),                  # more rows than the map takes
+                      ([3, 4, 5], [1, 1, 2 ** 31 - 1])):
+        pairs = i32([[9, 9]] * 3)
+        rows.fill_(9)
+        ap.apack_pages_extend(t, i32(grow), cu, rows, seqs=i32(seq), pairs=pairs, ws=w)
+        unchanged(3)
+    if width > pages:
+        big, c4 = torch.empty(9000, dtype=torch.int32, device="cuda"), i32([9, 9])
+        ap.apack_pages_extend(t, i32([16 * 21]), c4, big, seqs=i32([3]), ws=w)       # more pages than are free (19)
+        assert ap.apack_device_error(w) == ap.APACK_EDEVICE and (big == -1).all() and c4.tolist() == [0, 0]
+        assert all(torch.equal(a, b) for a, b in zip(before, state(t)))
+    for seq, keep in (([0, 0], [1, 1]), ([0, seqs], [1, 0]), ([0, 1], [41, 1]), ([0, 1], [1, -1]), ([0, 3], [1, 1])):
+        ap.apack_pages_release(t, i32(keep), seqs=i32(seq), ws=w)
+        unchanged()
+    for parent, seq in (([0, 1], [3, 3]), ([0, seqs], [3, 4]), ([0, -1], [3, 4]), ([0, 0], [3, 1]), ([3, 0], [3, 4])):
+        ap.apack_pages_fork(t, i32(parent), i32(seq), ws=w)
+        unchanged()
+    # tables that disagree with the counts: a page that nobody holds, one outside the pool
+    t.refs[int(t.page_table[0, 0])] = 0
+    before = state(t)
+    ap.apack_pages_release(t, i32([0]), seqs=i32([0]), ws=w)
+    unchanged()
+    ap.apack_pages_fork(t, i32([0]), i32([3]), ws=w)
+    unchanged()
+    t.refs[int(t.page_table[0, 0])] = 1
+    t.page_table[1, 0] = pages
+    before = state(t)
+    ap.apack_pages_release(t, i32([0]), seqs=i32([1]), ws=w)
+    unchanged()
+    t.free_list[int(t.free_count) - 1] = -4
+    before = state(t)
+    pairs = i32([[9, 9]])
+    c2 = i32([9, 9])
+    ap.apack_pages_extend(t, i32([20]), c2, rows, seqs=i32([3]), pairs=pairs, ws=w)
+    assert ap.apack_device_error(w) == ap.APACK_EDEVICE and c2.tolist() == [0, 0] and (rows == -1).all()
+    assert all(torch.equal(a, b) for a, b in zip(before, state(t)))
+    # without a workspace the same, unrecorded
+    ap.apack_pages_release(t, i32([99]), seqs=i32([2]))
+    assert all(torch.equal(a, b) for a, b in zip(before, state(t))) and ap.apack_device_error(w) == 0
+
+
+def test_no_entries_and_no_rows(ap):
+    t = ap.PageTables.new(3, 4, 9, 16)
+    cu, rows = i32([9]), i32([9] * 5)
+    none = i32([])
+    ap.apack_pages_extend(t, none, cu, rows, seqs=none)
+    assert cu.tolist() == [0] and rows.tolist() == [-1] * 5
+    ap.apack_pages_extend(t, i32([0, 0, 0]), i32([9] * 4), i32([]))
+    assert t.lengths.tolist() == [0, 0, 0] and int(t.free_count) == 9
+    ap.apack_pages_extend(t, i32([16, 1, 0]), i32([9] * 4), i32([9] * 17))              # seqs None: entry i is sequence i
+    assert t.lengths.tolist() == [16, 1, 0] and t.page_table[:, 0].tolist() == [0, 1, -1]
+    ap.apack_pages_release(t, i32([16, 0, 0]))
+    assert t.lengths.tolist() == [16, 0, 0] and int(t.free_count) == 8
+
+
+def test_padding_copies_nothing_beside_a_page_that_is_written(ap):
+    """Pairs of page 0 with itself, as apack_pages_extend leaves them, beside a pair that writes page 0."""
+    k = torch.randn(3, 6, 16, 2, 64, device="cuda").half()
+    v = torch.randn_like(k)
+    cache = ap.PagedCache(k, v, i32([[0]]))
+    want = k.clone(), v.clone()
+    for x in want:
+        x[:, 0] = x[:, 4]
+    ap.apack_copy_pages(cache, i32([[0, 0]] * 40 + [[4, 0]] + [[0, 0]] * 40))
+    assert torch.equal(k, want[0]) and torch.equal(v, want[1])
