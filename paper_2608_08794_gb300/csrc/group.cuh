@@ -74,6 +74,7 @@ struct GroupArgs {
   uint8_t *out;
   float *lse;
   int32_t box;                       // tokens of a TMA box, 0: rows are copied by the lanes
+  int64_t seg_off;                   // of the segments in ws
   DeviceError *err;
 };
 

@@ -400,13 +400,15 @@ __global__ void __launch_bounds__(kThreads, 1)
   pdl_wait_and_release();
   const uint32_t tmem = b->tmem;
   GroupHead h;
+  GroupSeg first_seg = {};
+  if (warp >= kLoadWarp) first_seg = reinterpret_cast<const GroupSeg *>(A.ws + A.seg_off)[blockIdx.x];     // beside the head (there are more places than CTAs)
   const bool planned = group_head(A, h);
   int item = 0;                                                   // tiles issued by a load warp
   if (!planned) {
     if (threadIdx.x == 0 && blockIdx.x == 0) raise_device_error(A.err, APACK_EDEVICE, 150);
   } else if (warp >= kLoadWarp) {
     // ------------------------------------------------------------ loads
-    const GroupSeg *segs = reinterpret_cast<const GroupSeg *>(A.ws + h.seg_off);
+    const GroupSeg *segs = reinterpret_cast<const GroupSeg *>(A.ws + A.seg_off);
     unsigned int *claims = reinterpret_cast<unsigned int *>(A.ws + kGClaimOff);
     const uint32_t ring = smem_u32(smem) + L::kOffRing;
     if (A.box && warp < kLoadWarp + 2) {
@@ -428,7 +430,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const unsigned i = __shfl_sync(0xffffffffu, claimed, 0);
           g.seq = -1;
           if (i >= static_cast<unsigned>(h.segs)) return g;
-          g = segs[i];
+          g = i == blockIdx.x ? first_seg : segs[i];
           if (lane == 0) claimed = gridDim.x + atomicAdd(claims, 1u);
           if (g.key0 < g.key1) return g;
         }
@@ -504,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const unsigned i = __shfl_sync(0xffffffffu, claimed, 0);
             g.seq = -1;
             if (i >= static_cast<unsigned>(h.segs)) break;
-            g = segs[i];
+            g = i == blockIdx.x ? first_seg : segs[i];
             if (lane == 0) claimed = gridDim.x + atomicAdd(claims, 1u);
             if (g.key0 < g.key1) break;
           }
@@ -566,7 +568,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int s = warp >> 2, row = threadIdx.x & 127;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t sc = tmem + lanes + s * kGTile, oc = tmem + lanes + 256 + s * 128;
-    const GroupTok *toks = reinterpret_cast<const GroupTok *>(A.ws + h.tok_off);
+    const GroupTok *toks = reinterpret_cast<const GroupTok *>(A.ws + kGFixed);
     float2 *ml = reinterpret_cast<float2 *>(A.ws + h.ml_off);
     float *parts = reinterpret_cast<float *>(A.ws + h.part_off);
     uint8_t *qs = smem + s * (kGSlot * D * 2);
@@ -770,18 +772,35 @@ __device__ __forceinline__ void load_values(float (&o)[D / 32], const float *p) 
   }
 }
 
-// A row's parts of one item: those from number `from` on, every `step`th, added to a.
+// A row's parts of an item: [split][sub][KV head][rows], `two` of a split where its segment had few rows.
+struct Parts {
+  int n, tiles, chunk, sub, rows, base;
+  bool two;
+  __device__ __forceinline__ void set(const GroupArgs &A, const GroupItem &it, int head, int packed) {
+    const int rr = packed - it.row0, run = rr / kGRows, here = min(kGRows, it.rows - run * kGRows);
+    two = it.sub == 2 && here <= kGSlot;
+    int key1 = it.key1;                        // the keys that the row's segments had (as the plan cuts them)
+    if (it.causal) key1 = min(key1, it.key1 - it.rows / A.group + 1 + (run * kGRows + here - 1) / A.group);
+    tiles = max((key1 - it.key0 + kGTile - 1) / kGTile, 0);
+    chunk = it.chunk;
+    sub = it.sub;
+    rows = it.rows * A.hkv;
+    base = it.part + head * it.rows + rr;
+    n = tiles ? (tiles + chunk - 1) / chunk * (two ? 2 : 1) : 0;
+  }
+  // Row number of part j, or -1: the second of a single tile.
+  __device__ __forceinline__ int64_t at(int j) const {
+    const int split = two ? j >> 1 : j, u = two ? j & 1 : 0;
+    return u && min(chunk, tiles - split * chunk) < 2 ? -1 : base + static_cast<int64_t>(split * sub + u) * rows;
+  }
+};
+
+// The row's parts from number `from` on, every `step`th, added to a: the shared rows' first.
 template <int D>
-__device__ __forceinline__ void merge_item(const GroupArgs &A, const GroupHead &h, const GroupTok *toks, const GroupItem &it,
-                                           int head, int packed, int from, int step, Row<D> &a) {
+__device__ __forceinline__ void merge_parts(const GroupArgs &A, const GroupHead &h, const Parts &x0, const Parts &x1, int from,
+                                            int step, Row<D> &a) {
   constexpr int kF = D / 32;
-  const int lane = threadIdx.x & 31, rr = packed - it.row0, run = rr / kGRows;
-  const int rows = min(kGRows, it.rows - run * kGRows);
-  const bool two = it.sub == 2 && rows <= kGSlot;
-  int key1 = it.key1;
-  if (it.causal) key1 = min(key1, toks[(it.row0 + run * kGRows + rows - 1) / A.group].limit);
-  const int tiles = (key1 - it.key0 + kGTile - 1) / kGTile, splits = (tiles + it.chunk - 1) / it.chunk;
-  const int n = splits * (two ? 2 : 1);
+  const int lane = threadIdx.x & 31, n = x0.n + x1.n;
   const float2 *ml = reinterpret_cast<const float2 *>(A.ws + h.ml_off);
   const float *parts = reinterpret_cast<const float *>(A.ws + h.part_off);
   for (int k = from; k < n; k += kBatch * step) {
@@ -789,12 +808,12 @@ __device__ __forceinline__ void merge_item(const GroupArgs &A, const GroupHead &
     float x[kBatch][kF];
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      const int j = k + i * step, split = two ? j >> 1 : j, u = two ? j & 1 : 0;
+      const int j = k + i * step;
+      const int64_t at = j >= n ? -1 : j < x0.n ? x0.at(j) : x1.at(j - x0.n);
       st[i] = make_float2(-INFINITY, 0.f);
 #pragma unroll
       for (int e = 0; e < kF; ++e) x[i][e] = 0.f;
-      if (j < n && (u == 0 || tiles - split * it.chunk > 1) && !(u == 1 && it.chunk < 2)) {
-        const int64_t at = static_cast<int64_t>(it.part) + static_cast<int64_t>((split * it.sub + u) * A.hkv + head) * it.rows + rr;
+      if (at >= 0) {
         st[i] = ml[at];
         load_values<D>(x[i], parts + at * D + lane * kF);
       }
@@ -825,21 +844,27 @@ __global__ void __launch_bounds__(256) group_merge_kernel(const __grid_constant_
   __shared__ float qs[8][D];
   __shared__ float2 stat[8];
   pdl_wait_and_release();
-  GroupHead h;
-  if (!group_head(A, h)) return;                       // recorded by the kernel before
-  if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<unsigned int *>(A.ws + kGClaimOff) = 0;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t u = blockIdx.x * (8ll / W) + warp / W;
   if (u >= static_cast<int64_t>(A.n_q) * A.hq) return;
   const int t = static_cast<int>(u / A.hq), hd = static_cast<int>(u - static_cast<int64_t>(t) * A.hq);
-  const GroupTok *toks = reinterpret_cast<const GroupTok *>(A.ws + h.tok_off);
-  const GroupTok tok = toks[t];
+  // three trips: head and token, both items, parts
+  const GroupTok tok = reinterpret_cast<const GroupTok *>(A.ws + kGFixed)[t];
+  GroupHead h;
+  if (!group_head(A, h)) return;                       // recorded by the kernel before
+  if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<unsigned int *>(A.ws + kGClaimOff) = 0;
   if (!tok.real) return;
   const GroupItem *items = reinterpret_cast<const GroupItem *>(A.ws + h.item_off);
   const int head = hd / A.group, packed = t * A.group + hd - head * A.group;
+  GroupItem i0 = {}, i1 = {};
+  if (tok.prefix >= 0) i0 = items[tok.prefix];
+  if (tok.own >= 0) i1 = items[tok.own];
+  Parts x0, x1;
+  x0.n = x1.n = 0;
+  if (tok.prefix >= 0) x0.set(A, i0, head, packed);
+  if (tok.own >= 0) x1.set(A, i1, head, packed);
   Row<D> a = {-INFINITY, 0.f, {}};
-  if (tok.prefix >= 0) merge_item<D>(A, h, toks, items[tok.prefix], head, packed, warp % W, W, a);
-  if (tok.own >= 0) merge_item<D>(A, h, toks, items[tok.own], head, packed, warp % W, W, a);
+  merge_parts<D>(A, h, x0, x1, warp % W, W, a);
   if (W > 1) {
     stat[warp] = make_float2(a.m, a.l);
 #pragma unroll
@@ -950,6 +975,7 @@ extern "C" apack_status apack_paged_group_attention(const apack_paged_cache *cac
   A.out = static_cast<uint8_t *>(out);
   A.lse = lse;
   A.box = group_box(cache->page_tokens);
+  A.seg_off = static_cast<int64_t>(s.seg_off);
   A.err = static_cast<DeviceError *>(ws);
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
   CUtensorMap kmap, vmap;

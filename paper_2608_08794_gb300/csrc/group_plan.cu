@@ -346,10 +346,11 @@ apack_status group_shape(const apack_paged_cache *c, int32_t hq, int32_t n_seqs,
   s->cap_rows = rows * (s->halves ? 4 : 2) + std::min(rows * sms, sms * 4 * kGRows) + 64;
   s->cap_segs = c->num_kv_heads * (2 * (packed / kGRows) + 2 * static_cast<int64_t>(n_seqs)) + 8 * sms + 64;
   auto up = [](int64_t x) { return static_cast<size_t>((x + 255) & ~int64_t{255}); };
+  // (places that the attention's kernels read first follow n_q alone, which they know without the plan's head)
   s->tok_off = kGFixed;
-  s->item_off = up(s->tok_off + n_q * sizeof(GroupTok));
-  s->seg_off = up(s->item_off + 2 * static_cast<int64_t>(n_seqs) * sizeof(GroupItem));
-  s->ml_off = up(s->seg_off + s->cap_segs * sizeof(GroupSeg));
+  s->seg_off = up(s->tok_off + n_q * sizeof(GroupTok));
+  s->item_off = up(s->seg_off + s->cap_segs * sizeof(GroupSeg));
+  s->ml_off = up(s->item_off + 2 * static_cast<int64_t>(n_seqs) * sizeof(GroupItem));
   s->part_off = up(s->ml_off + s->cap_rows * sizeof(float2));
   s->total = up(s->part_off + s->cap_rows * c->head_dim * sizeof(float));
   return APACK_OK;
