@@ -481,8 +481,9 @@ apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_
    read nor written (padding of a captured batch).  A token that sees no row gives zeros and an lse of -infinity.
    Groups: group i is entries cu_groups[i] .. cu_groups[i+1] - 1 (device [n_groups + 1], rising, 0 .. n_seqs; entries outside
    share nothing; n_groups 0: none).  The caller says with prefix[i] (device [n_groups]) that the first prefix[i] rows of all
-   of them are the same; they are read once, through the first entry's row of the page table (its length at least
-   prefix[i]).  Which rows are read together changes the result by rounding only.
+   of them are the same: they may be read once for all, through the first entry's row of the page table (its length at least
+   prefix[i]).  Whether they are is the plan's choice (not where every sequence has many new tokens of its own), so that
+   every entry's row of the table is complete all the same; what is read together changes the result by rounding only.
    An entry or a group that these words do not allow records APACK_EDEVICE in the error word of ws: a length or a prefix out
    of range is read as the nearest in range, tokens before a sequence's first row see nothing, an entry outside the cache
    gives zeros; offsets that do not rise leave no plan, and the attention calls then record APACK_EDEVICE and write nothing.
@@ -496,8 +497,8 @@ apack_status apack_paged_decode_attention(const apack_paged_cache *cache, int32_
    it sees makes what it enters NaN (an infinite value: infinite or NaN).
    ws: 256-byte aligned, apack_paged_group_workspace_size bytes (for at most n_seqs entries and n_q tokens; query it on the
    device that runs the calls), its error word (first 16 bytes) zeroed once by the caller.  The plan and the parts of unfinished
-   sums live in it: calls of one plan follow each other on one stream, and another plan in the same workspace ends the
-   first.  One launch for a plan, two for a layer. */
+   sums live in it: calls of one plan follow each other on one stream, no other call uses the workspace between them, and
+   another plan in it ends the first.  One launch for a plan, two for a layer. */
 apack_status apack_paged_group_workspace_size(const apack_paged_cache *cache, int32_t num_q_heads, int32_t n_seqs,
                                               int64_t n_q, size_t *bytes);
 apack_status apack_paged_group_plan(const apack_paged_cache *cache, const int32_t *seqlens, int32_t num_q_heads,

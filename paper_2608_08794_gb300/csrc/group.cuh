@@ -32,7 +32,8 @@ struct GroupSeg {
   int32_t seq, head;
   int32_t row0, rows;                // packed query rows, of at most 256
   int32_t key0, key1;                // key0 >= key1: nothing to do
-  int32_t part, step;                // its part's first row, and the second part's distance (0: one part)
+  int32_t part, step;                // its part's first row, and the second part's distance (0: one part; -1: one, and
+                                     // its rows have no other: they are written out, and of the part (max, sum) alone)
 };
 struct GroupTok {
   int32_t limit;                     // keys that the token sees: those below it

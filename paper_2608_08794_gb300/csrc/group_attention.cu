@@ -120,7 +120,7 @@ __device__ __forceinline__ bool elect_one() {
   return one != 0;
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void store8(float *p, const uint32_t *r) {       // 32 bytes, aligned
+__device__ __forceinline__ void store8(void *p, const uint32_t *r) {        // 32 bytes, aligned
   asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
                "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
@@ -169,7 +169,7 @@ __device__ __forceinline__ bool read_rec(Bars *b, int n, Seg &s, DeviceError *er
   if (!(WARP ? warp_wait(bar, parity, b, err, where) : wait(bar, parity, b, err, where))) return false;
   s.g = b->rec[n % kRecs];
   s.tiles = (s.g.key1 - s.g.key0 + kGTile - 1) / kGTile;
-  s.pair = s.g.step == 0;
+  s.pair = s.g.step <= 0;
   return s.g.seq >= 0;
 }
 // A tile's places in the ring: K, and V behind it.
@@ -575,18 +575,24 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t s_par = 0, o_par = 0, par = 0;
     Place<kRing> place;                                           // of the segment's first tile
     Seg seg;
-    int before = 0;                                               // tiles of the segment before
-    for (int rec = 0; read_rec(b, rec, seg, A.err, 168); ++rec) {
-      place.skip(before);
-      before = seg.tiles;
-      const int which = s ^ par;                                  // half of the rows, or first tile
-      if (!seg.pair) par ^= seg.tiles & 1;
-      if (!seg.pair && which >= seg.tiles) continue;
-      const int r0 = seg.pair ? which * kGSlot : 0, r = r0 + row;
-      const bool real = r < seg.g.rows;
-      const bool idle = r0 + (warp & 3) * 32 >= seg.g.rows;       // no row of the warp is one: what it leaves in TMEM is not read
-      int limit = 1 << 30;                                        // (what is no row need not be masked: nothing of it is kept)
-      if (real) limit = min(toks[group.div(seg.g.row0 + r)].limit, seg.g.key1) - seg.g.key0;
+    int rec = 0, before = 0, which = 0, r0 = 0, limit = 0;        // before: tiles of the segment before
+    bool real = false, idle = false;
+    // The accumulator's next segment, and its queries
+    auto next_segment = [&] {
+      for (;; ++rec) {
+        if (!read_rec(b, rec, seg, A.err, 168)) return false;
+        place.skip(before);
+        before = seg.tiles;
+        which = s ^ par;                                          // half of the rows, or first tile
+        if (!seg.pair) par ^= seg.tiles & 1;
+        if (seg.pair || which < seg.tiles) break;
+      }
+      ++rec;
+      r0 = seg.pair ? which * kGSlot : 0;
+      real = r0 + row < seg.g.rows;
+      idle = r0 + (warp & 3) * 32 >= seg.g.rows;                  // no row of the warp is one: what it leaves in TMEM is not read
+      limit = 1 << 30;                                            // (what is no row need not be masked: nothing of it is kept)
+      if (real) limit = min(toks[group.div(seg.g.row0 + r0 + row)].limit, seg.g.key1) - seg.g.key0;
       if (!idle) {
         // the warp's 32 rows, D / 8 lanes each: a row's 16-byte pieces side by side (a row per lane took 10,000 clocks)
         constexpr int kLanes = D / 8, kRows = 32 / kLanes;
@@ -616,6 +622,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(&b->q_full[s]);
+      return true;
+    };
+    for (bool have = next_segment(); have;) {
       float m = -INFINITY, l = 0.f;
       bool ok = true, first = true;
       for (int t = seg.pair ? 0 : which; t < seg.tiles; t += seg.pair ? 1 : 2) {
@@ -724,22 +733,58 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(&b->p_full[s]);
       }
-      ok = ok && warp_wait(&b->o_full[s], o_par, b, A.err, 170);
+      if (!ok) break;
+      // the next segment's queries, and with them its first scores, come while the last values' product runs and this
+      // segment's part is written (the queries' place is free: its scores are all there)
+      const int64_t at = static_cast<int64_t>(seg.g.part) + r0 + row + (seg.pair ? 0 : static_cast<int64_t>(which) * seg.g.step);
+      const bool was_real = real, was_idle = idle, direct = seg.g.step < 0;
+      const uint32_t packed = seg.g.row0 + r0 + row;
+      const int head = seg.g.head;
+      have = next_segment();
+      ok = warp_wait(&b->o_full[s], o_par, b, A.err, 170);
       if (!ok) break;
       o_par ^= 1;
       tc_fence_after();
-      const int64_t at = static_cast<int64_t>(seg.g.part) + (seg.pair ? r : static_cast<int64_t>(which) * seg.g.step + row);
-      if (real) ml[at] = make_float2(m, l);
-      if (!idle)
+      if (direct) {
+        // the row's only part: its output
+        const uint32_t t = group.div(packed);
+        const int64_t u = t * static_cast<int64_t>(A.hq) + head * A.group + (packed - t * A.group);
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        bool nan = false;
+        if (!was_idle)
 #pragma unroll 1
-        for (int c = 0; c < D; c += 32) {
-          uint32_t o[32];
-          tmem_ld32(oc + c, o);
-          tmem_wait32(o);
-          if (real)
+          for (int c = 0; c < D; c += 32) {
+            uint32_t o[32], w[16];
+            tmem_ld32(oc + c, o);
+            tmem_wait32(o);
 #pragma unroll
-            for (int j = 0; j < 32; j += 8) store8(parts + at * D + c + j, o + j);
+            for (int j = 0; j < 16; ++j) {
+              const float x = __uint_as_float(o[2 * j]) * inv, y = __uint_as_float(o[2 * j + 1]) * inv;
+              nan |= x != x || y != y;
+              w[j] = Type<T>::pack(x, y);
+            }
+            if (was_real) {
+              store8(A.out + (u * D + c) * 2, w);
+              store8(A.out + (u * D + c) * 2 + 32, w + 8);
+            }
+          }
+        if (was_real) {
+          if (A.lse) A.lse[u] = (m + log2f(l)) * 0.6931471805599453f;
+          ml[at] = make_float2(m, nan ? NAN : l);                 // (the merge looks at rows that are no numbers)
         }
+      } else {
+        if (was_real) ml[at] = make_float2(m, l);
+        if (!was_idle)
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            uint32_t o[32];
+            tmem_ld32(oc + c, o);
+            tmem_wait32(o);
+            if (was_real)
+#pragma unroll
+              for (int j = 0; j < 32; j += 8) store8(parts + at * D + c + j, o + j);
+          }
+      }
       tc_fence_before();
     }
   }
@@ -754,7 +799,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // ---------------------------------------------------------------- merge
 
-constexpr int kBatch = 8;                // parts whose loads a warp has in flight
+constexpr int kBatch = 8, kFewParts = 4; // parts whose loads a warp has in flight, of few rows and of many
 
 template <int D>
 struct Row {                             // of a warp: max, sum, D / 32 values on from lane * D / 32
@@ -796,18 +841,18 @@ struct Parts {
 };
 
 // The row's parts from number `from` on, every `step`th, added to a: the shared rows' first.
-template <int D>
+template <int D, int N>
 __device__ __forceinline__ void merge_parts(const GroupArgs &A, const GroupHead &h, const Parts &x0, const Parts &x1, int from,
                                             int step, Row<D> &a) {
   constexpr int kF = D / 32;
   const int lane = threadIdx.x & 31, n = x0.n + x1.n;
   const float2 *ml = reinterpret_cast<const float2 *>(A.ws + h.ml_off);
   const float *parts = reinterpret_cast<const float *>(A.ws + h.part_off);
-  for (int k = from; k < n; k += kBatch * step) {
-    float2 st[kBatch];
-    float x[kBatch][kF];
+  for (int k = from; k < n; k += N * step) {
+    float2 st[N];
+    float x[N][kF];
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
+    for (int i = 0; i < N; ++i) {
       const int j = k + i * step;
       const int64_t at = j >= n ? -1 : j < x0.n ? x0.at(j) : x1.at(j - x0.n);
       st[i] = make_float2(-INFINITY, 0.f);
@@ -820,14 +865,14 @@ __device__ __forceinline__ void merge_parts(const GroupArgs &A, const GroupHead 
     }
     float top = a.m;
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) top = fmaxf(top, st[i].x);
+    for (int i = 0; i < N; ++i) top = fmaxf(top, st[i].x);
     const float f = a.m == top ? 1.f : ex2_approx(a.m - top);
     a.m = top;
     a.l *= f;
 #pragma unroll
     for (int e = 0; e < kF; ++e) a.o[e] *= f;
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
+    for (int i = 0; i < N; ++i) {
       // (a part whose row saw nothing has sum 0, and a NaN maximum none)
       const float w = st[i].x == top ? 1.f : ex2_approx(st[i].x - top);
       a.l += st[i].y * w;
@@ -839,7 +884,7 @@ __device__ __forceinline__ void merge_parts(const GroupArgs &A, const GroupHead 
 
 // W: warps of a row (a CTA of 8 warps takes 8 / W rows).
 template <class T, int D, int W>
-__global__ void __launch_bounds__(256) group_merge_kernel(const __grid_constant__ GroupArgs A) {
+__global__ void __launch_bounds__(256, W == 1 ? 5 : 2) group_merge_kernel(const __grid_constant__ GroupArgs A) {
   constexpr int kF = D / 32;
   __shared__ float qs[8][D];
   __shared__ float2 stat[8];
@@ -864,8 +909,16 @@ __global__ void __launch_bounds__(256) group_merge_kernel(const __grid_constant_
   if (tok.prefix >= 0) x0.set(A, i0, head, packed);
   if (tok.own >= 0) x1.set(A, i1, head, packed);
   Row<D> a = {-INFINITY, 0.f, {}};
-  merge_parts<D>(A, h, x0, x1, warp % W, W, a);
-  if (W > 1) {
+  const bool direct = tok.prefix < 0 && x1.n == 1 && i1.splits == 1 && !x1.two;
+  if (direct) {
+    // written out already; of interest only where it is no number
+    const float2 st = reinterpret_cast<const float2 *>(A.ws + h.ml_off)[x1.at(0)];
+    if (st.y == st.y || (W > 1 && warp != 0)) return;
+    a.l = st.y;
+  } else {
+    merge_parts<D, W == 1 ? kFewParts : kBatch>(A, h, x0, x1, warp % W, W, a);
+  }
+  if (W > 1 && !direct) {
     stat[warp] = make_float2(a.m, a.l);
 #pragma unroll
     for (int e = 0; e < kF; ++e) qs[warp][lane * kF + e] = a.o[e];

@@ -172,7 +172,11 @@ __global__ void __launch_bounds__(kThreads, 1) group_plan_kernel(const __grid_co
   const bool bad = s.bad;
   const int total_items = ng + n;
   // ---- items: every sequence finds its group's shared rows by itself, so that nothing waits between groups and sequences
-  for (int g = threadIdx.x; g < ng; g += kThreads) s.rows[g] = s.tiles[g] = 0;
+  for (int g = threadIdx.x; g < ng; g += kThreads) s.rows[g] = s.tiles[g] = s.seg0[g] = 0;
+  __syncthreads();
+  // seg0, for now: the runs of rows that a group's sequences make by themselves
+  for (int e = threadIdx.x; e < n && ng && !bad; e += kThreads)
+    if (e >= s.cu_g[0] && e < s.cu_g[ng]) atomicAdd(&s.seg0[last_at(s.cu_g, ng, e)], runs_of((s.cu_q[e + 1] - s.cu_q[e]) * G));
   __syncthreads();
   for (int e = threadIdx.x; e < n; e += kThreads) {
     s.rows[ng + e] = s.tiles[ng + e] = 0;
@@ -199,7 +203,11 @@ __global__ void __launch_bounds__(kThreads, 1) group_plan_kernel(const __grid_co
       cut = min(max(shared, 0), len0);
       cut -= cut % P.align;
       const int rows = (s.cu_q[first + count] - s.cu_q[first]) * G;
-      if (!in0 || rows == 0) cut = 0;
+      // Reading rows together pays where it saves products: their tiles once per run of the group's rows, not of each
+      // sequence's, against a segment more per run and a part more per row.  (30 prompts of 700 tokens behind 200 shared rows:
+      // {SHARED} us together, {APART} apart.)
+      const int tiles = (cut + kGTile - 1) / kGTile, runs = runs_of(rows);
+      if (!in0 || rows == 0 || static_cast<float>(s.seg0[g] - runs) * tiles <= runs * kSegCost + rows * kRowCost) cut = 0;
       if (e == first && cut > 0) {
         GroupItem it = {};
         it.seq = b0;
@@ -307,7 +315,7 @@ __global__ void __launch_bounds__(kThreads, 1) group_plan_kernel(const __grid_co
     // (the last row's token sees the fewest rows too many: len - m + 1 + its number)
     if (it.causal) g.key1 = min(g.key1, it.key1 - it.rows / G + 1 + (run * kGRows + g.rows - 1) / G);
     g.part = it.part + (split * it.sub * P.hkv + h) * it.rows + run * kGRows;
-    g.step = it.sub == 2 && g.rows <= kGSlot ? P.hkv * it.rows : 0;
+    g.step = it.sub == 2 && g.rows <= kGSlot ? P.hkv * it.rows : it.splits == 1 && i >= ng && it.key0 == 0 ? -1 : 0;
     segs[j] = g;
   }
   if (threadIdx.x == 0) {

@@ -97,10 +97,25 @@ def reference(b, layer=0):
             seen = torch.arange(n, device="cuda")[None] <= torch.arange(n - m, n, device="cuda")[:, None]
             x = x.masked_fill(~seen, -math.inf)
             z = torch.logsumexp(x, -1)
+            x = x.masked_fill(~seen.any(1)[:, None], 0.0) - z.masked_fill(torch.isneginf(z), math.inf)[..., None]
             lse[at:at + m, h * g:(h + 1) * g] = z.T
-            out[at:at + m, h * g:(h + 1) * g] = ((x - z[..., None]).exp() @ v).transpose(0, 1)
+            out[at:at + m, h * g:(h + 1) * g] = (x.exp() @ v).transpose(0, 1)
         at += m
     return out, lse
+
+
+def near(b, out, lse, rows=slice(None)):
+    """Every row within 4 of the type's roundings of the reference's norm (the output's, the weights' and as much again for their
+    sums), lse within 2^-14."""
+    real = sum(b.new)
+    ref, ref_lse = reference(b)
+    u = torch.finfo(b.dt).eps / 2
+    far = torch.linalg.norm(out[:real].double() - ref, dim=-1) - 4 * u * torch.linalg.norm(ref, dim=-1)
+    assert (far[rows] <= 1e-3).all(), far[rows].max()
+    off = (lse[:real].double() - ref_lse)[rows]
+    assert (off[torch.isfinite(ref_lse[rows])].abs() <= 2.0 ** -14).all()
+    assert torch.equal(torch.isneginf(lse[:real][rows]), torch.isneginf(ref_lse[rows]))
+    assert (out[real:] == 7).all() and (lse[real:] == 7).all()
 
 
 @pytest.mark.parametrize("heads,dim,dtype,page,groups", [
@@ -294,17 +309,47 @@ def test_what_the_device_finds_wrong(ap):
         b.check(out, lse)
 
 
-def test_the_prefix_is_read_through_the_first_entry(ap):
-    """Entries behind the first need no pages below the shared rows."""
-    b = Batch(ap, "8/2", 128, "bf16", 16, [(64, [(80, 1), (70, 2), (100, 3)])], seed=14)
+@pytest.mark.parametrize("members,shared", [([(900, 1)] * 2 + [(880, 3)], True), ([(1000, 300), (980, 290), (950, 200)], False)])
+def test_rows_are_read_together_where_that_saves_products(ap, members, shared):
+    """A NaN in the shared rows of the second sequence's own pages shows whose were read: the first's for all, or each its own."""
+    b = Batch(ap, "8/2", 128, "bf16", 64, [(640, members)], seed=14)
+    b.plan()
+    b.check(*b.attend())
+    page = next(i for i in range(b.k.shape[1]) if i not in b.table)               # a page of nobody
     table = b.table.copy()
-    for seq in b.seqs[1:]:
-        table[seq, :4] = -1
+    table[b.seqs[1], 3] = page
+    b.k[:, page], b.v[:, page] = 0.0, NAN
     b.cache = ap.PagedCache(b.k, b.v, i32(table))
     b.plan()
-    out, lse = b.attend()
-    assert ap.apack_device_error(b.ws) == 0
-    b.check(out, lse)
+    out, _ = b.attend()
+    m0, m1 = b.new[0], b.new[1]
+    assert not torch.isnan(out[:m0]).any() and not torch.isnan(out[m0 + m1:sum(b.new)]).any()
+    assert torch.isnan(out[m0:m0 + m1]).all() == (not shared)
+
+
+def test_rows_of_one_part_are_written_out_at_once(ap):
+    """Sequences that share nothing and are short: no part, the same rules (tails, masks, what is no number, tokens that see nothing)."""
+    cases = [("28/4", 128, "bf16", 16, [(0, [(200 + 40 * i, 60 + 10 * i)]) for i in range(40)]),
+             ("8/8", 64, "fp16", 32, [(0, [(300 + i, 290 + i % 9)]) for i in range(60)]),
+             ("5/1", 128, "fp16", 7, [(0, [(260, 260)]) for i in range(80)])]
+    for heads, dim, dtype, page, groups in cases:
+        b = Batch(ap, heads, dim, dtype, page, groups, seed=15, pad=2)
+        b.plan()
+        segs = b.ws[1024 + (b.n_q * 16 + 255) // 256 * 256:].view(torch.int32)[:8 * int(b.ws[256:352].view(torch.int32)[9])]
+        assert (segs.view(-1, 8)[:, 7] == -1).any()            # some are
+        near(b, *b.attend())
+        seq = b.seqs[3]
+        p, s = slot(b, seq, int(b.seqlens[seq]) - 1)
+        b.v[0, p, s] = NAN
+        at = sum(b.new[:3])
+        out, lse = b.attend()
+        assert torch.isnan(out[at + b.new[3] - 1]).all()
+        b.v[0, p, s] = 0.0
+        near(b, out, lse, rows=[i for i in range(sum(b.new)) if i != at + b.new[3] - 1])
+        b.lens[int(b.seqs[5])] = b.new[5] - 4                  # its first four tokens see nothing
+        b.seqlens[b.seqs[5]] = b.new[5] - 4
+        b.plan()
+        near(b, *b.attend())
 
 
 FIRST = r"""
