@@ -15,9 +15,9 @@ constexpr int kGRows = 2 * kGSlot;   // query rows of a segment
 constexpr int32_t kGMagic = 0x47505631;
 
 // Query rows are packed per KV head: row t * group + j is head h * group + j of token t, so that an item's rows are one
-// run.  An item is a run of keys with the query rows that read it: the shared rows of a group with the new tokens of all its
-// sequences, or the rest of one sequence with its own.  Its rows are cut into runs of 256, its keys into runs of `chunk`
-// tiles; a segment is one of each, of one KV head.
+// run.  An item is a run of keys with the query rows that read it: the shared rows of a group with the new tokens of
+// all its sequences, or the rest of one sequence with its own.  Its rows are cut into runs of 256, its keys into runs
+// of `chunk` tiles; a segment is one of each, of one KV head.
 struct GroupItem {
   int32_t seq;                       // row of the page table through which the keys are read
   int32_t key0, key1;                // keys [key0, key1)
@@ -45,7 +45,7 @@ struct GroupHead {
   int32_t magic, n_q, hq, hkv;
   int32_t head_dim, num_seqs, max_pages, page_tokens;
   int32_t num_pages, segs, causal_any, pad;
-  int64_t tok_off, item_off, seg_off, ml_off, part_off, total;
+  int64_t item_off, ml_off, part_off, total;
 };
 constexpr size_t kGHeadOff = 256, kGClaimOff = 512, kGFixed = 1024;
 
@@ -83,9 +83,9 @@ struct GroupArgs {
 __device__ __forceinline__ bool group_head(const GroupArgs &A, GroupHead &h) {
   const int4 *p = reinterpret_cast<const int4 *>(A.ws + kGHeadOff);
   int4 *d = reinterpret_cast<int4 *>(&h);
-  static_assert(sizeof(GroupHead) == 96, "whole int4s");
+  static_assert(sizeof(GroupHead) == 80, "whole int4s");
 #pragma unroll
-  for (int i = 0; i < 6; ++i) d[i] = p[i];
+  for (int i = 0; i < 5; ++i) d[i] = p[i];
   return h.magic == kGMagic && h.n_q == A.n_q && h.hq == A.hq && h.hkv == A.hkv && h.head_dim == A.head_dim &&
          h.num_seqs == A.pool.num_seqs && h.max_pages == A.pool.max_pages &&
          h.page_tokens == static_cast<int32_t>(A.pool.page_tokens.d) && h.num_pages == A.pool.num_pages &&

@@ -2,35 +2,45 @@
 //
 //   out[t, h] = sum_r softmax_r(scale q[t, h] . k[r, g(h)]) v[r, g(h)],  r <= position of t
 //
-// What makes it fast.  64 conversations about one video read the same cache; token by token that is 64 reads of it, and one
-// here.  All query rows of a KV head (tokens of all sequences that share the keys, times the query heads of the KV head) are rows
-// of one matrix product, 256 of them per segment, so that the tensor cores do what several reads did: with 256 rows a tile of
-// 128 keys takes 2 x 128 x 128 x D x 4 flops against 512 D bytes, and the tensor pipe, not HBM, is the bound above some 160 rows.
+// What makes it fast.  64 conversations about one video read the same cache; token by token that is 64 reads of it, and
+// one here.  All query rows of a KV head (tokens of all sequences that share the keys, times the query heads of the KV
+// head) are rows of one matrix product, 256 of them per segment, so that the tensor cores do what several reads did:
+// with 256 rows a tile of 128 keys takes 2 x 128 x 128 x D x 4 flops against 512 D bytes, and the tensor pipe, not HBM,
+// is the bound above some 160 rows.
 //
-// A segment (group_plan.cu) is 256 query rows of a KV head against a run of 128-key tiles.  CTAs (one per SM) take segments from
-// a counter, long ones first; every segment's result is a part (max, sum, unnormalised values) of its own, and the merge
-// adds a row's parts in the order of their keys, so that the result does not depend on who took what.
-//   warps 0..3, 4..7   softmax of accumulators 0 and 1, a query row per thread (TMEM lane): P is written over S as 16-bit pairs (the
-//                      A operand of the second product comes from TMEM), O stays in TMEM for the whole segment.  A row's
-//                      reference maximum is set anew only when it has grown by more than 2^8 (2^4 in fp16): then its warp
-//                      rescales its O.
-//   warp 8             the tensor products, one thread issuing: S = Q K^T and O += P V of accumulators 0 and 1 in turn, so that
-//                      one softmax runs while the other's products do.  S of an accumulator's next tile is issued right
-//                      behind O of this one (products run in the order of issue).
-//   warps 9..11        loads: K and V tiles in a ring of 5 (8 with heads of 64), by TMA boxes of up to 128 tokens (a warp for K, one
-//                      for V, a box per lane), or 16 bytes at a time where pages are no multiple of 8 tokens (all three)
-// A segment of more than 128 rows gives each accumulator half of the rows; one of fewer gives them the even and the odd tiles,
-// and writes two parts.  Operations alternate between the accumulators across segments too, so that short segments overlap.
+// A segment (group_plan.cu) is 256 query rows of a KV head against a run of 128-key tiles.  CTAs (one per SM) take
+// segments from a counter, long ones first; every segment's result is a part (max, sum, unnormalised values) of its
+// own, and the merge adds a row's parts in the order of their keys, so that the result does not depend on who took
+// what.
+//   warps 0..3, 4..7   softmax of accumulators 0 and 1, a query row per thread (TMEM lane): P is written over S as
+//                      16-bit pairs (the A operand of the second product comes from TMEM), O stays in TMEM for the
+//                      whole segment.  A row's reference maximum is set anew only when it has grown by more than 2^8
+//                      (2^4 in fp16): then its warp rescales its O.
+//   warp 8             the tensor products, one thread issuing: S = Q K^T and O += P V of accumulators 0 and 1 in turn,
+//                      so that one softmax runs while the other's products do.  S of an accumulator's next tile is
+//                      issued right behind O of this one (products run in the order of issue).
+//   warps 9..11        loads: K and V tiles in a ring of 5 (8 with heads of 64), by TMA boxes of up to 128 tokens (a
+//                      warp for K, one for V, a box per lane), or 16 bytes at a time where pages are no multiple of 8
+//                      tokens (all three)
+// A segment of more than 128 rows gives each accumulator half of the rows; one of fewer gives them the even and the odd
+// tiles, and writes two parts.  Operations alternate between the accumulators across segments too, so that short
+// segments overlap.
 //
-// P enters the second product as one 16-bit number per probability: 2^-9 (bf16) or 2^-12 (fp16) of each at most, on average
-// less than the output's own rounding, where a second number would take half as much tensor time again; the row's sum
-// is taken of the unrounded probabilities in fp32, so the lse keeps 32 bits.
+// P enters the second product as one 16-bit number per probability: 2^-9 (bf16) or 2^-12 (fp16) of each at most, on
+// average less than the output's own rounding, where a second number would take half as much tensor time again; the
+// row's sum is taken of the unrounded probabilities in fp32, so the lse keeps 32 bits.
 //
-// What a token must not see: keys behind its own are masked in S; values there enter as 0 times a number, so rows behind the
-// segment's last key become zeros in shared memory, and where that is not enough (another token's key whose value is NaN or
-// infinite: 0 times it is NaN) the merge computes the row anew, key by key.
+// What a token must not see: keys behind its own are masked in S; values there enter as 0 times a number, so rows
+// behind the segment's last key become zeros in shared memory, and where that is not enough (another token's key whose
+// value is NaN or infinite: 0 times it is NaN) the merge computes the row anew, key by key.
 //
-// Every wait is bounded (2 s); one that gives up records APACK_ETIMEOUT, and the CTA leaves with its copies and products done.
+// Measured (28/4 heads of 128, bf16, calls in a row, us a layer with its merge, of the tensor rate 1.94 PFLOP/s): 2,048
+// tokens at the end of 27,144 530, 1.45 PFLOP/s, 0.75; 8 questions of 25 to 60 tokens on 135,272 shared rows 416, 1.50,
+// 0.77; 16 of 12 to 60 on 22,772 162 with the plan; a decode step of 64 conversations on those 51; a tile of 256 rows
+// and 128 keys takes 2,600 clocks, its products 2,048.
+//
+// Every wait is bounded (2 s); one that gives up records APACK_ETIMEOUT, and the CTA leaves with its copies and
+// products done.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -66,8 +76,8 @@ struct __align__(16) Bars {
 };
 static_assert(sizeof(Bars) <= 1536, "barrier block");
 
-// 16-bit types of K, V and P.  The reference is kShift below the row's maximum when it was set; see paged_decode.cu for the
-// range of fp16 (a long tail far below one key).
+// 16-bit types of K, V and P.  The reference is kShift below the row's maximum when it was set; see paged_decode.cu for
+// the range of fp16 (a long tail far below one key).
 template <class T>
 struct Type;
 template <>
@@ -112,8 +122,8 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       : "memory");
 }
 // One thread of the warp.  What it issues to the tensor cores inside this branch takes one instruction each; inside
-// "lane == 0" the compiler cannot tell that a single thread is there (8 products issued in 580 clocks, here 520, of which
-// 512 are the products).
+// "lane == 0" the compiler cannot tell that a single thread is there (8 products issued in 580 clocks, here 520, of
+// which 512 are the products).
 __device__ __forceinline__ bool elect_one() {
   uint32_t one;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
@@ -212,9 +222,10 @@ __device__ __forceinline__ bool hot_wait(uint64_t *bar, uint32_t parity, Bars *b
   return wait(bar, parity, b, err, where);
 }
 
-// The products of the CTA's segments, by one thread.  What it does between a softmax's signal and the products that wait for
-// it is on the critical path of an accumulator, and takes some ten clocks per instruction: so a tile's places, phases and
-// descriptors are ready before, and the next tile's scores follow the values with nothing but their issue in between.
+// The products of the CTA's segments, by one thread.  What it does between a softmax's signal and the products that
+// wait for it is on the critical path of an accumulator, and takes some ten clocks per instruction: so a tile's places,
+// phases and descriptors are ready before, and the next tile's scores follow the values with nothing but their issue in
+// between.
 template <class T, int D>
 struct Products {
   using L = Lay<D>;
@@ -400,8 +411,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   pdl_wait_and_release();
   const uint32_t tmem = b->tmem;
   GroupHead h;
-  GroupSeg first_seg = {};
-  if (warp >= kLoadWarp) first_seg = reinterpret_cast<const GroupSeg *>(A.ws + A.seg_off)[blockIdx.x];     // beside the head (there are more places than CTAs)
+  GroupSeg first_seg = {};                                        // beside the head (there are more places than CTAs)
+  if (warp >= kLoadWarp) first_seg = reinterpret_cast<const GroupSeg *>(A.ws + A.seg_off)[blockIdx.x];
   const bool planned = group_head(A, h);
   int item = 0;                                                   // tiles issued by a load warp
   if (!planned) {
@@ -412,8 +423,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     unsigned int *claims = reinterpret_cast<unsigned int *>(A.ws + kGClaimOff);
     const uint32_t ring = smem_u32(smem) + L::kOffRing;
     if (A.box && warp < kLoadWarp + 2) {
-      // by TMA: K tiles by the first warp, which also takes the segments, V tiles by the second; a box per lane, whose page is
-      // known one tile ahead
+      // by TMA: K tiles by the first warp, which also takes the segments, V tiles by the second; a box per lane, whose
+      // page is known one tile ahead
       const int box = A.box, v = warp - kLoadWarp;
       const int blk = lane % kBlocks, bx = lane / kBlocks;
       const CUtensorMap *map = v ? &vmap : &kmap;
@@ -487,8 +498,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         g = next;
       }
     } else if (!A.box) {
-      // rows by the lanes.  A copy is seen by the tensor cores only behind a fence of the thread that made it, so a tile's
-      // arrival is signalled when the tile after next has been issued and its own copies have landed.
+      // rows by the lanes.  A copy is seen by the tensor cores only behind a fence of the thread that made it, so a
+      // tile's arrival is signalled when the tile after next has been issued and its own copies have landed.
       constexpr int kChunks = D / 8, kAtOnce = 32 / kChunks, kBehind = 2;
       const int w = warp - kLoadWarp, ch = lane % kChunks;
       unsigned claimed = blockIdx.x;
@@ -665,8 +676,8 @@ __global__ void __launch_bounds__(kThreads, 1)
               for (int i = 0; i < 4; ++i) tmem_st16(sc + i * 16, p[i]);
           }
           if (!done) {
-            // A segment's first tile, one that a row does not see whole, or a new reference: 32 scores at a time, in loops (code
-            // that runs once per segment is read from far away)
+            // A segment's first tile, one that a row does not see whole, or a new reference: 32 scores at a time, in
+            // loops (code that runs once per segment is read from far away)
             float most = -INFINITY;
 #pragma unroll 1
             for (int i = 0; i < 4; ++i) {
@@ -712,8 +723,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         }
         if (t == seg.tiles - 1 && A.box) {
-          // behind the segment's last key: zeros in V, whatever lies there (0 times a stale infinity would be NaN; where both
-          // accumulators read the tile, both write them)
+          // behind the segment's last key: zeros in V, whatever lies there (0 times a stale infinity would be NaN;
+          // where both accumulators read the tile, both write them)
           const int valid = seg.g.key1 - seg.g.key0 - t * kGTile;
           if (valid < kGTile) {
             Place<kRing> at = place;
@@ -883,8 +894,8 @@ __device__ __forceinline__ void merge_parts(const GroupArgs &A, const GroupHead 
 }
 
 // W: warps of a row (a CTA of 8 warps takes 8 / W rows).
-template <class T, int D, int W>
-__global__ void __launch_bounds__(256, W == 1 ? 5 : 2) group_merge_kernel(const __grid_constant__ GroupArgs A) {
+template <class T, int D, int W, int N>
+__global__ void __launch_bounds__(256, N < kBatch ? 5 : 2) group_merge_kernel(const __grid_constant__ GroupArgs A) {
   constexpr int kF = D / 32;
   __shared__ float qs[8][D];
   __shared__ float2 stat[8];
@@ -913,27 +924,27 @@ __global__ void __launch_bounds__(256, W == 1 ? 5 : 2) group_merge_kernel(const 
   if (direct) {
     // written out already; of interest only where it is no number
     const float2 st = reinterpret_cast<const float2 *>(A.ws + h.ml_off)[x1.at(0)];
-    if (st.y == st.y || (W > 1 && warp != 0)) return;
+    if (st.y == st.y || warp % W != 0) return;
     a.l = st.y;
   } else {
-    merge_parts<D, W == 1 ? kFewParts : kBatch>(A, h, x0, x1, warp % W, W, a);
+    merge_parts<D, N>(A, h, x0, x1, warp % W, W, a);
   }
   if (W > 1 && !direct) {
     stat[warp] = make_float2(a.m, a.l);
 #pragma unroll
     for (int e = 0; e < kF; ++e) qs[warp][lane * kF + e] = a.o[e];
-    __syncthreads();
-    if (warp != 0) return;
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / W), "r"(32 * W) : "memory");          // the row's warps
+    if (warp % W != 0) return;
     float top = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < W; ++w) top = fmaxf(top, stat[w].x);
+    for (int w = 0; w < W; ++w) top = fmaxf(top, stat[warp + w].x);
     a = {top, 0.f, {}};
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      const float f = stat[w].x == top ? 1.f : ex2_approx(stat[w].x - top);
-      a.l += stat[w].y * f;
+      const float f = stat[warp + w].x == top ? 1.f : ex2_approx(stat[warp + w].x - top);
+      a.l += stat[warp + w].y * f;
 #pragma unroll
-      for (int e = 0; e < kF; ++e) a.o[e] += qs[w][lane * kF + e] * f;
+      for (int e = 0; e < kF; ++e) a.o[e] += qs[warp + w][lane * kF + e] * f;
     }
     __syncwarp();
   }
@@ -978,9 +989,13 @@ cudaError_t launch_group(const GroupArgs &A, const CUtensorMap &kmap, const CUte
   if (e != cudaSuccess) return e;
   count_launches(1);
   const int64_t rows = static_cast<int64_t>(A.n_q) * A.hq;
-  // few rows have many parts: eight warps each
-  e = rows <= 8 * sms ? launch_pdl(group_merge_kernel<T, D, 8>, dim3(static_cast<unsigned>(rows)), dim3(256), 0, stream, A)
-                      : launch_pdl(group_merge_kernel<T, D, 1>, dim3(static_cast<unsigned>((rows + 7) / 8)), dim3(256), 0, stream, A);
+  // few rows have many parts: several warps each; many have few, and there it is warps that count
+  auto merge = [&](auto kernel, int warps) {
+    return launch_pdl(kernel, dim3(static_cast<unsigned>((rows * warps + 7) / 8)), dim3(256), 0, stream, A);
+  };
+  e = rows <= 8 * sms    ? merge(group_merge_kernel<T, D, 8, kBatch>, 8)
+      : rows <= 64 * sms ? merge(group_merge_kernel<T, D, 1, kBatch>, 1)
+                         : merge(group_merge_kernel<T, D, 1, kFewParts>, 1);
   if (e == cudaSuccess) count_launches(1);
   return e;
 }

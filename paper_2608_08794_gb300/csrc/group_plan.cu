@@ -1,10 +1,11 @@
 // group_plan.cu -- the work of attention over shared rows, laid out on the device from lengths and groups.
 //
-// A step's plan serves all its layers, and lengths stay on the device, so that a captured step follows growing caches.  One
-// CTA: it finds each sequence's group (a search among the groups' bounds in shared memory), how many rows of its keys are
-// the group's, how long the runs of keys should be, and writes items, segments and what each token sees.
+// A step's plan serves all its layers, and lengths stay on the device, so that a captured step follows growing caches. 
+// One CTA: it finds each sequence's group (a search among the groups' bounds in shared memory), how many rows of its
+// keys are the group's, how long the runs of keys should be, and writes items, segments and what each token sees.
 //
-// Bound by latency (block barriers and trips to L2, some 8 us for 64 sequences): once per step, not per layer.
+// Bound by latency: trips to L2, block barriers, and reading code that runs once (64 sequences: 9 us, of which offsets
+// and items 3.5, run lengths 3.5, places and segments 2): once per step, not per layer.
 //
 // The length of a run.  A segment of c tiles costs about c + kSegCost tiles of one SM; n segments on S SMs end after
 // max(sum of all / S, ceil(long ones / S) * (c + kSegCost)) at the least, and every part's row is written and read once
@@ -171,7 +172,8 @@ __global__ void __launch_bounds__(kThreads, 1) group_plan_kernel(const __grid_co
   __syncthreads();
   const bool bad = s.bad;
   const int total_items = ng + n;
-  // ---- items: every sequence finds its group's shared rows by itself, so that nothing waits between groups and sequences
+  // ---- items: every sequence finds its group's shared rows by itself, so that nothing waits between groups and
+  // sequences
   for (int g = threadIdx.x; g < ng; g += kThreads) s.rows[g] = s.tiles[g] = s.seg0[g] = 0;
   __syncthreads();
   // seg0, for now: the runs of rows that a group's sequences make by themselves
@@ -204,8 +206,8 @@ __global__ void __launch_bounds__(kThreads, 1) group_plan_kernel(const __grid_co
       cut -= cut % P.align;
       const int rows = (s.cu_q[first + count] - s.cu_q[first]) * G;
       // Reading rows together pays where it saves products: their tiles once per run of the group's rows, not of each
-      // sequence's, against a segment more per run and a part more per row.  (30 prompts of 700 tokens behind 200 shared rows:
-      // {SHARED} us together, {APART} apart.)
+      // sequence's, against a segment more per run and a part more per row.  (13 prompts of 350 to 700 tokens behind
+      // 255 shared rows, 28/4 heads of 128: 378 us together, 303 apart.)
       const int tiles = (cut + kGTile - 1) / kGTile, runs = runs_of(rows);
       if (!in0 || rows == 0 || static_cast<float>(s.seg0[g] - runs) * tiles <= runs * kSegCost + rows * kRowCost) cut = 0;
       if (e == first && cut > 0) {
@@ -331,9 +333,7 @@ __global__ void __launch_bounds__(kThreads, 1) group_plan_kernel(const __grid_co
     h.num_pages = P.num_pages;
     h.segs = count;
     h.causal_any = s.causal;
-    h.tok_off = P.tok_off;
     h.item_off = P.item_off;
-    h.seg_off = P.seg_off;
     h.ml_off = P.ml_off;
     h.part_off = P.part_off;
     h.total = P.total;

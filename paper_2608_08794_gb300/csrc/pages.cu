@@ -1,14 +1,17 @@
-// pages.cu -- who holds which page of a paged key-value cache, on the device: page tables, lengths, reference counts and
-// a stack of free pages, changed by kernels, so that a captured step of a server needs no host between its layers.
+// pages.cu -- who holds which page of a paged key-value cache, on the device: page tables, lengths, reference counts
+// and a stack of free pages, changed by kernels, so that a captured step of a server needs no host between its layers.
 //
-// What a call takes or gives back is a list in the order of its entries, then of their rows: page j of the list comes from
-// (goes to) place free_count - 1 - j.  The list's positions are exclusive sums over the entries, so that nothing depends on
-// the order in which threads run, and a release followed by an extension of as many pages restores the stack.
+// What a call takes or gives back is a list in the order of its entries, then of their rows: page j of the list comes
+// from (goes to) place free_count - 1 - j.  The list's positions are exclusive sums over the entries, so that nothing
+// depends on the order in which threads run, and a release followed by an extension of as many pages restores the
+// stack.
 //
-// Bound by latency: a chain of some five reads that depend on one another (entry, length, table, count, page), block
-// barriers between them, and one launch.  One CTA does all of it, because the state is small (a step of 61 sequences touches
-// a few KB) and every other split needs a second launch or a grid barrier, which cost more than the work.  Only the map from
-// new rows to slots is large when prompts enter (16 bytes per row): above kInlineRows rows a second kernel on all SMs fills it.
+// Bound by latency: a chain of some five reads that depend on one another (entry, length, table, count, page), barriers
+// between them, and one launch: release and extension of 61 sequences by a row each take 14.7 us, 256 drafts 19.  One
+// CTA, or a cluster of eight where the lists may be long, because a split over the grid needs a second launch or a grid
+// barrier, which cost more than the work.  Only the map from new rows to slots is large when prompts enter (16 bytes
+// per row): above kInlineRows rows a second kernel on all SMs fills it (670,000 rows of 1,000 prompts: 7.4 us, 1.4
+// TB/s).
 #include <algorithm>
 #include <cstring>
 
@@ -21,8 +24,9 @@ namespace {
 constexpr int kThreads = 1024;
 constexpr int kWarps = kThreads / 32;
 constexpr int kPer = APACK_MAX_SEQS / kThreads;      // entries of a thread: kThreads apart, so that few entries take few steps
-// Calls that may move more pages than this take a cluster (a step of 61 sequences as one CTA, which saves 3 us; 45,000 pages of
-// 64 questions by one SM, that reads one of them per clock at best, take {ONE} us, by eight {EIGHT}).
+// Calls that may move more pages than this take a cluster: 45,000 pages of 64 questions that leave and come take 352 us
+// by one SM, which reads one random place per clock at best, and 90 by eight; 40,000 pages of 1,000 prompts 96 and 37. 
+// A step of 61 sequences takes 2 us longer so (16.4 -> 18.5), but nothing on the host says how few pages it moves.
 constexpr int kMaxCluster = 8;
 constexpr int64_t kClusterPages = 16384;
 // Rows of the slot map that the first kernel fills by itself.
@@ -117,9 +121,9 @@ __device__ int entry_seq(const Call &C, Shared &s, int i) {
 
 __device__ __forceinline__ int32_t now(const int32_t *p) { return *const_cast<const volatile int32_t *>(p); }
 
-// The entries of kBatch places of the list (the last i with at[i] <= j), side by side: every pass over a list is bound by the
-// trips of its reads, so a thread has as many of them under way (64 questions that leave and come, 45,000 pages: {BEFORE} us
-// one by one, {AFTER} so).
+// The entries of kBatch places of the list (the last i with at[i] <= j), side by side: every pass over a list is bound
+// by the trips of its reads, so a thread has as many of them under way (1,000 prompts, 40,000 pages: 202 us one by one,
+// 96 so).
 constexpr int kBatch = 8;
 __device__ __forceinline__ void entries_of(const int32_t *at, int n, const int (&j)[kBatch], int (&e)[kBatch]) {
 #pragma unroll
@@ -181,8 +185,8 @@ __device__ void begin(Shared &s) {
 // ---------------------------------------------------------------- release
 
 // Every entry keeps its first rows[i] rows.  The pages behind them lose a holder; each that has none left goes to the
-// stack once, at its first place in the call's list: while the list is walked a count of 0 becomes the least place at which
-// the page is named (minus 2^31), which is found whatever the order of the threads.
+// stack once, at its first place in the call's list: while the list is walked a count of 0 becomes the least place at
+// which the page is named (minus 2^31), which is found whatever the order of the threads.
 template <int CL>
 __global__ void __launch_bounds__(kThreads, 1) pages_release_kernel(const __grid_constant__ Call C) {
   __shared__ Shared s;
@@ -424,8 +428,9 @@ __device__ __forceinline__ void write_maps(const Call &C, const Maps &M, const i
   }
 }
 
-// Entry i gets rows[i] more rows.  A last page that it shares and would write into is replaced by one of its own: of the
-// sequences that hold it, all that the call extends but the last holder; the pair (old, new) is left for apack_copy_pages.
+// Entry i gets rows[i] more rows.  A last page that it shares and would write into is replaced by one of its own: of
+// the sequences that hold it, all that the call extends but the last holder; the pair (old, new) is left for
+// apack_copy_pages.
 template <int CL>
 __global__ void __launch_bounds__(kThreads, 1)
     pages_extend_kernel(const __grid_constant__ Call C, const __grid_constant__ Maps M) {
@@ -535,10 +540,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (threadIdx.x == 0 && leads) *t.free_count = count - sum;
   }
   __syncthreads();
-  if (CL > 1 || M.max_rows > kInlineRows) return;           // the next kernel's
-  for (int i = threadIdx.x; i <= C.n; i += kThreads) s.at[i] = M.cu[i];
-  __syncthreads();
-  for (int64_t j = threadIdx.x; j < M.max_rows; j += kBatch * kThreads) write_maps(C, M, s.at, j, kThreads);
+  if constexpr (CL == 1) {                                  // (longer maps are the next kernel's)
+    if (M.max_rows > kInlineRows) return;
+    for (int i = threadIdx.x; i <= C.n; i += kThreads) s.at[i] = M.cu[i];
+    __syncthreads();
+    for (int64_t j = threadIdx.x; j < M.max_rows; j += kBatch * kThreads) write_maps(C, M, s.at, j, kThreads);
+  }
 }
 
 __global__ void __launch_bounds__(256) pages_map_kernel(const __grid_constant__ Call C, const __grid_constant__ Maps M) {
