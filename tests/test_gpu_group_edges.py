@@ -352,6 +352,33 @@ def test_rows_of_one_part_are_written_out_at_once(ap):
         near(b, *b.attend())
 
 
+@pytest.mark.parametrize("page", [16, 7])
+def test_pages_beyond_four_gigabytes(ap, page):
+    """TMA boxes and rows by the lanes, from the end of a pool of 5 GB of keys.
+
+    Per value: half a step of bf16 for each probability, half a step for the output, and as much again for fp32's sums and exponentials.
+    """
+    n, pages = 300, 5 * 2 ** 30 // (page * 4 * 128 * 2)
+    k, v = (torch.empty(1, pages, page, 4, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    need = -(-n // page)
+    used = torch.arange(pages - need, pages, device="cuda").flip(0)
+    for x in (k, v):
+        x[0, used] = torch.randn(need, page, 4, 128, device="cuda").bfloat16()
+    cache = ap.PagedCache(k, v, used.to(torch.int32)[None].repeat(2, 1))
+    q = torch.randn(5, 28, 128, device="cuda").bfloat16()
+    out = torch.empty_like(q)
+    ws = workspace(ap.apack_paged_group_workspace_size(cache, 28, 2, 5))
+    ap.apack_paged_group_plan(cache, i32([n, n]), 28, 5, ws, cu_q=i32([0, 2, 5]), cu_groups=i32([0, 2]), prefix=i32([n - 40]))
+    ap.apack_paged_group_attention(cache, 0, q, out, ws)
+    assert ap.apack_device_error(ws) == 0
+    kk, vv = (x[0, used].flatten(0, 1)[:n].double() for x in (k, v))
+    for t, seen in enumerate((n - 1, n, n - 2, n - 1, n)):
+        for h in range(28):
+            p = torch.softmax(kk[:seen, h // 7] @ q[t, h].double() / math.sqrt(128), 0)
+            ref = p @ vv[:seen, h // 7]
+            assert ((out[t, h].double() - ref).abs() <= 2.0 ** -8 * (ref.abs() + 2 * (p @ vv[:seen, h // 7].abs()))).all()
+
+
 FIRST = r"""
 import sys, threading
 import torch
