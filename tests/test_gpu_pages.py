@@ -213,3 +213,84 @@ def test_padding_copies_nothing_beside_a_page_that_is_written(ap):
         x[:, 0] = x[:, 4]
     ap.apack_copy_pages(cache, i32([[0, 0]] * 40 + [[4, 0]] + [[0, 0]] * 40))
     assert torch.equal(k, want[0]) and torch.equal(v, want[1])
+
+
+def test_rows_of_a_wider_table(ap):
+    """Tables whose rows lie apart: what lies between them stays."""
+    p = Pair(ap, 40, 500, 20000, 16)                         # (40 x 500 entries: a cluster)
+    wide = torch.full((40, 517), 77, dtype=torch.int32, device="cuda")
+    wide[:, 9:509] = -1
+    t = p.t
+    p.t = ap.PageTables(wide[:, 9:509], t.lengths, t.refs, t.free_list, t.free_count, 16)
+    seqs = np.random.default_rng(2).permutation(40).tolist()
+    p.extend(seqs[:30], [1 + (997 * b) % 8000 for b in seqs[:30]])
+    p.same()
+    p.fork(seqs[:5], seqs[30:35])
+    p.same()
+    p.release(seqs[3:33], [p.ref.lengths[b] // 2 for b in seqs[3:33]])
+    p.same()
+    p.extend(seqs[:33], [3] * 33)
+    p.same()
+    assert (wide[:, :9] == 77).all() and (wide[:, 509:] == 77).all()
+
+
+def test_lists_that_are_the_lengths(ap):
+    """The pool's own lengths as the rows to keep, and as the rows to add."""
+    t, ref = ap.PageTables.new(300, 90, 27000, 16), PageLists(300, 90, 27000, 16)
+    w, grow = ws(), [(37 * b) % 700 for b in range(300)]
+    cu = i32([0] * 301)
+    ap.apack_pages_extend(t, i32(grow), cu, i32([0] * sum(grow)), ws=w)
+    ref.extend(list(range(300)), grow)
+    ap.apack_pages_release(t, t.lengths, ws=w)
+    assert t.lengths.tolist() == grow
+    rows = i32([0] * sum(grow))
+    ap.apack_pages_extend(t, t.lengths, cu, rows, ws=w)
+    want = ref.extend(list(range(300)), grow)
+    assert cu.tolist() == want[0] and rows.tolist() == want[1]
+    assert t.page_table.tolist() == ref.table and t.lengths.tolist() == ref.lengths and ap.apack_device_error(w) == 0
+
+
+@pytest.mark.parametrize("most", [90, 9000])
+def test_a_captured_step_follows_its_inputs(ap, most):
+    """Release, fork and extension in one graph; a map by the first kernel, and one by the second."""
+    n, width, page = 12, 64, 16
+    t, ref, w = ap.PageTables.new(2 * n, width, 2 * n * width, page), PageLists(2 * n, width, 2 * n * width, page), ws()
+    seqs, parents, keep, grow = (i32([0] * n) for _ in range(4))
+    seqs.copy_(i32(range(n)))
+    kids, none = i32(range(n, n + 4)), i32([0] * 4)
+    cu, rows, owners = i32([0] * (n + 1)), i32([0] * most), i32([0] * most)
+    slots, pairs = torch.zeros(most, dtype=torch.int64, device="cuda"), i32([0] * (2 * n)).view(n, 2)
+
+    def step():
+        ap.apack_pages_release(t, keep, seqs=seqs, ws=w)
+        ap.apack_pages_release(t, none, seqs=kids, ws=w)
+        ap.apack_pages_fork(t, parents[:4], kids, ws=w)
+        ap.apack_pages_extend(t, grow, cu, rows, seqs=seqs, row_seqs=owners, slots=slots, pairs=pairs, ws=w)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()                                                # (all empty)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            step()
+    torch.cuda.current_stream().wait_stream(s)
+    rng = np.random.default_rng(most)
+    for _ in range(12):
+        order = rng.permutation(n).tolist()
+        from_ = rng.permutation(n)[:4].tolist()
+        kept = [int(rng.integers(0, ref.lengths[b] + 1)) if rng.random() < 0.5 else ref.lengths[b] for b in order]
+        after = dict(zip(order, kept))
+        more = [min(int(rng.integers(0, most // n)), width * page - after[b]) for b in order]
+        seqs.copy_(i32(order)), keep.copy_(i32(kept)), grow.copy_(i32(more)), parents[:4].copy_(i32(from_))
+        g.replay()
+        ref.release(order, kept)
+        ref.release(list(range(n, n + 4)), [0] * 4)
+        ref.fork(from_, list(range(n, n + 4)))
+        want = ref.extend(order, more)
+        pad = [-1] * (most - sum(more))
+        assert ap.apack_device_error(w) == 0
+        assert t.page_table.tolist() == ref.table and t.lengths.tolist() == ref.lengths and t.refs.tolist() == ref.refs
+        assert t.free_list[:int(t.free_count)].tolist() == ref.free
+        assert cu.tolist() == want[0] and rows.tolist() == want[1] + pad and owners.tolist() == want[2] + pad
+        assert slots.tolist() == want[3] + pad and [tuple(x) for x in pairs.tolist()] == want[4]
