@@ -1,6 +1,6 @@
 // group_plan.cu -- the work of attention over shared rows, laid out on the device from lengths and groups.
 //
-// A step's plan serves all its layers, and lengths stay on the device, so that a captured step follows growing caches. 
+// A step's plan serves all its layers, and lengths stay on the device, so that a captured step follows growing caches.
 // One CTA: it finds each sequence's group (a search among the groups' bounds in shared memory), how many rows of its
 // keys are the group's, how long the runs of keys should be, and writes items, segments and what each token sees.
 //

@@ -25,7 +25,7 @@ constexpr int kThreads = 1024;
 constexpr int kWarps = kThreads / 32;
 constexpr int kPer = APACK_MAX_SEQS / kThreads;      // entries of a thread: kThreads apart, so that few entries take few steps
 // Calls that may move more pages than this take a cluster: 45,000 pages of 64 questions that leave and come take 352 us
-// by one SM, which reads one random place per clock at best, and 90 by eight; 40,000 pages of 1,000 prompts 96 and 37. 
+// by one SM, which reads one random place per clock at best, and 90 by eight; 40,000 pages of 1,000 prompts 96 and 37.
 // A step of 61 sequences takes 2 us longer so (16.4 -> 18.5), but nothing on the host says how few pages it moves.
 constexpr int kMaxCluster = 8;
 constexpr int64_t kClusterPages = 16384;
