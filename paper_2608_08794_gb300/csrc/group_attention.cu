@@ -499,7 +499,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     } else if (!A.box) {
       // rows by the lanes.  A copy is seen by the tensor cores only behind a fence of the thread that made it, so a
-      // tile's arrival is signalled when the tile after next has been issued and its own copies have landed.
+      // tile's arrival is signalled when the tile after next has been issued and its own copies have landed, or before
+      // the warp waits for a place.
       constexpr int kChunks = D / 8, kAtOnce = 32 / kChunks, kBehind = 2;
       const int w = warp - kLoadWarp, ch = lane % kChunks;
       unsigned claimed = blockIdx.x;
@@ -543,9 +544,19 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           for (int v = 0; v < 2; ++v, ++item) {
             const int slot = item % kRing;
-            if (item >= kRing && !warp_wait(&b->empty[slot], ((item / kRing) - 1) & 1u, b, A.err, 162)) {
-              ok = false;
-              break;
+            if (item >= kRing) {
+              // While the place is taken, nothing that was issued may stay behind: where the accumulators take the tiles
+              // in turn, it is given back only when the keys two tiles on have been signalled, which are the item before
+              // this one in a ring of five.
+              const uint32_t parity = ((item / kRing) - 1) & 1u;
+              if (!__all_sync(0xffffffffu, passed(&b->empty[slot], parity))) {
+                cp_async_wait<0>();
+                signal(item);
+              }
+              if (!warp_wait(&b->empty[slot], parity, b, A.err, 162)) {
+                ok = false;
+                break;
+              }
             }
             const uint8_t *base = v ? A.pool.v : A.pool.k;
             const uint32_t dst = ring + slot * L::kTileBytes + (ch >> 3) * kHalfBytes;
