@@ -940,9 +940,9 @@ __global__ void __launch_bounds__(256, N < kBatch ? 5 : 2) group_merge_kernel(co
   Row<D> a = {-INFINITY, 0.f, {}};
   const bool direct = tok.prefix < 0 && x1.n == 1 && i1.splits == 1 && !x1.two;
   if (direct) {
-    // written out already; of interest only where it is no number
+    // written out already, with its lse; of interest only where it is no number and what the row does not see may be why
     const float2 st = reinterpret_cast<const float2 *>(A.ws + h.ml_off)[x1.at(0)];
-    if (st.y == st.y || warp % W != 0) return;
+    if (st.y == st.y || !h.causal_any || warp % W != 0) return;
     a.l = st.y;
   } else {
     merge_parts<D, N>(A, h, x0, x1, warp % W, W, a);

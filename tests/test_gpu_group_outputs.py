@@ -1,10 +1,12 @@
 """Attention over shared rows: outputs of rows of a single part, which are written without a merge."""
 
+import math
+
 import pytest
 import torch
 
 from test_gpu_group import Batch
-from test_gpu_group_edges import near
+from test_gpu_group_edges import near, slot
 
 pytestmark = pytest.mark.gpu
 
@@ -40,4 +42,31 @@ def test_outputs_that_start_on_16_bytes(ap, heads, dim, dtype, page, groups):
     assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
     assert (room[:off] == 7).all() and (room[off + n:] == 7).all()
     assert (room_lse[:1] == 7).all() and (room_lse[1 + want[1].numel():] == 7).all()
+    assert ap.apack_device_error(b.ws) == 0
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("heads,dim,dtype,page,count", [
+    ("32/1", 128, "bf16", 16, 300), ("32/1", 64, "fp16", 16, 330), ("32/2", 128, "fp16", 7, 600),
+    ("160/1", 128, "bf16", 16, 3), ("400/2", 64, "bf16", 32, 9),              # 129 to 256 query heads of a KV head
+    ("28/4", 128, "bf16", 16, 40),                                            # (in parts)
+])
+def test_one_feature_that_is_no_number(ap, heads, dim, dtype, page, count, bad):
+    """One token per sequence, so that every row sees all of its keys: a NaN or an infinity in one feature of one value reaches
+    that feature of its KV head's rows and nothing else, and not the lse."""
+    b = Batch(ap, heads, dim, dtype, page, [(0, [(1 + 31 * i % 200, 1)]) for i in range(count)], seed=22, pad=2)
+    b.plan()
+    want, want_lse = b.attend()
+    near(b, want, want_lse)
+    hit = torch.zeros_like(want, dtype=torch.bool)
+    g = b.hq // b.hkv
+    for i, feature in ((count - 1, 3), (count // 2, dim - 1)):
+        row, head = int(b.seqlens[b.seqs[i]]) // 2, i % b.hkv
+        p, s = slot(b, b.seqs[i], row)
+        b.v[0, p, s, head, feature] = bad
+        hit[i, head * g:(head + 1) * g, feature] = True
+    out, lse = b.attend()
+    assert torch.equal(lse, want_lse)
+    assert torch.equal(out[~hit], want[~hit])
+    assert torch.isnan(out[hit]).all() if math.isnan(bad) else not torch.isfinite(out[hit]).any()
     assert ap.apack_device_error(b.ws) == 0
