@@ -577,8 +577,8 @@ apack_status apack_pages_fork(const apack_page_tables *tables, int32_t n, const 
 /* Room for new_rows[i] >= 0 more rows behind each entry's, in pages from the top of the stack (in the order of entries, then of
    rows).  A partly filled last page that other sequences hold too is not written to: the entry gets a page of its own in its
    place, first of its pages, and pairs[i] = (old, new) for apack_copy_pages, (0, 0) elsewhere, which copies nothing (int32
-   [n][2], 8-byte aligned, or NULL where no page is shared).  Of the sequences that share it, all that the call extends
-   get their own but the last holder.
+   [n][2], 8-byte aligned; with NULL an entry that needs a page of its own cannot be carried out).  Of the sequences that
+   share it, all that the call extends get their own but the last holder.
    The map of the new rows, packed over the entries: cu_new (int32 [n+1]) their offsets; rows[j] (int32 [max_rows]) the row in
    its sequence, row_seqs[j] (int32 [max_rows] or NULL) that sequence, as apack_rotary_append takes them; slots[j] (int64
    [max_rows], 8-byte aligned, or NULL) page * page_tokens + slot in the page.  Behind the last new row, and all of them in

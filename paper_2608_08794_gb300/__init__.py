@@ -921,7 +921,7 @@ def apack_pages_extend(tables, new_rows, cu_new, rows, seqs=None, row_seqs=None,
                        stream=None):
     """Room for new_rows[i] more rows behind sequence seqs[i] (None: i).  cu_new int32 [n + 1], rows and row_seqs int32
     [max_rows] and slots int64 [max_rows] receive the map of the new rows, pairs int32 [n, 2] the pages to copy
-    (apack_copy_pages) before they are written."""
+    (apack_copy_pages) before they are written; without it a call that has any to copy cannot be carried out."""
     stream = _on_device((tables, new_rows, cu_new, rows, seqs, row_seqs, slots, pairs, ws), stream)
     n = _entries(tables, new_rows, "new_rows", seqs)
     _int32(cu_new, "cu_new", (n + 1,))

@@ -485,10 +485,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (last[k] < 0) continue;
       int left = t.refs[last[k]];
       for (int x = 0; x < i; ++x) left -= sharing[x] == last[k];
-      if (left > 1)
-        ++take[k];
-      else
+      if (left <= 1) {
         last[k] = -1;
+      } else if (!M.pairs) {                                // nobody would learn which page to copy
+        report(C, 130, i, last[k]);
+        s.bad = 1;
+      } else {
+        ++take[k];
+      }
     }
   }
   const int64_t total = entry_sums(take, C.n, s.at, s), all_rows = entry_sums(grow, C.n, M.cu, s);
