@@ -545,10 +545,11 @@ apack_status apack_copy_pages(const apack_paged_cache *cache, const int32_t *pai
    page_table and lengths are those that apack_paged_cache and the attention calls read.  Start: lengths 0, refs 0,
    free_list all pages, *free_count num_pages.  One call at a time may change them (calls on one stream).
    In every call: n entries, 0 .. APACK_MAX_SEQS; seqs (device [n]): the sequence of an entry, NULL: entry i is sequence i
-   (n <= num_seqs); no sequence twice.  An entry that cannot be carried out (a sequence outside the table or named twice,
-   rows or pages that it does not have, pages that are wanted and not free, a page of the table that nobody holds)
-   leaves everything as it was, and records APACK_EDEVICE in the error word of ws (NULL, or a 16-byte aligned workspace)
-   for the whole call.  Which pages a call takes and leaves depends on its arguments and the state alone
+   (n <= num_seqs); no sequence twice.  Rows to keep or to add may be entries of lengths, as they are before the call; no
+   other list of a call lies in the tables' memory.  An entry that cannot be carried out (a sequence outside the table or
+   named twice, rows or pages that it does not have, pages that are wanted and not free, a page of the table that nobody
+   holds) leaves everything as it was, and records APACK_EDEVICE in the error word of ws (NULL, or a 16-byte aligned
+   workspace) for the whole call.  Which pages a call takes and leaves depends on its arguments and the state alone
    (deterministic).  n = 0 does nothing, except that apack_pages_extend writes its maps. */
 typedef struct apack_page_tables {
   int32_t *page_table;          /* [num_seqs][max_pages]; -1 where a sequence has no page */

@@ -190,6 +190,9 @@ __device__ void begin(Shared &s) {
 template <int CL>
 __global__ void __launch_bounds__(kThreads, 1) pages_release_kernel(const __grid_constant__ Call C) {
   __shared__ Shared s;
+  // of an entry's first page to give up; read from here later on, because the rows to keep may be lengths, which others
+  // of the call's threads write in the end
+  __shared__ int32_t column[APACK_MAX_SEQS];
   begin<CL>(s);
   const PagesView &t = C.t;
   int seq[kPer], keep[kPer], drop[kPer];
@@ -213,7 +216,8 @@ __global__ void __launch_bounds__(kThreads, 1) pages_release_kernel(const __grid
       continue;
     }
     seq[k] = b;
-    drop[k] = t.pages_of(len) - t.pages_of(keep[k]);
+    column[i] = t.pages_of(keep[k]);
+    drop[k] = t.pages_of(len) - column[i];
   }
   const int64_t total = entry_sums(drop, C.n, s.at, s);
   if (total > INT32_MAX - 1 && threadIdx.x == 0) {
@@ -226,7 +230,7 @@ __global__ void __launch_bounds__(kThreads, 1) pages_release_kernel(const __grid
   const int n = C.n, sum = static_cast<int>(total);
   auto place_of = [&](int j, int e) {                       // the table's entry of the list's page j
     const int b = C.seqs ? __ldg(C.seqs + e) : e;
-    return t.row(b) + t.pages_of(C.rows[e]) + (j - s.at[e]);
+    return t.row(b) + column[e] + (j - s.at[e]);
   };
   int32_t *place[kBatch];
   int p[kBatch], r[kBatch];

@@ -1,4 +1,4 @@
-"""Page tables kept on the device: calls without a list of pages to copy."""
+"""Page tables kept on the device: calls without a list of pages to copy, and lists that are other sequences' lengths."""
 
 import pytest
 import torch
@@ -54,3 +54,32 @@ def test_extension_without_pairs(ap, page, pages, room):
     ap.apack_pages_fork(t, i32([2]), i32([4]), ws=w)
     ref.fork([2], [4])
     extend([2, 4], [1, 1], False)                                              # whole pages are shared and not written to
+
+
+@pytest.mark.parametrize("seqs,width", [(150, 90), (300, 90), (1500, 40)])                       # one CTA, a cluster
+@pytest.mark.parametrize("shared", [False, True])
+def test_lists_that_are_other_lengths(ap, seqs, width, shared):
+    """Every sequence is cut to, or grows by, the length that the one before it has before the call."""
+    pages = seqs * width
+    t, ref, w = ap.PageTables.new(seqs + 1, width, pages, 16), PageLists(seqs + 1, width, pages, 16), ws()
+    order = list(range(seqs))
+    grow = [1 + 300 * b // seqs + b % 2 * 20 for b in order]
+    grow = sorted(grow)
+    cu, pairs = i32([0] * (seqs + 1)), i32([[0, 0]] * seqs)
+    rows = i32([0] * (sum(grow) + 3))
+    ap.apack_pages_extend(t, i32(grow), cu, rows, seqs=i32(order), ws=w)
+    ref.extend(order, grow)
+    if shared:
+        ap.apack_pages_fork(t, i32([seqs - 1]), i32([seqs]), ws=w)
+        ref.fork([seqs - 1], [seqs])
+    behind = order[1:]
+    ap.apack_pages_release(t, t.lengths[:seqs - 1], seqs=i32(behind), ws=w)
+    ref.release(behind, grow[:-1])
+    assert ap.apack_device_error(w) == 0
+    assert t.lengths.tolist() == ref.lengths and t.page_table.tolist() == ref.table and t.refs.tolist() == ref.refs
+    assert t.free_list[:int(t.free_count)].tolist() == ref.free
+    now = t.lengths[:seqs - 1].tolist()
+    ap.apack_pages_extend(t, t.lengths[:seqs - 1], cu[:seqs], rows, seqs=i32(behind), pairs=pairs[:seqs - 1], ws=w)
+    want = ref.extend(behind, now)
+    assert ap.apack_device_error(w) == 0 and cu[:seqs].tolist() == want[0] and rows[:len(want[1])].tolist() == want[1]
+    assert t.lengths.tolist() == ref.lengths and t.page_table.tolist() == ref.table and t.refs.tolist() == ref.refs
