@@ -9,9 +9,9 @@
 // is the bound above some 160 rows.
 //
 // A segment (group_plan.cu) is 256 query rows of a KV head against a run of 128-key tiles.  CTAs (one per SM) take
-// segments from a counter, long ones first; every segment's result is a part (max, sum, unnormalised values) of its
-// own, and the merge adds a row's parts in the order of their keys, so that the result does not depend on who took
-// what.
+// segments from a counter, in the plan's order (groups, then the sequences as the caller names them); every segment's
+// result is a part (max, sum, unnormalised values) of its own, and the merge adds a row's parts in the order of their
+// keys, so that the result does not depend on who took what.
 //   warps 0..3, 4..7   softmax of accumulators 0 and 1, a query row per thread (TMEM lane): P is written over S as
 //                      16-bit pairs (the A operand of the second product comes from TMEM), O stays in TMEM for the
 //                      whole segment.  A row's reference maximum is set anew only when it has grown by more than 2^8
@@ -35,9 +35,14 @@
 // value is NaN or infinite: 0 times it is NaN) the merge computes the row anew, key by key.
 //
 // Measured (28/4 heads of 128, bf16, calls in a row, us a layer with its merge, of the tensor rate 1.94 PFLOP/s): 2,048
-// tokens at the end of 27,144 530, 1.45 PFLOP/s, 0.75; 8 questions of 25 to 60 tokens on 135,272 shared rows 416, 1.50,
-// 0.77; 16 of 12 to 60 on 22,772 162 with the plan; a decode step of 64 conversations on those 51; a tile of 256 rows
+// tokens at the end of 27,144 518, 1.48 PFLOP/s, 0.76; 8 questions of 25 to 60 tokens on 135,272 shared rows 427, 1.46,
+// 0.75; 16 of 12 to 60 on 22,772 161 with the plan; a decode step of 64 conversations on those 53; a tile of 256 rows
 // and 128 keys takes 2,600 clocks, its products 2,048.
+//
+// One token per sequence, against apack_paged_decode_attention, which reads every sequence by itself (28/4 heads, 30 own
+// rows each, us a layer with keys from HBM, the plan's 8 to 10 not counted): 2 sequences on 500 shared rows 10.9 and 8.6,
+// 64 on them 22.5 and 14.8; 8, 16 and 64 on 4,644 14.6 and 14.5, 17.5 and 19.1, 29.5 and 50; 4, 8 and 64 on 22,772 24.5
+// and 23.2, 25.9 and 33.7, 43 and 205; 64 of 4,000 rows that share nothing 162 and 88.
 //
 // Every wait is bounded (2 s); one that gives up records APACK_ETIMEOUT, and the CTA leaves with its copies and
 // products done.
@@ -1007,7 +1012,10 @@ cudaError_t launch_group(const GroupArgs &A, const CUtensorMap &kmap, const CUte
   if (e != cudaSuccess) return e;
   count_launches(1);
   const int64_t rows = static_cast<int64_t>(A.n_q) * A.hq;
-  // few rows have many parts: several warps each; many have few, and there it is warps that count
+  // Few rows have many parts: several warps each; many have few, and there it is warps that count.  A layer with 28
+  // query heads on 9,000 rows by 8 warps a row, by one with eight loads under way, and by one with four: 560 rows 20.5,
+  // 23.2 and 36.1 us, 1,120 30.5, 29.5 and 44.5, 4,200 56.9, 33.4 and 34.5, 14,000 174, 80.0 and 79.1, 56,000 554, 265
+  // and 245.
   auto merge = [&](auto kernel, int warps) {
     return launch_pdl(kernel, dim3(static_cast<unsigned>((rows * warps + 7) / 8)), dim3(256), 0, stream, A);
   };

@@ -4,8 +4,9 @@
 // One CTA: it finds each sequence's group (a search among the groups' bounds in shared memory), how many rows of its
 // keys are the group's, how long the runs of keys should be, and writes items, segments and what each token sees.
 //
-// Bound by latency: trips to L2, block barriers, and reading code that runs once (64 sequences: 9 us, of which offsets
-// and items 3.5, run lengths 3.5, places and segments 2): once per step, not per layer.
+// Bound by latency: trips to L2, block barriers, and reading code that runs once (64 sequences: 9 to 10 us, of which
+// offsets and items 3.5, run lengths 3.5, places and segments 2; 300 19, 1,000 47, 4,096 156): once per step, not per
+// layer.
 //
 // The length of a run.  A segment of c tiles costs about c + kSegCost tiles of one SM; n segments on S SMs end after
 // max(sum of all / S, ceil(long ones / S) * (c + kSegCost)) at the least, and every part's row is written and read once
@@ -56,6 +57,12 @@ struct PlanShared {
 };
 
 __device__ __forceinline__ int runs_of(int rows) { return (rows + kGRows - 1) / kGRows; }
+// Parts of a segment of at most 128 rows: two, where its tiles go to the accumulators in turn, or one, where the second
+// accumulator has no rows.  Two halve the segment and double its parts; they pay where most segments are such, the
+// rows one run (300 to 3,000 sequences of 400 rows, 28/4 heads: 85 to 635 us a layer, 99 to 794 with one).  Where only an
+// item's last run is, one part is better: on 9,000 shared rows 40 sequences, 280 rows, 34.4 us against 36.7, 120
+// sequences, 840 rows, 43.0 against 44.5; on 22,772 rows 350 of one sequence 34.1 against 37.9, 1,631 72.6 against 78.1.
+// So items of more than four runs never write two.
 __device__ __forceinline__ int sub_of(const PlanArgs &P, int rows) {
   const int last = rows - (runs_of(rows) - 1) * kGRows;
   return P.halves && rows <= 4 * kGRows && last <= kGSlot ? 2 : 1;
@@ -349,7 +356,10 @@ apack_status group_shape(const apack_paged_cache *c, int32_t hq, int32_t n_seqs,
   if (n_seqs < 1 || n_seqs > APACK_MAX_SEQS || n_q < 0 || n_q > (1 << 24) || n_q * hq > (1 << 28)) return APACK_EINVAL;
   s->group = hq / c->num_kv_heads;
   const int64_t rows = n_q * hq, packed = n_q * s->group, sms = device_sm_count();
-  // every item once (shared and own rows; twice in halves), and what runs of keys add for all SMs
+  // every item once (shared and own rows; twice in halves), and what runs of keys add for all SMs.  Halves double the
+  // room for parts (1,170 tokens of 28/4 heads: a workspace of 149 MB), which is what bounds them here, by the tokens that
+  // there is room for.  With more, 1,500 decode tokens take 409 us where halves would 326; 1,200 tokens of a prompt beside
+  // 40 decode tokens take 145 and would 160.
   s->halves = packed <= 8192;
   s->cap_rows = rows * (s->halves ? 4 : 2) + std::min(rows * sms, sms * 4 * kGRows) + 64;
   s->cap_segs = c->num_kv_heads * (2 * (packed / kGRows) + 2 * static_cast<int64_t>(n_seqs)) + 8 * sms + 64;

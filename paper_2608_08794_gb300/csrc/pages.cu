@@ -7,10 +7,10 @@
 // stack.
 //
 // Bound by latency: a chain of some five reads that depend on one another (entry, length, table, count, page), barriers
-// between them, and one launch: release and extension of 61 sequences by a row each take 14.7 us, 256 drafts 19.  One
+// between them, and one launch: release and extension of 61 sequences by a row each take 14.5 us, 256 drafts 19.3.  One
 // CTA, or a cluster of eight where the lists may be long, because a split over the grid needs a second launch or a grid
 // barrier, which cost more than the work.  Only the map from new rows to slots is large when prompts enter (16 bytes
-// per row): above kInlineRows rows a second kernel on all SMs fills it (670,000 rows of 1,000 prompts: 7.4 us, 1.4
+// per row): above kInlineRows rows a second kernel on all SMs fills it (298,112 rows of 1,000 prompts: 7.1 us, 0.67
 // TB/s).
 #include <algorithm>
 #include <cstring>
@@ -24,9 +24,10 @@ namespace {
 constexpr int kThreads = 1024;
 constexpr int kWarps = kThreads / 32;
 constexpr int kPer = APACK_MAX_SEQS / kThreads;      // entries of a thread: kThreads apart, so that few entries take few steps
-// Calls that may move more pages than this take a cluster: 45,000 pages of 64 questions that leave and come take 352 us
-// by one SM, which reads one random place per clock at best, and 90 by eight; 40,000 pages of 1,000 prompts 96 and 37.
-// A step of 61 sequences takes 2 us longer so (16.4 -> 18.5), but nothing on the host says how few pages it moves.
+// Calls that may move more pages than this take a cluster: 64 questions that leave and come, whose 64,186 table entries
+// name some 5,260 pages, take 409 us by one SM, which reads one random place per clock at best, and 88 by eight; 18,803
+// pages of 1,000 prompts that leave and come 92 and 37.  A step of 61 sequences takes 0.5 us longer so (14.2 -> 14.8),
+// but nothing on the host says how few pages it moves.
 constexpr int kMaxCluster = 8;
 constexpr int64_t kClusterPages = 16384;
 // Rows of the slot map that the first kernel fills by itself.
@@ -122,8 +123,8 @@ __device__ int entry_seq(const Call &C, Shared &s, int i) {
 __device__ __forceinline__ int32_t now(const int32_t *p) { return *const_cast<const volatile int32_t *>(p); }
 
 // The entries of kBatch places of the list (the last i with at[i] <= j), side by side: every pass over a list is bound
-// by the trips of its reads, so a thread has as many of them under way (1,000 prompts, 40,000 pages: 202 us one by one,
-// 96 so).
+// by the trips of its reads, so a thread has as many of them under way (by one SM: the 64 questions 563 us one by one,
+// 409 so; 1,000 prompts 100 and 92; 256 drafts, which move 67 pages, 13.0 and 18.8).
 constexpr int kBatch = 8;
 __device__ __forceinline__ void entries_of(const int32_t *at, int n, const int (&j)[kBatch], int (&e)[kBatch]) {
 #pragma unroll
